@@ -5,7 +5,7 @@ A case names the operator (``op``), the rows, channels and symbols of the head, 
 the gradients are wanted:
 
   code_length  bits_r = (lse_r - z_r[symbol_r]) / ln 2 of the linear head z = h w + b, and lse_r; rows whose symbol
-               is -1 have no bits and no gradient; with gradients those of sum_r weight_r bits_r for h, w and b
+               is -1 are left out (all zero); with gradients those of sum_r weight_r bits_r for h, w and b
   distill      bits_r = sum_j q_rj log2(q_rj / p_r[index_rj]), q the softmax of the teacher's kept logits at the
                temperature, p the student's at the same; entries whose index is -1 are not there
   top          the k largest logits of each row, their indices (ties to the lowest) and the row's normaliser
@@ -160,10 +160,10 @@ def _plain_head(s):
         q = t / t.sum(1, keepdim=True).clamp(min=1e-38)
     logq = torch.where(q > 0, q, 1.0).log()
     bits = torch.where(q > 0, q * (logq - logp.gather(1, index)), 0.0).sum(1) / LN2
-    lse = (m + total.log())[:, 0]
+    row = there.any(1)
+    lse = torch.where(row, (m + total.log())[:, 0], 0.0)
     if not case["grad"]:
         return {"bits": bits, "lse": lse}
-    row = there.any(1)
     dz = torch.where(row[:, None], e / total, 0.0).scatter_add(1, index, -q)
     dz = dz * (s["weight"] / (T * LN2))[:, None]
     x = torch.where(row[:, None], h, 0.0)
@@ -221,8 +221,7 @@ def exact(case, seed):
         rows = slice(r0, min(case["rows"], r0 + step))
         h = s["h"][rows].double()
         z = torch.addmm(b, h, w) / T
-        lse.append(torch.logsumexp(z, 1))
-        logp = z - lse[-1][:, None]
+        logp = torch.log_softmax(z, 1)
         target = torch.zeros_like(logp)
         if case["op"] == "code_length":
             here = torch.nonzero(s["symbol"][rows] >= 0).flatten()
@@ -233,8 +232,9 @@ def exact(case, seed):
             q = torch.softmax(logit, 1).nan_to_num(0.0)   # a row without any entry has no distribution
             target.scatter_add_(1, index.clamp(min=0), q)
         bits.append((torch.xlogy(target, target) - torch.xlogy(target, logp.exp())).sum(1) / LN2)
+        full = target.sum(1, keepdim=True) > 0
+        lse.append(torch.logsumexp(z, 1) * full[:, 0])
         if case["grad"]:
-            full = target.sum(1, keepdim=True) > 0
             d = (logp.exp() - target) * full * (s["weight"][rows].double() / (T * LN2))[:, None]
             dh.append(d @ w.T)
             dw += (h * full).T @ d
