@@ -1,6 +1,7 @@
 """MI355X (gfx950) hot path of the RENO LiDAR geometry codec.
 
-Thin ctypes binding over the C ABI of libreno.so (declared in include/reno.h):
+Thin ctypes binding over the C ABI of libreno.so (declared in include/reno.h
+and, for the head's training operators, include/reno_head.h):
 argument marshalling only.  Device memory and streams come from PyTorch; every
 step of the codec runs in the library's HIP kernels.  Importing works without
 a GPU; creating a context needs one, and the library must have been built
@@ -8,8 +9,10 @@ a GPU; creating a context needs one, and the library must have been built
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
+import typing
 
 import numpy as np
 
@@ -105,6 +108,35 @@ _SIGS = {
     "reno_profile_read": (_int, [_vp, _vp, _vp]),
 }
 
+RENO_T_FP32 = 0
+RENO_T_BF16 = 1
+RENO_T_FP16 = 2
+RENO_HEAD_MAX_CHANNELS = 16384
+RENO_HEAD_MAX_SYMBOLS = 1 << 20
+RENO_HEAD_MAX_TOP = 128
+
+
+class reno_head(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("channels", ctypes.c_int), ("symbols", ctypes.c_int),
+                ("type", ctypes.c_int), ("h_stride", ctypes.c_int64), ("w_stride", ctypes.c_int64)]
+
+
+class reno_head_data(ctypes.Structure):
+    _fields_ = [("h", ctypes.c_void_p), ("w", ctypes.c_void_p), ("b", ctypes.c_void_p),
+                ("row_weight", ctypes.c_void_p), ("bits", ctypes.c_void_p), ("lse", ctypes.c_void_p),
+                ("dh", ctypes.c_void_p), ("dw", ctypes.c_void_p), ("db", ctypes.c_void_p)]
+
+
+# the same for include/reno_head.h
+_HEAD_SIGS = {
+    "reno_head_workspace": (_int, [ctypes.POINTER(reno_head), _int, _int, ctypes.POINTER(_i64)]),
+    "reno_head_code_length": (_int, [ctypes.POINTER(reno_head), ctypes.POINTER(reno_head_data), _vp, _vp, _i64, _vp]),
+    "reno_head_distill": (_int, [ctypes.POINTER(reno_head), ctypes.POINTER(reno_head_data), _vp, _vp, _int,
+                                 ctypes.c_float, _vp, _i64, _vp]),
+    "reno_top_logits": (_int, [_vp, _int, _i64, _int, _i64, _int, _vp, _vp, _vp, _vp]),
+    "reno_features": (_int, [_vp, _int, _vp]),
+}
+
 KERNELS = ["zero", "quantize", "sort", "pyramid", "codes", "set_base", "expand", "conv_first",
            "conv_mid", "conv_last", "code_length", "other", "top_input", "entropy"]
 
@@ -123,7 +155,7 @@ def lib():
             raise RuntimeError(f"{LIB_PATH} is missing: build it with "
                                "`python -m paper_2503_12382_amd.build` (no CPU fallback exists)")
         L = ctypes.CDLL(LIB_PATH)
-        for name, (res, args) in _SIGS.items():
+        for name, (res, args) in {**_SIGS, **_HEAD_SIGS}.items():
             f = getattr(L, name)
             f.restype = res
             f.argtypes = args
@@ -359,6 +391,18 @@ class Context:
         self._check(lib().reno_profile_read(self._h, ms.ctypes.data_as(_vp), n.ctypes.data_as(_vp)))
         return {k: (float(ms[i]), int(n[i])) for i, k in enumerate(KERNELS) if n[i]}
 
+    def features(self, scale: int):
+        """Features [N_scale][C] (fp32) that the head is applied to, as the last
+        predict_probs of the scale left them; RENO_ALL_SCALES concatenates the
+        model scales.  Channels that no head weight reads come back as NaN."""
+        if scale == RENO_ALL_SCALES:
+            n = sum(self.num_voxels(b) for b in range(self.b0 + 1, self.B))
+        else:
+            n = self.num_voxels(scale)
+        out = self._empty((max(n, 1), self.channels), self.torch.float32)
+        self._check(lib().reno_features(self._h, scale, _ptr(out)))
+        return out[:n]
+
     def symbol_freqs16(self, scale: int, stage: int):
         """Two-stage head: uint16 [N][16] table of stage 1 or 2 per voxel."""
         n = self.num_voxels(scale)
@@ -449,6 +493,168 @@ def expand_noalloc(keys, codes, child_keys, child_parent, result, first_child=No
                                    _ptr(first_child), _ptr(result), ctypes.c_void_p(st.cuda_stream))
     if rc != RENO_OK:
         raise RenoError(rc, lib().reno_last_error(None).decode())
+
+
+class HeadResult(typing.NamedTuple):
+    """Results of head_code_length and head_distill (None: not asked for)."""
+    bits: object          # float32 [N]
+    lse: object           # float32 [N], natural log
+    dh: object = None     # [N][C], dw [C][V], db [V]: in the operands' type
+    dw: object = None
+    db: object = None
+
+
+class TopLogits(typing.NamedTuple):
+    index: object         # int32 [N][k]
+    value: object         # float32 [N][k]
+    lse: object           # float32 [N], natural log
+
+
+_TYPES = {"torch.float32": RENO_T_FP32, "torch.bfloat16": RENO_T_BF16, "torch.float16": RENO_T_FP16}
+
+
+def _need(cond, msg):
+    if not cond:
+        raise ValueError(msg)
+
+
+def _rows(t, name, dtype=None, device=None, shape=None):
+    """A device matrix whose rows are contiguous (a copy where they are not)."""
+    _need(t.is_cuda, f"{name} must be a device tensor")
+    _need(device is None or t.device == device, f"{name} must be on the device of the other arguments")
+    _need(dtype is None or t.dtype == dtype, f"{name} must be {dtype}")
+    _need(shape is None or tuple(t.shape) == tuple(shape), f"{name} must have shape {tuple(shape or ())}")
+    if t.dim() == 2 and t.shape[1] > 1 and (t.stride(1) != 1 or (t.shape[0] > 1 and t.stride(0) < t.shape[1])):
+        return t.contiguous()
+    return t if t.dim() == 2 else t.contiguous()
+
+
+def _stride(t):
+    """Elements between the rows of a matrix that _rows returned."""
+    return t.stride(0) if t.shape[0] > 1 and t.stride(0) >= t.shape[1] else t.shape[1]
+
+
+def head_workspace(rows: int, channels: int, symbols: int, dtype, top_k: int = 1, grad: bool = False) -> int:
+    """Bytes of workspace for such a call (reno_head_workspace)."""
+    p = reno_head(rows, channels, symbols, _TYPES[str(dtype)], channels, symbols)
+    n = ctypes.c_int64()
+    _head_check(lib().reno_head_workspace(ctypes.byref(p), top_k, int(bool(grad)), ctypes.byref(n)))
+    return n.value
+
+
+def _head_check(rc):
+    if rc != RENO_OK:
+        raise RenoError(rc, lib().reno_last_error(None).decode())
+
+
+@contextlib.contextmanager
+def _on(dev, stream):
+    """The stream a call is enqueued on (default: torch's current one of the
+    device), made current together with its device."""
+    import torch
+    with torch.cuda.device(dev):
+        st = stream if stream is not None else torch.cuda.current_stream()
+        _need(st.device == dev, "stream must belong to the device of the arguments")
+        with torch.cuda.stream(st):
+            yield st
+
+
+def _read_on(stream, *tensors):
+    """A tensor that its owner frees is not reused before a stream of the
+    caller's choice has read it."""
+    if stream is not None:
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+
+
+def _head_call(h, w, b, targets, row_weight, grad, workspace, stream, k, call):
+    import torch
+    _need(h.dim() == 2 and w.dim() == 2, "h must be [N][C] and w [C][V]")
+    dt, dev = h.dtype, h.device
+    _need(h.is_cuda, "h must be a device tensor")
+    _need(str(dt) in _TYPES, "h must be float32, bfloat16 or float16")
+    n, c, v = h.shape[0], h.shape[1], w.shape[1]
+    names = ("dh", "dw", "db") if grad is True else tuple(grad or ())
+    _need(all(x in ("dh", "dw", "db") for x in names), "grad must be True, False or some of dh, dw, db")
+    with _on(dev, stream) as st:
+        h = _rows(h, "h")
+        w = _rows(w, "w", dt, dev, (c, v))
+        b = None if b is None else _rows(b, "b", dt, dev, (v,))
+        g = None if row_weight is None else _rows(row_weight, "row_weight", torch.float32, dev, (n,))
+        targets = [_rows(t, name, kind, dev, shape).contiguous() for t, name, kind, shape in targets]
+        p = reno_head(n, c, v, _TYPES[str(dt)], _stride(h), _stride(w))
+        need = ctypes.c_int64()
+        _head_check(lib().reno_head_workspace(ctypes.byref(p), k, int(bool(names)), ctypes.byref(need)))
+        if workspace is None:
+            workspace = torch.empty(need.value, dtype=torch.uint8, device=dev)
+        _need(workspace.is_cuda and workspace.device == dev and workspace.is_contiguous(),
+              "workspace must be contiguous and on the device of the arguments")
+        bits = torch.empty(n, dtype=torch.float32, device=dev)
+        lse = torch.empty(n, dtype=torch.float32, device=dev)
+        shapes = {"dh": (n, c), "dw": (c, v), "db": (v,)}
+        out = {x: torch.empty(shapes[x], dtype=dt, device=dev) for x in names}
+        ptr = [None if t is None else t.data_ptr() for t in (h, w, b, g, bits, lse, *map(out.get, shapes))]
+        _head_check(call(ctypes.byref(p), ctypes.byref(reno_head_data(*ptr)), *map(_ptr, targets), _ptr(workspace),
+                         workspace.numel() * workspace.element_size(), ctypes.c_void_p(st.cuda_stream)))
+        _read_on(stream, h, w, b, g, workspace, *targets)
+    return HeadResult(bits, lse, *(out.get(x) for x in shapes))
+
+
+def head_code_length(h, w, b, symbol, row_weight=None, grad=False, workspace=None, stream=None) -> HeadResult:
+    """Ideal code length of the linear head z = h w + b and its gradient
+    (reno_head_code_length), without keeping the logits: h [N][C], w [C][V], b [V]
+    or None (float32, bfloat16 or float16, one type), symbol int32 [N] (negative:
+    the row is left out), row_weight float32 [N] or None.  grad: True or a
+    selection of "dh", "dw", "db", the gradients of sum_r row_weight_r bits_r.
+    workspace: a uint8 tensor of head_workspace bytes, or None to take it from
+    torch's allocator.  Enqueued on ``stream`` (default: the current stream of
+    the tensors' device); rows may be strided."""
+    import torch
+
+    def call(p, d, s, ws, nbytes, st):
+        return lib().reno_head_code_length(p, d, s, ws, nbytes, st)
+    return _head_call(h, w, b, [(symbol, "symbol", torch.int32, (h.shape[0],))], row_weight, grad, workspace, stream, 1,
+                      call)
+
+
+def head_distill(h, w, b, top_index, top_logit, temperature: float = 1.0, row_weight=None, grad=False, workspace=None,
+                 stream=None) -> HeadResult:
+    """Distillation of the head into a teacher's top logits (reno_head_distill):
+    top_index int32 [N][k] (negative: no entry) and top_logit float32 [N][k], as
+    top_logits gives them.  bits are the divergence of the student's
+    distribution at the temperature from the teacher's over its entries; the
+    other arguments and the results as for head_code_length."""
+    import torch
+    _need(top_index.dim() == 2, "top_index must be [N][k]")
+    k = int(top_index.shape[1])
+    shape = (h.shape[0], k)
+
+    def call(p, d, ix, lg, ws, nbytes, st):
+        return lib().reno_head_distill(p, d, ix, lg, k, float(temperature), ws, nbytes, st)
+    return _head_call(h, w, b, [(top_index, "top_index", torch.int32, shape),
+                                (top_logit, "top_logit", torch.float32, shape)], row_weight, grad, workspace, stream, k,
+                      call)
+
+
+def top_logits(logits, k: int, stream=None) -> TopLogits:
+    """The k largest logits of each row of [N][V] (float32, bfloat16 or float16,
+    rows may be strided) in descending order, ties by ascending index, with the
+    row's normaliser (reno_top_logits); entries past V are -1 and -inf."""
+    import torch
+    _need(logits.dim() == 2 and logits.is_cuda, "logits must be a device tensor [N][V]")
+    _need(str(logits.dtype) in _TYPES, "logits must be float32, bfloat16 or float16")
+    k, dev = int(k), logits.device
+    n, v = logits.shape
+    with _on(dev, stream) as st:
+        x = _rows(logits, "logits")
+        index = torch.empty((n, max(k, 0)), dtype=torch.int32, device=dev)
+        value = torch.empty((n, max(k, 0)), dtype=torch.float32, device=dev)
+        lse = torch.empty(n, dtype=torch.float32, device=dev)
+        _head_check(lib().reno_top_logits(_ptr(x), _TYPES[str(x.dtype)], n, v, _stride(x), k, _ptr(index), _ptr(value),
+                                          _ptr(lse), ctypes.c_void_p(st.cuda_stream)))
+        _read_on(stream, x)
+    return TopLogits(index, value, lse)
 
 
 def rans_encode(sym: np.ndarray, freq: np.ndarray) -> np.ndarray:

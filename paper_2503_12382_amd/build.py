@@ -19,9 +19,10 @@ BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(HERE, "libreno.so")
 ARCH = "gfx950"
 
-HIP_SOURCES = ["k_prep.hip", "k_dec.hip", "k_model.hip", "k_post.hip", "k_code.hip", "api.cpp", "frame.cpp"]
+HIP_SOURCES = ["k_prep.hip", "k_dec.hip", "k_model.hip", "k_post.hip", "k_code.hip", "k_head.hip", "k_top.hip", "api.cpp",
+               "frame.cpp", "head.cpp"]
 HOST_SOURCES = ["rans.cpp"]
-HEADERS = ["dev.h", "ctx.h"]
+HEADERS = ["dev.h", "ctx.h", "head.h", "gemm.h"]
 
 
 def hipcc() -> str:

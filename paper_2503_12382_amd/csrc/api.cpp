@@ -8,6 +8,7 @@
 #include <string>
 
 #include "ctx.h"
+#include "head.h"
 
 namespace {
 
@@ -120,6 +121,15 @@ bool stage2_ok(const Ctx* c, int b) {
 }
 
 }  // namespace
+
+reno_status reno::fail_thread(reno_status s, const char* msg) {
+  try {
+    return fail(nullptr, s, msg);
+  } catch (...) {  // no memory for the message
+    g_create_err.clear();
+    return s;
+  }
+}
 
 extern "C" {
 
@@ -315,6 +325,7 @@ reno_status reno_set_weights(reno_ctx* c, const reno_weights* w) {
   }
   RENO_HIP(c, reno::launch_pack_weights(*c, *w));
   c->have_weights = true;
+  c->have_features = 0;
   return RENO_OK;
 }
 
@@ -496,8 +507,22 @@ reno_status reno_predict_probs(reno_ctx* c, int scale, const reno_weights* weigh
   const bool second = two && (c->have_codes & bits_range(lo, hi)) == bits_range(lo, hi);
   RENO_HIP(c, reno::launch_model(*c, lo, hi, logits, second));
   c->have_pred |= bits_range(lo, hi);
+  c->have_features |= bits_range(lo, hi);
   c->have_pred2 &= ~bits_range(lo, hi);
   if (second) c->have_pred2 |= bits_range(lo, hi);
+  return RENO_OK;
+}
+
+reno_status reno_features(reno_ctx* c, int scale, float* features) {
+  if (!c || !features) return fail(c, RENO_E_INVALID, "null argument");
+  if (c->B == 0) return fail(c, RENO_E_STATE, "no frame");
+  const bool all = scale == RENO_ALL_SCALES;
+  if (!all && !model_scale(c, scale)) return fail(c, RENO_E_INVALID, "not a model scale");
+  const int lo = all ? c->b0() + 1 : scale, hi = all ? c->B - 1 : scale;
+  for (int b = lo; b <= hi; ++b)
+    if (!has(c->have_pred, b) || !has(c->have_features, b))
+      return fail(c, RENO_E_STATE, "the scale needs predict_probs with the present weights");
+  if (lo <= hi) RENO_HIP(c, reno::launch_features(*c, lo, hi, features));
   return RENO_OK;
 }
 

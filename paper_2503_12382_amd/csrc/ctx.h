@@ -271,6 +271,7 @@ hipError_t launch_coords(Ctx& c, int b, int32_t* xyz, uint64_t* keys);
 hipError_t launch_copy_level_u8(Ctx& c, int b, uint8_t* out);
 hipError_t launch_copy_level_i32(Ctx& c, int b, const int32_t* src, int32_t* out);
 hipError_t launch_neighbor_map(Ctx& c, int b, int32_t* out);
+hipError_t launch_features(Ctx& c, int b_lo, int b_hi, float* out);
 
 // whole-frame entropy coder (k_code.hip)
 int64_t rans_stream_bound(const Ctx& c, int sections, int L);
@@ -290,4 +291,6 @@ void frame_free(Ctx& c);
 }  // namespace reno
 
 // the opaque handle of the C ABI
-struct reno_ctx : reno::Ctx {};
+struct reno_ctx : reno::Ctx {
+  uint32_t have_features = 0;  // bit b: TOP evaluated on V_b with the present weights
+};

@@ -1,0 +1,819 @@
+// Code length of a linear head with its gradient, and distillation from a
+// teacher's top logits with its gradient (reno_head.h).
+//
+// With t = z log2(e) / T (logits at the temperature, in powers of two) a row's
+// loss in bits is sum_j q_j (log2 q_j + lse2 - t_j), lse2 = log2 sum_v 2^t_v, over
+// its target entries (one with q = 1: the code length), and its gradient for z
+// is g / (T ln 2) (2^(t - lse2) - q).  Steps, over pieces of rows so that the logits
+// are never kept whole:
+//   k_head_targets  (distillation) q, entries of one index joined
+//   k_head_pack_*   operands as 16-bit planes, padded; rows left out as zeros
+//   k_head_logits   z by MFMA; every wave leaves the maximum and the sum of 2^(t - max)
+//                   of its part of the alphabet for each row, the t of the rows' targets, and
+//                   (gradient) t itself for this piece
+//   k_head_rows     lse2 and the bits from the parts
+//   k_head_dz       dz as 16-bit planes, and its sums over rows
+//   k_head_product  dh = dz w^T and dw = h^T dz by MFMA, split over k where the
+//                   outputs alone do not fill the chip
+//   k_head_reduce   joins splits, pieces and db's partial sums in a fixed order
+// dz is carried over the largest |g| (a power of two, G) and put right in the
+// products' results: fp16 and the low planes of fp32 lose nothing of it for small g.
+
+#include <algorithm>
+
+#include "dev.h"
+#include "gemm.h"
+#include "head.h"
+
+namespace reno {
+namespace {
+
+constexpr float LN2 = 0.6931471805599453f;
+constexpr int GPARTS = 64;       // partial maxima of |g|
+constexpr int DZ_ROWS = 64;      // rows of a wave of k_head_dz
+constexpr int HALF_SHIFT = 14;   // dz in fp16 is scaled by 2^14
+
+__device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float log2_hw(float x) { return __builtin_amdgcn_logf(x); }
+
+// ---- element types ----
+template <int TYPE>
+__device__ __forceinline__ float load_as_float(const void* p, int64_t i) {
+  if constexpr (TYPE == RENO_T_FP32) return static_cast<const float*>(p)[i];
+  else if constexpr (TYPE == RENO_T_BF16) return __uint_as_float((uint32_t)static_cast<const uint16_t*>(p)[i] << 16);
+  else return (float)static_cast<const _Float16*>(p)[i];
+}
+__device__ __forceinline__ uint16_t to_bf16(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
+__device__ __forceinline__ uint16_t to_fp16(float x) { return __builtin_bit_cast(uint16_t, (_Float16)x); }
+
+// The three bf16 planes of x: each takes the leading 8 bits of what is left, cut off, so that
+// the parts add up to x exactly.  An infinity or NaN stays in the first.
+__device__ __forceinline__ void split3(float x, uint16_t (&o)[3]) {
+  const uint32_t u = __float_as_uint(x);
+  o[0] = (uint16_t)(u >> 16);
+  if ((u & 0x7f800000u) == 0x7f800000u) {
+    if ((u & 0x007fffffu) != 0) o[0] |= 0x40;  // a NaN whose payload lies below stays one
+    o[1] = o[2] = 0;
+    return;
+  }
+  float r = x - __uint_as_float(u & 0xffff0000u);
+  const uint32_t v = __float_as_uint(r);
+  o[1] = (uint16_t)(v >> 16);
+  r -= __uint_as_float(v & 0xffff0000u);
+  o[2] = (uint16_t)(__float_as_uint(r) >> 16);
+}
+
+template <int TYPE, int PLANES>
+__device__ __forceinline__ void to_planes(float x, uint16_t (&o)[PLANES]) {
+  if constexpr (TYPE == RENO_T_FP32) split3(x, o);
+  else if constexpr (TYPE == RENO_T_BF16) o[0] = to_bf16(x);
+  else o[0] = to_fp16(x);
+}
+constexpr int planes_of(int type) { return type == RENO_T_FP32 ? 3 : 1; }
+
+// What every kernel of one call needs.
+struct HeadArgs {
+  int64_t N;               // rows of the call
+  int64_t r0, R;           // first row and rows of this piece
+  int C, V, k;
+  int64_t Cp, Vp;          // padded to BK
+  int64_t h_stride, w_stride;
+  const void *h, *w, *b;
+  const float* g;
+  const int32_t* index;    // targets as given (code length) or joined (distillation)
+  const float* q;          // their probabilities, or null: 1
+  const float* ent;        // sum q log2 q a row (distillation)
+  const uint8_t* flag;     // row state (distillation)
+  float scale;             // log2(e) / T
+  float* bias;             // b * scale
+  uint16_t* hp;            // planes of h [R][Cp]
+  uint16_t* wp;            // planes of w [C][Vp], if they are made
+  int64_t h_plane, w_plane, d_plane;
+  float2* part;            // [parts][R] maximum and sum
+  int parts;
+  float* tt;               // [R][k] t of the targets
+  float* t;                // [R][Vp]
+  float* lse2;             // [R]
+  uint16_t* dz;            // planes [R][Vp]
+  float* dbp;              // [ceil(R / DZ_ROWS)][Vp]
+  const float* gpart;      // [GPARTS]
+  float *bits, *lse;       // of the call
+};
+
+// 0: left out, 1: taken, 2: a target outside the alphabet
+__device__ __forceinline__ int row_flag(const HeadArgs& a, int64_t row) {
+  if (a.flag) return a.flag[row];
+  const int32_t s = a.index[row];
+  return s < 0 ? 0 : s < a.V ? 1 : 2;
+}
+
+// ---- weights' scale ----
+// Partial maxima of the finite |g| (one per block).
+__global__ void __launch_bounds__(256) k_head_gmax(const float* __restrict__ g, int64_t n, float* __restrict__ part) {
+  __shared__ float s[4];
+  float m = 0.0f;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += GPARTS * 256) {
+    const float x = fabsf(g[i]);
+    if (x < INFINITY) m = fmaxf(m, x);
+  }
+  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+  if (lane_id() == 0) s[threadIdx.x >> 6] = m;
+  __syncthreads();
+  if (threadIdx.x == 0) part[blockIdx.x] = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
+}
+
+// G: the power of two at or above the largest |g| (1 without weights), kept where its inverse is normal.
+__device__ __forceinline__ float weight_scale(const float* gpart) {
+  if (!gpart) return 1.0f;
+  float m = gpart[lane_id()];
+  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+  if (m == 0.0f) return 1.0f;
+  const int e = min(max((int)(__float_as_uint(m) >> 23) + 1, 2), 252);
+  return __uint_as_float((uint32_t)e << 23);
+}
+
+// ---- targets of a distillation: one wave a row ----
+__device__ __forceinline__ float wave_max(float v) {
+  for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
+  return v;
+}
+__device__ __forceinline__ float wave_sum(float v) {
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+  return v;
+}
+
+__global__ void __launch_bounds__(256) k_head_targets(const int32_t* __restrict__ index, const float* __restrict__ logit,
+                                                      int64_t n, int k, int V, float scale, int32_t* __restrict__ out,
+                                                      float* __restrict__ q_out, float* __restrict__ ent,
+                                                      uint8_t* __restrict__ flag) {
+  const int lane = lane_id();
+  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (row >= n) return;
+  const int32_t* ix = index + row * k;
+  const float* tl = logit + row * k;
+  int32_t id[2];
+  float t[2], q[2];
+  bool bad = false;
+  float m = -INFINITY;
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    const int j = c * 64 + lane;
+    id[c] = j < k ? ix[j] : -1;
+    t[c] = id[c] >= 0 ? tl[j] : -INFINITY;
+    bad |= id[c] >= V || t[c] != t[c];
+    m = fmaxf(m, t[c]);
+  }
+  m = wave_max(m);
+  const bool any_bad = __ballot(bad) != 0 || m == INFINITY;
+  float sum = 0.0f;
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    q[c] = m > -INFINITY ? exp2_hw((t[c] - m) * scale) : 0.0f;
+    sum += q[c];
+  }
+  sum = wave_sum(sum);
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    q[c] = sum > 0.0f ? q[c] / sum : 0.0f;
+    if (q[c] == 0.0f) id[c] = -1;
+  }
+  // entries of one index: the first takes the sum, in order, the others go
+  float joined[2] = {0.0f, 0.0f};
+  bool later[2] = {false, false};
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    const int cnt = min(max(k - s * 64, 0), 64);
+    for (int l = 0; l < cnt; ++l) {
+      const int32_t oi = __shfl(id[s], l);
+      const float oq = __shfl(q[s], l);
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+        if (oi == id[c]) {
+          joined[c] += oq;
+          later[c] |= s * 64 + l < c * 64 + lane;
+        }
+    }
+  }
+  float e = 0.0f;
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    const int j = c * 64 + lane;
+    const bool keep = id[c] >= 0 && !later[c] && !any_bad;
+    if (j < k) {
+      out[row * k + j] = keep ? id[c] : -1;
+      q_out[row * k + j] = keep ? joined[c] : 0.0f;
+    }
+    if (keep) e += joined[c] * log2_hw(joined[c]);
+  }
+  e = wave_sum(e);
+  if (lane == 0) {
+    ent[row] = e;
+    flag[row] = any_bad ? 2 : m > -INFINITY ? 1 : 0;
+  }
+}
+
+// ---- operands as planes ----
+template <int TYPE>
+__global__ void __launch_bounds__(256) k_head_pack_h(HeadArgs a) {
+  constexpr int P = planes_of(TYPE);
+  const int64_t per = a.Cp / 8, total = a.R * per;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / per;
+    const int c0 = (int)(i % per) * 8;
+    const bool in = row_flag(a, a.r0 + r) != 0;
+    uint16_t o[P][8];
+    const int64_t src = (a.r0 + r) * a.h_stride;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      uint16_t v[P];
+      to_planes<TYPE, P>(in && c0 + e < a.C ? load_as_float<TYPE>(a.h, src + c0 + e) : 0.0f, v);
+#pragma unroll
+      for (int p = 0; p < P; ++p) o[p][e] = v[p];
+    }
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+      *reinterpret_cast<uint4*>(a.hp + p * a.h_plane + r * a.Cp + c0) = *reinterpret_cast<const uint4*>(o[p]);
+  }
+}
+
+template <int TYPE>
+__global__ void __launch_bounds__(256) k_head_pack_w(HeadArgs a) {
+  constexpr int P = planes_of(TYPE);
+  const int64_t per = a.Vp / 8, total = a.C * per;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+    const int64_t c = i / per;
+    const int64_t v0 = (i % per) * 8;
+    uint16_t o[P][8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      uint16_t v[P];
+      to_planes<TYPE, P>(v0 + e < a.V ? load_as_float<TYPE>(a.w, c * a.w_stride + v0 + e) : 0.0f, v);
+#pragma unroll
+      for (int p = 0; p < P; ++p) o[p][e] = v[p];
+    }
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+      *reinterpret_cast<uint4*>(a.wp + p * a.w_plane + c * a.Vp + v0) = *reinterpret_cast<const uint4*>(o[p]);
+  }
+}
+
+template <int TYPE>
+__global__ void __launch_bounds__(256) k_head_bias(HeadArgs a, int64_t n) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i < n) a.bias[i] = a.b && i < a.V ? load_as_float<TYPE>(a.b, i) * a.scale : 0.0f;
+}
+
+// ---- logits ----
+// m runs over symbols, n over rows: a lane holds one row and 4 consecutive
+// symbols of each 16, so that a row's maximum and sum need two lane exchanges.
+template <int BM, int BN, int WM, int WN, bool HALF>
+__global__ void __launch_bounds__(WM* WN * 64) k_head_logits(HeadArgs a, Operand W, Operand H, TileOrder order, int terms) {
+  using Tile = GemmTile<BM, BN, WM, WN, true, false, HALF>;
+  __shared__ __attribute__((aligned(1024))) char lds[Tile::LDS];
+  int tm, tn, split;
+  order.at(blockIdx.x, gridDim.x, tm, tn, split);
+  f32x4 acc[Tile::MF][Tile::NF];
+  Tile::run(lds, W, H, (int64_t)tm * BM, (int64_t)tn * BN, 0, a.Cp, terms, acc);
+  const int lane = lane_id(), wave = threadIdx.x >> 6;
+  const int l15 = lane & 15, g = lane >> 4;
+  const int v0 = tm * BM + (wave / WN) * (BM / WM);
+  const int64_t n0 = (int64_t)tn * BN + (wave % WN) * (BN / WN);
+#pragma unroll
+  for (int i = 0; i < Tile::MF; ++i) {
+    const int v = v0 + 16 * i + 4 * g;
+    const f32x4 bs = *reinterpret_cast<const f32x4*>(a.bias + v);
+#pragma unroll
+    for (int j = 0; j < Tile::NF; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[i][j][e] = v + e < a.V ? fmaf(acc[i][j][e], a.scale, bs[e]) : -INFINITY;
+  }
+  const int p = v0 / (BM / WM);
+#pragma unroll
+  for (int j = 0; j < Tile::NF; ++j) {
+    const int64_t r = n0 + 16 * j + l15;
+    float m = -INFINITY, s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < Tile::MF; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) m = fmaxf(m, acc[i][j][e]);
+    m = fmaxf(m, __shfl_xor(m, 16));
+    m = fmaxf(m, __shfl_xor(m, 32));
+    const float base = m > -INFINITY ? m : 0.0f;
+#pragma unroll
+    for (int i = 0; i < Tile::MF; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s += exp2_hw(acc[i][j][e] - base);
+    s += __shfl_xor(s, 16);
+    s += __shfl_xor(s, 32);
+    if (g == 0 && r < a.R && p < a.parts) a.part[(int64_t)p * a.R + r] = make_float2(m, s);
+    if (a.t && r < a.R) {
+#pragma unroll
+      for (int i = 0; i < Tile::MF; ++i) {
+        const int v = v0 + 16 * i + 4 * g;
+        if (v < a.Vp) *reinterpret_cast<f32x4*>(a.t + r * a.Vp + v) = acc[i][j];
+      }
+    }
+  }
+  // the targets' t
+  if (a.k == 1) {
+#pragma unroll
+    for (int j = 0; j < Tile::NF; ++j) {
+      const int64_t r = n0 + 16 * j + l15;
+      const int id = r < a.R ? a.index[a.r0 + r] : -1;
+      const int want = id < 0 ? -1 : id - v0 - 4 * g;
+#pragma unroll
+      for (int i = 0; i < Tile::MF; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (id >= 0 && want == 16 * i + e) a.tt[r] = acc[i][j][e];
+    }
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < Tile::NF; ++j) {
+    for (int rr = 0; rr < 16; ++rr) {
+      const int64_t r = n0 + 16 * j + rr;
+      if (r >= a.R) break;
+      for (int k0 = 0; k0 < a.k; k0 += 64) {
+        const int at = k0 + lane;
+        const int id = at < a.k ? a.index[(a.r0 + r) * a.k + at] - v0 : -1;
+        uint64_t hits = __ballot(id >= 0 && id < BM / WM);
+        while (hits) {
+          const int l = __builtin_ctzll(hits);
+          hits &= hits - 1;
+          const int want = __builtin_amdgcn_readlane(id, l);
+          float x = 0.0f;
+#pragma unroll
+          for (int i = 0; i < Tile::MF; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if ((want & ~12) == 16 * i + e) x = acc[i][j][e];
+          if (l15 == rr && g == ((want >> 2) & 3)) a.tt[r * a.k + k0 + l] = x;
+        }
+      }
+    }
+  }
+}
+
+// ---- rows: lse2 and bits from the parts; 16 rows a block, 16 lanes each ----
+__global__ void __launch_bounds__(256) k_head_rows(HeadArgs a) {
+  __shared__ float2 s_p[16][17];
+  __shared__ float s_b[16][17];
+  const int rl = threadIdx.x & 15, pl = threadIdx.x >> 4;
+  const int64_t r = (int64_t)blockIdx.x * 16 + rl;
+  const bool in = r < a.R;
+  float m = -INFINITY, s = 0.0f;
+  if (in)
+    for (int p = pl; p < a.parts; p += 16) {
+      const float2 x = a.part[(int64_t)p * a.R + r];
+      const float n = fmaxf(m, x.x);
+      const float base = n > -INFINITY ? n : 0.0f;
+      s = s * exp2_hw(m - base) + x.y * exp2_hw(x.x - base);
+      m = n;
+    }
+  s_p[rl][pl] = make_float2(m, s);
+  __syncthreads();
+  float top = -INFINITY;
+  for (int p = 0; p < 16; ++p) top = fmaxf(top, s_p[rl][p].x);
+  const float base = top > -INFINITY ? top : 0.0f;
+  float sum = 0.0f;
+  for (int p = 0; p < 16; ++p) sum += s_p[rl][p].y * exp2_hw(s_p[rl][p].x - base);
+  const float lse2 = base + log2_hw(sum);
+  const int flag = in ? row_flag(a, a.r0 + r) : 0;
+  float b = 0.0f;
+  if (flag == 1) {
+    for (int j = pl; j < a.k; j += 16) {
+      const float q = a.q ? a.q[(a.r0 + r) * a.k + j] : 1.0f;
+      if (q != 0.0f) b += q * (lse2 - a.tt[r * a.k + j]);
+    }
+  }
+  s_b[rl][pl] = b;
+  __syncthreads();
+  if (pl != 0 || !in) return;
+  b = a.ent && flag == 1 ? a.ent[a.r0 + r] : 0.0f;
+  for (int p = 0; p < 16; ++p) b += s_b[rl][p];
+  a.lse2[r] = lse2;
+  a.bits[a.r0 + r] = flag == 2 ? NAN : b;
+  if (a.lse) a.lse[a.r0 + r] = flag ? lse2 * LN2 : 0.0f;
+}
+
+// ---- dz of a piece: a wave takes 256 symbols of DZ_ROWS rows ----
+template <int TYPE>
+__global__ void __launch_bounds__(256) k_head_dz(HeadArgs a) {
+  constexpr int P = planes_of(TYPE);
+  constexpr float SHIFT = TYPE == RENO_T_FP16 ? (float)(1 << HALF_SHIFT) : 1.0f;
+  const int lane = lane_id();
+  const float inv_g = 1.0f / weight_scale(a.gpart);
+  const int64_t groups = (a.Vp + 255) / 256, blocks = (a.R + DZ_ROWS - 1) / DZ_ROWS;
+  const int64_t task = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (task >= groups * blocks) return;
+  const int v0 = (int)(task % groups) * 256;
+  const int64_t rb = task / groups;
+  const int v = v0 + lane * 4;
+  const bool mine = v < a.Vp;
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+  const int64_t end = min(a.R, (rb + 1) * DZ_ROWS);
+  for (int64_t r = rb * DZ_ROWS; r < end; ++r) {
+    const int64_t row = a.r0 + r;
+    const int flag = row_flag(a, row);
+    f32x4 d = {0.f, 0.f, 0.f, 0.f};
+    if (flag) {
+      const float lse2 = a.lse2[r];
+      const float w = flag == 2 ? NAN : (a.g ? a.g[row] * inv_g : 1.0f);
+      const f32x4 t = mine ? *reinterpret_cast<const f32x4*>(a.t + r * a.Vp + v) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) d[e] = exp2_hw(t[e] - lse2);
+      if (!a.q) {
+        const int want = a.index[row] - v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (want == e) d[e] -= 1.0f;
+      } else {
+        for (int k0 = 0; k0 < a.k; k0 += 64) {
+          const int at = k0 + lane;
+          const int id = at < a.k ? a.index[row * a.k + at] - v0 : -1;
+          const float q = at < a.k ? a.q[row * a.k + at] : 0.0f;
+          uint64_t hits = __ballot(id >= 0 && id < 256);
+          while (hits) {
+            const int l = __builtin_ctzll(hits);
+            hits &= hits - 1;
+            const int want = __builtin_amdgcn_readlane(id, l);
+            const float qq = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(q), l));
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (want == lane * 4 + e) d[e] -= qq;
+          }
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        d[e] = v + e < a.V ? d[e] * w : 0.0f;
+        sum[e] += d[e];
+      }
+    }
+    if (!mine) continue;
+    uint16_t o[P][4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      uint16_t x[P];
+      to_planes<TYPE, P>(d[e] * SHIFT, x);
+#pragma unroll
+      for (int p = 0; p < P; ++p) o[p][e] = x[p];
+    }
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+      *reinterpret_cast<uint2*>(a.dz + p * a.d_plane + r * a.Vp + v) = *reinterpret_cast<const uint2*>(o[p]);
+  }
+  if (mine) *reinterpret_cast<f32x4*>(a.dbp + rb * a.Vp + v) = sum;
+}
+
+// ---- dh and dw ----
+// Where a product's result goes: out [n][m] of the operands' type, times scale
+// and G, or fp32 sums of one split (added to what an earlier piece left there).
+struct ProductOut {
+  void* out;
+  int type;
+  float scale;
+  const float* gpart;
+  float* part;       // [splits][N][M], or null
+  int add;           // part holds sums of earlier pieces
+  int last;          // with one split: the result goes to out
+  int64_t M, N;
+};
+
+__device__ __forceinline__ void store_typed(void* out, int type, int64_t i, float x) {
+  if (type == RENO_T_FP32) static_cast<float*>(out)[i] = x;
+  else static_cast<uint16_t*>(out)[i] = type == RENO_T_BF16 ? to_bf16(x) : to_fp16(x);
+}
+
+template <int BM, int BN, int WM, int WN, bool ACOL, bool BCOL, bool HALF>
+__global__ void __launch_bounds__(WM* WN * 64) k_head_product(Operand A, Operand B, int64_t K, TileOrder order, int terms,
+                                                              ProductOut o) {
+  using Tile = GemmTile<BM, BN, WM, WN, ACOL, BCOL, HALF>;
+  __shared__ __attribute__((aligned(1024))) char lds[Tile::LDS];
+  int tm, tn, split;
+  order.at(blockIdx.x, gridDim.x, tm, tn, split);
+  const int64_t steps = (K + GEMM_BK - 1) / GEMM_BK;
+  const int64_t each = (steps + order.splits - 1) / order.splits;
+  const int64_t k0 = min(steps, split * each) * GEMM_BK, k1 = min(steps, (split + 1) * each) * GEMM_BK;
+  f32x4 acc[Tile::MF][Tile::NF];
+  Tile::run(lds, A, B, (int64_t)tm * BM, (int64_t)tn * BN, k0, k1, terms, acc);
+  const int lane = lane_id(), wave = threadIdx.x >> 6;
+  const int64_t m0 = (int64_t)tm * BM + (wave / WN) * (BM / WM) + 4 * (lane >> 4);
+  const int64_t n0 = (int64_t)tn * BN + (wave % WN) * (BN / WN) + (lane & 15);
+  const float scale = o.scale * weight_scale(o.gpart);
+  float* part = o.part ? o.part + split * o.M * o.N : nullptr;
+  const bool typed = !o.part || (o.last && order.splits == 1);
+  const bool wide = o.M % 4 == 0;
+#pragma unroll
+  for (int j = 0; j < Tile::NF; ++j) {
+    const int64_t n = n0 + 16 * j;
+    if (n >= o.N) continue;
+#pragma unroll
+    for (int i = 0; i < Tile::MF; ++i) {
+      const int64_t m = m0 + 16 * i;
+      if (m >= o.M) continue;
+      const int64_t at = n * o.M + m;
+      f32x4 x = acc[i][j];
+      if (wide) {
+        if (part && o.add) x += *reinterpret_cast<const f32x4*>(part + at);
+        if (!typed) {
+          *reinterpret_cast<f32x4*>(part + at) = x;
+          continue;
+        }
+        if (o.type == RENO_T_FP32 && (uintptr_t)o.out % 16 == 0) {
+          *reinterpret_cast<f32x4*>(static_cast<float*>(o.out) + at) = x * scale;
+          continue;
+        }
+        if (o.type != RENO_T_FP32 && (uintptr_t)o.out % 8 == 0) {
+          uint16_t h[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) h[e] = o.type == RENO_T_BF16 ? to_bf16(x[e] * scale) : to_fp16(x[e] * scale);
+          *reinterpret_cast<uint2*>(static_cast<uint16_t*>(o.out) + at) = *reinterpret_cast<const uint2*>(h);
+          continue;
+        }
+      } else if (part && o.add) {
+        for (int e = 0; e < 4; ++e)
+          if (m + e < o.M) x[e] += part[at + e];
+      }
+      for (int e = 0; e < 4; ++e)
+        if (m + e < o.M) {
+          if (typed) store_typed(o.out, o.type, at + e, x[e] * scale);
+          else part[at + e] = x[e];
+        }
+    }
+  }
+}
+
+// out[i] = scale G (sum over s of part[s][i]), i < n; rows of `width` values of which `cols` are stored
+__global__ void __launch_bounds__(256) k_head_reduce(const float* __restrict__ part, int64_t count, int64_t n, void* out,
+                                                     int type, float scale, const float* __restrict__ gpart) {
+  const float s = scale * weight_scale(gpart);
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+    float x = 0.0f;
+    for (int64_t p = 0; p < count; ++p) x += part[p * n + i];
+    store_typed(out, type, i, x * s);
+  }
+}
+
+// Column sums of dz: acc[v] (+)= sum over the piece's row blocks, four lanes'
+// worth of blocks at a time; the last piece stores db.
+__global__ void __launch_bounds__(256) k_head_db(const float* __restrict__ dbp, int64_t blocks, int64_t Vp, int V,
+                                                 float* __restrict__ acc, int add, int last, void* out, int type, float scale,
+                                                 const float* __restrict__ gpart) {
+  __shared__ float s[4][64];
+  const float sc = scale * weight_scale(gpart);
+  const int lane = lane_id(), w = threadIdx.x >> 6;
+  const int64_t v = (int64_t)blockIdx.x * 64 + lane;
+  float x = 0.0f;
+  for (int64_t b = w; b < blocks; b += 4) x += dbp[b * Vp + v];
+  s[w][lane] = x;
+  __syncthreads();
+  if (w != 0) return;
+  x = s[0][lane] + s[1][lane] + s[2][lane] + s[3][lane];
+  if (add) x += acc[v];
+  if (!last) acc[v] = x;
+  else if (v < V) store_typed(out, type, v, x * sc);
+}
+
+__global__ void __launch_bounds__(256) k_head_zero(void* out, int64_t bytes) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < bytes / 2; i += (int64_t)gridDim.x * 256)
+    static_cast<uint16_t*>(out)[i] = 0;
+}
+
+// ---------------------------------------------------------------------------
+// Host: the sizes of a call and where its scratch lies.
+
+int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
+
+// Tiles of 256 x 256 by 8 waves once they give most of the 256 CUs a block, else 128 x 128 by 4 waves.
+bool big_tiles(int64_t M, int64_t N) { return ((M + 255) / 256) * ((N + 255) / 256) >= 192; }
+
+// splits of k so that the outputs' tiles fill the chip, none shorter than 8 steps
+int splits_for(int64_t tiles, int64_t K, int terms) {
+  const int64_t steps = (K + GEMM_BK - 1) / GEMM_BK * terms;
+  int64_t s = std::min<int64_t>((512 + tiles - 1) / tiles, steps / 8);
+  return (int)std::max<int64_t>(1, std::min<int64_t>(s, 256));
+}
+
+struct Plan {
+  int planes, terms;
+  int64_t Cp, Vp, Vb;   // Vb: padded to whole tiles
+  int64_t R;            // rows of a piece
+  int64_t pieces;
+  int part_width;       // symbols of one part
+  bool big1, big2, big3;
+  int split2, split3;
+  // offsets into the workspace
+  int64_t bias, wp, idx, q, ent, flag, gpart, hp, part, tt, lse2, t, dz, dbp, dba, dhp, dwp, bytes;
+};
+
+bool w_in_place(const reno_head& p, const void* w) {
+  return p.type != RENO_T_FP32 && p.symbols % GEMM_BK == 0 && p.w_stride % 8 == 0 && p.w_stride <= GEMM_MAX_LD &&
+         (uintptr_t)w % 16 == 0;
+}
+
+Plan make_plan(const reno_head& p, int k, bool grad) {
+  Plan a{};
+  a.planes = planes_of(p.type);
+  a.terms = p.type == RENO_T_FP32 ? GEMM_TERMS : 1;
+  a.Cp = up(p.channels, GEMM_BK);
+  a.Vp = up(p.symbols, GEMM_BK);
+  a.Vb = up(p.symbols, 256);
+  // a piece: at most 2^28 logits (2^27 in fp32) where they are kept for the
+  // gradient, 2^32 where they are not
+  const int64_t most = !grad ? int64_t(1) << 32 : p.type == RENO_T_FP32 ? int64_t(1) << 27 : int64_t(1) << 28;
+  const int64_t N = std::max<int64_t>(p.rows, 1);
+  int64_t R = std::max<int64_t>(256, most / a.Vp / 256 * 256);
+  a.pieces = (N + R - 1) / R;
+  a.R = std::min(N, up((N + a.pieces - 1) / a.pieces, 256));
+  a.pieces = (N + a.R - 1) / a.R;
+  a.big1 = big_tiles(p.symbols, a.R);
+  a.big2 = big_tiles(p.channels, a.R);
+  a.big3 = big_tiles(p.symbols, p.channels);
+  a.part_width = a.big1 ? 128 : 64;
+  const int64_t parts = (p.symbols + a.part_width - 1) / a.part_width;
+  const auto tiles = [](bool big, int64_t m, int64_t n) {
+    const int64_t b = big ? 256 : 128;
+    return ((m + b - 1) / b) * ((n + b - 1) / b);
+  };
+  a.split2 = splits_for(tiles(a.big2, p.channels, a.R), a.Vp, a.terms);
+  a.split3 = splits_for(tiles(a.big3, p.symbols, p.channels), a.R, a.terms);
+  int64_t at = 0;
+  const auto take = [&](int64_t bytes) {
+    const int64_t o = at;
+    at += up(bytes, 256);
+    return o;
+  };
+  a.bias = take(a.Vb * 4);
+  a.wp = take(a.planes * (int64_t)p.channels * a.Vp * 2);
+  a.idx = take(N * k * 4);
+  a.q = take(N * k * 4);
+  a.ent = take(N * 4);
+  a.flag = take(N);
+  a.gpart = take(GPARTS * 4);
+  a.hp = take(a.planes * a.R * a.Cp * 2);
+  a.part = take(parts * a.R * 8);
+  a.tt = take(a.R * k * 4);
+  a.lse2 = take(a.R * 4);
+  if (grad) {
+    a.t = take(a.R * a.Vp * 4);
+    a.dz = take(a.planes * a.R * a.Vp * 2);
+    a.dbp = take((a.R + DZ_ROWS - 1) / DZ_ROWS * a.Vp * 4);
+    a.dba = take(a.Vp * 4);
+    a.dhp = a.split2 > 1 ? take(a.split2 * a.R * p.channels * 4) : at;
+    a.dwp = a.split3 > 1 || a.pieces > 1 ? take((int64_t)a.split3 * p.channels * p.symbols * 4) : at;
+  }
+  a.bytes = at;
+  return a;
+}
+
+unsigned blocks_for(int64_t n, int64_t per, int64_t most = 8192) {
+  return (unsigned)std::max<int64_t>(1, std::min(most, (n + per - 1) / per));
+}
+
+template <bool HALF>
+void run_logits(const HeadArgs& a, const Operand& W, const Operand& H, bool big, int terms, hipStream_t st) {
+  const int64_t b = big ? 256 : 128;
+  const TileOrder o{(int)((a.V + b - 1) / b), (int)((a.R + b - 1) / b), 1};
+  const dim3 grid((unsigned)((int64_t)o.tm * o.tn));
+  if (big) hipLaunchKernelGGL((k_head_logits<256, 256, 2, 4, HALF>), grid, dim3(512), 0, st, a, W, H, o, terms);
+  else hipLaunchKernelGGL((k_head_logits<128, 128, 2, 2, HALF>), grid, dim3(256), 0, st, a, W, H, o, terms);
+}
+
+template <bool ACOL, bool BCOL, bool HALF>
+void run_product(const Operand& A, const Operand& B, int64_t K, bool big, int splits, int terms, const ProductOut& po,
+                 hipStream_t st) {
+  const int64_t b = big ? 256 : 128;
+  const TileOrder o{(int)((po.M + b - 1) / b), (int)((po.N + b - 1) / b), splits};
+  const dim3 grid((unsigned)((int64_t)o.tm * o.tn * splits));
+  if (big)
+    hipLaunchKernelGGL((k_head_product<256, 256, 2, 4, ACOL, BCOL, HALF>), grid, dim3(512), 0, st, A, B, K, o, terms, po);
+  else
+    hipLaunchKernelGGL((k_head_product<128, 128, 2, 2, ACOL, BCOL, HALF>), grid, dim3(256), 0, st, A, B, K, o, terms, po);
+}
+
+template <int TYPE>
+hipError_t run_head(const HeadCall& c, hipStream_t st) {
+  constexpr bool HALF = TYPE == RENO_T_FP16;
+  const reno_head& p = c.p;
+  const int64_t N = p.rows;
+  const int size = TYPE == RENO_T_FP32 ? 4 : 2;
+  if (N == 0) {  // nothing reaches the weights
+    const auto zero = [&](void* out, int64_t n) {
+      if (out) hipLaunchKernelGGL(k_head_zero, dim3(blocks_for(n * size / 2, 256)), dim3(256), 0, st, out, n * size);
+    };
+    zero(c.d.dw, (int64_t)p.channels * p.symbols);
+    zero(c.d.db, p.symbols);
+    return hipGetLastError();
+  }
+  const Plan pl = make_plan(p, c.k, c.grad);
+  char* ws = c.ws;
+  HeadArgs a{};
+  a.N = N;
+  a.C = p.channels;
+  a.V = p.symbols;
+  a.k = c.k;
+  a.Cp = pl.Cp;
+  a.Vp = pl.Vp;
+  a.h_stride = p.h_stride;
+  a.w_stride = p.w_stride;
+  a.h = c.d.h;
+  a.w = c.d.w;
+  a.b = c.d.b;
+  a.g = c.d.row_weight;
+  a.scale = (float)(1.4426950408889634 / (double)c.temperature);
+  a.bias = reinterpret_cast<float*>(ws + pl.bias);
+  a.hp = reinterpret_cast<uint16_t*>(ws + pl.hp);
+  a.wp = reinterpret_cast<uint16_t*>(ws + pl.wp);
+  a.h_plane = pl.R * pl.Cp;
+  a.w_plane = (int64_t)p.channels * pl.Vp;
+  a.d_plane = pl.R * pl.Vp;
+  a.part = reinterpret_cast<float2*>(ws + pl.part);
+  a.parts = (p.symbols + pl.part_width - 1) / pl.part_width;
+  a.tt = reinterpret_cast<float*>(ws + pl.tt);
+  a.lse2 = reinterpret_cast<float*>(ws + pl.lse2);
+  a.bits = c.d.bits;
+  a.lse = c.d.lse;
+  a.index = c.index;
+  if (c.logit) {
+    int32_t* idx = reinterpret_cast<int32_t*>(ws + pl.idx);
+    float* q = reinterpret_cast<float*>(ws + pl.q);
+    float* ent = reinterpret_cast<float*>(ws + pl.ent);
+    uint8_t* flag = reinterpret_cast<uint8_t*>(ws + pl.flag);
+    hipLaunchKernelGGL(k_head_targets, dim3((unsigned)((N + 3) / 4)), dim3(256), 0, st, c.index, c.logit, N, c.k, p.symbols,
+                       a.scale, idx, q, ent, flag);
+    a.index = idx;
+    a.q = q;
+    a.ent = ent;
+    a.flag = flag;
+  }
+  if (c.grad) {
+    a.t = reinterpret_cast<float*>(ws + pl.t);
+    a.dz = reinterpret_cast<uint16_t*>(ws + pl.dz);
+    a.dbp = reinterpret_cast<float*>(ws + pl.dbp);
+    if (c.d.row_weight) {
+      float* gp = reinterpret_cast<float*>(ws + pl.gpart);
+      hipLaunchKernelGGL(k_head_gmax, dim3(GPARTS), dim3(256), 0, st, c.d.row_weight, N, gp);
+      a.gpart = gp;
+    }
+  }
+  hipLaunchKernelGGL(k_head_bias<TYPE>, dim3((unsigned)(pl.Vb / 256)), dim3(256), 0, st, a, pl.Vb);
+  const bool in_place = w_in_place(p, c.d.w);
+  if (!in_place)
+    hipLaunchKernelGGL(k_head_pack_w<TYPE>, dim3(blocks_for(a.C * a.Vp / 8, 256)), dim3(256), 0, st, a);
+  const int64_t wl = in_place ? p.w_stride : pl.Vp;
+  const Operand W{in_place ? static_cast<const uint16_t*>(c.d.w) : a.wp, wl, p.channels,
+                  (p.channels - 1) * wl + (in_place ? p.symbols : pl.Vp), a.w_plane};
+  const float scale = (float)(1.0 / (0.6931471805599453 * (double)c.temperature));
+  const float scale_d = HALF ? scale / (float)(1 << HALF_SHIFT) : scale;
+  for (int64_t i = 0; i < pl.pieces; ++i) {
+    a.r0 = i * pl.R;
+    a.R = std::min(pl.R, N - a.r0);
+    const bool last = i + 1 == pl.pieces;
+    hipLaunchKernelGGL(k_head_pack_h<TYPE>, dim3(blocks_for(a.R * a.Cp / 8, 256)), dim3(256), 0, st, a);
+    const Operand H{a.hp, pl.Cp, a.R, a.R * pl.Cp, a.h_plane};
+    run_logits<HALF>(a, W, H, pl.big1, pl.terms, st);
+    hipLaunchKernelGGL(k_head_rows, dim3((unsigned)((a.R + 15) / 16)), dim3(256), 0, st, a);
+    if (!c.grad) continue;
+    const int64_t row_blocks = (a.R + DZ_ROWS - 1) / DZ_ROWS;
+    hipLaunchKernelGGL(k_head_dz<TYPE>, dim3((unsigned)(((a.Vp + 255) / 256 * row_blocks + 3) / 4)), dim3(256), 0, st, a);
+    const Operand D{a.dz, pl.Vp, a.R, a.R * pl.Vp, a.d_plane};
+    if (c.d.dh) {
+      void* out = static_cast<char*>(c.d.dh) + a.r0 * p.channels * size;
+      float* part = reinterpret_cast<float*>(ws + pl.dhp);
+      const ProductOut po{out, TYPE, scale_d, a.gpart, pl.split2 > 1 ? part : nullptr, 0, 1, p.channels, a.R};
+      run_product<false, false, HALF>(W, D, a.Vp, pl.big2, pl.split2, pl.terms, po, st);
+      if (pl.split2 > 1)
+        hipLaunchKernelGGL(k_head_reduce, dim3(blocks_for(a.R * a.C, 256)), dim3(256), 0, st, part, (int64_t)pl.split2,
+                           a.R * a.C, out, TYPE, scale_d, a.gpart);
+    }
+    if (c.d.dw) {
+      float* part = reinterpret_cast<float*>(ws + pl.dwp);
+      const bool keep = pl.split3 > 1 || pl.pieces > 1;
+      const ProductOut po{c.d.dw, TYPE, scale_d, a.gpart, keep ? part : nullptr, i > 0, last, p.symbols, p.channels};
+      run_product<true, true, HALF>(D, H, a.R, pl.big3, pl.split3, pl.terms, po, st);
+      if (last && pl.split3 > 1)
+        hipLaunchKernelGGL(k_head_reduce, dim3(blocks_for((int64_t)a.C * a.V, 256)), dim3(256), 0, st, part,
+                           (int64_t)pl.split3, (int64_t)a.C * a.V, c.d.dw, TYPE, scale_d, a.gpart);
+    }
+    if (c.d.db)
+      hipLaunchKernelGGL(k_head_db, dim3((unsigned)(a.Vp / 64)), dim3(256), 0, st, a.dbp, row_blocks, a.Vp, a.V,
+                         reinterpret_cast<float*>(ws + pl.dba), (int)(i > 0), (int)last, c.d.db, TYPE, scale, a.gpart);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+int64_t head_workspace(const reno_head& p, int k, bool grad) { return make_plan(p, k, grad).bytes; }
+
+hipError_t launch_head(const HeadCall& c, hipStream_t st) {
+  switch (c.p.type) {
+    case RENO_T_FP32: return run_head<RENO_T_FP32>(c, st);
+    case RENO_T_BF16: return run_head<RENO_T_BF16>(c, st);
+    default: return run_head<RENO_T_FP16>(c, st);
+  }
+}
+
+}  // namespace reno

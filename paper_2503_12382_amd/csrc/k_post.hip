@@ -889,4 +889,30 @@ hipError_t launch_neighbor_map(Ctx& c, int b, int32_t* out) {
   return hipGetLastError();
 }
 
+// Features of the model scales b_lo .. b_hi, whose packed rows are consecutive,
+// without the balance that the stored rows carry (a power of two; 0 where no
+// head weight reads the channel, whose values are then lost).
+__global__ void __launch_bounds__(256) k_copy_features(const int32_t* __restrict__ count,
+                                                       const int32_t* __restrict__ moff, int b_lo, int b_hi,
+                                                       int64_t cap_model, int C, const float* __restrict__ hL,
+                                                       const float* __restrict__ bal, float* __restrict__ out) {
+  const int64_t first = moff[b_lo];
+  int64_t rows = 0;
+  for (int b = b_lo; b <= b_hi; ++b) {
+    if ((int64_t)moff[b] + count[b] > cap_model) break;
+    rows += count[b];
+  }
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * C; i += (int64_t)gridDim.x * 256) {
+    const float f = bal[i % C];
+    out[i] = f > 0.0f ? hL[first * C + i] / f : NAN;
+  }
+}
+
+hipError_t launch_features(Ctx& c, int b_lo, int b_hi, float* out) {
+  ProfScope ps_(c, RENO_K_OTHER);
+  hipLaunchKernelGGL(k_copy_features, dim3(grid_for(c.cap_model * c.p.channels, 256)), dim3(256), 0, c.stream, c.d_count,
+                     c.d_moff, b_lo, b_hi, (int64_t)c.cap_model, c.p.channels, c.hlast(), c.w_hbal, out);
+  return hipGetLastError();
+}
+
 }  // namespace reno
