@@ -1,9 +1,19 @@
 // The k largest logits of each row with the row's normaliser (reno_head.h).
 //
 // A logit's order and its index are one 64-bit key: the float's bits as an
-// integer that sorts the same way (NaN above everything), then the index
-// complemented, so that the largest key is the largest logit of the lowest
-// index and no two keys are equal.
+// integer that sorts the same way (NaN above everything, -0 with +0), then the
+// index complemented, so that the largest key is the largest logit of the
+// lowest index and no two keys are equal.  Bound by the one read of the logits
+// as long as a row's selection costs fewer instructions than its bytes take:
+//   k_top_short  rows of up to 256: 16 lanes a row, so that one wave's
+//                instructions serve four rows; every lane sorts its 16 logits
+//                in registers, then the largest head of 16 sorted lists is
+//                taken k times
+//   k_top_long   a block a row.  The k-th largest of many groups' maxima bounds
+//                the k-th largest logit from below, so a second look at the row
+//                (from L2) keeps little more than k candidates, whose ranks are
+//                counted; rows with too many equal logits for that are cut
+//                exactly, by a radix selection
 
 #include <algorithm>
 
@@ -23,63 +33,374 @@ __device__ __forceinline__ float logit(const void* p, int64_t i) {
   else return (float)static_cast<const _Float16*>(p)[i];
 }
 
-// An unsigned integer in the order of the floats: all NaN on top, -0 with +0.
+// logits of 16 bytes in memory
+template <int TYPE>
+struct Vec {
+  static constexpr int N = TYPE == RENO_T_FP32 ? 4 : 8;
+  float x[N];
+  __device__ __forceinline__ void load(const void* p, int64_t i) {
+    if constexpr (TYPE == RENO_T_FP32) {
+      const float4 v = *reinterpret_cast<const float4*>(static_cast<const float*>(p) + i);
+      x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
+    } else {
+      const uint4 v = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + i);
+      const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if constexpr (TYPE == RENO_T_BF16) {
+          x[2 * e] = __uint_as_float(u[e] << 16);
+          x[2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u);
+        } else {
+          x[2 * e] = (float)__builtin_bit_cast(_Float16, (uint16_t)u[e]);
+          x[2 * e + 1] = (float)__builtin_bit_cast(_Float16, (uint16_t)(u[e] >> 16));
+        }
+      }
+    }
+  }
+};
+
+// An unsigned integer in the order of the floats, from 1 (0: no logit).
 __device__ __forceinline__ uint32_t ordered(float x) {
-  if (x != x) return 0xfffffffeu;  // below the key of nothing, all ones
+  if (x != x) return 0xfffffffeu;
   const uint32_t u = __float_as_uint(x + 0.0f);
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
-__device__ __forceinline__ uint64_t key_of(float x, uint32_t i) { return (uint64_t)ordered(x) << 32 | (uint32_t)~i; }
+__device__ __forceinline__ float from_ordered(uint32_t o) {
+  if (o == 0xfffffffeu) return NAN;
+  return o == 0 ? -INFINITY : __uint_as_float(o & 0x80000000u ? o & 0x7fffffffu : ~o);
+}
+__device__ __forceinline__ uint64_t make_key(uint32_t o, uint32_t i) { return (uint64_t)o << 32 | (uint32_t)~i; }
 
-__device__ __forceinline__ uint64_t wave_max64(uint64_t v) {
-  for (int o = 32; o > 0; o >>= 1) {
-    const uint64_t w = __shfl_xor(v, o);
-    v = w > v ? w : v;
-  }
-  return v;
+// ---------------------------------------------------------------------------
+// Rows of up to 256 logits.  233737 rows of 256 fp32, k = 16: see launch_top.
+
+constexpr int SHORT_LANE = 16;      // logits of a lane, lanes of a row
+constexpr int SHORT_ROWS = 4;       // rows of a wave
+
+__device__ __forceinline__ uint32_t row16_max(uint32_t v) {
+  v = max(v, dpp<0x128>(v));
+  v = max(v, dpp<0x124>(v));
+  v = max(v, dpp<0x122>(v));
+  return max(v, dpp<0x121>(v));
+}
+__device__ __forceinline__ float row16_sum(float v) {
+  v += __uint_as_float(dpp<0x128>(__float_as_uint(v)));
+  v += __uint_as_float(dpp<0x124>(__float_as_uint(v)));
+  v += __uint_as_float(dpp<0x122>(__float_as_uint(v)));
+  return v + __uint_as_float(dpp<0x121>(__float_as_uint(v)));
 }
 
-// One wave a row: k times the largest key below the last one.
-template <int TYPE>
-__global__ void __launch_bounds__(256) k_top_scan(const void* __restrict__ z, int64_t rows, int V, int64_t stride, int k,
-                                                  int32_t* __restrict__ index, float* __restrict__ value,
-                                                  float* __restrict__ lse) {
-  const int lane = lane_id();
-  const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (r >= rows) return;
+// PL: logits of a lane (a power of two, 16 PL >= V); a lane's are consecutive, so that of two lanes with
+// equal heads the lower one holds the lower index.
+template <int TYPE, int PL>
+__global__ void __launch_bounds__(256) k_top_short(const void* __restrict__ z, int64_t rows, int V, int64_t stride, int k,
+                                                   int wide, int32_t* __restrict__ index, float* __restrict__ value,
+                                                   float* __restrict__ lse) {
+  __shared__ uint64_t s_list[4][PL + 1][64];               // sorted lists, a row of lanes for each place
+  __shared__ uint64_t s_out[4][SHORT_ROWS * RENO_HEAD_MAX_TOP];
+  const int lane = lane_id(), wave = threadIdx.x >> 6, l15 = lane & 15, rw = lane >> 4;
+  const int64_t r0 = ((int64_t)blockIdx.x * 4 + wave) * SHORT_ROWS;
+  if (r0 >= rows) return;
+  const int64_t r = min(r0 + rw, rows - 1);
   const int64_t at = r * stride;
-  uint64_t below = ~uint64_t(0);
-  float first = 0.0f;
-  for (int j = 0; j < k; ++j) {
-    uint64_t best = 0;
-    for (int v = lane; v < V; v += 64) {
-      const uint64_t key = key_of(logit<TYPE>(z, at + v), (uint32_t)v);
-      if (key < below && key > best) best = key;
+  const int v0 = l15 * PL;
+  float x[PL];
+  if (PL == SHORT_LANE && wide && v0 + PL <= V) {
+#pragma unroll
+    for (int i = 0; i < PL; i += Vec<TYPE>::N) {
+      Vec<TYPE> t;
+      t.load(z, at + v0 + i);
+#pragma unroll
+      for (int e = 0; e < Vec<TYPE>::N && i + e < PL; ++e) x[i + e] = t.x[e];
     }
-    best = wave_max64(best);
-    const uint32_t i = ~(uint32_t)best;
-    const bool have = best != 0;
-    const float x = have ? logit<TYPE>(z, at + i) : -INFINITY;
-    if (lane == 0) {
-      index[r * k + j] = have ? (int32_t)i : -1;
-      value[r * k + j] = x;
-    }
-    if (j == 0) first = x;
-    below = best;
+  } else {
+#pragma unroll
+    for (int i = 0; i < PL; ++i) x[i] = v0 + i < V ? logit<TYPE>(z, at + v0 + i) : 0.0f;
   }
-  if (!lse) return;
-  const float base = first > -INFINITY ? first : 0.0f;
-  float s = 0.0f;
-  for (int v = lane; v < V; v += 64) s += __builtin_amdgcn_exp2f((logit<TYPE>(z, at + v) - base) * LOG2E);
-  for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
-  if (lane == 0) lse[r] = base + __builtin_amdgcn_logf(s) * LN2;
+  uint64_t key[PL];
+#pragma unroll
+  for (int i = 0; i < PL; ++i) key[i] = v0 + i < V ? make_key(ordered(x[i]), (uint32_t)(v0 + i)) : 0;
+  // a lane's list, largest first: odd-even merges of runs of p
+#pragma unroll
+  for (int p = 1; p < PL; p *= 2)
+#pragma unroll
+    for (int q = p; q >= 1; q /= 2)
+#pragma unroll
+      for (int j = q % p; j + q < PL; j += 2 * q)
+#pragma unroll
+        for (int i = 0; i < q; ++i)
+          if (i + j + q < PL && (i + j) / (2 * p) == (i + j + q) / (2 * p)) {
+            const uint64_t a = key[i + j], b = key[i + j + q];
+            const bool swap = a < b;
+            key[i + j] = swap ? b : a;
+            key[i + j + q] = swap ? a : b;
+          }
+#pragma unroll
+  for (int i = 0; i < PL; ++i) s_list[wave][i][lane] = key[i];
+  s_list[wave][PL][lane] = 0;
+  wave_lds_fence();
+  if (lse) {
+    const float m = from_ordered(row16_max((uint32_t)(key[0] >> 32)));
+    const float base = m > -INFINITY ? m : 0.0f;
+    float s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < PL; ++i) s += v0 + i < V ? __builtin_amdgcn_exp2f((x[i] - base) * LOG2E) : 0.0f;
+    s = row16_sum(s);
+    if (l15 == 0 && r0 + rw < rows) lse[r] = m != m ? m : base + __builtin_amdgcn_logf(s) * LN2;
+  }
+  uint64_t head = key[0];
+  int place = 0;
+  for (int j = 0; j < k; ++j) {
+    const uint32_t o = (uint32_t)(head >> 32);
+    const uint32_t top = row16_max(o);
+    const uint32_t tied = (uint32_t)(__ballot(o == top) >> (lane & 48)) & 0xffffu;
+    const bool won = (tied & (0u - tied)) == 1u << l15;
+    if (won) s_out[wave][rw * k + j] = head;
+    place += won && place < PL ? 1 : 0;
+    head = s_list[wave][place][lane];
+  }
+  wave_lds_fence();
+  const int n = (int)min((int64_t)SHORT_ROWS, rows - r0) * k;
+  for (int i = lane; i < n; i += 64) {
+    const uint64_t h = s_out[wave][i];
+    index[r0 * k + i] = h ? (int32_t)~(uint32_t)h : -1;
+    value[r0 * k + i] = from_ordered((uint32_t)(h >> 32));
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Longer rows: a block a row.
+
+constexpr int LONG_CAP = 1024;      // candidates kept
+constexpr int LONG_GROUPS = 4;      // groups of a thread
+
+template <int TYPE, int THREADS>
+struct LongRow {
+  const void* z;
+  int64_t at;
+  int V;
+  bool wide;   // 16-byte loads
+
+  // f(index, logit) for every logit, in an order of its own
+  template <typename F>
+  __device__ __forceinline__ void each(const F& f) const {
+    constexpr int N = Vec<TYPE>::N;
+    const int tid = threadIdx.x;
+    const int whole = wide ? V / N : 0;
+    for (int i = tid; i < whole; i += THREADS) {
+      Vec<TYPE> t;
+      t.load(z, at + (int64_t)i * N);
+#pragma unroll
+      for (int e = 0; e < N; ++e) f(i * N + e, t.x[e]);
+    }
+    for (int v = whole * N + tid; v < V; v += THREADS) f(v, logit<TYPE>(z, at + v));
+  }
+};
+
+template <int THREADS>
+__device__ __forceinline__ int block_count(int mine, int* s, int phase) {
+  // sum of one value a wave; two buffers, so that one barrier a call is enough
+  const int wave = threadIdx.x >> 6;
+  int* b = s + (phase & 1) * (THREADS / 64);
+  if (lane_id() == 0) b[wave] = mine;
+  __syncthreads();
+  int n = 0;
+#pragma unroll
+  for (int i = 0; i < THREADS / 64; ++i) n += b[i];
+  return n;
+}
+
+// Exact cut of a row: the k-th largest ordered value *cut and how many lie above it.
+template <int TYPE, int THREADS>
+__device__ void radix_cut(const LongRow<TYPE, THREADS>& row, int k, uint32_t* hist, uint32_t* found, uint32_t* cut,
+                          int* above) {
+  uint32_t prefix = 0;
+  int want = k;
+  for (int shift = 24; shift >= 0; shift -= 8) {
+    for (int i = threadIdx.x; i < 256; i += THREADS) hist[i] = 0;
+    __syncthreads();
+    row.each([&](int, float x) {
+      const uint32_t o = ordered(x);
+      if (shift == 24 || o >> (shift + 8) == prefix >> (shift + 8)) {
+        const uint32_t bin = o >> shift & 255u;
+        // equal logits fall into one bin: one add for all lanes that agree with the first
+        const uint32_t first = (uint32_t)__builtin_amdgcn_readfirstlane((int)bin);
+        const uint64_t same = __ballot(bin == first);
+        if (bin != first) atomicAdd(&hist[bin], 1u);
+        else if (rank_below(same) == 0) atomicAdd(&hist[bin], (uint32_t)__popcll(same));
+      }
+    });
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      int left = want, b = 255;
+      while (b > 0 && (int)hist[b] < left) left -= (int)hist[b--];
+      found[0] = (uint32_t)b;
+      found[1] = (uint32_t)left;
+    }
+    __syncthreads();
+    prefix |= found[0] << shift;
+    want = (int)found[1];
+    __syncthreads();
+  }
+  *cut = prefix;
+  *above = k - want;
+}
+
+template <int TYPE, int THREADS>
+__global__ void __launch_bounds__(THREADS) k_top_long(const void* __restrict__ z, int V, int64_t stride, int k, int wide,
+                                                      int32_t* __restrict__ index, float* __restrict__ value,
+                                                      float* __restrict__ lse) {
+  constexpr int WAVES = THREADS / 64, N = Vec<TYPE>::N;
+  __shared__ uint64_t s_key[LONG_CAP];
+  __shared__ uint32_t s_hist[256];
+  __shared__ uint32_t s_found[2];
+  __shared__ int s_sum[2 * WAVES];
+  __shared__ float2 s_ms[WAVES];
+  __shared__ int s_n;
+  const int tid = threadIdx.x, lane = lane_id(), wave = tid >> 6;
+  const int64_t r = blockIdx.x;
+  const LongRow<TYPE, THREADS> row{z, r * stride, V, wide != 0};
+  if (tid == 0) s_n = 0;
+  // one look: maxima of the thread's groups, running maximum and sum of exponentials
+  uint32_t group[LONG_GROUPS] = {};
+  float m = -INFINITY, s = 0.0f;
+  const int whole = row.wide ? V / N : 0;
+  const auto take = [&](const float (&x)[N], int n, uint32_t& g) {
+    float top = x[0];
+#pragma unroll
+    for (int e = 1; e < N; ++e) top = e < n ? fmaxf(top, x[e]) : top;
+    bool nan = false;
+#pragma unroll
+    for (int e = 0; e < N; ++e) nan |= e < n && x[e] != x[e];
+    g = max(g, nan ? 0xfffffffeu : ordered(top));
+    const float next = fmaxf(m, top);
+    const float base = next > -INFINITY ? next : 0.0f;
+    s *= __builtin_amdgcn_exp2f((m - base) * LOG2E);
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      if (e < n) s += __builtin_amdgcn_exp2f((x[e] - base) * LOG2E);
+    m = next;
+  };
+  for (int i0 = tid; i0 < whole; i0 += LONG_GROUPS * THREADS) {
+    Vec<TYPE> t[LONG_GROUPS];
+#pragma unroll
+    for (int u = 0; u < LONG_GROUPS; ++u)
+      if (i0 + u * THREADS < whole) t[u].load(z, row.at + (int64_t)(i0 + u * THREADS) * N);
+#pragma unroll
+    for (int u = 0; u < LONG_GROUPS; ++u)
+      if (i0 + u * THREADS < whole) take(t[u].x, N, group[u]);
+  }
+  for (int v0 = whole * N + tid; v0 < V; v0 += LONG_GROUPS * THREADS) {
+#pragma unroll
+    for (int u = 0; u < LONG_GROUPS; ++u)
+      if (v0 + u * THREADS < V) {
+        float x[N];
+        x[0] = logit<TYPE>(z, row.at + v0 + u * THREADS);
+        take(x, 1, group[u]);
+      }
+  }
+  // the row's normaliser
+  for (int o = 32; o > 0; o >>= 1) {
+    const float om = __shfl_xor(m, o), os = __shfl_xor(s, o);
+    const float next = fmaxf(m, om), base = next > -INFINITY ? next : 0.0f;
+    s = s * __builtin_amdgcn_exp2f((m - base) * LOG2E) + os * __builtin_amdgcn_exp2f((om - base) * LOG2E);
+    m = next;
+  }
+  if (lane == 0) s_ms[wave] = make_float2(m, s);
+  __syncthreads();
+  if (tid == 0 && lse) {
+    for (int i = 1; i < WAVES; ++i) {
+      const float2 o = s_ms[i];
+      const float next = fmaxf(m, o.x), base = next > -INFINITY ? next : 0.0f;
+      s = s * __builtin_amdgcn_exp2f((m - base) * LOG2E) + o.y * __builtin_amdgcn_exp2f((o.x - base) * LOG2E);
+      m = next;
+    }
+    const float base = m > -INFINITY ? m : 0.0f;
+    lse[r] = base + __builtin_amdgcn_logf(s) * LN2;
+  }
+  // the largest 16-bit prefix that at least k groups' maxima reach (0 where there are fewer groups)
+  uint32_t cut = 0;
+  for (int bit = 31; bit >= 16; --bit) {
+    const uint32_t next = cut | 1u << bit;
+    int n = 0;
+#pragma unroll
+    for (int u = 0; u < LONG_GROUPS; ++u) n += (int)__popcll(__ballot(group[u] >= next));
+    if (block_count<THREADS>(n, s_sum, bit) >= k) cut = next;
+  }
+  cut = max(cut, 1u);
+  row.each([&](int v, float x) {
+    const uint32_t o = ordered(x);
+    if (o >= cut) {
+      const int i = atomicAdd(&s_n, 1);
+      if (i < LONG_CAP) s_key[i] = make_key(o, (uint32_t)v);
+    }
+  });
+  __syncthreads();
+  int n = s_n;
+  if (n > LONG_CAP) {  // equal logits past the cut: what lies above the exact one, and the first that equal it
+    __syncthreads();
+    int above;
+    radix_cut(row, k, s_hist, s_found, &cut, &above);
+    if (tid == 0) s_n = 0;
+    __syncthreads();
+    row.each([&](int v, float x) {
+      const uint32_t o = ordered(x);
+      if (o > cut) s_key[atomicAdd(&s_n, 1)] = make_key(o, (uint32_t)v);
+    });
+    int have = above;
+    for (int v0 = 0, phase = 0; v0 < V && have < k; v0 += THREADS, ++phase) {
+      const int v = v0 + tid;
+      const bool eq = v < V && ordered(logit<TYPE>(z, row.at + v)) == cut;
+      const uint64_t b = __ballot(eq);
+      const int before_all = block_count<THREADS>((int)__popcll(b), s_sum, phase);
+      int before = 0;
+      for (int i = 0; i < wave; ++i) before += s_sum[(phase & 1) * WAVES + i];
+      const int at = have + before + (int)rank_below(b);
+      if (eq && at < k) s_key[at] = make_key(cut, (uint32_t)v);
+      have += before_all;
+    }
+    __syncthreads();
+    n = k;
+  }
+  // ranks among the candidates
+  for (int i = tid; i < n; i += THREADS) {
+    const uint64_t mine = s_key[i];
+    int rank = 0;
+    for (int j = 0; j < n; ++j) rank += s_key[j] > mine ? 1 : 0;
+    if (rank < k) {
+      index[r * k + rank] = (int32_t)~(uint32_t)mine;
+      value[r * k + rank] = from_ordered((uint32_t)(mine >> 32));
+    }
+  }
+  for (int j = n + tid; j < k; j += THREADS) {
+    index[r * k + j] = -1;
+    value[r * k + j] = -INFINITY;
+  }
 }
 
 template <int TYPE>
 void run(const void* z, int64_t rows, int V, int64_t stride, int k, int32_t* index, float* value, float* lse,
          hipStream_t st) {
-  hipLaunchKernelGGL(k_top_scan<TYPE>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, z, rows, V, stride, k, index,
-                     value, lse);
+  const int per = 16 / (TYPE == RENO_T_FP32 ? 4 : 2);
+  const int wide = (uintptr_t)z % 16 == 0 && stride % per == 0;
+  if (V <= 16 * SHORT_LANE) {
+    const dim3 grid((unsigned)((rows + 4 * SHORT_ROWS - 1) / (4 * SHORT_ROWS)));
+    const auto args = [&](auto kern) {
+      hipLaunchKernelGGL(kern, grid, dim3(256), 0, st, z, rows, V, stride, k, wide, index, value, lse);
+    };
+    if (V <= 16) args(k_top_short<TYPE, 1>);
+    else if (V <= 64) args(k_top_short<TYPE, 4>);
+    else args(k_top_short<TYPE, 16>);
+    return;
+  }
+  const dim3 grid((unsigned)rows);
+  const auto args = [&](auto kern, int threads) {
+    hipLaunchKernelGGL(kern, grid, dim3(threads), 0, st, z, V, stride, k, wide, index, value, lse);
+  };
+  // threads: about 32 logits each, so that the groups outnumber k several times
+  if (V <= 2048) args(k_top_long<TYPE, 64>, 64);
+  else if (V <= 65536) args(k_top_long<TYPE, 256>, 256);
+  else args(k_top_long<TYPE, 1024>, 1024);
 }
 
 }  // namespace
