@@ -19,10 +19,10 @@ BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(HERE, "libreno.so")
 ARCH = "gfx950"
 
-HIP_SOURCES = ["k_prep.hip", "k_dec.hip", "k_model.hip", "k_post.hip", "k_code.hip", "k_head.hip", "k_top.hip", "api.cpp",
-               "frame.cpp", "head.cpp"]
+HIP_SOURCES = ["k_prep.hip", "k_dec.hip", "k_model.hip", "k_post.hip", "k_code.hip", "k_head.hip",
+               "k_head_narrow.hip", "k_top.hip", "api.cpp", "frame.cpp", "head.cpp"]
 HOST_SOURCES = ["rans.cpp"]
-HEADERS = ["dev.h", "ctx.h", "head.h", "gemm.h"]
+HEADERS = ["dev.h", "ctx.h", "head.h", "head_dev.h", "gemm.h"]
 
 
 def hipcc() -> str:

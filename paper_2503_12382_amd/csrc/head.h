@@ -23,6 +23,20 @@ struct HeadCall {
   char* ws = nullptr;
 };
 
+// Targets of the rows: as given (code length: one symbol a row, the rest null),
+// or a distillation's entries with those of one index joined.
+struct HeadTargets {
+  const int32_t* index;   // [N][k], -1: none
+  const float* q;         // [N][k]
+  const float* ent;       // [N] sum q log2 q
+  const uint8_t* flag;    // [N] 0: left out, 1: taken, 2: an index outside the alphabet
+};
+
+// fp32 heads that one kernel takes whole (k_head_narrow.hip)
+bool head_is_narrow(const reno_head& p);
+int64_t head_narrow_bytes(const reno_head& p, bool grad);
+hipError_t launch_head_narrow(const HeadCall& c, const HeadTargets& t, char* ws, hipStream_t stream);
+
 int64_t head_workspace(const reno_head& p, int k, bool grad);
 hipError_t launch_head(const HeadCall& c, hipStream_t stream);
 hipError_t launch_top(const void* logits, int type, int64_t rows, int symbols, int64_t stride, int k, int32_t* index,

@@ -1,0 +1,59 @@
+// Device helpers that the kernels of the head's training operators share.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "gemm.h"
+
+namespace reno {
+
+constexpr float LN2 = 0.6931471805599453f;
+
+__device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float log2_hw(float x) { return __builtin_amdgcn_logf(x); }
+
+// The three bf16 planes of x: each takes the leading 8 bits of what is left, cut off, so that
+// the parts add up to x exactly.  An infinity or NaN stays in the first.
+__device__ __forceinline__ void split3(float x, uint16_t (&o)[3]) {
+  const uint32_t u = __float_as_uint(x);
+  o[0] = (uint16_t)(u >> 16);
+  if ((u & 0x7f800000u) == 0x7f800000u) {
+    if ((u & 0x007fffffu) != 0) o[0] |= 0x40;  // a NaN whose payload lies below stays one
+    o[1] = o[2] = 0;
+    return;
+  }
+  float r = x - __uint_as_float(u & 0xffff0000u);
+  const uint32_t v = __float_as_uint(r);
+  o[1] = (uint16_t)(v >> 16);
+  r -= __uint_as_float(v & 0xffff0000u);
+  o[2] = (uint16_t)(__float_as_uint(r) >> 16);
+}
+
+// The planes of 8 values as three fragments.  An infinity leaves NaN in the lower planes (inf - inf), so
+// products with it are NaN where fp32 might keep an infinity; NaN stays NaN.
+__device__ __forceinline__ void split_any8(const float (&x)[8], s16x8 (&o)[3]) {
+  uint32_t w[3][4];
+#pragma unroll
+  for (int e = 0; e < 8; e += 2) {
+    uint32_t p[3][2];
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const uint32_t u = __float_as_uint(x[e + q]);
+      const float r = x[e + q] - __uint_as_float(u & 0xffff0000u);
+      const uint32_t v = __float_as_uint(r);
+      p[0][q] = u;
+      p[1][q] = v;
+      p[2][q] = __float_as_uint(r - __uint_as_float(v & 0xffff0000u));
+    }
+#pragma unroll
+    for (int t = 0; t < 3; ++t) w[t][e / 2] = __builtin_amdgcn_perm(p[t][1], p[t][0], 0x07060302u);
+  }
+#pragma unroll
+  for (int t = 0; t < 3; ++t) {
+    const i32x4 v = {(int)w[t][0], (int)w[t][1], (int)w[t][2], (int)w[t][3]};
+    o[t] = __builtin_bit_cast(s16x8, v);
+  }
+}
+
+}  // namespace reno

@@ -24,17 +24,14 @@
 #include "dev.h"
 #include "gemm.h"
 #include "head.h"
+#include "head_dev.h"
 
 namespace reno {
 namespace {
 
-constexpr float LN2 = 0.6931471805599453f;
 constexpr int GPARTS = 64;       // partial maxima of |g|
 constexpr int DZ_ROWS = 64;      // rows of a wave of k_head_dz
 constexpr int HALF_SHIFT = 14;   // dz in fp16 is scaled by 2^14
-
-__device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
-__device__ __forceinline__ float log2_hw(float x) { return __builtin_amdgcn_logf(x); }
 
 // ---- element types ----
 template <int TYPE>
@@ -45,23 +42,6 @@ __device__ __forceinline__ float load_as_float(const void* p, int64_t i) {
 }
 __device__ __forceinline__ uint16_t to_bf16(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
 __device__ __forceinline__ uint16_t to_fp16(float x) { return __builtin_bit_cast(uint16_t, (_Float16)x); }
-
-// The three bf16 planes of x: each takes the leading 8 bits of what is left, cut off, so that
-// the parts add up to x exactly.  An infinity or NaN stays in the first.
-__device__ __forceinline__ void split3(float x, uint16_t (&o)[3]) {
-  const uint32_t u = __float_as_uint(x);
-  o[0] = (uint16_t)(u >> 16);
-  if ((u & 0x7f800000u) == 0x7f800000u) {
-    if ((u & 0x007fffffu) != 0) o[0] |= 0x40;  // a NaN whose payload lies below stays one
-    o[1] = o[2] = 0;
-    return;
-  }
-  float r = x - __uint_as_float(u & 0xffff0000u);
-  const uint32_t v = __float_as_uint(r);
-  o[1] = (uint16_t)(v >> 16);
-  r -= __uint_as_float(v & 0xffff0000u);
-  o[2] = (uint16_t)(__float_as_uint(r) >> 16);
-}
 
 template <int TYPE, int PLANES>
 __device__ __forceinline__ void to_planes(float x, uint16_t (&o)[PLANES]) {
@@ -605,7 +585,7 @@ struct Plan {
   bool big1, big2, big3;
   int split2, split3;
   // offsets into the workspace
-  int64_t bias, wp, idx, q, ent, flag, gpart, hp, part, tt, lse2, t, dz, dbp, dba, dhp, dwp, bytes;
+  int64_t idx, q, ent, flag, narrow, bias, wp, gpart, hp, part, tt, lse2, t, dz, dbp, dba, dhp, dwp, bytes;
 };
 
 bool w_in_place(const reno_head& p, const void* w) {
@@ -615,6 +595,22 @@ bool w_in_place(const reno_head& p, const void* w) {
 
 Plan make_plan(const reno_head& p, int k, bool grad) {
   Plan a{};
+  const int64_t N = std::max<int64_t>(p.rows, 1);
+  int64_t at = 0;
+  const auto take = [&](int64_t bytes) {
+    const int64_t o = at;
+    at += up(bytes, 256);
+    return o;
+  };
+  a.idx = take(N * k * 4);
+  a.q = take(N * k * 4);
+  a.ent = take(N * 4);
+  a.flag = take(N);
+  a.narrow = at;
+  if (head_is_narrow(p)) {
+    a.bytes = at + std::max<int64_t>(256, head_narrow_bytes(p, grad));
+    return a;
+  }
   a.planes = planes_of(p.type);
   a.terms = p.type == RENO_T_FP32 ? GEMM_TERMS : 1;
   a.Cp = up(p.channels, GEMM_BK);
@@ -623,7 +619,6 @@ Plan make_plan(const reno_head& p, int k, bool grad) {
   // a piece: at most 2^28 logits (2^27 in fp32) where they are kept for the
   // gradient, 2^32 where they are not
   const int64_t most = !grad ? int64_t(1) << 32 : p.type == RENO_T_FP32 ? int64_t(1) << 27 : int64_t(1) << 28;
-  const int64_t N = std::max<int64_t>(p.rows, 1);
   int64_t R = std::max<int64_t>(256, most / a.Vp / 256 * 256);
   a.pieces = (N + R - 1) / R;
   a.R = std::min(N, up((N + a.pieces - 1) / a.pieces, 256));
@@ -639,18 +634,8 @@ Plan make_plan(const reno_head& p, int k, bool grad) {
   };
   a.split2 = splits_for(tiles(a.big2, p.channels, a.R), a.Vp, a.terms);
   a.split3 = splits_for(tiles(a.big3, p.symbols, p.channels), a.R, a.terms);
-  int64_t at = 0;
-  const auto take = [&](int64_t bytes) {
-    const int64_t o = at;
-    at += up(bytes, 256);
-    return o;
-  };
   a.bias = take(a.Vb * 4);
   a.wp = take(a.planes * (int64_t)p.channels * a.Vp * 2);
-  a.idx = take(N * k * 4);
-  a.q = take(N * k * 4);
-  a.ent = take(N * 4);
-  a.flag = take(N);
   a.gpart = take(GPARTS * 4);
   a.hp = take(a.planes * a.R * a.Cp * 2);
   a.part = take(parts * a.R * 8);
@@ -709,6 +694,17 @@ hipError_t run_head(const HeadCall& c, hipStream_t st) {
   }
   const Plan pl = make_plan(p, c.k, c.grad);
   char* ws = c.ws;
+  HeadTargets t{c.index, nullptr, nullptr, nullptr};
+  if (c.logit) {
+    int32_t* idx = reinterpret_cast<int32_t*>(ws + pl.idx);
+    float* q = reinterpret_cast<float*>(ws + pl.q);
+    float* ent = reinterpret_cast<float*>(ws + pl.ent);
+    uint8_t* flag = reinterpret_cast<uint8_t*>(ws + pl.flag);
+    hipLaunchKernelGGL(k_head_targets, dim3((unsigned)((N + 3) / 4)), dim3(256), 0, st, c.index, c.logit, N, c.k, p.symbols,
+                       (float)(1.4426950408889634 / (double)c.temperature), idx, q, ent, flag);
+    t = HeadTargets{idx, q, ent, flag};
+  }
+  if (head_is_narrow(p)) return launch_head_narrow(c, t, ws + pl.narrow, st);
   HeadArgs a{};
   a.N = N;
   a.C = p.channels;
@@ -735,19 +731,10 @@ hipError_t run_head(const HeadCall& c, hipStream_t st) {
   a.lse2 = reinterpret_cast<float*>(ws + pl.lse2);
   a.bits = c.d.bits;
   a.lse = c.d.lse;
-  a.index = c.index;
-  if (c.logit) {
-    int32_t* idx = reinterpret_cast<int32_t*>(ws + pl.idx);
-    float* q = reinterpret_cast<float*>(ws + pl.q);
-    float* ent = reinterpret_cast<float*>(ws + pl.ent);
-    uint8_t* flag = reinterpret_cast<uint8_t*>(ws + pl.flag);
-    hipLaunchKernelGGL(k_head_targets, dim3((unsigned)((N + 3) / 4)), dim3(256), 0, st, c.index, c.logit, N, c.k, p.symbols,
-                       a.scale, idx, q, ent, flag);
-    a.index = idx;
-    a.q = q;
-    a.ent = ent;
-    a.flag = flag;
-  }
+  a.index = t.index;
+  a.q = t.q;
+  a.ent = t.ent;
+  a.flag = t.flag;
   if (c.grad) {
     a.t = reinterpret_cast<float*>(ws + pl.t);
     a.dz = reinterpret_cast<uint16_t*>(ws + pl.dz);

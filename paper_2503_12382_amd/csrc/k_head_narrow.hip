@@ -1,0 +1,527 @@
+// Narrow fp32 heads (C <= 128, V <= 256: the codec's own): code length and
+// distillation with their gradients in one pass over the rows.
+//
+// A block of 8 waves takes 128 rows at a time, 16 a wave, all V logits of
+// a row in the registers of 4 lanes: softmax statistics are two lane exchanges,
+// and nothing of the logits goes to memory.  Every operand is three bf16 parts
+// (24 bits), a product the six terms above 2^-24.
+//   z   = W^T h     A: 16 symbols x 32 channels of W, B: 32 channels x 16 rows
+//   dh  = W dz      the accumulator layout of z (row = lane & 15, symbols 4 (lane >> 4) + i
+//                   of each 16) taken as it is for B: k runs over the symbols in that
+//                   order, and W is read in the same one
+//   dw  = h dz^T    k runs over rows, so dz crosses lanes through LDS, 64 symbols of
+//                   128 rows at a time, and is read back transposed; each wave holds the
+//                   sums of its own tiles of dw over all rows of the block
+// W lies in LDS for C <= 32 (one copy serves both products: transposed reads
+// for z, rows for dh); wider ones stream from L2, laid out as the lanes read them.
+// The blocks' sums of dw and db are joined in a fixed order by k_narrow_join.
+//
+// Bound: matrix instructions (6 terms x 3 products) and the vector work of a
+// logit (scaling, exponential, splitting: about 17 instructions) take turns;
+// memory would allow several times the rate.
+
+#include <algorithm>
+
+#include "dev.h"
+#include "gemm.h"
+#include "head.h"
+#include "head_dev.h"
+
+namespace reno {
+namespace {
+
+constexpr int NB_WAVES = 8, NB_THREADS = 64 * NB_WAVES, NB_ROWS = 16 * NB_WAVES;
+constexpr int NB_BLOCKS = 256;      // one a CU
+
+struct NarrowArgs {
+  int64_t N;
+  int C, V, k;
+  int64_t h_stride, w_stride;
+  const float *h, *w, *b, *g;
+  const int32_t* index;    // [N][k]
+  const float* q;          // [N][k] joined probabilities, or null: one entry with 1
+  const float* ent;
+  const uint8_t* flag;
+  float scale, out_scale;  // log2(e) / T, 1 / (T ln 2)
+  const uint16_t* wz;      // streamed W: [16 symbols][32 channels] fragments, then [16 channels][32 symbols]
+  const uint16_t* wd;
+  float *bits, *lse, *dh;
+  float* part;             // [blocks][C + 2][V]: dw, two halves of db
+  int wide;                // rows of h in 16-byte pieces
+};
+
+// acc += the six terms of a b, the smallest first
+__device__ __forceinline__ f32x4 mfma6(const s16x8 (&a)[3], const s16x8 (&b)[3], f32x4 acc) {
+  acc = mfma<false>(a[2], b[0], acc);
+  acc = mfma<false>(a[0], b[2], acc);
+  acc = mfma<false>(a[1], b[1], acc);
+  acc = mfma<false>(a[1], b[0], acc);
+  acc = mfma<false>(a[0], b[1], acc);
+  return mfma<false>(a[0], b[0], acc);
+}
+
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+__device__ __forceinline__ s16x8 read_tr(const char* lo, const char* hi) {
+  const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)lo);
+  const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)hi);
+  return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+// Places of 32-byte slots so that a transposed read (one slot of 16 rows 8 g + j) meets each bank twice
+// at most, for rows of 512 or 256, 128 and 64 bytes.
+__device__ __forceinline__ int swz512(int r) { return (r & 3) | ((r >> 3 & 1) << 2); }
+__device__ __forceinline__ int swz128(int r) { return (r >> 1 & 1) | ((r >> 3 & 1) << 1); }
+template <int CP>
+__device__ __forceinline__ int swz_h(int r) {
+  if constexpr (CP == 32) return r >> 3 & 1;
+  else if constexpr (CP == 64) return swz128(r);
+  else return swz512(r);
+}
+
+template <int CT, int VQ, bool GRAD>
+struct NarrowLds {
+  static constexpr int CP = 16 * CT;
+  static constexpr bool W_HERE = CT == 2;
+  static constexpr int W_PLANE = CP * VQ * 128, H_PLANE = NB_ROWS * CP * 2, D_PLANE = NB_ROWS * 128;
+  static constexpr int W = 0, H = W + (W_HERE ? 3 * W_PLANE : 0), D = H + (GRAD ? 3 * H_PLANE : 0);
+  static constexpr int Q = D + 3 * D_PLANE;   // D also holds the targets' probabilities
+  static constexpr int B = Q, BYTES = B + VQ * 64 * 4;
+};
+
+// VQ: 64 symbols each; rows of W in LDS are 128 VQ bytes
+template <int VQ>
+__device__ __forceinline__ int swz_w(int c) {
+  if constexpr (VQ == 4) return swz512(c);
+  else return swz128(c);
+}
+
+// DENSE: targets with probabilities (a distillation); the registers then keep the logits, whose
+// exponentials are taken again for dz, so that no probability is too small for its bits.
+template <int CT, int VQ, bool GRAD, bool DENSE>
+__global__ void __launch_bounds__(NB_THREADS) k_narrow(NarrowArgs a) {
+  using L = NarrowLds<CT, VQ, GRAD>;
+  constexpr int CP = L::CP, KS = CP / 32, VT = 4 * VQ;
+  __shared__ __attribute__((aligned(1024))) char lds[L::BYTES];
+  const int tid = threadIdx.x, lane = tid & 63, l15 = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  float* s_bias = reinterpret_cast<float*>(lds + L::B);
+  for (int i = tid; i < VQ * 64; i += NB_THREADS) s_bias[i] = i >= a.V ? -INFINITY : a.b ? a.b[i] * a.scale : 0.0f;
+  if constexpr (L::W_HERE) {
+    for (int i = tid; i < CP * VQ * 8; i += NB_THREADS) {  // 8 symbols of a channel
+      const int c = i / (VQ * 8), v = i % (VQ * 8) * 8;
+      float x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = c < a.C && v + e < a.V ? a.w[c * a.w_stride + v + e] : 0.0f;
+      s16x8 p[3];
+      split_any8(x, p);
+#pragma unroll
+      for (int t = 0; t < 3; ++t)
+        *reinterpret_cast<s16x8*>(lds + L::W + t * L::W_PLANE + c * (VQ * 128) + ((v / 16) ^ swz_w<VQ>(c)) * 32 +
+                                  (v & 8) * 2) = p[t];
+    }
+  }
+  __syncthreads();
+  // What the loop over rows reads of W is the same every time, but does not fit the registers: with the lane and
+  // the pointers opaque to the compiler it is not taken out of the loop (and spilled).
+  int lane_w = lane;
+  const uint16_t *wz = a.wz, *wd = a.wd;
+  // fragments of W: 16 symbols x 32 channels (z), and 16 channels x 32 symbols in the order of z's registers (dh)
+  const auto frag_z = [&](int vt, int ks, s16x8 (&o)[3]) {
+    if constexpr (L::W_HERE) {
+      const int c = 32 * ks + 8 * (lane_w >> 4) + (lane_w >> 2 & 3);
+      const char* p = lds + L::W + c * (VQ * 128) + (lane_w & 3) * 8;
+      const int s0 = (vt ^ swz_w<VQ>(c)) * 32, s1 = (vt ^ swz_w<VQ>(c + 4)) * 32 + 4 * (VQ * 128);
+#pragma unroll
+      for (int t = 0; t < 3; ++t) o[t] = read_tr(p + t * L::W_PLANE + s0, p + t * L::W_PLANE + s1);
+    } else {
+      const s16x8* p = reinterpret_cast<const s16x8*>(wz) + (vt * KS + ks) * 192 + lane_w;
+#pragma unroll
+      for (int t = 0; t < 3; ++t) o[t] = p[t * 64];
+    }
+  };
+  const auto frag_d = [&](int u, int ct, s16x8 (&o)[3]) {
+    if constexpr (L::W_HERE) {
+      const int c = 16 * ct + (lane_w & 15), f = swz_w<VQ>(c);
+      const char* p = lds + L::W + c * (VQ * 128) + (lane_w >> 4) * 8;
+#pragma unroll
+      for (int t = 0; t < 3; ++t) {
+        const s16x4 lo = *reinterpret_cast<const s16x4*>(p + t * L::W_PLANE + ((2 * u) ^ f) * 32);
+        const s16x4 hi = *reinterpret_cast<const s16x4*>(p + t * L::W_PLANE + ((2 * u + 1) ^ f) * 32);
+        o[t] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+      }
+    } else {
+      const s16x8* p = reinterpret_cast<const s16x8*>(wd) + (u * CT + ct) * 192 + lane_w;
+#pragma unroll
+      for (int t = 0; t < 3; ++t) o[t] = p[t * 64];
+    }
+  };
+
+  constexpr int DW_N = CT * 4 / NB_WAVES > 0 ? CT * 4 / NB_WAVES : 1;   // tiles of dw a wave holds of 64 symbols
+  f32x4 dw[GRAD ? VQ : 1][DW_N], db[GRAD ? VQ : 1];
+  if constexpr (GRAD) {
+#pragma unroll
+    for (int i = 0; i < VQ; ++i) {
+      db[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < DW_N; ++j) dw[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+  }
+  const int64_t steps = (a.N + NB_ROWS - 1) / NB_ROWS;
+  // this lane's piece of its row: channels 32 ks + 8 g .. + 7
+  float x[KS][8];
+  const auto load_h = [&](int64_t step) {
+    const int64_t r = step * NB_ROWS + 16 * wave + l15;
+    const bool in = r < a.N;
+    const float* p = a.h + r * a.h_stride;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      const int c = 32 * ks + 8 * g;
+      if (a.wide && in && c + 8 <= a.C) {
+        const float4 u = *reinterpret_cast<const float4*>(p + c), v = *reinterpret_cast<const float4*>(p + c + 4);
+        x[ks][0] = u.x, x[ks][1] = u.y, x[ks][2] = u.z, x[ks][3] = u.w;
+        x[ks][4] = v.x, x[ks][5] = v.y, x[ks][6] = v.z, x[ks][7] = v.w;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[ks][e] = in && c + e < a.C ? p[c + e] : 0.0f;
+      }
+    }
+  };
+  constexpr bool AHEAD = CT < 8;   // rows of the next step are loaded early where registers are left
+  if (AHEAD && (int64_t)blockIdx.x < steps) load_h(blockIdx.x);
+  for (int64_t step = blockIdx.x; step < steps; step += gridDim.x) {
+    asm volatile("" : "+v"(lane_w), "+s"(wz), "+s"(wd));
+    const int64_t row = step * NB_ROWS + 16 * wave + l15;
+    const bool in = row < a.N;
+    int32_t target = -1;
+    int flag = 0;
+    if (in) {
+      if constexpr (DENSE) {
+        flag = a.flag[row];
+      } else {
+        target = max(a.index[row], -1);
+        flag = target < 0 ? 0 : target < a.V ? 1 : 2;
+      }
+    }
+    float weight = 1.0f;
+    if (GRAD && a.g && flag) weight = a.g[row];
+    if (!AHEAD) load_h(step);
+    s16x8 hf[KS][3];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[ks][e] = flag ? x[ks][e] : 0.0f;
+      split_any8(x[ks], hf[ks]);
+      if constexpr (GRAD) {
+        const int r = 16 * wave + l15;
+#pragma unroll
+        for (int t = 0; t < 3; ++t)
+          *reinterpret_cast<s16x8*>(lds + L::H + t * L::H_PLANE + r * (CP * 2) + ((2 * ks + (g >> 1)) ^ swz_h<CP>(r)) * 32 +
+                                    (g & 1) * 16) = hf[ks][t];
+      }
+    }
+    if (AHEAD && step + gridDim.x < steps) load_h(step + gridDim.x);
+    // logits
+    f32x4 z[VT];
+    s16x8 w[2][3];
+    frag_z(0, 0, w[0]);
+#pragma unroll
+    for (int vt = 0; vt < VT; ++vt) {
+      z[vt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const int i = vt * KS + ks;
+        if (i + 1 < VT * KS) frag_z((i + 1) / KS, (i + 1) % KS, w[(i + 1) & 1]);
+        z[vt] = mfma6(w[i & 1], hf[ks], z[vt]);
+        __builtin_amdgcn_sched_barrier(0);   // one fragment ahead, not all of them
+      }
+    }
+    float m = -INFINITY, s = 0.0f;
+#pragma unroll
+    for (int vt = 0; vt < VT; ++vt) {
+      const int v = 16 * vt + 4 * g;
+      const f32x4 bs = *reinterpret_cast<const f32x4*>(s_bias + v);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        z[vt][e] = fmaf(z[vt][e], a.scale, bs[e]);   // W is zero and the bias -inf past the alphabet
+        m = fmaxf(m, z[vt][e]);
+      }
+    }
+    m = fmaxf(m, __shfl_xor(m, 16));
+    m = fmaxf(m, __shfl_xor(m, 32));
+    const float base = m > -INFINITY ? m : 0.0f;
+    float at_target = 0.0f;   // of the lane that holds the target, z - base
+#pragma unroll
+    for (int vt = 0; vt < VT; ++vt)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float t = z[vt][e] - base, y = exp2_hw(t);
+        if (!DENSE && target - 4 * g == 16 * vt + e) at_target = t;
+        z[vt][e] = DENSE ? t : y;
+        s += y;
+      }
+    asm volatile("" : "+v"(target));   // the comparisons below are made again: 64 of them kept fill the scalar registers
+    s += __shfl_xor(s, 16);
+    s += __shfl_xor(s, 32);
+    const float lse = log2_hw(s);  // over base
+    float bits = 0.0f;
+    if constexpr (!DENSE) {
+      const bool mine = flag == 1 && ((target >> 2) & 3) == g;
+      bits = mine ? lse - at_target : 0.0f;
+    }
+    if (lane < 16 && in && a.lse) a.lse[row] = flag ? (base + lse) * LN2 : 0.0f;
+    const float inv = flag == 2 ? NAN : weight / s;
+    const float w1 = flag == 2 ? NAN : weight;
+    f32x4 dh[GRAD ? CT : 1];
+#pragma unroll
+    for (int ct = 0; ct < (GRAD ? CT : 1); ++ct) dh[ct] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int vq = 0; vq < VQ; ++vq) {
+      f32x4 q[4];
+      if constexpr (DENSE) {  // the targets' probabilities of 16 rows and 64 symbols, dense in LDS: rows 0-7 in plane 0, 8-15 in 1
+        char* mine = lds + L::D + wave * 2048;
+        const int rl = lane >> 2;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          *reinterpret_cast<f32x4*>(mine + (i >> 1) * L::D_PLANE + (i & 1) * 1024 + lane * 16) = f32x4{0.f, 0.f, 0.f, 0.f};
+        wave_lds_fence();
+        const int64_t r = step * NB_ROWS + 16 * wave + rl;
+        if (r < a.N)
+          for (int j = lane & 3; j < a.k; j += 4) {
+            const int id = a.index[r * a.k + j] - 64 * vq;
+            if (id >= 0 && id < 64)
+              *reinterpret_cast<float*>(mine + (rl >> 3) * L::D_PLANE + (rl & 7) * 256 + id * 4) = a.q[r * a.k + j];
+          }
+        wave_lds_fence();
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          q[i] = *reinterpret_cast<const f32x4*>(mine + (l15 >> 3) * L::D_PLANE + (l15 & 7) * 256 + (16 * i + 4 * g) * 4);
+        wave_lds_fence();
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (q[i][e] != 0.0f) bits += q[i][e] * (lse - z[4 * vq + i][e]);
+      }
+      if constexpr (GRAD) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          float d[8];
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int vt = 4 * vq + 2 * u + i;
+              const float one = DENSE ? q[2 * u + i][e] : target - 4 * g == 16 * vt + e ? 1.0f : 0.0f;
+              const float y = fmaf(DENSE ? exp2_hw(z[vt][e]) : z[vt][e], inv, -one * w1);
+              d[4 * i + e] = flag ? y : 0.0f;
+            }
+          s16x8 p[3];
+          split_any8(d, p);
+          const int r = 16 * wave + l15;
+#pragma unroll
+          for (int t = 0; t < 3; ++t) {
+            char* o = lds + L::D + t * L::D_PLANE + r * 128 + g * 8;
+            *reinterpret_cast<s16x4*>(o + ((2 * u) ^ swz128(r)) * 32) = __builtin_shufflevector(p[t], p[t], 0, 1, 2, 3);
+            *reinterpret_cast<s16x4*>(o + ((2 * u + 1) ^ swz128(r)) * 32) = __builtin_shufflevector(p[t], p[t], 4, 5, 6, 7);
+          }
+          frag_d(2 * vq + u, 0, w[0]);
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct) {
+            if (ct + 1 < CT) frag_d(2 * vq + u, ct + 1, w[(ct + 1) & 1]);
+            dh[ct] = mfma6(w[ct & 1], p, dh[ct]);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        }
+        __syncthreads();
+        const int vt = wave & 3;
+#pragma unroll
+        for (int ks = 0; ks < NB_ROWS / 32; ++ks) {
+          const int r = 32 * ks + 8 * g + (l15 >> 2);
+          const char* pd = lds + L::D + r * 128 + (l15 & 3) * 8;
+          const int d0 = (vt ^ swz128(r)) * 32, d1 = (vt ^ swz128(r + 4)) * 32 + 4 * 128;
+          s16x8 dz[3];
+#pragma unroll
+          for (int t = 0; t < 3; ++t) dz[t] = read_tr(pd + t * L::D_PLANE + d0, pd + t * L::D_PLANE + d1);
+#pragma unroll
+          for (int j = 0; j < DW_N; ++j) {
+            const int ct = (wave >> 2) + 2 * j;
+            const char* ph = lds + L::H + r * (CP * 2) + (l15 & 3) * 8;
+            const int h0 = (ct ^ swz_h<CP>(r)) * 32, h1 = (ct ^ swz_h<CP>(r + 4)) * 32 + 4 * (CP * 2);
+            s16x8 h[3];
+#pragma unroll
+            for (int t = 0; t < 3; ++t) h[t] = read_tr(ph + t * L::H_PLANE + h0, ph + t * L::H_PLANE + h1);
+            dw[vq][j] = mfma6(h, dz, dw[vq][j]);
+          }
+          if ((ks & 1) == (wave >> 2)) {  // db: ones for h, every second 32 rows
+            const s16x8 ones = {0x3f80, 0x3f80, 0x3f80, 0x3f80, 0x3f80, 0x3f80, 0x3f80, 0x3f80};
+#pragma unroll
+            for (int t = 2; t >= 0; --t) db[vq] = mfma<false>(ones, dz[t], db[vq]);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        __syncthreads();
+      }
+    }
+    bits += __shfl_xor(bits, 16);
+    bits += __shfl_xor(bits, 32);
+    if (DENSE && flag == 1) bits += a.ent[row];
+    if (lane < 16 && in) a.bits[row] = flag == 2 ? NAN : flag ? bits : 0.0f;
+    if constexpr (GRAD) {
+      if (a.dh && in) {
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+          const int c = 16 * ct + 4 * g;
+          float* o = a.dh + row * a.C + c;
+          const f32x4 y = dh[ct] * a.out_scale;
+          if (a.C % 4 == 0 && (uintptr_t)a.dh % 16 == 0) {
+            if (c < a.C) *reinterpret_cast<f32x4*>(o) = y;
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (c + e < a.C) o[e] = y[e];
+          }
+        }
+      }
+    }
+  }
+  if constexpr (GRAD) {
+    float* part = a.part + (int64_t)blockIdx.x * (a.C + 2) * a.V;
+#pragma unroll
+    for (int vq = 0; vq < VQ; ++vq) {
+      const int v = 64 * vq + 16 * (wave & 3) + l15;
+      if (v >= a.V) continue;
+#pragma unroll
+      for (int j = 0; j < DW_N; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int c = 16 * ((wave >> 2) + 2 * j) + 4 * g + e;
+          if (c < a.C) part[(int64_t)c * a.V + v] = dw[vq][j][e];
+        }
+      if (g == 0) part[(int64_t)(a.C + (wave >> 2)) * a.V + v] = db[vq][0];
+    }
+  }
+}
+
+// W as the lanes of k_narrow read it where it does not lie in LDS.
+__global__ void __launch_bounds__(256) k_narrow_pack(NarrowArgs a, int KS, int CT, int VT, uint16_t* wz, uint16_t* wd) {
+  const int nz = VT * KS * 64, nd = VT / 2 * CT * 64;
+  for (int i = blockIdx.x * 256 + threadIdx.x; i < nz + nd; i += gridDim.x * 256) {
+    const bool z = i < nz;
+    const int f = (z ? i : i - nz) / 64, lane = i % 64, l15 = lane & 15, g = lane >> 4;
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int v = z ? 16 * (f / KS) + l15 : 32 * (f / CT) + 16 * (e >> 2) + 4 * g + (e & 3);
+      const int c = z ? 32 * (f % KS) + 8 * g + e : 16 * (f % CT) + l15;
+      x[e] = c < a.C && v < a.V ? a.w[c * a.w_stride + v] : 0.0f;
+    }
+    s16x8 p[3];
+    split_any8(x, p);
+    s16x8* o = reinterpret_cast<s16x8*>(z ? wz : wd) + (int64_t)f * 3 * 64 + lane;
+#pragma unroll
+    for (int t = 0; t < 3; ++t) o[t * 64] = p[t];
+  }
+}
+
+// dw and db from the blocks' sums: 32 values a block, 8 shares of the blocks each.
+__global__ void __launch_bounds__(256) k_narrow_join(const float* __restrict__ part, int blocks, int C, int V, float scale,
+                                                     float* __restrict__ dw, float* __restrict__ db) {
+  __shared__ float s[8][33];
+  const int i = threadIdx.x & 31, share = threadIdx.x >> 5;
+  const int64_t n = (int64_t)C * V, all = n + 2 * V, at = (int64_t)blockIdx.x * 32 + i;
+  float x = 0.0f;
+  if (at < n + V) {
+#pragma unroll 8
+    for (int b = share; b < blocks; b += 8) {
+      const float* p = part + b * all + at;
+      x += at < n ? p[0] : p[0] + p[V];
+    }
+  }
+  s[share][i] = x;
+  __syncthreads();
+  if (share != 0 || at >= n + V) return;
+  x = 0.0f;
+  for (int k = 0; k < 8; ++k) x += s[k][i];
+  if (at < n) {
+    if (dw) dw[at] = x * scale;
+  } else if (db) db[at - n] = x * scale;
+}
+
+int narrow_blocks(int64_t rows) { return (int)std::min<int64_t>(NB_BLOCKS, (rows + NB_ROWS - 1) / NB_ROWS); }
+int64_t up256(int64_t x) { return (x + 255) / 256 * 256; }
+
+template <int CT, int VQ>
+void run(const NarrowArgs& a, bool grad, int blocks, hipStream_t st) {
+  const auto args = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(blocks), dim3(NB_THREADS), 0, st, a); };
+  if (a.q) grad ? args(k_narrow<CT, VQ, true, true>) : args(k_narrow<CT, VQ, false, true>);
+  else grad ? args(k_narrow<CT, VQ, true, false>) : args(k_narrow<CT, VQ, false, false>);
+}
+
+}  // namespace
+
+bool head_is_narrow(const reno_head& p) { return p.type == RENO_T_FP32 && p.channels <= 128 && p.symbols <= 256; }
+
+// workspace: the blocks' sums, then W as it is streamed
+int64_t head_narrow_bytes(const reno_head& p, bool grad) {
+  const int64_t cp = p.channels <= 32 ? 32 : p.channels <= 64 ? 64 : 128;
+  int64_t n = grad ? up256((int64_t)narrow_blocks(p.rows) * (p.channels + 2) * p.symbols * 4) : 0;
+  if (cp > 32) n += 2 * up256(cp * 256 * 3 * 2);
+  return n;
+}
+
+hipError_t launch_head_narrow(const HeadCall& c, const HeadTargets& t, char* ws, hipStream_t st) {
+  const reno_head& p = c.p;
+  NarrowArgs a{};
+  a.N = p.rows;
+  a.C = p.channels;
+  a.V = p.symbols;
+  a.k = c.k;
+  a.h_stride = p.h_stride;
+  a.w_stride = p.w_stride;
+  a.h = static_cast<const float*>(c.d.h);
+  a.w = static_cast<const float*>(c.d.w);
+  a.b = static_cast<const float*>(c.d.b);
+  a.g = c.d.row_weight;
+  a.index = t.index;
+  a.q = t.q;
+  a.ent = t.ent;
+  a.flag = t.flag;
+  a.scale = (float)(1.4426950408889634 / (double)c.temperature);
+  a.out_scale = (float)(1.0 / (0.6931471805599453 * (double)c.temperature));
+  a.bits = c.d.bits;
+  a.lse = c.d.lse;
+  a.dh = static_cast<float*>(c.d.dh);
+  a.wide = (uintptr_t)a.h % 16 == 0 && p.h_stride % 4 == 0;
+  const int blocks = narrow_blocks(p.rows);
+  char* at = ws;
+  if (c.grad) {
+    a.part = reinterpret_cast<float*>(at);
+    at += up256((int64_t)blocks * (p.channels + 2) * p.symbols * 4);
+  }
+  const int CT = p.channels <= 32 ? 2 : p.channels <= 64 ? 4 : 8, VQ = p.symbols <= 64 ? 1 : 4;
+  if (CT > 2) {
+    uint16_t* wz = reinterpret_cast<uint16_t*>(at);
+    uint16_t* wd = reinterpret_cast<uint16_t*>(at + up256((int64_t)CT * 16 * 256 * 3 * 2));
+    a.wz = wz;
+    a.wd = wd;
+    const int n = 4 * VQ * (CT / 2) * 64 + 2 * VQ * CT * 64;
+    hipLaunchKernelGGL(k_narrow_pack, dim3((n + 255) / 256), dim3(256), 0, st, a, CT / 2, CT, 4 * VQ, wz, wd);
+  }
+  if (VQ == 1) {
+    if (CT == 2) run<2, 1>(a, c.grad, blocks, st);
+    else if (CT == 4) run<4, 1>(a, c.grad, blocks, st);
+    else run<8, 1>(a, c.grad, blocks, st);
+  } else {
+    if (CT == 2) run<2, 4>(a, c.grad, blocks, st);
+    else if (CT == 4) run<4, 4>(a, c.grad, blocks, st);
+    else run<8, 4>(a, c.grad, blocks, st);
+  }
+  if (c.d.dw || c.d.db) {
+    const int64_t n = (int64_t)(a.C + 1) * a.V;
+    hipLaunchKernelGGL(k_narrow_join, dim3((unsigned)((n + 31) / 32)), dim3(256), 0, st, a.part, blocks, a.C, a.V,
+                       a.out_scale, static_cast<float*>(c.d.dw), static_cast<float*>(c.d.db));
+  }
+  return hipGetLastError();
+}
+
+}  // namespace reno
