@@ -9,7 +9,6 @@ a GPU; creating a context needs one, and the library must have been built
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import os
 import typing
@@ -510,7 +509,16 @@ class TopLogits(typing.NamedTuple):
     lse: object           # float32 [N], natural log
 
 
-_TYPES = {"torch.float32": RENO_T_FP32, "torch.bfloat16": RENO_T_BF16, "torch.float16": RENO_T_FP16}
+def _type_of(dtype):
+    """reno_type of a torch dtype, or None."""
+    global _TYPES
+    if _TYPES is None:
+        import torch
+        _TYPES = {torch.float32: RENO_T_FP32, torch.bfloat16: RENO_T_BF16, torch.float16: RENO_T_FP16}
+    return _TYPES.get(dtype)
+
+
+_TYPES = None
 
 
 def _need(cond, msg):
@@ -518,28 +526,20 @@ def _need(cond, msg):
         raise ValueError(msg)
 
 
-def _rows(t, name, dtype=None, device=None, shape=None):
-    """A device matrix whose rows are contiguous (a copy where they are not)."""
-    _need(t.is_cuda, f"{name} must be a device tensor")
-    _need(device is None or t.device == device, f"{name} must be on the device of the other arguments")
-    _need(dtype is None or t.dtype == dtype, f"{name} must be {dtype}")
-    _need(shape is None or tuple(t.shape) == tuple(shape), f"{name} must have shape {tuple(shape or ())}")
-    if t.dim() == 2 and t.shape[1] > 1 and (t.stride(1) != 1 or (t.shape[0] > 1 and t.stride(0) < t.shape[1])):
-        return t.contiguous()
-    return t if t.dim() == 2 else t.contiguous()
+def _rows(t, name, dtype, device, shape):
+    """A device tensor whose rows are contiguous (a copy where they are not)."""
+    if t.device != device or t.dtype != dtype or tuple(t.shape) != shape:
+        raise ValueError(f"{name} must be {dtype} of shape {shape} on {device}")
+    if t.is_contiguous():
+        return t
+    if t.dim() == 2 and t.stride(1) == 1 and t.stride(0) >= t.shape[1]:
+        return t
+    return t.contiguous()
 
 
 def _stride(t):
     """Elements between the rows of a matrix that _rows returned."""
-    return t.stride(0) if t.shape[0] > 1 and t.stride(0) >= t.shape[1] else t.shape[1]
-
-
-def head_workspace(rows: int, channels: int, symbols: int, dtype, top_k: int = 1, grad: bool = False) -> int:
-    """Bytes of workspace for such a call (reno_head_workspace)."""
-    p = reno_head(rows, channels, symbols, _TYPES[str(dtype)], channels, symbols)
-    n = ctypes.c_int64()
-    _head_check(lib().reno_head_workspace(ctypes.byref(p), top_k, int(bool(grad)), ctypes.byref(n)))
-    return n.value
+    return t.shape[1] if t.is_contiguous() else t.stride(0)
 
 
 def _head_check(rc):
@@ -547,16 +547,28 @@ def _head_check(rc):
         raise RenoError(rc, lib().reno_last_error(None).decode())
 
 
-@contextlib.contextmanager
-def _on(dev, stream):
-    """The stream a call is enqueued on (default: torch's current one of the
-    device), made current together with its device."""
+def head_workspace(rows: int, channels: int, symbols: int, dtype, top_k: int = 1, grad: bool = False) -> int:
+    """Bytes of workspace for such a call (reno_head_workspace)."""
+    kind = _type_of(dtype)
+    _need(kind is not None, "dtype must be float32, bfloat16 or float16")
+    p = reno_head(rows, channels, symbols, kind, channels, symbols)
+    n = ctypes.c_int64()
+    _head_check(lib().reno_head_workspace(ctypes.byref(p), top_k, int(bool(grad)), ctypes.byref(n)))
+    return n.value
+
+
+def _on(dev, stream, call):
+    """call(stream) on the device of the arguments, with the stream that it is
+    enqueued on (default: torch's current one of that device) current."""
     import torch
-    with torch.cuda.device(dev):
-        st = stream if stream is not None else torch.cuda.current_stream()
-        _need(st.device == dev, "stream must belong to the device of the arguments")
-        with torch.cuda.stream(st):
-            yield st
+    if stream is None:
+        if torch.cuda.current_device() == dev.index:
+            return call(torch.cuda.current_stream())
+        with torch.cuda.device(dev):
+            return call(torch.cuda.current_stream())
+    _need(stream.device == dev, "stream must belong to the device of the arguments")
+    with torch.cuda.stream(stream):
+        return call(stream)
 
 
 def _read_on(stream, *tensors):
@@ -568,37 +580,42 @@ def _read_on(stream, *tensors):
                 t.record_stream(stream)
 
 
+_GRADS = ("dh", "dw", "db")
+
+
 def _head_call(h, w, b, targets, row_weight, grad, workspace, stream, k, call):
     import torch
     _need(h.dim() == 2 and w.dim() == 2, "h must be [N][C] and w [C][V]")
     dt, dev = h.dtype, h.device
+    kind = _type_of(dt)
     _need(h.is_cuda, "h must be a device tensor")
-    _need(str(dt) in _TYPES, "h must be float32, bfloat16 or float16")
-    n, c, v = h.shape[0], h.shape[1], w.shape[1]
-    names = ("dh", "dw", "db") if grad is True else tuple(grad or ())
-    _need(all(x in ("dh", "dw", "db") for x in names), "grad must be True, False or some of dh, dw, db")
-    with _on(dev, stream) as st:
-        h = _rows(h, "h")
-        w = _rows(w, "w", dt, dev, (c, v))
-        b = None if b is None else _rows(b, "b", dt, dev, (v,))
+    _need(kind is not None, "h must be float32, bfloat16 or float16")
+    (n, c), v = h.shape, w.shape[1]
+    names = _GRADS if grad is True else tuple(grad or ())
+    _need(all(x in _GRADS for x in names), "grad must be True, False or some of dh, dw, db")
+
+    def run(st):
+        hr, wr = _rows(h, "h", dt, dev, (n, c)), _rows(w, "w", dt, dev, (c, v))
+        br = None if b is None else _rows(b, "b", dt, dev, (v,))
         g = None if row_weight is None else _rows(row_weight, "row_weight", torch.float32, dev, (n,))
-        targets = [_rows(t, name, kind, dev, shape).contiguous() for t, name, kind, shape in targets]
-        p = reno_head(n, c, v, _TYPES[str(dt)], _stride(h), _stride(w))
+        rows = [_rows(t, name, x, dev, shape).contiguous() for t, name, x, shape in targets]
+        p = reno_head(n, c, v, kind, _stride(hr), _stride(wr))
         need = ctypes.c_int64()
         _head_check(lib().reno_head_workspace(ctypes.byref(p), k, int(bool(names)), ctypes.byref(need)))
-        if workspace is None:
-            workspace = torch.empty(need.value, dtype=torch.uint8, device=dev)
-        _need(workspace.is_cuda and workspace.device == dev and workspace.is_contiguous(),
-              "workspace must be contiguous and on the device of the arguments")
+        ws = workspace
+        if ws is None:
+            ws = torch.empty(need.value, dtype=torch.uint8, device=dev)
+        _need(ws.device == dev and ws.is_contiguous(), "workspace must be contiguous and on the device of the arguments")
         bits = torch.empty(n, dtype=torch.float32, device=dev)
         lse = torch.empty(n, dtype=torch.float32, device=dev)
-        shapes = {"dh": (n, c), "dw": (c, v), "db": (v,)}
-        out = {x: torch.empty(shapes[x], dtype=dt, device=dev) for x in names}
-        ptr = [None if t is None else t.data_ptr() for t in (h, w, b, g, bits, lse, *map(out.get, shapes))]
-        _head_check(call(ctypes.byref(p), ctypes.byref(reno_head_data(*ptr)), *map(_ptr, targets), _ptr(workspace),
-                         workspace.numel() * workspace.element_size(), ctypes.c_void_p(st.cuda_stream)))
-        _read_on(stream, h, w, b, g, workspace, *targets)
-    return HeadResult(bits, lse, *(out.get(x) for x in shapes))
+        out = [torch.empty(shape, dtype=dt, device=dev) if x in names else None
+               for x, shape in zip(_GRADS, ((n, c), (c, v), (v,)))]
+        d = reno_head_data(*(None if t is None else t.data_ptr() for t in (hr, wr, br, g, bits, lse, *out)))
+        _head_check(call(ctypes.byref(p), ctypes.byref(d), *(t.data_ptr() for t in rows), ws.data_ptr(),
+                         ws.numel() * ws.element_size(), st.cuda_stream))
+        _read_on(stream, hr, wr, br, g, ws, *rows)
+        return HeadResult(bits, lse, *out)
+    return _on(dev, stream, run)
 
 
 def head_code_length(h, w, b, symbol, row_weight=None, grad=False, workspace=None, stream=None) -> HeadResult:
@@ -643,18 +660,20 @@ def top_logits(logits, k: int, stream=None) -> TopLogits:
     row's normaliser (reno_top_logits); entries past V are -1 and -inf."""
     import torch
     _need(logits.dim() == 2 and logits.is_cuda, "logits must be a device tensor [N][V]")
-    _need(str(logits.dtype) in _TYPES, "logits must be float32, bfloat16 or float16")
+    _need(_type_of(logits.dtype) is not None, "logits must be float32, bfloat16 or float16")
     k, dev = int(k), logits.device
     n, v = logits.shape
-    with _on(dev, stream) as st:
-        x = _rows(logits, "logits")
+
+    def run(st):
+        x = _rows(logits, "logits", logits.dtype, dev, (n, v))
         index = torch.empty((n, max(k, 0)), dtype=torch.int32, device=dev)
         value = torch.empty((n, max(k, 0)), dtype=torch.float32, device=dev)
         lse = torch.empty(n, dtype=torch.float32, device=dev)
-        _head_check(lib().reno_top_logits(_ptr(x), _TYPES[str(x.dtype)], n, v, _stride(x), k, _ptr(index), _ptr(value),
-                                          _ptr(lse), ctypes.c_void_p(st.cuda_stream)))
+        _head_check(lib().reno_top_logits(x.data_ptr(), _type_of(x.dtype), n, v, _stride(x), k, index.data_ptr(),
+                                          value.data_ptr(), lse.data_ptr(), st.cuda_stream))
         _read_on(stream, x)
-    return TopLogits(index, value, lse)
+        return TopLogits(index, value, lse)
+    return _on(dev, stream, run)
 
 
 def rans_encode(sym: np.ndarray, freq: np.ndarray) -> np.ndarray:

@@ -72,7 +72,9 @@ struct HeadArgs {
   float2* part;            // [parts][R] maximum and sum
   int parts;
   float* tt;               // [R][k] t of the targets
-  float* t;                // [R][Vp]
+  float* t;                // [R][Vp], or (bf16)
+  uint16_t* t16;           // [R][Vp]: 2^(t - the part's maximum + 15) in fp16; dz takes its place
+  int part_width;          // symbols of a part
   float* lse2;             // [R]
   uint16_t* dz;            // planes [R][Vp]
   float* dbp;              // [ceil(R / DZ_ROWS)][Vp]
@@ -88,12 +90,20 @@ __device__ __forceinline__ int row_flag(const HeadArgs& a, int64_t row) {
 }
 
 // ---- weights' scale ----
-// Partial maxima of the finite |g| (one per block).
-__global__ void __launch_bounds__(256) k_head_gmax(const float* __restrict__ g, int64_t n, float* __restrict__ part) {
+// Partial maxima of the finite |g|, one of each of GPARTS blocks; the others: b * scale, padded.
+template <int TYPE>
+__global__ void __launch_bounds__(256) k_head_prep(HeadArgs a, int64_t n, float* __restrict__ part) {
   __shared__ float s[4];
+  if (blockIdx.x >= GPARTS) {
+    const int64_t i = (int64_t)(blockIdx.x - GPARTS) * 256 + threadIdx.x;
+    if (i < n) a.bias[i] = a.b && i < a.V ? load_as_float<TYPE>(a.b, i) * a.scale : 0.0f;
+    return;
+  }
+  if (!part) return;
   float m = 0.0f;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += GPARTS * 256) {
-    const float x = fabsf(g[i]);
+#pragma unroll 4
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < a.N; i += GPARTS * 256) {
+    const float x = fabsf(a.g[i]);
     if (x < INFINITY) m = fmaxf(m, x);
   }
   for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
@@ -112,81 +122,79 @@ __device__ __forceinline__ float weight_scale(const float* gpart) {
   return __uint_as_float((uint32_t)e << 23);
 }
 
-// ---- targets of a distillation: one wave a row ----
-__device__ __forceinline__ float wave_max(float v) {
-  for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
-  return v;
-}
-__device__ __forceinline__ float wave_sum(float v) {
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
-  return v;
-}
-
+// ---- targets of a distillation ----
+// LW lanes a row, PER entries a lane (k <= LW PER).
+template <int LW, int PER>
 __global__ void __launch_bounds__(256) k_head_targets(const int32_t* __restrict__ index, const float* __restrict__ logit,
                                                       int64_t n, int k, int V, float scale, int32_t* __restrict__ out,
                                                       float* __restrict__ q_out, float* __restrict__ ent,
                                                       uint8_t* __restrict__ flag) {
-  const int lane = lane_id();
-  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (row >= n) return;
-  const int32_t* ix = index + row * k;
-  const float* tl = logit + row * k;
-  int32_t id[2];
-  float t[2], q[2];
-  bool bad = false;
-  float m = -INFINITY;
+  const int lane = threadIdx.x % LW;
+  const int64_t row = (int64_t)blockIdx.x * (256 / LW) + threadIdx.x / LW;
+  const bool in = row < n;
+  const auto top_of = [](float v) {
+    for (int o = LW / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
+    return v;
+  };
+  const auto sum_of = [](float v) {
+    for (int o = LW / 2; o > 0; o >>= 1) v += __shfl_xor(v, o);
+    return v;
+  };
+  int32_t id[PER];
+  float t[PER], q[PER];
+  float m = -INFINITY, bad = 0.0f;
 #pragma unroll
-  for (int c = 0; c < 2; ++c) {
-    const int j = c * 64 + lane;
-    id[c] = j < k ? ix[j] : -1;
-    t[c] = id[c] >= 0 ? tl[j] : -INFINITY;
-    bad |= id[c] >= V || t[c] != t[c];
+  for (int c = 0; c < PER; ++c) {
+    const int j = c * LW + lane;
+    id[c] = in && j < k ? index[row * k + j] : -1;
+    t[c] = id[c] >= 0 ? logit[row * k + j] : -INFINITY;
+    if (id[c] >= V || t[c] != t[c]) bad = 1.0f;
     m = fmaxf(m, t[c]);
   }
-  m = wave_max(m);
-  const bool any_bad = __ballot(bad) != 0 || m == INFINITY;
+  m = top_of(m);
+  const bool any_bad = top_of(bad) != 0.0f || m == INFINITY;
   float sum = 0.0f;
 #pragma unroll
-  for (int c = 0; c < 2; ++c) {
+  for (int c = 0; c < PER; ++c) {
     q[c] = m > -INFINITY ? exp2_hw((t[c] - m) * scale) : 0.0f;
     sum += q[c];
   }
-  sum = wave_sum(sum);
+  sum = sum_of(sum);
 #pragma unroll
-  for (int c = 0; c < 2; ++c) {
+  for (int c = 0; c < PER; ++c) {
     q[c] = sum > 0.0f ? q[c] / sum : 0.0f;
     if (q[c] == 0.0f) id[c] = -1;
   }
   // entries of one index: the first takes the sum, in order, the others go
-  float joined[2] = {0.0f, 0.0f};
-  bool later[2] = {false, false};
+  float joined[PER] = {};
+  bool later[PER] = {};
 #pragma unroll
-  for (int s = 0; s < 2; ++s) {
-    const int cnt = min(max(k - s * 64, 0), 64);
+  for (int s = 0; s < PER; ++s) {
+    const int cnt = min(max(k - s * LW, 0), LW);
     for (int l = 0; l < cnt; ++l) {
-      const int32_t oi = __shfl(id[s], l);
-      const float oq = __shfl(q[s], l);
+      const int32_t oi = __shfl(id[s], l, LW);
+      const float oq = __shfl(q[s], l, LW);
 #pragma unroll
-      for (int c = 0; c < 2; ++c)
+      for (int c = 0; c < PER; ++c)
         if (oi == id[c]) {
           joined[c] += oq;
-          later[c] |= s * 64 + l < c * 64 + lane;
+          later[c] |= s * LW + l < c * LW + lane;
         }
     }
   }
   float e = 0.0f;
 #pragma unroll
-  for (int c = 0; c < 2; ++c) {
-    const int j = c * 64 + lane;
+  for (int c = 0; c < PER; ++c) {
+    const int j = c * LW + lane;
     const bool keep = id[c] >= 0 && !later[c] && !any_bad;
-    if (j < k) {
+    if (in && j < k) {
       out[row * k + j] = keep ? id[c] : -1;
       q_out[row * k + j] = keep ? joined[c] : 0.0f;
     }
     if (keep) e += joined[c] * log2_hw(joined[c]);
   }
-  e = wave_sum(e);
-  if (lane == 0) {
+  e = sum_of(e);
+  if (lane == 0 && in) {
     ent[row] = e;
     flag[row] = any_bad ? 2 : m > -INFINITY ? 1 : 0;
   }
@@ -237,12 +245,6 @@ __global__ void __launch_bounds__(256) k_head_pack_w(HeadArgs a) {
   }
 }
 
-template <int TYPE>
-__global__ void __launch_bounds__(256) k_head_bias(HeadArgs a, int64_t n) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i < n) a.bias[i] = a.b && i < a.V ? load_as_float<TYPE>(a.b, i) * a.scale : 0.0f;
-}
-
 // ---- logits ----
 // m runs over symbols, n over rows: a lane holds one row and 4 consecutive
 // symbols of each 16, so that a row's maximum and sum need two lane exchanges.
@@ -286,6 +288,16 @@ __global__ void __launch_bounds__(WM* WN * 64) k_head_logits(HeadArgs a, Operand
     s += __shfl_xor(s, 16);
     s += __shfl_xor(s, 32);
     if (g == 0 && r < a.R && p < a.parts) a.part[(int64_t)p * a.R + r] = make_float2(m, s);
+    if (a.t16 && r < a.R) {
+#pragma unroll
+      for (int i = 0; i < Tile::MF; ++i) {
+        const int v = v0 + 16 * i + 4 * g;
+        uint16_t o[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = to_fp16(exp2_hw(acc[i][j][e] - base + 15.0f));
+        if (v < a.Vp) *reinterpret_cast<uint2*>(a.t16 + r * a.Vp + v) = *reinterpret_cast<const uint2*>(o);
+      }
+    }
     if (a.t && r < a.R) {
 #pragma unroll
       for (int i = 0; i < Tile::MF; ++i) {
@@ -309,28 +321,140 @@ __global__ void __launch_bounds__(WM* WN * 64) k_head_logits(HeadArgs a, Operand
     }
     return;
   }
+  // several entries a row: 16 PR rows at a time pass through the wave's share of LDS, and every lane looks up
+  // the entries of its own
+  constexpr int MW = BM / WM, PR = 16384 / (MW * 4) / 16;   // symbols of the wave, groups of 16 rows in 16 KB
+  static_assert(Tile::LDS >= WM * WN * 16384 && Tile::NF % PR == 0, "a wave's share of LDS holds 16 PR rows");
+  char* mine = lds + wave * 16384;
 #pragma unroll
-  for (int j = 0; j < Tile::NF; ++j) {
-    for (int rr = 0; rr < 16; ++rr) {
-      const int64_t r = n0 + 16 * j + rr;
-      if (r >= a.R) break;
-      for (int k0 = 0; k0 < a.k; k0 += 64) {
-        const int at = k0 + lane;
-        const int id = at < a.k ? a.index[(a.r0 + r) * a.k + at] - v0 : -1;
-        uint64_t hits = __ballot(id >= 0 && id < BM / WM);
-        while (hits) {
-          const int l = __builtin_ctzll(hits);
-          hits &= hits - 1;
-          const int want = __builtin_amdgcn_readlane(id, l);
-          float x = 0.0f;
+  for (int j0 = 0; j0 < Tile::NF; j0 += PR) {
 #pragma unroll
-          for (int i = 0; i < Tile::MF; ++i)
+    for (int j = 0; j < PR; ++j)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if ((want & ~12) == 16 * i + e) x = acc[i][j][e];
-          if (l15 == rr && g == ((want >> 2) & 3)) a.tt[r * a.k + k0 + l] = x;
-        }
+      for (int i = 0; i < Tile::MF; ++i)   // pieces of 16 bytes, spread over the banks by the row
+        *reinterpret_cast<f32x4*>(mine + (16 * j + l15) * (MW * 4) + (((4 * i + g) ^ l15) * 16)) = acc[i][j0 + j];
+    wave_lds_fence();
+    const int64_t r0 = n0 + 16 * j0;
+    const int rows = (int)max((int64_t)0, min((int64_t)(16 * PR), a.R - r0));
+#pragma unroll 4
+    for (int x = lane; x < rows * a.k; x += 64) {
+      const int rl = x / a.k;
+      const int id = a.index[(a.r0 + r0) * a.k + x];
+      if (id >= v0 && id < v0 + MW)
+        a.tt[r0 * a.k + x] =
+            *reinterpret_cast<const float*>(mine + rl * (MW * 4) + ((((id - v0) >> 2) ^ (rl & 15)) * 16) + ((id - v0) & 3) * 4);
+    }
+    wave_lds_fence();
+  }
+}
+
+// ---- few rows, no gradient: w is read once, by vector instructions ----
+// A block takes CB symbols and all channels; a lane 8 consecutive symbols of every (512 / (CB / 8))th
+// channel, so that a wave reads whole lines of w with 16-byte loads (fp32: two), FEW_AHEAD of them in
+// flight.  Bound by the read of w: an FMA a weight and row costs less than its bytes up to FEW_ROWS.
+constexpr int FEW_ROWS = 8, FEW_AHEAD = 8;
+constexpr int FEW_H = 16384;   // values of h that are held in LDS
+
+template <int TYPE, int CB, int NR>
+__global__ void __launch_bounds__(512) k_head_few(HeadArgs a, int wide) {
+  constexpr int LANES = CB / 8, SHARES = 512 / LANES;
+  __shared__ float s_h[FEW_H];
+  __shared__ float s_sum[512 / 64][NR][CB];
+  const int tid = threadIdx.x, lane = lane_id(), wave = tid >> 6;
+  for (int i = tid; i < NR * a.C; i += 512) {
+    const int r = i / a.C, c = i % a.C;
+    s_h[i] = r < a.R && row_flag(a, r) != 0 ? load_as_float<TYPE>(a.h, r * a.h_stride + c) : 0.0f;
+  }
+  __syncthreads();
+  const int v0 = blockIdx.x * CB, v = v0 + tid % LANES * 8;
+  float acc[NR][8] = {};
+  const auto fma8 = [&](int c, const float (&x)[8]) {
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+      const float y = s_h[r * a.C + c];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[r][e] = fmaf(y, x[e], acc[r][e]);
+    }
+  };
+  if (wide && v + 8 <= a.V) {
+    constexpr int Q = TYPE == RENO_T_FP32 ? 2 : 1;
+    const char* p = static_cast<const char*>(a.w) + (int64_t)v * (TYPE == RENO_T_FP32 ? 4 : 2);
+    const int64_t ld = a.w_stride * (TYPE == RENO_T_FP32 ? 4 : 2);
+    for (int c0 = tid / LANES; c0 < a.C; c0 += SHARES * FEW_AHEAD) {
+      uint4 raw[FEW_AHEAD][Q];
+#pragma unroll
+      for (int u = 0; u < FEW_AHEAD; ++u) {
+        const int c = min(c0 + u * SHARES, a.C - 1);
+#pragma unroll
+        for (int q = 0; q < Q; ++q) raw[u][q] = *reinterpret_cast<const uint4*>(p + c * ld + q * 16);
       }
+#pragma unroll
+      for (int u = 0; u < FEW_AHEAD; ++u) {
+        if (c0 + u * SHARES >= a.C) break;
+        float x[8];
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+          const uint32_t b[4] = {raw[u][q].x, raw[u][q].y, raw[u][q].z, raw[u][q].w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if constexpr (TYPE == RENO_T_FP32) x[4 * q + e] = __uint_as_float(b[e]);
+            else if constexpr (TYPE == RENO_T_BF16) {
+              x[2 * e] = __uint_as_float(b[e] << 16);
+              x[2 * e + 1] = __uint_as_float(b[e] & 0xffff0000u);
+            } else {
+              x[2 * e] = (float)__builtin_bit_cast(_Float16, (uint16_t)b[e]);
+              x[2 * e + 1] = (float)__builtin_bit_cast(_Float16, (uint16_t)(b[e] >> 16));
+            }
+          }
+        }
+        fma8(c0 + u * SHARES, x);
+      }
+    }
+  } else {
+#pragma unroll 4
+    for (int c = tid / LANES; c < a.C; c += SHARES) {
+      float x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = v + e < a.V ? load_as_float<TYPE>(a.w, c * a.w_stride + v + e) : 0.0f;
+      fma8(c, x);
+    }
+  }
+  // channels' shares of a wave, then the waves'
+#pragma unroll
+  for (int r = 0; r < NR; ++r)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+#pragma unroll
+      for (int o = LANES; o < 64; o *= 2) acc[r][e] += __shfl_xor(acc[r][e], o);
+      if (lane < LANES) s_sum[wave][r][lane * 8 + e] = acc[r][e];
+    }
+  __syncthreads();
+  // a wave a row: t, maximum and sum, the row's entries
+  for (int r = wave; r < NR && r < a.R; r += 8) {
+    float m = -INFINITY, s = 0.0f, t[CB / 64];
+#pragma unroll
+    for (int i = 0; i < CB / 64; ++i) {
+      const int x = lane + 64 * i;
+      float z = 0.0f;
+#pragma unroll
+      for (int w = 0; w < 8; ++w) z += s_sum[w][r][x];
+      const float b = a.b && v0 + x < a.V ? load_as_float<TYPE>(a.b, v0 + x) : 0.0f;
+      t[i] = v0 + x < a.V ? fmaf(z, a.scale, b * a.scale) : -INFINITY;
+      m = fmaxf(m, t[i]);
+    }
+    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+    const float base = m > -INFINITY ? m : 0.0f;
+#pragma unroll
+    for (int i = 0; i < CB / 64; ++i) {
+      s += exp2_hw(t[i] - base);
+      s_sum[0][r][lane + 64 * i] = t[i];   // a wave's own row from here on
+    }
+    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
+    if (lane == 0) a.part[(int64_t)blockIdx.x * a.R + r] = make_float2(m, s);
+    wave_lds_fence();
+    for (int j = lane; j < a.k; j += 64) {
+      const int id = a.index[r * a.k + j];
+      if (id >= v0 && id < min(v0 + CB, a.V)) a.tt[r * a.k + j] = s_sum[0][r][id - v0];
     }
   }
 }
@@ -344,11 +468,18 @@ __global__ void __launch_bounds__(256) k_head_rows(HeadArgs a) {
   const bool in = r < a.R;
   float m = -INFINITY, s = 0.0f;
   if (in)
-    for (int p = pl; p < a.parts; p += 16) {
-      const float2 x = a.part[(int64_t)p * a.R + r];
-      const float n = fmaxf(m, x.x);
+    for (int p0 = pl; p0 < a.parts; p0 += 16 * 8) {   // 8 loads in flight
+      float2 x[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        x[u] = p0 + 16 * u < a.parts ? a.part[(int64_t)(p0 + 16 * u) * a.R + r] : make_float2(-INFINITY, 0.0f);
+      float n = m;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) n = fmaxf(n, x[u].x);
       const float base = n > -INFINITY ? n : 0.0f;
-      s = s * exp2_hw(m - base) + x.y * exp2_hw(x.x - base);
+      s *= exp2_hw(m - base);
+#pragma unroll
+      for (int u = 0; u < 8; ++u) s += x[u].y * exp2_hw(x[u].x - base);
       m = n;
     }
   s_p[rl][pl] = make_float2(m, s);
@@ -378,9 +509,12 @@ __global__ void __launch_bounds__(256) k_head_rows(HeadArgs a) {
 }
 
 // ---- dz of a piece: a wave takes 256 symbols of DZ_ROWS rows ----
+// Bound by memory: t read, dz written (bf16 in its place: 4 bytes a logit in all).
 template <int TYPE>
 __global__ void __launch_bounds__(256) k_head_dz(HeadArgs a) {
   constexpr int P = planes_of(TYPE);
+  constexpr bool T16 = TYPE == RENO_T_BF16;
+  constexpr int U = 4;   // rows whose loads are in flight
   constexpr float SHIFT = TYPE == RENO_T_FP16 ? (float)(1 << HALF_SHIFT) : 1.0f;
   const int lane = lane_id();
   const float inv_g = 1.0f / weight_scale(a.gpart);
@@ -391,58 +525,103 @@ __global__ void __launch_bounds__(256) k_head_dz(HeadArgs a) {
   const int64_t rb = task / groups;
   const int v = v0 + lane * 4;
   const bool mine = v < a.Vp;
+  const int vc = mine ? v : 0;
   f32x4 sum = {0.f, 0.f, 0.f, 0.f};
   const int64_t end = min(a.R, (rb + 1) * DZ_ROWS);
-  for (int64_t r = rb * DZ_ROWS; r < end; ++r) {
-    const int64_t row = a.r0 + r;
-    const int flag = row_flag(a, row);
-    f32x4 d = {0.f, 0.f, 0.f, 0.f};
-    if (flag) {
-      const float lse2 = a.lse2[r];
-      const float w = flag == 2 ? NAN : (a.g ? a.g[row] * inv_g : 1.0f);
-      const f32x4 t = mine ? *reinterpret_cast<const f32x4*>(a.t + r * a.Vp + v) : f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int64_t r1 = rb * DZ_ROWS; r1 < end; r1 += U) {
+    f32x4 t[U];
+    uint2 t16[U];
+    float pm[U], lse2[U], w[U], tt[U], q[U];
+    int id[U], flag[U];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) d[e] = exp2_hw(t[e] - lse2);
-      if (!a.q) {
-        const int want = a.index[row] - v;
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (want == e) d[e] -= 1.0f;
+    for (int u = 0; u < U; ++u) {
+      const int64_t r = min(r1 + u, end - 1), row = a.r0 + r;
+      if constexpr (T16) {
+        t16[u] = *reinterpret_cast<const uint2*>(a.t16 + r * a.Vp + vc);
+        pm[u] = a.part[(int64_t)min(vc / a.part_width, a.parts - 1) * a.R + r].x;
       } else {
-        for (int k0 = 0; k0 < a.k; k0 += 64) {
-          const int at = k0 + lane;
-          const int id = at < a.k ? a.index[row * a.k + at] - v0 : -1;
-          const float q = at < a.k ? a.q[row * a.k + at] : 0.0f;
-          uint64_t hits = __ballot(id >= 0 && id < 256);
-          while (hits) {
-            const int l = __builtin_ctzll(hits);
-            hits &= hits - 1;
-            const int want = __builtin_amdgcn_readlane(id, l);
-            const float qq = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(q), l));
+        t[u] = *reinterpret_cast<const f32x4*>(a.t + r * a.Vp + vc);
+      }
+      flag[u] = row_flag(a, row);
+      lse2[u] = a.lse2[r];
+      w[u] = a.g ? a.g[row] : 1.0f;
+      if (a.q) {
+        id[u] = lane < a.k ? a.index[row * a.k + lane] : -1;
+        q[u] = lane < a.k ? a.q[row * a.k + lane] : 0.0f;
+        tt[u] = T16 && lane < a.k ? a.tt[r * a.k + lane] : 0.0f;
+      } else {
+        id[u] = a.index[row];
+        tt[u] = a.tt[r];
+      }
+    }
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (want == lane * 4 + e) d[e] -= qq;
+    for (int u = 0; u < U; ++u) {
+      const int64_t r = r1 + u, row = a.r0 + r;
+      if (r >= end) break;
+      f32x4 d = {0.f, 0.f, 0.f, 0.f};
+      if (flag[u]) {
+        const float wr = flag[u] == 2 ? NAN : a.g ? w[u] * inv_g : 1.0f;
+        if constexpr (T16) {
+          const float base = pm[u] > -INFINITY ? pm[u] : 0.0f;
+          const float f = exp2_hw(base - lse2[u] - 15.0f);
+          d[0] = (float)__builtin_bit_cast(_Float16, (uint16_t)t16[u].x) * f;
+          d[1] = (float)__builtin_bit_cast(_Float16, (uint16_t)(t16[u].x >> 16)) * f;
+          d[2] = (float)__builtin_bit_cast(_Float16, (uint16_t)t16[u].y) * f;
+          d[3] = (float)__builtin_bit_cast(_Float16, (uint16_t)(t16[u].y >> 16)) * f;
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) d[e] = exp2_hw(t[u][e] - lse2[u]);
+        }
+        // targets: p - q from the t that was kept exactly
+        if (!a.q) {
+          const int want = id[u] - v;
+          const float y = (T16 ? exp2_hw(tt[u] - lse2[u]) : 0.0f) - 1.0f;
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (want == e) d[e] = T16 ? y : d[e] - 1.0f;
+        } else {
+          for (int k0 = 0; k0 < a.k; k0 += 64) {
+            int32_t ids = id[u];
+            float qs = q[u], ts = tt[u];
+            if (k0) {
+              const int at = k0 + lane;
+              ids = at < a.k ? a.index[row * a.k + at] : -1;
+              qs = at < a.k ? a.q[row * a.k + at] : 0.0f;
+              ts = T16 && at < a.k ? a.tt[r * a.k + at] : 0.0f;
+            }
+            const float y = T16 ? exp2_hw(ts - lse2[u]) - qs : qs;
+            uint64_t hits = __ballot(ids >= v0 && ids < v0 + 256);
+            while (hits) {
+              const int l = __builtin_ctzll(hits);
+              hits &= hits - 1;
+              const int want = __builtin_amdgcn_readlane(ids, l) - v0;
+              const float yy = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(y), l));
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (want == lane * 4 + e) d[e] = T16 ? yy : d[e] - yy;
+            }
           }
         }
-      }
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        d[e] = v + e < a.V ? d[e] * w : 0.0f;
-        sum[e] += d[e];
+        for (int e = 0; e < 4; ++e) {
+          d[e] = v + e < a.V ? d[e] * wr : 0.0f;
+          sum[e] += d[e];
+        }
+      }
+      if (mine) {
+        uint16_t o[P][4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          uint16_t x[P];
+          to_planes<TYPE, P>(d[e] * SHIFT, x);
+#pragma unroll
+          for (int p = 0; p < P; ++p) o[p][e] = x[p];
+        }
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+          *reinterpret_cast<uint2*>(a.dz + p * a.d_plane + r * a.Vp + v) = *reinterpret_cast<const uint2*>(o[p]);
       }
     }
-    if (!mine) continue;
-    uint16_t o[P][4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      uint16_t x[P];
-      to_planes<TYPE, P>(d[e] * SHIFT, x);
-#pragma unroll
-      for (int p = 0; p < P; ++p) o[p][e] = x[p];
-    }
-#pragma unroll
-    for (int p = 0; p < P; ++p)
-      *reinterpret_cast<uint2*>(a.dz + p * a.d_plane + r * a.Vp + v) = *reinterpret_cast<const uint2*>(o[p]);
   }
   if (mine) *reinterpret_cast<f32x4*>(a.dbp + rb * a.Vp + v) = sum;
 }
@@ -576,6 +755,12 @@ int splits_for(int64_t tiles, int64_t K, int terms) {
   return (int)std::max<int64_t>(1, std::min<int64_t>(s, 256));
 }
 
+// Symbols a block of k_head_few takes; 0: not for this call.
+int few_width(const reno_head& p, bool grad) {
+  if (grad || p.rows > FEW_ROWS || (int64_t)(p.rows <= 1 ? 1 : p.rows <= 4 ? 4 : 8) * p.channels > FEW_H) return 0;
+  return p.symbols >= 32768 ? 256 : 64;
+}
+
 struct Plan {
   int planes, terms;
   int64_t Cp, Vp, Vb;   // Vb: padded to whole tiles
@@ -611,6 +796,14 @@ Plan make_plan(const reno_head& p, int k, bool grad) {
     a.bytes = at + std::max<int64_t>(256, head_narrow_bytes(p, grad));
     return a;
   }
+  if (const int few = few_width(p, grad)) {
+    a.part_width = few;
+    a.part = take((p.symbols + few - 1) / few * N * 8);
+    a.tt = take(N * k * 4);
+    a.lse2 = take(N * 4);
+    a.bytes = at;
+    return a;
+  }
   a.planes = planes_of(p.type);
   a.terms = p.type == RENO_T_FP32 ? GEMM_TERMS : 1;
   a.Cp = up(p.channels, GEMM_BK);
@@ -642,7 +835,7 @@ Plan make_plan(const reno_head& p, int k, bool grad) {
   a.tt = take(a.R * k * 4);
   a.lse2 = take(a.R * 4);
   if (grad) {
-    a.t = take(a.R * a.Vp * 4);
+    a.t = p.type == RENO_T_BF16 ? at : take(a.R * a.Vp * 4);
     a.dz = take(a.planes * a.R * a.Vp * 2);
     a.dbp = take((a.R + DZ_ROWS - 1) / DZ_ROWS * a.Vp * 4);
     a.dba = take(a.Vp * 4);
@@ -700,8 +893,15 @@ hipError_t run_head(const HeadCall& c, hipStream_t st) {
     float* q = reinterpret_cast<float*>(ws + pl.q);
     float* ent = reinterpret_cast<float*>(ws + pl.ent);
     uint8_t* flag = reinterpret_cast<uint8_t*>(ws + pl.flag);
-    hipLaunchKernelGGL(k_head_targets, dim3((unsigned)((N + 3) / 4)), dim3(256), 0, st, c.index, c.logit, N, c.k, p.symbols,
-                       (float)(1.4426950408889634 / (double)c.temperature), idx, q, ent, flag);
+    const int per = c.k <= 16 ? 16 : c.k <= 32 ? 8 : 4;   // rows a block
+    const auto args = [&](auto kern) {
+      hipLaunchKernelGGL(kern, dim3((unsigned)((N + per - 1) / per)), dim3(256), 0, st, c.index, c.logit, N, c.k, p.symbols,
+                         (float)(1.4426950408889634 / (double)c.temperature), idx, q, ent, flag);
+    };
+    if (c.k <= 16) args(k_head_targets<16, 1>);
+    else if (c.k <= 32) args(k_head_targets<32, 1>);
+    else if (c.k <= 64) args(k_head_targets<64, 1>);
+    else args(k_head_targets<64, 2>);
     t = HeadTargets{idx, q, ent, flag};
   }
   if (head_is_narrow(p)) return launch_head_narrow(c, t, ws + pl.narrow, st);
@@ -727,6 +927,7 @@ hipError_t run_head(const HeadCall& c, hipStream_t st) {
   a.d_plane = pl.R * pl.Vp;
   a.part = reinterpret_cast<float2*>(ws + pl.part);
   a.parts = (p.symbols + pl.part_width - 1) / pl.part_width;
+  a.part_width = pl.part_width;
   a.tt = reinterpret_cast<float*>(ws + pl.tt);
   a.lse2 = reinterpret_cast<float*>(ws + pl.lse2);
   a.bits = c.d.bits;
@@ -735,17 +936,25 @@ hipError_t run_head(const HeadCall& c, hipStream_t st) {
   a.q = t.q;
   a.ent = t.ent;
   a.flag = t.flag;
-  if (c.grad) {
-    a.t = reinterpret_cast<float*>(ws + pl.t);
-    a.dz = reinterpret_cast<uint16_t*>(ws + pl.dz);
-    a.dbp = reinterpret_cast<float*>(ws + pl.dbp);
-    if (c.d.row_weight) {
-      float* gp = reinterpret_cast<float*>(ws + pl.gpart);
-      hipLaunchKernelGGL(k_head_gmax, dim3(GPARTS), dim3(256), 0, st, c.d.row_weight, N, gp);
-      a.gpart = gp;
-    }
+  if (const int few = few_width(p, c.grad)) {
+    const dim3 grid((unsigned)a.parts);
+    const int wide = (uintptr_t)a.w % 16 == 0 && p.w_stride * size % 16 == 0;
+    a.R = N;
+    const auto args = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(512), 0, st, a, wide); };
+    if (few == 256) N <= 1 ? args(k_head_few<TYPE, 256, 1>) : N <= 4 ? args(k_head_few<TYPE, 256, 4>) : args(k_head_few<TYPE, 256, 8>);
+    else N <= 1 ? args(k_head_few<TYPE, 64, 1>) : N <= 4 ? args(k_head_few<TYPE, 64, 4>) : args(k_head_few<TYPE, 64, 8>);
+    hipLaunchKernelGGL(k_head_rows, dim3((unsigned)((N + 15) / 16)), dim3(256), 0, st, a);
+    return hipGetLastError();
   }
-  hipLaunchKernelGGL(k_head_bias<TYPE>, dim3((unsigned)(pl.Vb / 256)), dim3(256), 0, st, a, pl.Vb);
+  if (c.grad) {
+    a.dz = reinterpret_cast<uint16_t*>(ws + pl.dz);
+    if (TYPE == RENO_T_BF16) a.t16 = a.dz;
+    else a.t = reinterpret_cast<float*>(ws + pl.t);
+    a.dbp = reinterpret_cast<float*>(ws + pl.dbp);
+    if (c.d.row_weight) a.gpart = reinterpret_cast<float*>(ws + pl.gpart);
+  }
+  hipLaunchKernelGGL(k_head_prep<TYPE>, dim3((unsigned)(GPARTS + pl.Vb / 256)), dim3(256), 0, st, a, pl.Vb,
+                     a.gpart ? reinterpret_cast<float*>(ws + pl.gpart) : nullptr);
   const bool in_place = w_in_place(p, c.d.w);
   if (!in_place)
     hipLaunchKernelGGL(k_head_pack_w<TYPE>, dim3(blocks_for(a.C * a.Vp / 8, 256)), dim3(256), 0, st, a);
