@@ -336,13 +336,19 @@ __global__ void __launch_bounds__(WM* WN * 64) k_head_logits(HeadArgs a, Operand
     wave_lds_fence();
     const int64_t r0 = n0 + 16 * j0;
     const int rows = (int)max((int64_t)0, min((int64_t)(16 * PR), a.R - r0));
-#pragma unroll 4
-    for (int x = lane; x < rows * a.k; x += 64) {
-      const int rl = x / a.k;
-      const int id = a.index[(a.r0 + r0) * a.k + x];
-      if (id >= v0 && id < v0 + MW)
-        a.tt[r0 * a.k + x] =
-            *reinterpret_cast<const float*>(mine + rl * (MW * 4) + ((((id - v0) >> 2) ^ (rl & 15)) * 16) + ((id - v0) & 3) * 4);
+    const int all = rows * a.k;
+    const float inv_k = 1.0f / (float)a.k;
+    const int32_t* ix = a.index + (a.r0 + r0) * a.k;
+    for (int x0 = lane; x0 < all; x0 += 64 * 8) {   // 8 loads in flight
+      int id[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) id[u] = x0 + 64 * u < all ? ix[x0 + 64 * u] - v0 : -1;
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (id[u] >= 0 && id[u] < MW) {
+          const int x = x0 + 64 * u, rl = (int)(((float)x + 0.5f) * inv_k);   // x / k: exact below 2^12
+          a.tt[r0 * a.k + x] = *reinterpret_cast<const float*>(mine + rl * (MW * 4) + (((id[u] >> 2) ^ (rl & 15)) * 16) + (id[u] & 3) * 4);
+        }
     }
     wave_lds_fence();
   }
@@ -352,7 +358,7 @@ __global__ void __launch_bounds__(WM* WN * 64) k_head_logits(HeadArgs a, Operand
 // A block takes CB symbols and all channels; a lane 8 consecutive symbols of every (512 / (CB / 8))th
 // channel, so that a wave reads whole lines of w with 16-byte loads (fp32: two), FEW_AHEAD of them in
 // flight.  Bound by the read of w: an FMA a weight and row costs less than its bytes up to FEW_ROWS.
-constexpr int FEW_ROWS = 8, FEW_AHEAD = 8;
+constexpr int FEW_ROWS = 4, FEW_AHEAD = 8;
 constexpr int FEW_H = 16384;   // values of h that are held in LDS
 
 template <int TYPE, int CB, int NR>
@@ -508,39 +514,41 @@ __global__ void __launch_bounds__(256) k_head_rows(HeadArgs a) {
   if (a.lse) a.lse[a.r0 + r] = flag ? lse2 * LN2 : 0.0f;
 }
 
-// ---- dz of a piece: a wave takes 256 symbols of DZ_ROWS rows ----
+// ---- dz of a piece: a wave takes 512 symbols of DZ_ROWS rows ----
 // Bound by memory: t read, dz written (bf16 in its place: 4 bytes a logit in all).
 template <int TYPE>
 __global__ void __launch_bounds__(256) k_head_dz(HeadArgs a) {
   constexpr int P = planes_of(TYPE);
   constexpr bool T16 = TYPE == RENO_T_BF16;
   constexpr int U = 4;   // rows whose loads are in flight
+  constexpr int S = 8;   // symbols of a lane
   constexpr float SHIFT = TYPE == RENO_T_FP16 ? (float)(1 << HALF_SHIFT) : 1.0f;
   const int lane = lane_id();
   const float inv_g = 1.0f / weight_scale(a.gpart);
-  const int64_t groups = (a.Vp + 255) / 256, blocks = (a.R + DZ_ROWS - 1) / DZ_ROWS;
+  const int64_t groups = (a.Vp + 64 * S - 1) / (64 * S), blocks = (a.R + DZ_ROWS - 1) / DZ_ROWS;
   const int64_t task = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (task >= groups * blocks) return;
-  const int v0 = (int)(task % groups) * 256;
+  const int v0 = (int)(task % groups) * (64 * S);
   const int64_t rb = task / groups;
-  const int v = v0 + lane * 4;
+  const int v = v0 + lane * S;
   const bool mine = v < a.Vp;
   const int vc = mine ? v : 0;
-  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+  float sum[S] = {};
   const int64_t end = min(a.R, (rb + 1) * DZ_ROWS);
   for (int64_t r1 = rb * DZ_ROWS; r1 < end; r1 += U) {
-    f32x4 t[U];
-    uint2 t16[U];
+    f32x4 t[U][2];
+    uint4 t16[U];
     float pm[U], lse2[U], w[U], tt[U], q[U];
     int id[U], flag[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int64_t r = min(r1 + u, end - 1), row = a.r0 + r;
       if constexpr (T16) {
-        t16[u] = *reinterpret_cast<const uint2*>(a.t16 + r * a.Vp + vc);
+        t16[u] = *reinterpret_cast<const uint4*>(a.t16 + r * a.Vp + vc);
         pm[u] = a.part[(int64_t)min(vc / a.part_width, a.parts - 1) * a.R + r].x;
       } else {
-        t[u] = *reinterpret_cast<const f32x4*>(a.t + r * a.Vp + vc);
+        t[u][0] = *reinterpret_cast<const f32x4*>(a.t + r * a.Vp + vc);
+        t[u][1] = *reinterpret_cast<const f32x4*>(a.t + r * a.Vp + vc + 4);
       }
       flag[u] = row_flag(a, row);
       lse2[u] = a.lse2[r];
@@ -558,26 +566,28 @@ __global__ void __launch_bounds__(256) k_head_dz(HeadArgs a) {
     for (int u = 0; u < U; ++u) {
       const int64_t r = r1 + u, row = a.r0 + r;
       if (r >= end) break;
-      f32x4 d = {0.f, 0.f, 0.f, 0.f};
+      float d[S] = {};
       if (flag[u]) {
         const float wr = flag[u] == 2 ? NAN : a.g ? w[u] * inv_g : 1.0f;
         if constexpr (T16) {
           const float base = pm[u] > -INFINITY ? pm[u] : 0.0f;
           const float f = exp2_hw(base - lse2[u] - 15.0f);
-          d[0] = (float)__builtin_bit_cast(_Float16, (uint16_t)t16[u].x) * f;
-          d[1] = (float)__builtin_bit_cast(_Float16, (uint16_t)(t16[u].x >> 16)) * f;
-          d[2] = (float)__builtin_bit_cast(_Float16, (uint16_t)t16[u].y) * f;
-          d[3] = (float)__builtin_bit_cast(_Float16, (uint16_t)(t16[u].y >> 16)) * f;
+          const uint32_t x[4] = {t16[u].x, t16[u].y, t16[u].z, t16[u].w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            d[2 * e] = (float)__builtin_bit_cast(_Float16, (uint16_t)x[e]) * f;
+            d[2 * e + 1] = (float)__builtin_bit_cast(_Float16, (uint16_t)(x[e] >> 16)) * f;
+          }
         } else {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) d[e] = exp2_hw(t[u][e] - lse2[u]);
+          for (int e = 0; e < S; ++e) d[e] = exp2_hw(t[u][e >> 2][e & 3] - lse2[u]);
         }
         // targets: p - q from the t that was kept exactly
         if (!a.q) {
           const int want = id[u] - v;
           const float y = (T16 ? exp2_hw(tt[u] - lse2[u]) : 0.0f) - 1.0f;
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
+          for (int e = 0; e < S; ++e)
             if (want == e) d[e] = T16 ? y : d[e] - 1.0f;
         } else {
           for (int k0 = 0; k0 < a.k; k0 += 64) {
@@ -590,28 +600,28 @@ __global__ void __launch_bounds__(256) k_head_dz(HeadArgs a) {
               ts = T16 && at < a.k ? a.tt[r * a.k + at] : 0.0f;
             }
             const float y = T16 ? exp2_hw(ts - lse2[u]) - qs : qs;
-            uint64_t hits = __ballot(ids >= v0 && ids < v0 + 256);
+            uint64_t hits = __ballot(ids >= v0 && ids < v0 + 64 * S);
             while (hits) {
               const int l = __builtin_ctzll(hits);
               hits &= hits - 1;
               const int want = __builtin_amdgcn_readlane(ids, l) - v0;
               const float yy = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(y), l));
 #pragma unroll
-              for (int e = 0; e < 4; ++e)
-                if (want == lane * 4 + e) d[e] = T16 ? yy : d[e] - yy;
+              for (int e = 0; e < S; ++e)
+                if (want == lane * S + e) d[e] = T16 ? yy : d[e] - yy;
             }
           }
         }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
+        for (int e = 0; e < S; ++e) {
           d[e] = v + e < a.V ? d[e] * wr : 0.0f;
           sum[e] += d[e];
         }
       }
       if (mine) {
-        uint16_t o[P][4];
+        uint16_t o[P][S];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
+        for (int e = 0; e < S; ++e) {
           uint16_t x[P];
           to_planes<TYPE, P>(d[e] * SHIFT, x);
 #pragma unroll
@@ -619,11 +629,14 @@ __global__ void __launch_bounds__(256) k_head_dz(HeadArgs a) {
         }
 #pragma unroll
         for (int p = 0; p < P; ++p)
-          *reinterpret_cast<uint2*>(a.dz + p * a.d_plane + r * a.Vp + v) = *reinterpret_cast<const uint2*>(o[p]);
+          *reinterpret_cast<uint4*>(a.dz + p * a.d_plane + r * a.Vp + v) = *reinterpret_cast<const uint4*>(o[p]);
       }
     }
   }
-  if (mine) *reinterpret_cast<f32x4*>(a.dbp + rb * a.Vp + v) = sum;
+  if (!mine) return;
+#pragma unroll
+  for (int e = 0; e < S; e += 4)
+    *reinterpret_cast<f32x4*>(a.dbp + rb * a.Vp + v + e) = f32x4{sum[e], sum[e + 1], sum[e + 2], sum[e + 3]};
 }
 
 // ---- dh and dw ----
@@ -757,8 +770,8 @@ int splits_for(int64_t tiles, int64_t K, int terms) {
 
 // Symbols a block of k_head_few takes; 0: not for this call.
 int few_width(const reno_head& p, bool grad) {
-  if (grad || p.rows > FEW_ROWS || (int64_t)(p.rows <= 1 ? 1 : p.rows <= 4 ? 4 : 8) * p.channels > FEW_H) return 0;
-  return p.symbols >= 32768 ? 256 : 64;
+  if (grad || p.rows > FEW_ROWS || (int64_t)(p.rows <= 1 ? 1 : 4) * p.channels > FEW_H) return 0;
+  return p.symbols >= 32768 ? 128 : 64;
 }
 
 struct Plan {
@@ -941,8 +954,8 @@ hipError_t run_head(const HeadCall& c, hipStream_t st) {
     const int wide = (uintptr_t)a.w % 16 == 0 && p.w_stride * size % 16 == 0;
     a.R = N;
     const auto args = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(512), 0, st, a, wide); };
-    if (few == 256) N <= 1 ? args(k_head_few<TYPE, 256, 1>) : N <= 4 ? args(k_head_few<TYPE, 256, 4>) : args(k_head_few<TYPE, 256, 8>);
-    else N <= 1 ? args(k_head_few<TYPE, 64, 1>) : N <= 4 ? args(k_head_few<TYPE, 64, 4>) : args(k_head_few<TYPE, 64, 8>);
+    if (few == 128) N <= 1 ? args(k_head_few<TYPE, 128, 1>) : args(k_head_few<TYPE, 128, 4>);
+    else N <= 1 ? args(k_head_few<TYPE, 64, 1>) : args(k_head_few<TYPE, 64, 4>);
     hipLaunchKernelGGL(k_head_rows, dim3((unsigned)((N + 15) / 16)), dim3(256), 0, st, a);
     return hipGetLastError();
   }
@@ -973,7 +986,7 @@ hipError_t run_head(const HeadCall& c, hipStream_t st) {
     hipLaunchKernelGGL(k_head_rows, dim3((unsigned)((a.R + 15) / 16)), dim3(256), 0, st, a);
     if (!c.grad) continue;
     const int64_t row_blocks = (a.R + DZ_ROWS - 1) / DZ_ROWS;
-    hipLaunchKernelGGL(k_head_dz<TYPE>, dim3((unsigned)(((a.Vp + 255) / 256 * row_blocks + 3) / 4)), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(k_head_dz<TYPE>, dim3((unsigned)(((a.Vp + 511) / 512 * row_blocks + 3) / 4)), dim3(256), 0, st, a);
     const Operand D{a.dz, pl.Vp, a.R, a.R * pl.Vp, a.d_plane};
     if (c.d.dh) {
       void* out = static_cast<char*>(c.d.dh) + a.r0 * p.channels * size;

@@ -67,15 +67,19 @@ __device__ __forceinline__ s16x8 read_tr(const char* lo, const char* hi) {
   return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-// Places of 32-byte slots so that a transposed read (one slot of 16 rows 8 g + j) meets each bank twice
-// at most, for rows of 512 or 256, 128 and 64 bytes.
-__device__ __forceinline__ int swz512(int r) { return (r & 3) | ((r >> 3 & 1) << 2); }
-__device__ __forceinline__ int swz128(int r) { return (r >> 1 & 1) | ((r >> 3 & 1) << 1); }
-template <int CP>
-__device__ __forceinline__ int swz_h(int r) {
-  if constexpr (CP == 32) return r >> 3 & 1;
-  else if constexpr (CP == 64) return swz128(r);
-  else return swz512(r);
+__device__ __forceinline__ void store8(char* base, int lo, int hi, s16x8 x) {
+  *reinterpret_cast<s16x4*>(base + lo) = __builtin_shufflevector(x, x, 0, 1, 2, 3);
+  *reinterpret_cast<s16x4*>(base + hi) = __builtin_shufflevector(x, x, 4, 5, 6, 7);
+}
+
+// Where the 8-byte piece p of row r lies, for rows of B bytes (64, or a multiple of 128): pieces change places
+// by the row, so that neither a transposed read (4 pieces of 4 consecutive rows for each 16 lanes) nor one piece of
+// 16 rows meets a bank twice.
+// The low 4 (64-byte rows: 3) bits of p change with r mod 16 alone: 16 rows or 16 (8) pieces on are a constant away.
+template <int B>
+__device__ __forceinline__ int piece(int r, int p) {
+  const int s = B == 64 ? (r >> 1 & 1) << 2 | (r >> 2 & 3) : (r & 3) << 2 | (r >> 2 & 3);
+  return r * B + (p ^ s) * 8;
 }
 
 template <int CT, int VQ, bool GRAD>
@@ -87,13 +91,6 @@ struct NarrowLds {
   static constexpr int Q = D + 3 * D_PLANE;   // D also holds the targets' probabilities
   static constexpr int B = Q, BYTES = B + VQ * 64 * 4;
 };
-
-// VQ: 64 symbols each; rows of W in LDS are 128 VQ bytes
-template <int VQ>
-__device__ __forceinline__ int swz_w(int c) {
-  if constexpr (VQ == 4) return swz512(c);
-  else return swz128(c);
-}
 
 // DENSE: targets with probabilities (a distillation); the registers then keep the logits, whose
 // exponentials are taken again for dz, so that no probability is too small for its bits.
@@ -115,24 +112,43 @@ __global__ void __launch_bounds__(NB_THREADS) k_narrow(NarrowArgs a) {
       s16x8 p[3];
       split_any8(x, p);
 #pragma unroll
-      for (int t = 0; t < 3; ++t)
-        *reinterpret_cast<s16x8*>(lds + L::W + t * L::W_PLANE + c * (VQ * 128) + ((v / 16) ^ swz_w<VQ>(c)) * 32 +
-                                  (v & 8) * 2) = p[t];
+      for (int t = 0; t < 3; ++t) store8(lds + L::W + t * L::W_PLANE, piece<VQ * 128>(c, v / 4), piece<VQ * 128>(c, v / 4 + 1), p[t]);
     }
   }
   __syncthreads();
   // What the loop over rows reads of W is the same every time, but does not fit the registers: with the lane and
   // the pointers opaque to the compiler it is not taken out of the loop (and spilled).
   int lane_w = lane;
+  // LDS places: W for z (4 symbol groups, channels c and c + 4) and for dh, dz and h as written and as read back
+  int az[4][2], ad[2][2], dw_at[2][2], dr_at[2], hw_at[2], hr_at[2];
+  {
+    const int c = 8 * g + (l15 >> 2), r = 16 * wave + l15;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int q = 0; q < 2; ++q) az[i][q] = L::W + piece<VQ * 128>(c + 4 * q, 4 * i + (l15 & 3));
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        ad[i][q] = L::W + piece<VQ * 128>(l15, 8 * i + 4 * q + g);
+        dw_at[i][q] = L::D + piece<128>(r, 8 * i + 4 * q + g);
+      }
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      dr_at[q] = L::D + piece<128>(c + 4 * q, 4 * (wave & 3) + (l15 & 3));
+      hw_at[q] = L::H + piece<CP * 2>(r, 2 * g + q);
+      hr_at[q] = L::H + piece<CP * 2>(c + 4 * q, 4 * (wave >> 2) + (l15 & 3));
+    }
+  }
   const uint16_t *wz = a.wz, *wd = a.wd;
   // fragments of W: 16 symbols x 32 channels (z), and 16 channels x 32 symbols in the order of z's registers (dh)
   const auto frag_z = [&](int vt, int ks, s16x8 (&o)[3]) {
     if constexpr (L::W_HERE) {
-      const int c = 32 * ks + 8 * (lane_w >> 4) + (lane_w >> 2 & 3);
-      const char* p = lds + L::W + c * (VQ * 128) + (lane_w & 3) * 8;
-      const int s0 = (vt ^ swz_w<VQ>(c)) * 32, s1 = (vt ^ swz_w<VQ>(c + 4)) * 32 + 4 * (VQ * 128);
+      const char* p0 = lds + az[vt & 3][0] + (32 * ks * VQ * 128 + (vt >> 2) * 128);
+      const char* p1 = lds + az[vt & 3][1] + (32 * ks * VQ * 128 + (vt >> 2) * 128);
 #pragma unroll
-      for (int t = 0; t < 3; ++t) o[t] = read_tr(p + t * L::W_PLANE + s0, p + t * L::W_PLANE + s1);
+      for (int t = 0; t < 3; ++t) o[t] = read_tr(p0 + t * L::W_PLANE, p1 + t * L::W_PLANE);
     } else {
       const s16x8* p = reinterpret_cast<const s16x8*>(wz) + (vt * KS + ks) * 192 + lane_w;
 #pragma unroll
@@ -141,12 +157,12 @@ __global__ void __launch_bounds__(NB_THREADS) k_narrow(NarrowArgs a) {
   };
   const auto frag_d = [&](int u, int ct, s16x8 (&o)[3]) {
     if constexpr (L::W_HERE) {
-      const int c = 16 * ct + (lane_w & 15), f = swz_w<VQ>(c);
-      const char* p = lds + L::W + c * (VQ * 128) + (lane_w >> 4) * 8;
+      const char* p0 = lds + ad[u & 1][0] + (16 * ct * VQ * 128 + (u >> 1) * 128);
+      const char* p1 = lds + ad[u & 1][1] + (16 * ct * VQ * 128 + (u >> 1) * 128);
 #pragma unroll
       for (int t = 0; t < 3; ++t) {
-        const s16x4 lo = *reinterpret_cast<const s16x4*>(p + t * L::W_PLANE + ((2 * u) ^ f) * 32);
-        const s16x4 hi = *reinterpret_cast<const s16x4*>(p + t * L::W_PLANE + ((2 * u + 1) ^ f) * 32);
+        const s16x4 lo = *reinterpret_cast<const s16x4*>(p0 + t * L::W_PLANE);
+        const s16x4 hi = *reinterpret_cast<const s16x4*>(p1 + t * L::W_PLANE);
         o[t] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
       }
     } else {
@@ -212,11 +228,12 @@ __global__ void __launch_bounds__(NB_THREADS) k_narrow(NarrowArgs a) {
       for (int e = 0; e < 8; ++e) x[ks][e] = flag ? x[ks][e] : 0.0f;
       split_any8(x[ks], hf[ks]);
       if constexpr (GRAD) {
-        const int r = 16 * wave + l15;
 #pragma unroll
-        for (int t = 0; t < 3; ++t)
-          *reinterpret_cast<s16x8*>(lds + L::H + t * L::H_PLANE + r * (CP * 2) + ((2 * ks + (g >> 1)) ^ swz_h<CP>(r)) * 32 +
-                                    (g & 1) * 16) = hf[ks][t];
+        for (int t = 0; t < 3; ++t) {
+          // 8 ks pieces on: past the 16 that the rows exchange, or (ks odd) the same with bit 3 of the place flipped
+          const int far = t * L::H_PLANE + (ks >> 1) * 128, flip = ks & 1 ? 64 : 0;
+          store8(lds + far, hw_at[0] ^ flip, hw_at[1] ^ flip, hf[ks][t]);
+        }
       }
     }
     if (AHEAD && step + gridDim.x < steps) load_h(step + gridDim.x);
@@ -249,28 +266,35 @@ __global__ void __launch_bounds__(NB_THREADS) k_narrow(NarrowArgs a) {
     m = fmaxf(m, __shfl_xor(m, 16));
     m = fmaxf(m, __shfl_xor(m, 32));
     const float base = m > -INFINITY ? m : 0.0f;
-    float at_target = 0.0f;   // of the lane that holds the target, z - base
+    // the target is element sub of the 4 in register group tv, in the lane with its row and (target >> 2 & 3) = g
+    f32x4 at_target = {0.f, 0.f, 0.f, 0.f};
+    const int tv = DENSE || (target >> 2 & 3) != g ? -1 : target >> 4;
 #pragma unroll
     for (int vt = 0; vt < VT; ++vt)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const float t = z[vt][e] - base, y = exp2_hw(t);
-        if (!DENSE && target - 4 * g == 16 * vt + e) at_target = t;
+        if (!DENSE) at_target[e] = tv == vt ? t : at_target[e];
         z[vt][e] = DENSE ? t : y;
         s += y;
       }
-    asm volatile("" : "+v"(target));   // the comparisons below are made again: 64 of them kept fill the scalar registers
     s += __shfl_xor(s, 16);
     s += __shfl_xor(s, 32);
     const float lse = log2_hw(s);  // over base
     float bits = 0.0f;
     if constexpr (!DENSE) {
-      const bool mine = flag == 1 && ((target >> 2) & 3) == g;
-      bits = mine ? lse - at_target : 0.0f;
+      const int e = target & 3;
+      const float t = e == 0 ? at_target[0] : e == 1 ? at_target[1] : e == 2 ? at_target[2] : at_target[3];
+      bits = flag == 1 && tv >= 0 ? lse - t : 0.0f;
     }
     if (lane < 16 && in && a.lse) a.lse[row] = flag ? (base + lse) * LN2 : 0.0f;
-    const float inv = flag == 2 ? NAN : weight / s;
-    const float w1 = flag == 2 ? NAN : weight;
+    const float w1 = flag == 2 ? NAN : flag ? weight : 0.0f;
+    const float inv = flag ? w1 / s : 0.0f;
+    f32x4 sub;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sub[e] = (target & 3) == e ? -w1 : 0.0f;
+    int tq = tv;
+    asm volatile("" : "+v"(tq));   // the comparisons are made again: kept, they fill the scalar registers
     f32x4 dh[GRAD ? CT : 1];
 #pragma unroll
     for (int ct = 0; ct < (GRAD ? CT : 1); ++ct) dh[ct] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -311,19 +335,14 @@ __global__ void __launch_bounds__(NB_THREADS) k_narrow(NarrowArgs a) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const int vt = 4 * vq + 2 * u + i;
-              const float one = DENSE ? q[2 * u + i][e] : target - 4 * g == 16 * vt + e ? 1.0f : 0.0f;
-              const float y = fmaf(DENSE ? exp2_hw(z[vt][e]) : z[vt][e], inv, -one * w1);
-              d[4 * i + e] = flag ? y : 0.0f;
+              const float one = DENSE ? -w1 * q[2 * u + i][e] : tq == vt ? sub[e] : 0.0f;
+              d[4 * i + e] = fmaf(DENSE ? exp2_hw(z[vt][e]) : z[vt][e], inv, one);
             }
           s16x8 p[3];
           split_any8(d, p);
-          const int r = 16 * wave + l15;
 #pragma unroll
-          for (int t = 0; t < 3; ++t) {
-            char* o = lds + L::D + t * L::D_PLANE + r * 128 + g * 8;
-            *reinterpret_cast<s16x4*>(o + ((2 * u) ^ swz128(r)) * 32) = __builtin_shufflevector(p[t], p[t], 0, 1, 2, 3);
-            *reinterpret_cast<s16x4*>(o + ((2 * u + 1) ^ swz128(r)) * 32) = __builtin_shufflevector(p[t], p[t], 4, 5, 6, 7);
-          }
+          for (int t = 0; t < 3; ++t) store8(lds + t * L::D_PLANE, dw_at[u][0], dw_at[u][1], p[t]);
+          __builtin_amdgcn_sched_barrier(0);
           frag_d(2 * vq + u, 0, w[0]);
 #pragma unroll
           for (int ct = 0; ct < CT; ++ct) {
@@ -333,23 +352,21 @@ __global__ void __launch_bounds__(NB_THREADS) k_narrow(NarrowArgs a) {
           }
         }
         __syncthreads();
-        const int vt = wave & 3;
 #pragma unroll
         for (int ks = 0; ks < NB_ROWS / 32; ++ks) {
-          const int r = 32 * ks + 8 * g + (l15 >> 2);
-          const char* pd = lds + L::D + r * 128 + (l15 & 3) * 8;
-          const int d0 = (vt ^ swz128(r)) * 32, d1 = (vt ^ swz128(r + 4)) * 32 + 4 * 128;
           s16x8 dz[3];
 #pragma unroll
-          for (int t = 0; t < 3; ++t) dz[t] = read_tr(pd + t * L::D_PLANE + d0, pd + t * L::D_PLANE + d1);
+          for (int t = 0; t < 3; ++t)
+            dz[t] = read_tr(lds + dr_at[0] + (t * L::D_PLANE + 32 * ks * 128), lds + dr_at[1] + (t * L::D_PLANE + 32 * ks * 128));
 #pragma unroll
           for (int j = 0; j < DW_N; ++j) {
-            const int ct = (wave >> 2) + 2 * j;
-            const char* ph = lds + L::H + r * (CP * 2) + (l15 & 3) * 8;
-            const int h0 = (ct ^ swz_h<CP>(r)) * 32, h1 = (ct ^ swz_h<CP>(r + 4)) * 32 + 4 * (CP * 2);
+            // two tiles of channels on: 8 pieces, as above
             s16x8 h[3];
 #pragma unroll
-            for (int t = 0; t < 3; ++t) h[t] = read_tr(ph + t * L::H_PLANE + h0, ph + t * L::H_PLANE + h1);
+            for (int t = 0; t < 3; ++t) {
+              const int far = t * L::H_PLANE + 32 * ks * (CP * 2) + (j >> 1) * 128, flip = j & 1 ? 64 : 0;
+              h[t] = read_tr(lds + (hr_at[0] ^ flip) + far, lds + (hr_at[1] ^ flip) + far);
+            }
             dw[vq][j] = mfma6(h, dz, dw[vq][j]);
           }
           if ((ks & 1) == (wave >> 2)) {  // db: ones for h, every second 32 rows
@@ -372,7 +389,8 @@ __global__ void __launch_bounds__(NB_THREADS) k_narrow(NarrowArgs a) {
         for (int ct = 0; ct < CT; ++ct) {
           const int c = 16 * ct + 4 * g;
           float* o = a.dh + row * a.C + c;
-          const f32x4 y = dh[ct] * a.out_scale;
+          f32x4 y = dh[ct] * a.out_scale;
+          if (!flag) y = f32x4{0.f, 0.f, 0.f, 0.f};   // also where weights that are NaN reach it
           if (a.C % 4 == 0 && (uintptr_t)a.dh % 16 == 0) {
             if (c < a.C) *reinterpret_cast<f32x4*>(o) = y;
           } else {
