@@ -1,17 +1,16 @@
 // Narrow fp32 heads (C <= 128, V <= 256: the codec's own): code length and
 // distillation with their gradients in one pass over the rows.
 //
-// A block of 8 waves takes 128 rows at a time, 16 a wave, all V logits of
-// a row in the registers of 4 lanes: softmax statistics are two lane exchanges,
+// A block takes 16 rows a wave at a time, all V logits of a row in the registers of 4 lanes: softmax statistics are two lane exchanges,
 // and nothing of the logits goes to memory.  Every operand is three bf16 parts
 // (24 bits), a product the six terms above 2^-24.
 //   z   = W^T h     A: 16 symbols x 32 channels of W, B: 32 channels x 16 rows
 //   dh  = W dz      the accumulator layout of z (row = lane & 15, symbols 4 (lane >> 4) + i
 //                   of each 16) taken as it is for B: k runs over the symbols in that
 //                   order, and W is read in the same one
-//   dw  = h dz^T    k runs over rows, so dz crosses lanes through LDS, 64 symbols of
-//                   128 rows at a time, and is read back transposed; each wave holds the
-//                   sums of its own tiles of dw over all rows of the block
+//   dw  = h dz^T    k runs over rows, so dz crosses lanes through LDS, 32 symbols of
+//                   all the block's rows at a time, and is read back transposed; each wave
+//                   holds the sums of its own tiles of dw over all rows of the block
 // W lies in LDS for C <= 32 (one copy serves both products: transposed reads
 // for z, rows for dh); wider ones stream from L2, laid out as the lanes read them.
 // The blocks' sums of dw and db are joined in a fixed order by k_narrow_join.
@@ -30,8 +29,9 @@
 namespace reno {
 namespace {
 
-constexpr int NB_WAVES = 8, NB_THREADS = 64 * NB_WAVES, NB_ROWS = 16 * NB_WAVES;
-constexpr int NB_BLOCKS = 256;      // one a CU
+// Waves of a block.  C <= 32: two blocks of 4 waves a CU, so that one's products run during the other's
+// vector work; wider heads, whose tiles of dw would not fit the registers of so few waves: one block of 8.
+constexpr int waves_of(int ct) { return ct == 2 ? 4 : 8; }
 
 struct NarrowArgs {
   int64_t N;
@@ -46,7 +46,7 @@ struct NarrowArgs {
   const uint16_t* wz;      // streamed W: [16 symbols][32 channels] fragments, then [16 channels][32 symbols]
   const uint16_t* wd;
   float *bits, *lse, *dh;
-  float* part;             // [blocks][C + 2][V]: dw, two halves of db
+  float* part;             // [blocks][C + waves / 2][V]: dw, shares of db
   int wide;                // rows of h in 16-byte pieces
 };
 
@@ -82,21 +82,24 @@ __device__ __forceinline__ int piece(int r, int p) {
   return r * B + (p ^ s) * 8;
 }
 
-template <int CT, int VQ, bool GRAD>
+template <int CT, int VQ, bool GRAD, bool DENSE>
 struct NarrowLds {
-  static constexpr int CP = 16 * CT;
+  static constexpr int NW = waves_of(CT), ROWS = 16 * NW, CP = 16 * CT;
   static constexpr bool W_HERE = CT == 2;
-  static constexpr int W_PLANE = CP * VQ * 128, H_PLANE = NB_ROWS * CP * 2, D_PLANE = NB_ROWS * 128;
+  static constexpr int W_PLANE = CP * VQ * 128, H_PLANE = ROWS * CP * 2, D_PLANE = ROWS * 64;
   static constexpr int W = 0, H = W + (W_HERE ? 3 * W_PLANE : 0), D = H + (GRAD ? 3 * H_PLANE : 0);
-  static constexpr int Q = D + 3 * D_PLANE;   // D also holds the targets' probabilities
-  static constexpr int B = Q, BYTES = B + VQ * 64 * 4;
+  // 32 symbols' dz; a block alone on its CU has two such buffers and half the barriers.  They also hold
+  // the targets' probabilities while dz is made.
+  static constexpr int D_BUF = 3 * D_PLANE, BUFS = GRAD && NW == 8 ? 2 : 1;
+  static constexpr int B = D + (GRAD || DENSE ? BUFS * D_BUF : 0), BYTES = B + VQ * 64 * 4;
 };
 
 // DENSE: targets with probabilities (a distillation); the registers then keep the logits, whose
 // exponentials are taken again for dz, so that no probability is too small for its bits.
 template <int CT, int VQ, bool GRAD, bool DENSE>
-__global__ void __launch_bounds__(NB_THREADS) k_narrow(NarrowArgs a) {
-  using L = NarrowLds<CT, VQ, GRAD>;
+__global__ void __launch_bounds__(64 * waves_of(CT), 2) k_narrow(NarrowArgs a) {
+  using L = NarrowLds<CT, VQ, GRAD, DENSE>;
+  constexpr int NB_WAVES = L::NW, NB_THREADS = 64 * NB_WAVES, NB_ROWS = L::ROWS;
   constexpr int CP = L::CP, KS = CP / 32, VT = 4 * VQ;
   __shared__ __attribute__((aligned(1024))) char lds[L::BYTES];
   const int tid = threadIdx.x, lane = tid & 63, l15 = lane & 15, g = lane >> 4;
@@ -120,7 +123,8 @@ __global__ void __launch_bounds__(NB_THREADS) k_narrow(NarrowArgs a) {
   // the pointers opaque to the compiler it is not taken out of the loop (and spilled).
   int lane_w = lane;
   // LDS places: W for z (4 symbol groups, channels c and c + 4) and for dh, dz and h as written and as read back
-  int az[4][2], ad[2][2], dw_at[2][2], dr_at[2], hw_at[2], hr_at[2];
+  int az[4][2], ad[2][2], dw_at[2], dr_at[2], hw_at[2], hr_at[2];
+  const int my_v = wave & 1, my_c = wave >> 1;   // this wave's tiles of dw: 16 of 32 symbols, every (NW / 2)th 16 channels
   {
     const int c = 8 * g + (l15 >> 2), r = 16 * wave + l15;
 #pragma unroll
@@ -130,15 +134,13 @@ __global__ void __launch_bounds__(NB_THREADS) k_narrow(NarrowArgs a) {
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        ad[i][q] = L::W + piece<VQ * 128>(l15, 8 * i + 4 * q + g);
-        dw_at[i][q] = L::D + piece<128>(r, 8 * i + 4 * q + g);
-      }
+      for (int q = 0; q < 2; ++q) ad[i][q] = L::W + piece<VQ * 128>(l15, 8 * i + 4 * q + g);
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-      dr_at[q] = L::D + piece<128>(c + 4 * q, 4 * (wave & 3) + (l15 & 3));
+      dw_at[q] = L::D + piece<64>(r, 4 * q + g);
+      dr_at[q] = L::D + piece<64>(c + 4 * q, 4 * my_v + (l15 & 3));
       hw_at[q] = L::H + piece<CP * 2>(r, 2 * g + q);
-      hr_at[q] = L::H + piece<CP * 2>(c + 4 * q, 4 * (wave >> 2) + (l15 & 3));
+      hr_at[q] = L::H + piece<CP * 2>(c + 4 * q, 4 * my_c + (l15 & 3));
     }
   }
   const uint16_t *wz = a.wz, *wd = a.wd;
@@ -172,12 +174,12 @@ __global__ void __launch_bounds__(NB_THREADS) k_narrow(NarrowArgs a) {
     }
   };
 
-  constexpr int DW_N = CT * 4 / NB_WAVES > 0 ? CT * 4 / NB_WAVES : 1;   // tiles of dw a wave holds of 64 symbols
-  f32x4 dw[GRAD ? VQ : 1][DW_N], db[GRAD ? VQ : 1];
+  constexpr int DB = NB_WAVES / 2, DW_N = CT / DB, U = 2 * VQ;
+  f32x4 dw[GRAD ? U : 1][DW_N], db[(U + 3) / 4];   // db of u: the lanes with lane >> 4 = u & 3
   if constexpr (GRAD) {
 #pragma unroll
-    for (int i = 0; i < VQ; ++i) {
-      db[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < U; ++i) {
+      db[i / 4] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int j = 0; j < DW_N; ++j) dw[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
@@ -299,84 +301,85 @@ __global__ void __launch_bounds__(NB_THREADS) k_narrow(NarrowArgs a) {
 #pragma unroll
     for (int ct = 0; ct < (GRAD ? CT : 1); ++ct) dh[ct] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int vq = 0; vq < VQ; ++vq) {
-      f32x4 q[4];
-      if constexpr (DENSE) {  // the targets' probabilities of 16 rows and 64 symbols, dense in LDS: rows 0-7 in plane 0, 8-15 in 1
-        char* mine = lds + L::D + wave * 2048;
+    for (int u = 0; u < U; ++u) {
+      const int buf = (u % L::BUFS) * L::D_BUF;
+      f32x4 q[2];
+      if constexpr (DENSE) {  // the targets' probabilities of 16 rows and 32 symbols, dense: rows 0-7 in plane 0, 8-15 in 1
+        char* mine = lds + L::D + buf + wave * 1024;
         const int rl = lane >> 2;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          *reinterpret_cast<f32x4*>(mine + (i >> 1) * L::D_PLANE + (i & 1) * 1024 + lane * 16) = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < 2; ++i) *reinterpret_cast<f32x4*>(mine + i * L::D_PLANE + lane * 16) = f32x4{0.f, 0.f, 0.f, 0.f};
         wave_lds_fence();
         const int64_t r = step * NB_ROWS + 16 * wave + rl;
         if (r < a.N)
           for (int j = lane & 3; j < a.k; j += 4) {
-            const int id = a.index[r * a.k + j] - 64 * vq;
-            if (id >= 0 && id < 64)
-              *reinterpret_cast<float*>(mine + (rl >> 3) * L::D_PLANE + (rl & 7) * 256 + id * 4) = a.q[r * a.k + j];
+            const int id = a.index[r * a.k + j] - 32 * u;
+            if (id >= 0 && id < 32)
+              *reinterpret_cast<float*>(mine + (rl >> 3) * L::D_PLANE + (rl & 7) * 128 + id * 4) = a.q[r * a.k + j];
           }
         wave_lds_fence();
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          q[i] = *reinterpret_cast<const f32x4*>(mine + (l15 >> 3) * L::D_PLANE + (l15 & 7) * 256 + (16 * i + 4 * g) * 4);
+        for (int i = 0; i < 2; ++i)
+          q[i] = *reinterpret_cast<const f32x4*>(mine + (l15 >> 3) * L::D_PLANE + (l15 & 7) * 128 + (16 * i + 4 * g) * 4);
         wave_lds_fence();
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            if (q[i][e] != 0.0f) bits += q[i][e] * (lse - z[4 * vq + i][e]);
+            if (q[i][e] != 0.0f) bits += q[i][e] * (lse - z[2 * u + i][e]);
       }
       if constexpr (GRAD) {
+        float d[8];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          float d[8];
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
-          for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int vt = 4 * vq + 2 * u + i;
-              const float one = DENSE ? -w1 * q[2 * u + i][e] : tq == vt ? sub[e] : 0.0f;
-              d[4 * i + e] = fmaf(DENSE ? exp2_hw(z[vt][e]) : z[vt][e], inv, one);
-            }
-          s16x8 p[3];
-          split_any8(d, p);
-#pragma unroll
-          for (int t = 0; t < 3; ++t) store8(lds + t * L::D_PLANE, dw_at[u][0], dw_at[u][1], p[t]);
-          __builtin_amdgcn_sched_barrier(0);
-          frag_d(2 * vq + u, 0, w[0]);
-#pragma unroll
-          for (int ct = 0; ct < CT; ++ct) {
-            if (ct + 1 < CT) frag_d(2 * vq + u, ct + 1, w[(ct + 1) & 1]);
-            dh[ct] = mfma6(w[ct & 1], p, dh[ct]);
-            __builtin_amdgcn_sched_barrier(0);
+          for (int e = 0; e < 4; ++e) {
+            const int vt = 2 * u + i;
+            const float one = DENSE ? -w1 * q[i][e] : tq == vt ? sub[e] : 0.0f;
+            d[4 * i + e] = fmaf(DENSE ? exp2_hw(z[vt][e]) : z[vt][e], inv, one);
           }
+        s16x8 p[3];
+        split_any8(d, p);
+#pragma unroll
+        for (int t = 0; t < 3; ++t) store8(lds + buf + t * L::D_PLANE, dw_at[0], dw_at[1], p[t]);
+        __builtin_amdgcn_sched_barrier(0);
+        frag_d(u, 0, w[0]);
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+          if (ct + 1 < CT) frag_d(u, ct + 1, w[(ct + 1) & 1]);
+          dh[ct] = mfma6(w[ct & 1], p, dh[ct]);
+          __builtin_amdgcn_sched_barrier(0);
         }
         __syncthreads();
+        // products of these 32 symbols' dz with h for this wave's tiles
 #pragma unroll
         for (int ks = 0; ks < NB_ROWS / 32; ++ks) {
           s16x8 dz[3];
 #pragma unroll
           for (int t = 0; t < 3; ++t)
-            dz[t] = read_tr(lds + dr_at[0] + (t * L::D_PLANE + 32 * ks * 128), lds + dr_at[1] + (t * L::D_PLANE + 32 * ks * 128));
+            dz[t] = read_tr(lds + dr_at[0] + (buf + t * L::D_PLANE + 32 * ks * 64), lds + dr_at[1] + (buf + t * L::D_PLANE + 32 * ks * 64));
 #pragma unroll
           for (int j = 0; j < DW_N; ++j) {
-            // two tiles of channels on: 8 pieces, as above
+            // NW / 2 tiles of channels on: 8 or 16 pieces (NW = 8: past what the rows exchange)
+            static_assert(DW_N == 1 || NB_WAVES == 8, "one tile of channels a wave, or 64 channels apart");
             s16x8 h[3];
 #pragma unroll
             for (int t = 0; t < 3; ++t) {
-              const int far = t * L::H_PLANE + 32 * ks * (CP * 2) + (j >> 1) * 128, flip = j & 1 ? 64 : 0;
-              h[t] = read_tr(lds + (hr_at[0] ^ flip) + far, lds + (hr_at[1] ^ flip) + far);
+              const int far = t * L::H_PLANE + 32 * ks * (CP * 2) + j * 128;
+              h[t] = read_tr(lds + hr_at[0] + far, lds + hr_at[1] + far);
             }
-            dw[vq][j] = mfma6(h, dz, dw[vq][j]);
+            dw[u][j] = mfma6(h, dz, dw[u][j]);
           }
-          if ((ks & 1) == (wave >> 2)) {  // db: ones for h, every second 32 rows
-            const s16x8 ones = {0x3f80, 0x3f80, 0x3f80, 0x3f80, 0x3f80, 0x3f80, 0x3f80, 0x3f80};
+          if (ks == my_c) {  // db: ones for h, in four of the 16 output rows; the waves of other channels take other rows
+            const int one = (lane_w >> 2 & 3) == (u & 3) ? 0x3f803f80 : 0;
+            const s16x8 ones = __builtin_bit_cast(s16x8, i32x4{one, one, one, one});
 #pragma unroll
-            for (int t = 2; t >= 0; --t) db[vq] = mfma<false>(ones, dz[t], db[vq]);
+            for (int t = 2; t >= 0; --t) db[u / 4] = mfma<false>(ones, dz[t], db[u / 4]);
           }
           __builtin_amdgcn_sched_barrier(0);
         }
-        __syncthreads();
+        if (L::BUFS == 1 || u + 1 == U) __syncthreads();
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
     bits += __shfl_xor(bits, 16);
@@ -403,19 +406,19 @@ __global__ void __launch_bounds__(NB_THREADS) k_narrow(NarrowArgs a) {
     }
   }
   if constexpr (GRAD) {
-    float* part = a.part + (int64_t)blockIdx.x * (a.C + 2) * a.V;
+    float* part = a.part + (int64_t)blockIdx.x * (a.C + DB) * a.V;
 #pragma unroll
-    for (int vq = 0; vq < VQ; ++vq) {
-      const int v = 64 * vq + 16 * (wave & 3) + l15;
+    for (int u = 0; u < U; ++u) {
+      const int v = 32 * u + 16 * my_v + l15;
       if (v >= a.V) continue;
 #pragma unroll
       for (int j = 0; j < DW_N; ++j)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int c = 16 * ((wave >> 2) + 2 * j) + 4 * g + e;
-          if (c < a.C) part[(int64_t)c * a.V + v] = dw[vq][j][e];
+          const int c = 16 * (my_c + DB * j) + 4 * g + e;
+          if (c < a.C) part[(int64_t)c * a.V + v] = dw[u][j][e];
         }
-      if (g == 0) part[(int64_t)(a.C + (wave >> 2)) * a.V + v] = db[vq][0];
+      if (g == (u & 3)) part[(int64_t)(a.C + my_c) * a.V + v] = db[u / 4][0];
     }
   }
 }
@@ -441,36 +444,45 @@ __global__ void __launch_bounds__(256) k_narrow_pack(NarrowArgs a, int KS, int C
   }
 }
 
-// dw and db from the blocks' sums: 32 values a block, 8 shares of the blocks each.
-__global__ void __launch_bounds__(256) k_narrow_join(const float* __restrict__ part, int blocks, int C, int V, float scale,
-                                                     float* __restrict__ dw, float* __restrict__ db) {
-  __shared__ float s[8][33];
-  const int i = threadIdx.x & 31, share = threadIdx.x >> 5;
-  const int64_t n = (int64_t)C * V, all = n + 2 * V, at = (int64_t)blockIdx.x * 32 + i;
+// dw and db from the blocks' sums: 16 values a block, 16 shares of the blocks each.
+__global__ void __launch_bounds__(256) k_narrow_join(const float* __restrict__ part, int blocks, int C, int V, int DB,
+                                                     float scale, float* __restrict__ dw, float* __restrict__ db) {
+  __shared__ float s[16][17];
+  const int i = threadIdx.x & 15, share = threadIdx.x >> 4;
+  const int64_t n = (int64_t)C * V, all = n + (int64_t)DB * V, at = (int64_t)blockIdx.x * 16 + i;
   float x = 0.0f;
   if (at < n + V) {
-#pragma unroll 8
-    for (int b = share; b < blocks; b += 8) {
-      const float* p = part + b * all + at;
-      x += at < n ? p[0] : p[0] + p[V];
+    const int shares = at < n ? 1 : DB;   // db has DB rows, each a share of the block's rows
+    for (int q = 0; q < shares; ++q) {
+      const float* p = part + at + (int64_t)q * V;
+#pragma unroll 16
+      for (int b = share; b < blocks; b += 16) x += p[b * all];
     }
   }
   s[share][i] = x;
   __syncthreads();
   if (share != 0 || at >= n + V) return;
   x = 0.0f;
-  for (int k = 0; k < 8; ++k) x += s[k][i];
+  for (int k = 0; k < 16; ++k) x += s[k][i];
   if (at < n) {
     if (dw) dw[at] = x * scale;
   } else if (db) db[at - n] = x * scale;
 }
 
-int narrow_blocks(int64_t rows) { return (int)std::min<int64_t>(NB_BLOCKS, (rows + NB_ROWS - 1) / NB_ROWS); }
+int width_of(int channels) { return channels <= 32 ? 2 : channels <= 64 ? 4 : 8; }
+// as many as run at a time
+int narrow_blocks(const reno_head& p) {
+  const int nw = waves_of(width_of(p.channels));
+  return (int)std::min<int64_t>(256 * (8 / nw), (p.rows + 16 * nw - 1) / (16 * nw));
+}
+int64_t part_bytes(const reno_head& p) {
+  return (int64_t)narrow_blocks(p) * (p.channels + waves_of(width_of(p.channels)) / 2) * p.symbols * 4;
+}
 int64_t up256(int64_t x) { return (x + 255) / 256 * 256; }
 
 template <int CT, int VQ>
 void run(const NarrowArgs& a, bool grad, int blocks, hipStream_t st) {
-  const auto args = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(blocks), dim3(NB_THREADS), 0, st, a); };
+  const auto args = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(blocks), dim3(64 * waves_of(CT)), 0, st, a); };
   if (a.q) grad ? args(k_narrow<CT, VQ, true, true>) : args(k_narrow<CT, VQ, false, true>);
   else grad ? args(k_narrow<CT, VQ, true, false>) : args(k_narrow<CT, VQ, false, false>);
 }
@@ -481,8 +493,8 @@ bool head_is_narrow(const reno_head& p) { return p.type == RENO_T_FP32 && p.chan
 
 // workspace: the blocks' sums, then W as it is streamed
 int64_t head_narrow_bytes(const reno_head& p, bool grad) {
-  const int64_t cp = p.channels <= 32 ? 32 : p.channels <= 64 ? 64 : 128;
-  int64_t n = grad ? up256((int64_t)narrow_blocks(p.rows) * (p.channels + 2) * p.symbols * 4) : 0;
+  const int64_t cp = 16 * width_of(p.channels);
+  int64_t n = grad ? up256(part_bytes(p)) : 0;
   if (cp > 32) n += 2 * up256(cp * 256 * 3 * 2);
   return n;
 }
@@ -510,13 +522,13 @@ hipError_t launch_head_narrow(const HeadCall& c, const HeadTargets& t, char* ws,
   a.lse = c.d.lse;
   a.dh = static_cast<float*>(c.d.dh);
   a.wide = (uintptr_t)a.h % 16 == 0 && p.h_stride % 4 == 0;
-  const int blocks = narrow_blocks(p.rows);
+  const int blocks = narrow_blocks(p);
   char* at = ws;
   if (c.grad) {
     a.part = reinterpret_cast<float*>(at);
-    at += up256((int64_t)blocks * (p.channels + 2) * p.symbols * 4);
+    at += up256(part_bytes(p));
   }
-  const int CT = p.channels <= 32 ? 2 : p.channels <= 64 ? 4 : 8, VQ = p.symbols <= 64 ? 1 : 4;
+  const int CT = width_of(p.channels), VQ = p.symbols <= 64 ? 1 : 4;
   if (CT > 2) {
     uint16_t* wz = reinterpret_cast<uint16_t*>(at);
     uint16_t* wd = reinterpret_cast<uint16_t*>(at + up256((int64_t)CT * 16 * 256 * 3 * 2));
@@ -536,8 +548,8 @@ hipError_t launch_head_narrow(const HeadCall& c, const HeadTargets& t, char* ws,
   }
   if (c.d.dw || c.d.db) {
     const int64_t n = (int64_t)(a.C + 1) * a.V;
-    hipLaunchKernelGGL(k_narrow_join, dim3((unsigned)((n + 31) / 32)), dim3(256), 0, st, a.part, blocks, a.C, a.V,
-                       a.out_scale, static_cast<float*>(c.d.dw), static_cast<float*>(c.d.db));
+    hipLaunchKernelGGL(k_narrow_join, dim3((unsigned)((n + 15) / 16)), dim3(256), 0, st, a.part, blocks, a.C, a.V,
+                       waves_of(CT) / 2, a.out_scale, static_cast<float*>(c.d.dw), static_cast<float*>(c.d.db));
   }
   return hipGetLastError();
 }
