@@ -37,23 +37,24 @@ __device__ __forceinline__ float logit(const void* p, int64_t i) {
 template <int TYPE>
 struct Vec {
   static constexpr int N = TYPE == RENO_T_FP32 ? 4 : 8;
+  typedef uint4 Raw;
   float x[N];
-  __device__ __forceinline__ void load(const void* p, int64_t i) {
-    if constexpr (TYPE == RENO_T_FP32) {
-      const float4 v = *reinterpret_cast<const float4*>(static_cast<const float*>(p) + i);
-      x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
-    } else {
-      const uint4 v = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + i);
-      const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+  __device__ static __forceinline__ uint4 raw(const void* p, int64_t i) {
+    return *reinterpret_cast<const uint4*>(static_cast<const char*>(p) + i * (16 / N));
+  }
+  __device__ __forceinline__ void load(const void* p, int64_t i) { from(raw(p, i)); }
+  __device__ __forceinline__ void from(uint4 v) {
+    const uint32_t u[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if constexpr (TYPE == RENO_T_BF16) {
-          x[2 * e] = __uint_as_float(u[e] << 16);
-          x[2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u);
-        } else {
-          x[2 * e] = (float)__builtin_bit_cast(_Float16, (uint16_t)u[e]);
-          x[2 * e + 1] = (float)__builtin_bit_cast(_Float16, (uint16_t)(u[e] >> 16));
-        }
+    for (int e = 0; e < 4; ++e) {
+      if constexpr (TYPE == RENO_T_FP32) {
+        x[e] = __uint_as_float(u[e]);
+      } else if constexpr (TYPE == RENO_T_BF16) {
+        x[2 * e] = __uint_as_float(u[e] << 16);
+        x[2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u);
+      } else {
+        x[2 * e] = (float)__builtin_bit_cast(_Float16, (uint16_t)u[e]);
+        x[2 * e + 1] = (float)__builtin_bit_cast(_Float16, (uint16_t)(u[e] >> 16));
       }
     }
   }
@@ -96,14 +97,15 @@ template <int TYPE, int PL>
 __global__ void __launch_bounds__(256) k_top_short(const void* __restrict__ z, int64_t rows, int V, int64_t stride, int k,
                                                    int wide, int32_t* __restrict__ index, float* __restrict__ value,
                                                    float* __restrict__ lse) {
-  __shared__ uint64_t s_list[4][PL + 1][64];               // sorted lists, a row of lanes for each place
-  __shared__ uint64_t s_out[4][SHORT_ROWS * RENO_HEAD_MAX_TOP];
+  extern __shared__ uint64_t s_mem[];                      // for each wave: sorted lists, then the results
   const int lane = lane_id(), wave = threadIdx.x >> 6, l15 = lane & 15, rw = lane >> 4;
   const int64_t r0 = ((int64_t)blockIdx.x * 4 + wave) * SHORT_ROWS;
   if (r0 >= rows) return;
   const int64_t r = min(r0 + rw, rows - 1);
   const int64_t at = r * stride;
   const int v0 = l15 * PL;
+  uint64_t(*s_list)[64] = reinterpret_cast<uint64_t(*)[64]>(s_mem + wave * ((PL + 1) * 64 + SHORT_ROWS * k));   // [PL + 1]: a row of lanes for each place
+  uint64_t* s_out = s_list[PL + 1];
   float x[PL];
   if (PL == SHORT_LANE && wide && v0 + PL <= V) {
 #pragma unroll
@@ -136,8 +138,8 @@ __global__ void __launch_bounds__(256) k_top_short(const void* __restrict__ z, i
             key[i + j + q] = swap ? a : b;
           }
 #pragma unroll
-  for (int i = 0; i < PL; ++i) s_list[wave][i][lane] = key[i];
-  s_list[wave][PL][lane] = 0;
+  for (int i = 0; i < PL; ++i) s_list[i][lane] = key[i];
+  s_list[PL][lane] = 0;
   wave_lds_fence();
   if (lse) {
     const float m = from_ordered(row16_max((uint32_t)(key[0] >> 32)));
@@ -155,14 +157,14 @@ __global__ void __launch_bounds__(256) k_top_short(const void* __restrict__ z, i
     const uint32_t top = row16_max(o);
     const uint32_t tied = (uint32_t)(__ballot(o == top) >> (lane & 48)) & 0xffffu;
     const bool won = (tied & (0u - tied)) == 1u << l15;
-    if (won) s_out[wave][rw * k + j] = head;
+    if (won) s_out[rw * k + j] = head;
     place += won && place < PL ? 1 : 0;
-    head = s_list[wave][place][lane];
+    head = s_list[place][lane];
   }
   wave_lds_fence();
   const int n = (int)min((int64_t)SHORT_ROWS, rows - r0) * k;
   for (int i = lane; i < n; i += 64) {
-    const uint64_t h = s_out[wave][i];
+    const uint64_t h = s_out[i];
     index[r0 * k + i] = h ? (int32_t)~(uint32_t)h : -1;
     value[r0 * k + i] = from_ordered((uint32_t)(h >> 32));
   }
@@ -174,26 +176,41 @@ __global__ void __launch_bounds__(256) k_top_short(const void* __restrict__ z, i
 constexpr int LONG_CAP = 1024;      // candidates kept
 constexpr int LONG_GROUPS = 4;      // groups of a thread
 
+// A row as its 16-byte pieces and what lies before the first and after the last of them.
 template <int TYPE, int THREADS>
 struct LongRow {
+  static constexpr int N = Vec<TYPE>::N;
   const void* z;
   int64_t at;
-  int V;
-  bool wide;   // 16-byte loads
+  int V, head, whole;   // logits before the pieces, pieces
 
+  __device__ __forceinline__ LongRow(const void* z_, int64_t at_, int V_) : z(z_), at(at_), V(V_) {
+    constexpr int SIZE = 16 / N;
+    const uint32_t off = (uint32_t)((uintptr_t)z + (uint64_t)at * SIZE) & 15u;
+    head = min(V, (int)((16u - off) & 15u) / SIZE);
+    whole = (V - head) / N;
+  }
+  __device__ __forceinline__ Vec<TYPE> piece(int i) const {
+    Vec<TYPE> t;
+    t.load(z, at + head + (int64_t)i * N);
+    return t;
+  }
+  // f(index, logit) for the logits outside the pieces (fewer than 2 N)
+  template <typename F>
+  __device__ __forceinline__ void rest(const F& f) const {
+    const int tid = threadIdx.x, tail = head + whole * N;
+    if (tid < head) f(tid, logit<TYPE>(z, at + tid));
+    if (tid < V - tail) f(tail + tid, logit<TYPE>(z, at + tail + tid));
+  }
   // f(index, logit) for every logit, in an order of its own
   template <typename F>
   __device__ __forceinline__ void each(const F& f) const {
-    constexpr int N = Vec<TYPE>::N;
-    const int tid = threadIdx.x;
-    const int whole = wide ? V / N : 0;
-    for (int i = tid; i < whole; i += THREADS) {
-      Vec<TYPE> t;
-      t.load(z, at + (int64_t)i * N);
+    for (int i = threadIdx.x; i < whole; i += THREADS) {
+      const Vec<TYPE> t = piece(i);
 #pragma unroll
-      for (int e = 0; e < N; ++e) f(i * N + e, t.x[e]);
+      for (int e = 0; e < N; ++e) f(head + i * N + e, t.x[e]);
     }
-    for (int v = whole * N + tid; v < V; v += THREADS) f(v, logit<TYPE>(z, at + v));
+    rest(f);
   }
 };
 
@@ -246,8 +263,9 @@ __device__ void radix_cut(const LongRow<TYPE, THREADS>& row, int k, uint32_t* hi
   *above = k - want;
 }
 
-template <int TYPE, int THREADS>
-__global__ void __launch_bounds__(THREADS) k_top_long(const void* __restrict__ z, int V, int64_t stride, int k, int wide,
+// KEEP: pieces a thread holds between the two looks, where they fit (else 0: the row is read again).
+template <int TYPE, int THREADS, int KEEP>
+__global__ void __launch_bounds__(THREADS) k_top_long(const void* __restrict__ z, int V, int64_t stride, int k,
                                                       int32_t* __restrict__ index, float* __restrict__ value,
                                                       float* __restrict__ lse) {
   constexpr int WAVES = THREADS / 64, N = Vec<TYPE>::N;
@@ -259,12 +277,11 @@ __global__ void __launch_bounds__(THREADS) k_top_long(const void* __restrict__ z
   __shared__ int s_n;
   const int tid = threadIdx.x, lane = lane_id(), wave = tid >> 6;
   const int64_t r = blockIdx.x;
-  const LongRow<TYPE, THREADS> row{z, r * stride, V, wide != 0};
+  const LongRow<TYPE, THREADS> row(z, r * stride, V);
   if (tid == 0) s_n = 0;
   // one look: maxima of the thread's groups, running maximum and sum of exponentials
   uint32_t group[LONG_GROUPS] = {};
   float m = -INFINITY, s = 0.0f;
-  const int whole = row.wide ? V / N : 0;
   const auto take = [&](const float (&x)[N], int n, uint32_t& g) {
     float top = x[0];
 #pragma unroll
@@ -281,24 +298,34 @@ __global__ void __launch_bounds__(THREADS) k_top_long(const void* __restrict__ z
       if (e < n) s += __builtin_amdgcn_exp2f((x[e] - base) * LOG2E);
     m = next;
   };
-  for (int i0 = tid; i0 < whole; i0 += LONG_GROUPS * THREADS) {
-    Vec<TYPE> t[LONG_GROUPS];
+  typename Vec<TYPE>::Raw kept[KEEP ? KEEP : 1];
+  if constexpr (KEEP > 0) {
 #pragma unroll
-    for (int u = 0; u < LONG_GROUPS; ++u)
-      if (i0 + u * THREADS < whole) t[u].load(z, row.at + (int64_t)(i0 + u * THREADS) * N);
+    for (int u = 0; u < KEEP; ++u)
+      if (tid + u * THREADS < row.whole) kept[u] = Vec<TYPE>::raw(z, row.at + row.head + (int64_t)(tid + u * THREADS) * N);
 #pragma unroll
-    for (int u = 0; u < LONG_GROUPS; ++u)
-      if (i0 + u * THREADS < whole) take(t[u].x, N, group[u]);
-  }
-  for (int v0 = whole * N + tid; v0 < V; v0 += LONG_GROUPS * THREADS) {
-#pragma unroll
-    for (int u = 0; u < LONG_GROUPS; ++u)
-      if (v0 + u * THREADS < V) {
-        float x[N];
-        x[0] = logit<TYPE>(z, row.at + v0 + u * THREADS);
-        take(x, 1, group[u]);
+    for (int u = 0; u < KEEP; ++u)
+      if (tid + u * THREADS < row.whole) {
+        Vec<TYPE> t;
+        t.from(kept[u]);
+        take(t.x, N, group[u % LONG_GROUPS]);
       }
+  } else {
+    for (int i0 = tid; i0 < row.whole; i0 += LONG_GROUPS * THREADS) {
+      Vec<TYPE> t[LONG_GROUPS];
+#pragma unroll
+      for (int u = 0; u < LONG_GROUPS; ++u)
+        if (i0 + u * THREADS < row.whole) t[u] = row.piece(i0 + u * THREADS);
+#pragma unroll
+      for (int u = 0; u < LONG_GROUPS; ++u)
+        if (i0 + u * THREADS < row.whole) take(t[u].x, N, group[u]);
+    }
   }
+  row.rest([&](int, float y) {
+    float x[N];
+    x[0] = y;
+    take(x, 1, group[0]);
+  });
   // the row's normaliser
   for (int o = 32; o > 0; o >>= 1) {
     const float om = __shfl_xor(m, o), os = __shfl_xor(s, o);
@@ -328,13 +355,26 @@ __global__ void __launch_bounds__(THREADS) k_top_long(const void* __restrict__ z
     if (block_count<THREADS>(n, s_sum, bit) >= k) cut = next;
   }
   cut = max(cut, 1u);
-  row.each([&](int v, float x) {
+  const auto collect = [&](int v, float x) {
     const uint32_t o = ordered(x);
     if (o >= cut) {
       const int i = atomicAdd(&s_n, 1);
       if (i < LONG_CAP) s_key[i] = make_key(o, (uint32_t)v);
     }
-  });
+  };
+  if constexpr (KEEP > 0) {
+#pragma unroll
+    for (int u = 0; u < KEEP; ++u)
+      if (tid + u * THREADS < row.whole) {
+        Vec<TYPE> t;
+        t.from(kept[u]);
+#pragma unroll
+        for (int e = 0; e < N; ++e) collect(row.head + (tid + u * THREADS) * N + e, t.x[e]);
+      }
+    row.rest(collect);
+  } else {
+    row.each(collect);
+  }
   __syncthreads();
   int n = s_n;
   if (n > LONG_CAP) {  // equal logits past the cut: what lies above the exact one, and the first that equal it
@@ -385,22 +425,26 @@ void run(const void* z, int64_t rows, int V, int64_t stride, int k, int32_t* ind
   const int wide = (uintptr_t)z % 16 == 0 && stride % per == 0;
   if (V <= 16 * SHORT_LANE) {
     const dim3 grid((unsigned)((rows + 4 * SHORT_ROWS - 1) / (4 * SHORT_ROWS)));
-    const auto args = [&](auto kern) {
-      hipLaunchKernelGGL(kern, grid, dim3(256), 0, st, z, rows, V, stride, k, wide, index, value, lse);
+    const auto args = [&](auto kern, int pl) {
+      const unsigned lds = 4 * 8 * ((pl + 1) * 64 + SHORT_ROWS * k);   // 52 KB at most
+      hipLaunchKernelGGL(kern, grid, dim3(256), lds, st, z, rows, V, stride, k, wide, index, value, lse);
     };
-    if (V <= 16) args(k_top_short<TYPE, 1>);
-    else if (V <= 64) args(k_top_short<TYPE, 4>);
-    else args(k_top_short<TYPE, 16>);
+    if (V <= 16) args(k_top_short<TYPE, 1>, 1);
+    else if (V <= 64) args(k_top_short<TYPE, 4>, 4);
+    else args(k_top_short<TYPE, 16>, 16);
     return;
   }
   const dim3 grid((unsigned)rows);
   const auto args = [&](auto kern, int threads) {
-    hipLaunchKernelGGL(kern, grid, dim3(threads), 0, st, z, V, stride, k, wide, index, value, lse);
+    hipLaunchKernelGGL(kern, grid, dim3(threads), 0, st, z, V, stride, k, index, value, lse);
   };
-  // threads: about 32 logits each, so that the groups outnumber k several times
-  if (V <= 2048) args(k_top_long<TYPE, 64>, 64);
-  else if (V <= 65536) args(k_top_long<TYPE, 256>, 256);
-  else args(k_top_long<TYPE, 1024>, 1024);
+  // threads: about 32 logits each or more, so that the groups outnumber k; a row of up to 16 pieces a thread is kept
+  const int whole = V / Vec<TYPE>::N;
+  if (V <= 2048) args(k_top_long<TYPE, 64, 8>, 64);
+  else if (whole <= 8 * 256) args(k_top_long<TYPE, 256, 8>, 256);
+  else if (whole <= 16 * 256) args(k_top_long<TYPE, 256, 16>, 256);
+  else if (whole <= 16 * 1024) args(k_top_long<TYPE, 1024, 16>, 1024);
+  else args(k_top_long<TYPE, 1024, 0>, 1024);
 }
 
 }  // namespace
