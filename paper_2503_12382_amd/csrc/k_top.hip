@@ -91,6 +91,20 @@ __device__ __forceinline__ float row16_sum(float v) {
   return v + __uint_as_float(dpp<0x121>(__float_as_uint(v)));
 }
 
+// A lane sorts its logits as doubles from [1, 2), the ordered value over the index complemented in their
+// fraction: a comparison of two is one maximum and one minimum instead of a 64-bit comparison and four selects.
+__device__ __forceinline__ double sort_key(uint32_t o, int i) {
+  return __builtin_bit_cast(double, 0x3ff0000000000000ull | (uint64_t)o << 20 | (uint32_t)(255 - i));
+}
+__device__ __forceinline__ uint32_t key_value(uint64_t k) { return (uint32_t)(k >> 20); }
+__device__ __forceinline__ void sort_pair(double& a, double& b) {
+  double hi, lo;
+  asm("v_max_f64 %0, %1, %2" : "=v"(hi) : "v"(a), "v"(b));
+  asm("v_min_f64 %0, %1, %2" : "=v"(lo) : "v"(a), "v"(b));
+  a = hi;
+  b = lo;
+}
+
 // PL: logits of a lane (a power of two, 16 PL >= V); a lane's are consecutive, so that of two lanes with
 // equal heads the lower one holds the lower index.
 template <int TYPE, int PL>
@@ -119,9 +133,9 @@ __global__ void __launch_bounds__(256) k_top_short(const void* __restrict__ z, i
 #pragma unroll
     for (int i = 0; i < PL; ++i) x[i] = v0 + i < V ? logit<TYPE>(z, at + v0 + i) : 0.0f;
   }
-  uint64_t key[PL];
+  double key[PL];
 #pragma unroll
-  for (int i = 0; i < PL; ++i) key[i] = v0 + i < V ? make_key(ordered(x[i]), (uint32_t)(v0 + i)) : 0;
+  for (int i = 0; i < PL; ++i) key[i] = v0 + i < V ? sort_key(ordered(x[i]), v0 + i) : sort_key(0, 0);
   // a lane's list, largest first: odd-even merges of runs of p
 #pragma unroll
   for (int p = 1; p < PL; p *= 2)
@@ -131,18 +145,13 @@ __global__ void __launch_bounds__(256) k_top_short(const void* __restrict__ z, i
       for (int j = q % p; j + q < PL; j += 2 * q)
 #pragma unroll
         for (int i = 0; i < q; ++i)
-          if (i + j + q < PL && (i + j) / (2 * p) == (i + j + q) / (2 * p)) {
-            const uint64_t a = key[i + j], b = key[i + j + q];
-            const bool swap = a < b;
-            key[i + j] = swap ? b : a;
-            key[i + j + q] = swap ? a : b;
-          }
+          if (i + j + q < PL && (i + j) / (2 * p) == (i + j + q) / (2 * p)) sort_pair(key[i + j], key[i + j + q]);
 #pragma unroll
-  for (int i = 0; i < PL; ++i) s_list[i][lane] = key[i];
-  s_list[PL][lane] = 0;
+  for (int i = 0; i < PL; ++i) s_list[i][lane] = __builtin_bit_cast(uint64_t, key[i]);
+  s_list[PL][lane] = __builtin_bit_cast(uint64_t, sort_key(0, 0));
   wave_lds_fence();
   if (lse) {
-    const float m = from_ordered(row16_max((uint32_t)(key[0] >> 32)));
+    const float m = from_ordered(row16_max(key_value(__builtin_bit_cast(uint64_t, key[0]))));
     const float base = m > -INFINITY ? m : 0.0f;
     float s = 0.0f;
 #pragma unroll
@@ -150,10 +159,10 @@ __global__ void __launch_bounds__(256) k_top_short(const void* __restrict__ z, i
     s = row16_sum(s);
     if (l15 == 0 && r0 + rw < rows) lse[r] = m != m ? m : base + __builtin_amdgcn_logf(s) * LN2;
   }
-  uint64_t head = key[0];
+  uint64_t head = __builtin_bit_cast(uint64_t, key[0]);
   int place = 0;
   for (int j = 0; j < k; ++j) {
-    const uint32_t o = (uint32_t)(head >> 32);
+    const uint32_t o = key_value(head);
     const uint32_t top = row16_max(o);
     const uint32_t tied = (uint32_t)(__ballot(o == top) >> (lane & 48)) & 0xffffu;
     const bool won = (tied & (0u - tied)) == 1u << l15;
@@ -165,8 +174,9 @@ __global__ void __launch_bounds__(256) k_top_short(const void* __restrict__ z, i
   const int n = (int)min((int64_t)SHORT_ROWS, rows - r0) * k;
   for (int i = lane; i < n; i += 64) {
     const uint64_t h = s_out[i];
-    index[r0 * k + i] = h ? (int32_t)~(uint32_t)h : -1;
-    value[r0 * k + i] = from_ordered((uint32_t)(h >> 32));
+    const uint32_t o = key_value(h);
+    index[r0 * k + i] = o ? 255 - (int32_t)(h & 255) : -1;
+    value[r0 * k + i] = from_ordered(o);
   }
 }
 
@@ -286,10 +296,7 @@ __global__ void __launch_bounds__(THREADS) k_top_long(const void* __restrict__ z
     float top = x[0];
 #pragma unroll
     for (int e = 1; e < N; ++e) top = e < n ? fmaxf(top, x[e]) : top;
-    bool nan = false;
-#pragma unroll
-    for (int e = 0; e < N; ++e) nan |= e < n && x[e] != x[e];
-    g = max(g, nan ? 0xfffffffeu : ordered(top));
+    g = max(g, ordered(top));   // NaN beside a number does not count: it only lowers the bound
     const float next = fmaxf(m, top);
     const float base = next > -INFINITY ? next : 0.0f;
     s *= __builtin_amdgcn_exp2f((m - base) * LOG2E);
@@ -299,17 +306,36 @@ __global__ void __launch_bounds__(THREADS) k_top_long(const void* __restrict__ z
     m = next;
   };
   typename Vec<TYPE>::Raw kept[KEEP ? KEEP : 1];
+  float piece_max[KEEP ? KEEP : 1];
+  bool odd = false;   // the thread holds a NaN or +inf: its pieces' maxima do not tell
   if constexpr (KEEP > 0) {
 #pragma unroll
     for (int u = 0; u < KEEP; ++u)
       if (tid + u * THREADS < row.whole) kept[u] = Vec<TYPE>::raw(z, row.at + row.head + (int64_t)(tid + u * THREADS) * N);
 #pragma unroll
+    for (int u = 0; u < KEEP; ++u) {
+      piece_max[u] = -INFINITY;
+      if (tid + u * THREADS < row.whole) {
+        Vec<TYPE> t;
+        t.from(kept[u]);
+        float top = t.x[0];
+#pragma unroll
+        for (int e = 1; e < N; ++e) top = fmaxf(top, t.x[e]);
+        piece_max[u] = top;
+        group[u % LONG_GROUPS] = max(group[u % LONG_GROUPS], ordered(top));
+        m = fmaxf(m, top);
+      }
+    }
+    const float base = m > -INFINITY ? m : 0.0f;
+#pragma unroll
     for (int u = 0; u < KEEP; ++u)
       if (tid + u * THREADS < row.whole) {
         Vec<TYPE> t;
         t.from(kept[u]);
-        take(t.x, N, group[u % LONG_GROUPS]);
+#pragma unroll
+        for (int e = 0; e < N; ++e) s += __builtin_amdgcn_exp2f((t.x[e] - base) * LOG2E);
       }
+    odd = !(s < INFINITY);
   } else {
     for (int i0 = tid; i0 < row.whole; i0 += LONG_GROUPS * THREADS) {
       Vec<TYPE> t[LONG_GROUPS];
@@ -355,17 +381,17 @@ __global__ void __launch_bounds__(THREADS) k_top_long(const void* __restrict__ z
     if (block_count<THREADS>(n, s_sum, bit) >= k) cut = next;
   }
   cut = max(cut, 1u);
+  const float cut_x = from_ordered(cut);
   const auto collect = [&](int v, float x) {
-    const uint32_t o = ordered(x);
-    if (o >= cut) {
+    if (!(x < cut_x)) {   // NaN too
       const int i = atomicAdd(&s_n, 1);
-      if (i < LONG_CAP) s_key[i] = make_key(o, (uint32_t)v);
+      if (i < LONG_CAP) s_key[i] = make_key(ordered(x), (uint32_t)v);
     }
   };
   if constexpr (KEEP > 0) {
 #pragma unroll
     for (int u = 0; u < KEEP; ++u)
-      if (tid + u * THREADS < row.whole) {
+      if (tid + u * THREADS < row.whole && (odd || !(piece_max[u] < cut_x))) {
         Vec<TYPE> t;
         t.from(kept[u]);
 #pragma unroll
