@@ -90,28 +90,6 @@ __device__ __forceinline__ int row_flag(const HeadArgs& a, int64_t row) {
 }
 
 // ---- weights' scale ----
-// Partial maxima of the finite |g|, one of each of GPARTS blocks; the others: b * scale, padded.
-template <int TYPE>
-__global__ void __launch_bounds__(256) k_head_prep(HeadArgs a, int64_t n, float* __restrict__ part) {
-  __shared__ float s[4];
-  if (blockIdx.x >= GPARTS) {
-    const int64_t i = (int64_t)(blockIdx.x - GPARTS) * 256 + threadIdx.x;
-    if (i < n) a.bias[i] = a.b && i < a.V ? load_as_float<TYPE>(a.b, i) * a.scale : 0.0f;
-    return;
-  }
-  if (!part) return;
-  float m = 0.0f;
-#pragma unroll 4
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < a.N; i += GPARTS * 256) {
-    const float x = fabsf(a.g[i]);
-    if (x < INFINITY) m = fmaxf(m, x);
-  }
-  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-  if (lane_id() == 0) s[threadIdx.x >> 6] = m;
-  __syncthreads();
-  if (threadIdx.x == 0) part[blockIdx.x] = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
-}
-
 // G: the power of two at or above the largest |g| (1 without weights), kept where its inverse is normal.
 __device__ __forceinline__ float weight_scale(const float* gpart) {
   if (!gpart) return 1.0f;
@@ -200,48 +178,75 @@ __global__ void __launch_bounds__(256) k_head_targets(const int32_t* __restrict_
   }
 }
 
-// ---- operands as planes ----
+// ---- what the products need: operands as planes, the scaled bias, maxima of the weights ----
 template <int TYPE>
-__global__ void __launch_bounds__(256) k_head_pack_h(HeadArgs a) {
+__device__ __forceinline__ void pack8(const void* src, int64_t at, int n, uint16_t* dst, int64_t plane) {
   constexpr int P = planes_of(TYPE);
+  uint16_t o[P][8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    uint16_t v[P];
+    to_planes<TYPE, P>(e < n ? load_as_float<TYPE>(src, at + e) : 0.0f, v);
+#pragma unroll
+    for (int p = 0; p < P; ++p) o[p][e] = v[p];
+  }
+#pragma unroll
+  for (int p = 0; p < P; ++p) *reinterpret_cast<uint4*>(dst + p * plane) = *reinterpret_cast<const uint4*>(o[p]);
+}
+
+// Rows left out become zeros: nothing of them may reach dw.
+template <int TYPE>
+__device__ __forceinline__ void pack_h(const HeadArgs& a, int64_t block, int64_t blocks) {
   const int64_t per = a.Cp / 8, total = a.R * per;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+  for (int64_t i = block * 256 + threadIdx.x; i < total; i += blocks * 256) {
     const int64_t r = i / per;
     const int c0 = (int)(i % per) * 8;
-    const bool in = row_flag(a, a.r0 + r) != 0;
-    uint16_t o[P][8];
-    const int64_t src = (a.r0 + r) * a.h_stride;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      uint16_t v[P];
-      to_planes<TYPE, P>(in && c0 + e < a.C ? load_as_float<TYPE>(a.h, src + c0 + e) : 0.0f, v);
-#pragma unroll
-      for (int p = 0; p < P; ++p) o[p][e] = v[p];
-    }
-#pragma unroll
-    for (int p = 0; p < P; ++p)
-      *reinterpret_cast<uint4*>(a.hp + p * a.h_plane + r * a.Cp + c0) = *reinterpret_cast<const uint4*>(o[p]);
+    const int n = row_flag(a, a.r0 + r) != 0 ? a.C - c0 : 0;
+    pack8<TYPE>(a.h, (a.r0 + r) * a.h_stride + c0, n, a.hp + r * a.Cp + c0, a.h_plane);
   }
 }
 
 template <int TYPE>
-__global__ void __launch_bounds__(256) k_head_pack_w(HeadArgs a) {
-  constexpr int P = planes_of(TYPE);
-  const int64_t per = a.Vp / 8, total = a.C * per;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-    const int64_t c = i / per;
-    const int64_t v0 = (i % per) * 8;
-    uint16_t o[P][8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      uint16_t v[P];
-      to_planes<TYPE, P>(v0 + e < a.V ? load_as_float<TYPE>(a.w, c * a.w_stride + v0 + e) : 0.0f, v);
-#pragma unroll
-      for (int p = 0; p < P; ++p) o[p][e] = v[p];
+__global__ void __launch_bounds__(256) k_head_pack_h(HeadArgs a) {
+  pack_h<TYPE>(a, blockIdx.x, gridDim.x);
+}
+
+// Blocks of the first launch, by what they do: the first piece's rows of h, GPARTS partial maxima of the finite
+// |g|, b * scale padded to whole tiles, the weights (where they cannot be read in place).
+struct SetupBlocks {
+  unsigned h, g, b, w;
+};
+
+template <int TYPE>
+__global__ void __launch_bounds__(256) k_head_setup(HeadArgs a, SetupBlocks n, int64_t Vb, float* __restrict__ gpart) {
+  __shared__ float s[4];
+  unsigned x = blockIdx.x;
+  if (x < n.h) return pack_h<TYPE>(a, x, n.h);
+  x -= n.h;
+  if (x < n.g) {
+    float m = 0.0f;
+#pragma unroll 4
+    for (int64_t i = (int64_t)x * 256 + threadIdx.x; i < a.N; i += GPARTS * 256) {
+      const float y = fabsf(a.g[i]);
+      if (y < INFINITY) m = fmaxf(m, y);
     }
-#pragma unroll
-    for (int p = 0; p < P; ++p)
-      *reinterpret_cast<uint4*>(a.wp + p * a.w_plane + c * a.Vp + v0) = *reinterpret_cast<const uint4*>(o[p]);
+    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+    if (lane_id() == 0) s[threadIdx.x >> 6] = m;
+    __syncthreads();
+    if (threadIdx.x == 0) gpart[x] = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
+    return;
+  }
+  x -= n.g;
+  if (x < n.b) {
+    const int64_t i = (int64_t)x * 256 + threadIdx.x;
+    if (i < Vb) a.bias[i] = a.b && i < a.V ? load_as_float<TYPE>(a.b, i) * a.scale : 0.0f;
+    return;
+  }
+  x -= n.b;
+  const int64_t per = a.Vp / 8, total = a.C * per;
+  for (int64_t i = (int64_t)x * 256 + threadIdx.x; i < total; i += (int64_t)n.w * 256) {
+    const int64_t c = i / per, v0 = (i % per) * 8;
+    pack8<TYPE>(a.w, c * a.w_stride + v0, (int)min((int64_t)8, a.V - v0), a.wp + c * a.Vp + v0, a.w_plane);
   }
 }
 
@@ -966,11 +971,12 @@ hipError_t run_head(const HeadCall& c, hipStream_t st) {
     a.dbp = reinterpret_cast<float*>(ws + pl.dbp);
     if (c.d.row_weight) a.gpart = reinterpret_cast<float*>(ws + pl.gpart);
   }
-  hipLaunchKernelGGL(k_head_prep<TYPE>, dim3((unsigned)(GPARTS + pl.Vb / 256)), dim3(256), 0, st, a, pl.Vb,
-                     a.gpart ? reinterpret_cast<float*>(ws + pl.gpart) : nullptr);
   const bool in_place = w_in_place(p, c.d.w);
-  if (!in_place)
-    hipLaunchKernelGGL(k_head_pack_w<TYPE>, dim3(blocks_for(a.C * a.Vp / 8, 256)), dim3(256), 0, st, a);
+  a.R = std::min(pl.R, N);
+  const SetupBlocks sb{blocks_for(a.R * a.Cp / 8, 256, 2048), a.gpart ? (unsigned)GPARTS : 0u, (unsigned)(pl.Vb / 256),
+                       in_place ? 0u : blocks_for(a.C * a.Vp / 8, 256)};
+  hipLaunchKernelGGL(k_head_setup<TYPE>, dim3(sb.h + sb.g + sb.b + sb.w), dim3(256), 0, st, a, sb, pl.Vb,
+                     a.gpart ? reinterpret_cast<float*>(ws + pl.gpart) : nullptr);
   const int64_t wl = in_place ? p.w_stride : pl.Vp;
   const Operand W{in_place ? static_cast<const uint16_t*>(c.d.w) : a.wp, wl, p.channels,
                   (p.channels - 1) * wl + (in_place ? p.symbols : pl.Vp), a.w_plane};
@@ -980,7 +986,7 @@ hipError_t run_head(const HeadCall& c, hipStream_t st) {
     a.r0 = i * pl.R;
     a.R = std::min(pl.R, N - a.r0);
     const bool last = i + 1 == pl.pieces;
-    hipLaunchKernelGGL(k_head_pack_h<TYPE>, dim3(blocks_for(a.R * a.Cp / 8, 256)), dim3(256), 0, st, a);
+    if (i > 0) hipLaunchKernelGGL(k_head_pack_h<TYPE>, dim3(blocks_for(a.R * a.Cp / 8, 256)), dim3(256), 0, st, a);
     const Operand H{a.hp, pl.Cp, a.R, a.R * pl.Cp, a.h_plane};
     run_logits<HALF>(a, W, H, pl.big1, pl.terms, st);
     hipLaunchKernelGGL(k_head_rows, dim3((unsigned)((a.R + 15) / 16)), dim3(256), 0, st, a);

@@ -297,6 +297,20 @@ __global__ void __launch_bounds__(64 * waves_of(CT), 2) k_narrow(NarrowArgs a) {
     for (int e = 0; e < 4; ++e) sub[e] = (target & 3) == e ? -w1 : 0.0f;
     int tq = tv;
     asm volatile("" : "+v"(tq));   // the comparisons are made again: kept, they fill the scalar registers
+    // the first entries of the row lane >> 2, held by its four lanes; further ones are read for every 32 symbols
+    constexpr int NEAR = 4;
+    int near_id[DENSE ? NEAR : 1];
+    float near_q[DENSE ? NEAR : 1];
+    if constexpr (DENSE) {
+      const int64_t r = step * NB_ROWS + 16 * wave + (lane >> 2);
+#pragma unroll
+      for (int i = 0; i < NEAR; ++i) {
+        const int j = 4 * i + (lane & 3);
+        const bool have = r < a.N && j < a.k;
+        near_id[i] = have ? a.index[r * a.k + j] : -1;
+        near_q[i] = have ? a.q[r * a.k + j] : 0.0f;
+      }
+    }
     f32x4 dh[GRAD ? CT : 1];
 #pragma unroll
     for (int ct = 0; ct < (GRAD ? CT : 1); ++ct) dh[ct] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -311,12 +325,13 @@ __global__ void __launch_bounds__(64 * waves_of(CT), 2) k_narrow(NarrowArgs a) {
         for (int i = 0; i < 2; ++i) *reinterpret_cast<f32x4*>(mine + i * L::D_PLANE + lane * 16) = f32x4{0.f, 0.f, 0.f, 0.f};
         wave_lds_fence();
         const int64_t r = step * NB_ROWS + 16 * wave + rl;
-        if (r < a.N)
-          for (int j = lane & 3; j < a.k; j += 4) {
-            const int id = a.index[r * a.k + j] - 32 * u;
-            if (id >= 0 && id < 32)
-              *reinterpret_cast<float*>(mine + (rl >> 3) * L::D_PLANE + (rl & 7) * 128 + id * 4) = a.q[r * a.k + j];
-          }
+        const auto put = [&](int id, float y) {
+          if (id >> 5 == u) *reinterpret_cast<float*>(mine + (rl >> 3) * L::D_PLANE + (rl & 7) * 128 + (id & 31) * 4) = y;
+        };
+#pragma unroll
+        for (int i = 0; i < NEAR; ++i) put(near_id[i], near_q[i]);
+        if (a.k > 4 * NEAR && r < a.N)
+          for (int j = 4 * NEAR + (lane & 3); j < a.k; j += 4) put(a.index[r * a.k + j], a.q[r * a.k + j]);
         wave_lds_fence();
 #pragma unroll
         for (int i = 0; i < 2; ++i)
