@@ -30,7 +30,7 @@ namespace reno {
 namespace {
 
 constexpr int GPARTS = 64;       // partial maxima of |g|
-constexpr int DZ_ROWS = 64;      // rows of a wave of k_head_dz
+constexpr int DZ_COLS = 512;     // symbols of a wave of k_head_dz
 constexpr int HALF_SHIFT = 14;   // dz in fp16 is scaled by 2^14
 
 // ---- element types ----
@@ -77,7 +77,8 @@ struct HeadArgs {
   int part_width;          // symbols of a part
   float* lse2;             // [R]
   uint16_t* dz;            // planes [R][Vp]
-  float* dbp;              // [ceil(R / DZ_ROWS)][Vp]
+  float* dbp;              // [ceil(R / dz_rows)][Vp]
+  int dz_rows;             // rows of a wave of k_head_dz
   const float* gpart;      // [GPARTS]
   float *bits, *lse;       // of the call
 };
@@ -519,18 +520,18 @@ __global__ void __launch_bounds__(256) k_head_rows(HeadArgs a) {
   if (a.lse) a.lse[a.r0 + r] = flag ? lse2 * LN2 : 0.0f;
 }
 
-// ---- dz of a piece: a wave takes 512 symbols of DZ_ROWS rows ----
+// ---- dz of a piece: a wave takes 512 symbols of dz_rows rows ----
 // Bound by memory: t read, dz written (bf16 in its place: 4 bytes a logit in all).
 template <int TYPE>
 __global__ void __launch_bounds__(256) k_head_dz(HeadArgs a) {
   constexpr int P = planes_of(TYPE);
   constexpr bool T16 = TYPE == RENO_T_BF16;
   constexpr int U = 4;   // rows whose loads are in flight
-  constexpr int S = 8;   // symbols of a lane
+  constexpr int S = DZ_COLS / 64;   // symbols of a lane
   constexpr float SHIFT = TYPE == RENO_T_FP16 ? (float)(1 << HALF_SHIFT) : 1.0f;
   const int lane = lane_id();
   const float inv_g = 1.0f / weight_scale(a.gpart);
-  const int64_t groups = (a.Vp + 64 * S - 1) / (64 * S), blocks = (a.R + DZ_ROWS - 1) / DZ_ROWS;
+  const int64_t groups = (a.Vp + 64 * S - 1) / (64 * S), blocks = (a.R + a.dz_rows - 1) / a.dz_rows;
   const int64_t task = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (task >= groups * blocks) return;
   const int v0 = (int)(task % groups) * (64 * S);
@@ -539,8 +540,8 @@ __global__ void __launch_bounds__(256) k_head_dz(HeadArgs a) {
   const bool mine = v < a.Vp;
   const int vc = mine ? v : 0;
   float sum[S] = {};
-  const int64_t end = min(a.R, (rb + 1) * DZ_ROWS);
-  for (int64_t r1 = rb * DZ_ROWS; r1 < end; r1 += U) {
+  const int64_t end = min(a.R, (rb + 1) * a.dz_rows);
+  for (int64_t r1 = rb * a.dz_rows; r1 < end; r1 += U) {
     f32x4 t[U][2];
     uint4 t16[U];
     float pm[U], lse2[U], w[U], tt[U], q[U];
@@ -785,6 +786,7 @@ struct Plan {
   int64_t R;            // rows of a piece
   int64_t pieces;
   int part_width;       // symbols of one part
+  int dz_rows;
   bool big1, big2, big3;
   int split2, split3;
   // offsets into the workspace
@@ -834,6 +836,10 @@ Plan make_plan(const reno_head& p, int k, bool grad) {
   a.pieces = (N + R - 1) / R;
   a.R = std::min(N, up((N + a.pieces - 1) / a.pieces, 256));
   a.pieces = (N + a.R - 1) / a.R;
+  // Rows of a wave of k_head_dz: 64, so that the column sums it leaves are few, or fewer down to 4 where that would
+  // leave less than 4 waves a SIMD (100 x 8000 bf16: 51 us with 64 rows)
+  a.dz_rows = 64;
+  while (a.dz_rows > 4 && (a.Vp + DZ_COLS - 1) / DZ_COLS * ((a.R + a.dz_rows - 1) / a.dz_rows) < 4096) a.dz_rows /= 2;
   a.big1 = big_tiles(p.symbols, a.R);
   a.big2 = big_tiles(p.channels, a.R);
   a.big3 = big_tiles(p.symbols, p.channels);
@@ -855,7 +861,7 @@ Plan make_plan(const reno_head& p, int k, bool grad) {
   if (grad) {
     a.t = p.type == RENO_T_BF16 ? at : take(a.R * a.Vp * 4);
     a.dz = take(a.planes * a.R * a.Vp * 2);
-    a.dbp = take((a.R + DZ_ROWS - 1) / DZ_ROWS * a.Vp * 4);
+    a.dbp = take((a.R + a.dz_rows - 1) / a.dz_rows * a.Vp * 4);
     a.dba = take(a.Vp * 4);
     a.dhp = a.split2 > 1 ? take(a.split2 * a.R * p.channels * 4) : at;
     a.dwp = a.split3 > 1 || a.pieces > 1 ? take((int64_t)a.split3 * p.channels * p.symbols * 4) : at;
@@ -946,6 +952,7 @@ hipError_t run_head(const HeadCall& c, hipStream_t st) {
   a.part = reinterpret_cast<float2*>(ws + pl.part);
   a.parts = (p.symbols + pl.part_width - 1) / pl.part_width;
   a.part_width = pl.part_width;
+  a.dz_rows = pl.dz_rows;
   a.tt = reinterpret_cast<float*>(ws + pl.tt);
   a.lse2 = reinterpret_cast<float*>(ws + pl.lse2);
   a.bits = c.d.bits;
@@ -991,8 +998,8 @@ hipError_t run_head(const HeadCall& c, hipStream_t st) {
     run_logits<HALF>(a, W, H, pl.big1, pl.terms, st);
     hipLaunchKernelGGL(k_head_rows, dim3((unsigned)((a.R + 15) / 16)), dim3(256), 0, st, a);
     if (!c.grad) continue;
-    const int64_t row_blocks = (a.R + DZ_ROWS - 1) / DZ_ROWS;
-    hipLaunchKernelGGL(k_head_dz<TYPE>, dim3((unsigned)(((a.Vp + 511) / 512 * row_blocks + 3) / 4)), dim3(256), 0, st, a);
+    const int64_t row_blocks = (a.R + a.dz_rows - 1) / a.dz_rows;
+    hipLaunchKernelGGL(k_head_dz<TYPE>, dim3((unsigned)(((a.Vp + DZ_COLS - 1) / DZ_COLS * row_blocks + 3) / 4)), dim3(256), 0, st, a);
     const Operand D{a.dz, pl.Vp, a.R, a.R * pl.Vp, a.d_plane};
     if (c.d.dh) {
       void* out = static_cast<char*>(c.d.dh) + a.r0 * p.channels * size;

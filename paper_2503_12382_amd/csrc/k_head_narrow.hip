@@ -366,7 +366,8 @@ __global__ void __launch_bounds__(64 * waves_of(CT), 2) k_narrow(NarrowArgs a) {
           __builtin_amdgcn_sched_barrier(0);
         }
         __syncthreads();
-        // products of these 32 symbols' dz with h for this wave's tiles
+        // products of these 32 symbols' dz with h for this wave's tiles, before the other block's vector work
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int ks = 0; ks < NB_ROWS / 32; ++ks) {
           s16x8 dz[3];
@@ -393,6 +394,7 @@ __global__ void __launch_bounds__(64 * waves_of(CT), 2) k_narrow(NarrowArgs a) {
           }
           __builtin_amdgcn_sched_barrier(0);
         }
+        __builtin_amdgcn_s_setprio(0);
         if (L::BUFS == 1 || u + 1 == U) __syncthreads();
         __builtin_amdgcn_sched_barrier(0);
       }
