@@ -108,8 +108,13 @@ __global__ void __launch_bounds__(256) k_head_targets(const int32_t* __restrict_
                                                       int64_t n, int k, int V, float scale, int32_t* __restrict__ out,
                                                       float* __restrict__ q_out, float* __restrict__ ent,
                                                       uint8_t* __restrict__ flag) {
+  __shared__ uint32_t s_seen[256 / LW][128];   // a bit for each of 4096 hashes of the row's indices
   const int lane = threadIdx.x % LW;
   const int64_t row = (int64_t)blockIdx.x * (256 / LW) + threadIdx.x / LW;
+  uint32_t* seen = s_seen[threadIdx.x / LW];
+#pragma unroll
+  for (int i = 0; i < 128 / LW; ++i) seen[i * LW + lane] = 0;
+  wave_lds_fence();
   const bool in = row < n;
   const auto top_of = [](float v) {
     for (int o = LW / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
@@ -144,21 +149,35 @@ __global__ void __launch_bounds__(256) k_head_targets(const int32_t* __restrict_
     q[c] = sum > 0.0f ? q[c] / sum : 0.0f;
     if (q[c] == 0.0f) id[c] = -1;
   }
-  // entries of one index: the first takes the sum, in order, the others go
-  float joined[PER] = {};
+  // entries of one index: the first takes the sum, in order, the others go.  Most rows have none: no two entries
+  // then meet in a bit (up to 4096 symbols: exactly, beyond: of their hashes), and the walk over them is left out
+  float joined[PER];
   bool later[PER] = {};
+  bool met = false;
 #pragma unroll
-  for (int s = 0; s < PER; ++s) {
-    const int cnt = min(max(k - s * LW, 0), LW);
-    for (int l = 0; l < cnt; ++l) {
-      const int32_t oi = __shfl(id[s], l, LW);
-      const float oq = __shfl(q[s], l, LW);
+  for (int c = 0; c < PER; ++c) {
+    joined[c] = q[c];
+    if (id[c] >= 0) {
+      const uint32_t hash = V <= 4096 ? (uint32_t)id[c] & 4095u : (uint32_t)id[c] * 0x9e3779b1u >> 20;
+      met |= (atomicOr(&seen[hash >> 5], 1u << (hash & 31)) >> (hash & 31)) & 1;
+    }
+  }
+  if (__ballot(met)) {
 #pragma unroll
-      for (int c = 0; c < PER; ++c)
-        if (oi == id[c]) {
-          joined[c] += oq;
-          later[c] |= s * LW + l < c * LW + lane;
-        }
+    for (int c = 0; c < PER; ++c) joined[c] = 0.0f;
+#pragma unroll
+    for (int s = 0; s < PER; ++s) {
+      const int cnt = min(max(k - s * LW, 0), LW);
+      for (int l = 0; l < cnt; ++l) {
+        const int32_t oi = __shfl(id[s], l, LW);
+        const float oq = __shfl(q[s], l, LW);
+#pragma unroll
+        for (int c = 0; c < PER; ++c)
+          if (oi == id[c]) {
+            joined[c] += oq;
+            later[c] |= s * LW + l < c * LW + lane;
+          }
+      }
     }
   }
   float e = 0.0f;
@@ -744,6 +763,7 @@ __global__ void __launch_bounds__(256) k_head_db(const float* __restrict__ dbp, 
   const int lane = lane_id(), w = threadIdx.x >> 6;
   const int64_t v = (int64_t)blockIdx.x * 64 + lane;
   float x = 0.0f;
+#pragma unroll 8
   for (int64_t b = w; b < blocks; b += 4) x += dbp[b * Vp + v];
   s[w][lane] = x;
   __syncthreads();

@@ -330,8 +330,22 @@ __global__ void __launch_bounds__(64 * waves_of(CT), 2) k_narrow(NarrowArgs a) {
         };
 #pragma unroll
         for (int i = 0; i < NEAR; ++i) put(near_id[i], near_q[i]);
-        if (a.k > 4 * NEAR && r < a.N)
-          for (int j = 4 * NEAR + (lane & 3); j < a.k; j += 4) put(a.index[r * a.k + j], a.q[r * a.k + j]);
+        if (a.k > 4 * NEAR && r < a.N) {
+          const int32_t* ix = a.index + r * a.k;
+          const float* qx = a.q + r * a.k;
+          for (int j0 = 4 * NEAR + (lane & 3); j0 < a.k; j0 += 4 * 8) {   // 16 loads in flight
+            int id[8];
+            float y[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const int j = j0 + 4 * i;
+              id[i] = j < a.k ? ix[j] : -1;
+              y[i] = j < a.k ? qx[j] : 0.0f;
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) put(id[i], y[i]);
+          }
+        }
         wave_lds_fence();
 #pragma unroll
         for (int i = 0; i < 2; ++i)
