@@ -784,13 +784,25 @@ __global__ void __launch_bounds__(256) k_head_zero(void* out, int64_t bytes) {
 
 int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
-// Tiles of 256 x 256 by 8 waves once they give most of the 256 CUs a block, else 128 x 128 by 4 waves.
-bool big_tiles(int64_t M, int64_t N) { return ((M + 255) / 256) * ((N + 255) / 256) >= 192; }
+int64_t tiles_of(bool big, int64_t M, int64_t N) {
+  const int64_t b = big ? 256 : 128;
+  return ((M + b - 1) / b) * ((N + b - 1) / b);
+}
 
-// splits of k so that the outputs' tiles fill the chip, none shorter than 8 steps
-int splits_for(int64_t tiles, int64_t K, int terms) {
+// Tiles of 256 x 256 by 8 waves, one block a CU, or of 128 x 128 by 4 waves, two a CU: 512 of these are half the work
+// of 256 of the others.  Both reach the same rate when all CUs are full, so that what counts is how much of
+// the last turn is used (dw of 1021 x 1000 x 50021, 784 or 3128 tiles: 228 and 206 us); even, the large ones
+// move less.
+bool big_tiles(int64_t M, int64_t N) {
+  return (tiles_of(true, M, N) + 255) / 256 * 2 <= (tiles_of(false, M, N) + 511) / 512;
+}
+
+// Splits of k where the outputs' tiles leave most of the chip idle, none shorter than 8 steps.  A split costs a
+// write and a read of fp32 sums: not for tiles that fill more than half a turn (dw of 1024 x 512 x 50000,
+// 392 tiles: 190 us in two splits, 80 in one).
+int splits_for(bool big, int64_t tiles, int64_t K, int terms) {
   const int64_t steps = (K + GEMM_BK - 1) / GEMM_BK * terms;
-  int64_t s = std::min<int64_t>((512 + tiles - 1) / tiles, steps / 8);
+  const int64_t s = std::min<int64_t>((big ? 256 : 512) / tiles, steps / 8);
   return (int)std::max<int64_t>(1, std::min<int64_t>(s, 256));
 }
 
@@ -813,9 +825,12 @@ struct Plan {
   int64_t idx, q, ent, flag, narrow, bias, wp, gpart, hp, part, tt, lse2, t, dz, dbp, dba, dhp, dwp, bytes;
 };
 
+// Whether the products read w where it lies.  Its rows must start on 16 bytes; what they read past V (k is taken in
+// steps of BK) meets zeros of dz, and is the next row's start, whose NaN would be everywhere already: only
+// without a gap between the rows, of which nothing is known.
 bool w_in_place(const reno_head& p, const void* w) {
-  return p.type != RENO_T_FP32 && p.symbols % GEMM_BK == 0 && p.w_stride % 8 == 0 && p.w_stride <= GEMM_MAX_LD &&
-         (uintptr_t)w % 16 == 0;
+  return p.type != RENO_T_FP32 && (p.symbols % GEMM_BK == 0 || p.w_stride == p.symbols) && p.w_stride % 8 == 0 &&
+         p.w_stride <= GEMM_MAX_LD && (uintptr_t)w % 16 == 0;
 }
 
 Plan make_plan(const reno_head& p, int k, bool grad) {
@@ -865,12 +880,8 @@ Plan make_plan(const reno_head& p, int k, bool grad) {
   a.big3 = big_tiles(p.symbols, p.channels);
   a.part_width = a.big1 ? 128 : 64;
   const int64_t parts = (p.symbols + a.part_width - 1) / a.part_width;
-  const auto tiles = [](bool big, int64_t m, int64_t n) {
-    const int64_t b = big ? 256 : 128;
-    return ((m + b - 1) / b) * ((n + b - 1) / b);
-  };
-  a.split2 = splits_for(tiles(a.big2, p.channels, a.R), a.Vp, a.terms);
-  a.split3 = splits_for(tiles(a.big3, p.symbols, p.channels), a.R, a.terms);
+  a.split2 = splits_for(a.big2, tiles_of(a.big2, p.channels, a.R), a.Vp, a.terms);
+  a.split3 = splits_for(a.big3, tiles_of(a.big3, p.symbols, p.channels), a.R, a.terms);
   a.bias = take(a.Vb * 4);
   a.wp = take(a.planes * (int64_t)p.channels * a.Vp * 2);
   a.gpart = take(GPARTS * 4);
