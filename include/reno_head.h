@@ -22,6 +22,10 @@
  *    length, outputs are dense.  Element types are reno_type; sums, softmax
  *    statistics, bits and normalisers are fp32, gradients are rounded once to
  *    the type of what they belong to.
+ *  - Outputs overlap neither each other nor inputs.
+ *  - Logits are carried in powers of two over the temperature: |z / T| log2(e) of
+ *    2^128 or more counts as infinite.  A symbol whose logit is -inf has
+ *    probability 0; a row all of whose logits are -inf has NaN bits.
  *  - The same call gives the same bits every time.
  */
 #ifndef RENO_HEAD_H

@@ -12,6 +12,9 @@ namespace reno {
 // sets the calling thread's message of reno_last_error(NULL) (api.cpp)
 reno_status fail_thread(reno_status s, const char* msg);
 
+// rows of a launch that gives a row up to 256 threads: a grid has less than 2^32
+constexpr int64_t LAUNCH_ROWS = int64_t(1) << 23;
+
 struct HeadCall {
   reno_head p{};
   reno_head_data d{};

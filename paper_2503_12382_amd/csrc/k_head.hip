@@ -950,8 +950,12 @@ hipError_t run_head(const HeadCall& c, hipStream_t st) {
     uint8_t* flag = reinterpret_cast<uint8_t*>(ws + pl.flag);
     const int per = c.k <= 16 ? 16 : c.k <= 32 ? 8 : 4;   // rows a block
     const auto args = [&](auto kern) {
-      hipLaunchKernelGGL(kern, dim3((unsigned)((N + per - 1) / per)), dim3(256), 0, st, c.index, c.logit, N, c.k, p.symbols,
-                         (float)(1.4426950408889634 / (double)c.temperature), idx, q, ent, flag);
+      for (int64_t r = 0; r < N; r += LAUNCH_ROWS) {
+        const int64_t n = std::min(LAUNCH_ROWS, N - r);
+        hipLaunchKernelGGL(kern, dim3((unsigned)((n + per - 1) / per)), dim3(256), 0, st, c.index + r * c.k,
+                           c.logit + r * c.k, n, c.k, p.symbols, (float)(1.4426950408889634 / (double)c.temperature),
+                           idx + r * c.k, q + r * c.k, ent + r, flag + r);
+      }
     };
     if (c.k <= 16) args(k_head_targets<16, 1>);
     else if (c.k <= 32) args(k_head_targets<32, 1>);

@@ -477,10 +477,17 @@ void run(const void* z, int64_t rows, int V, int64_t stride, int k, int32_t* ind
 
 hipError_t launch_top(const void* z, int type, int64_t rows, int V, int64_t stride, int k, int32_t* index, float* value,
                       float* lse, hipStream_t st) {
-  switch (type) {
-    case RENO_T_FP32: run<RENO_T_FP32>(z, rows, V, stride, k, index, value, lse, st); break;
-    case RENO_T_BF16: run<RENO_T_BF16>(z, rows, V, stride, k, index, value, lse, st); break;
-    default: run<RENO_T_FP16>(z, rows, V, stride, k, index, value, lse, st);
+  // a row is given up to 1024 threads
+  for (int64_t r = 0; r < rows; r += LAUNCH_ROWS / 4) {
+    const int64_t n = std::min(LAUNCH_ROWS / 4, rows - r);
+    const char* x = static_cast<const char*>(z) + r * stride * (type == RENO_T_FP32 ? 4 : 2);
+    int32_t* ix = index + r * k;
+    float *v = value + r * k, *l = lse ? lse + r : nullptr;
+    switch (type) {
+      case RENO_T_FP32: run<RENO_T_FP32>(x, n, V, stride, k, ix, v, l, st); break;
+      case RENO_T_BF16: run<RENO_T_BF16>(x, n, V, stride, k, ix, v, l, st); break;
+      default: run<RENO_T_FP16>(x, n, V, stride, k, ix, v, l, st);
+    }
   }
   return hipGetLastError();
 }

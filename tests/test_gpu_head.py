@@ -34,8 +34,7 @@ def dev(*ts):
 
 def top_of(N, V, k, seed=0):
     g = torch.Generator().manual_seed(seed + 13 * N + V + k)
-    index = torch.stack([torch.randperm(V, generator=g)[:k] if V >= k else
-                         torch.randint(0, V, (k,), generator=g) for _ in range(N)]).int()
+    index = torch.rand(N, V, generator=g).topk(k, 1)[1].int() if V >= k else torch.randint(0, V, (N, k), generator=g).int()
     kept = torch.randint(0, k + 1, (N,), generator=g)
     index = torch.where(torch.arange(k) < torch.where(kept < k // 4, kept, k)[:, None], index, -1).int()
     return index, torch.randn(N, k, generator=g) * 3
@@ -57,6 +56,43 @@ def test_code_length(N, C, V, dt):
     f = reno.head_code_length(*dev(h, w, b, s))
     compare(f, ref, ("bits", "lse"))
     assert f.dh is None and f.dw is None and f.db is None
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("N,C,V", [(1, 300, 1000), (2, 129, 300), (4, 200, 40000), (3, 4096, 33000), (1, 16384, 300),
+                                   (2, 9000, 70), (5, 200, 400)])
+def test_few_rows(N, C, V, dt):
+    say("few rows", N, C, V, dt)
+    h, w, b, s, _ = head_of(N, C, V, dt, seed=11)
+    s[0] = V - 1
+    if N > 2:
+        s[1], h[1] = -1, math.nan
+    ref = reference(h, w, b, *targets_of(s, V))
+    compare(reno.head_code_length(*dev(h, w, b, s)), ref, ("bits", "lse"))
+    # rows of w that do not start on 16 bytes
+    wide = torch.full((C, V + 3), math.nan, dtype=dt, device="cuda")
+    wide[:, 1:V + 1] = w.cuda()
+    compare(reno.head_code_length(h.cuda(), wide[:, 1:V + 1], b.cuda(), s.cuda()), ref, ("bits", "lse"))
+    index, logit = top_of(N, V, 70)
+    compare(reno.head_distill(*dev(h.nan_to_num(0.0), w, b, index, logit), temperature=2.0),
+            reference(h.nan_to_num(0.0), w, b, *targets_of_top(index, logit, 2.0, V), None, 2.0), ("bits", "lse"))
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("N,C,V,k", [(600, 520, 20000, 1), (600, 520, 20001, 9), (4000, 4096, 300, 1), (130, 700, 9000, 33),
+                                     (900, 96, 8008, 1)])
+def test_large_tiles(N, C, V, k, dt):
+    """Sizes that take the 256 x 256 tiles of each product, weights in place and packed, splits and none."""
+    say("large tiles", N, C, V, k, dt)
+    h, w, b, s, g = dev(*head_of(N, C, V, dt, seed=12))
+    if k == 1:
+        ref = reference(h, w, b, *targets_of(s, V), g)
+        r = reno.head_code_length(h, w, b, s, row_weight=g, grad=True)
+    else:
+        index, logit = dev(*top_of(N, V, k))
+        ref = reference(h, w, b, *targets_of_top(index, logit, 1.5, V), g, 1.5)
+        r = reno.head_distill(h, w, b, index, logit, temperature=1.5, row_weight=g, grad=True)
+    compare(r, ref)
 
 
 @pytest.mark.parametrize("dt", TYPES)
