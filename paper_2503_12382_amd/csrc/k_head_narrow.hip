@@ -241,18 +241,18 @@ __global__ void __launch_bounds__(64 * waves_of(CT), 2) k_narrow(NarrowArgs a) {
     if (AHEAD && step + gridDim.x < steps) load_h(step + gridDim.x);
     // logits
     f32x4 z[VT];
-    s16x8 w[2][3];
-    frag_z(0, 0, w[0]);
+    // fragments of W on their way: one ahead from LDS; from L2, whose latency is that of some 30 products, three
+    constexpr int RING = L::W_HERE ? 2 : 4;
+    s16x8 w[RING][3];
 #pragma unroll
-    for (int vt = 0; vt < VT; ++vt) {
-      z[vt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < RING - 1; ++i) frag_z(i / KS, i % KS, w[i]);
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        const int i = vt * KS + ks;
-        if (i + 1 < VT * KS) frag_z((i + 1) / KS, (i + 1) % KS, w[(i + 1) & 1]);
-        z[vt] = mfma6(w[i & 1], hf[ks], z[vt]);
-        __builtin_amdgcn_sched_barrier(0);   // one fragment ahead, not all of them
-      }
+    for (int i = 0; i < VT * KS; ++i) {
+      const int vt = i / KS, ks = i % KS, n = i + RING - 1;
+      if (ks == 0) z[vt] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (n < VT * KS) frag_z(n / KS, n % KS, w[n % RING]);
+      z[vt] = mfma6(w[i % RING], hf[ks], z[vt]);
+      __builtin_amdgcn_sched_barrier(0);   // no more of them than that
     }
     float m = -INFINITY, s = 0.0f;
 #pragma unroll
@@ -358,6 +358,9 @@ __global__ void __launch_bounds__(64 * waves_of(CT), 2) k_narrow(NarrowArgs a) {
             if (q[i][e] != 0.0f) bits += q[i][e] * (lse - z[2 * u + i][e]);
       }
       if constexpr (GRAD) {
+#pragma unroll
+        for (int i = 0; i < RING - 1; ++i) frag_d(u, i, w[i]);
+        __builtin_amdgcn_sched_barrier(0);
         float d[8];
 #pragma unroll
         for (int i = 0; i < 2; ++i)
@@ -372,11 +375,11 @@ __global__ void __launch_bounds__(64 * waves_of(CT), 2) k_narrow(NarrowArgs a) {
 #pragma unroll
         for (int t = 0; t < 3; ++t) store8(lds + buf + t * L::D_PLANE, dw_at[0], dw_at[1], p[t]);
         __builtin_amdgcn_sched_barrier(0);
-        frag_d(u, 0, w[0]);
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
-          if (ct + 1 < CT) frag_d(u, ct + 1, w[(ct + 1) & 1]);
-          dh[ct] = mfma6(w[ct & 1], p, dh[ct]);
+          const int n = ct + RING - 1;
+          if (n < CT) frag_d(u, n, w[n % RING]);
+          dh[ct] = mfma6(w[ct % RING], p, dh[ct]);
           __builtin_amdgcn_sched_barrier(0);
         }
         __syncthreads();
