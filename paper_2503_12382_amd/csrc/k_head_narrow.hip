@@ -223,37 +223,36 @@ __global__ void __launch_bounds__(64 * waves_of(CT), 2) k_narrow(NarrowArgs a) {
     float weight = 1.0f;
     if (GRAD && a.g && flag) weight = a.g[row];
     if (!AHEAD) load_h(step);
-    s16x8 hf[KS][3];
+    // logits, 32 channels at a time.  Fragments of W on their way: one or two ahead
+    constexpr int RING = L::W_HERE && DENSE ? 2 : 3;
+    s16x8 w[RING][3];
+    f32x4 z[VT];
+#pragma unroll
+    for (int i = 0; i < RING - 1; ++i) frag_z(i % VT, i / VT, w[i]);
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
+      s16x8 hf[3];
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[ks][e] = flag ? x[ks][e] : 0.0f;
-      split_any8(x[ks], hf[ks]);
+      split_any8(x[ks], hf);
       if constexpr (GRAD) {
 #pragma unroll
         for (int t = 0; t < 3; ++t) {
           // 8 ks pieces on: past the 16 that the rows exchange, or (ks odd) the same with bit 3 of the place flipped
           const int far = t * L::H_PLANE + (ks >> 1) * 128, flip = ks & 1 ? 64 : 0;
-          store8(lds + far, hw_at[0] ^ flip, hw_at[1] ^ flip, hf[ks][t]);
+          store8(lds + far, hw_at[0] ^ flip, hw_at[1] ^ flip, hf[t]);
         }
+      }
+#pragma unroll
+      for (int vt = 0; vt < VT; ++vt) {
+        const int i = ks * VT + vt, n = i + RING - 1;
+        if (ks == 0) z[vt] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (n < VT * KS) frag_z(n % VT, n / VT, w[n % RING]);
+        z[vt] = mfma6(w[i % RING], hf, z[vt]);
+        __builtin_amdgcn_sched_barrier(0);   // no more of them than that
       }
     }
     if (AHEAD && step + gridDim.x < steps) load_h(step + gridDim.x);
-    // logits
-    f32x4 z[VT];
-    // fragments of W on their way: one ahead from LDS; from L2, whose latency is that of some 30 products, three
-    constexpr int RING = L::W_HERE ? 2 : 4;
-    s16x8 w[RING][3];
-#pragma unroll
-    for (int i = 0; i < RING - 1; ++i) frag_z(i / KS, i % KS, w[i]);
-#pragma unroll
-    for (int i = 0; i < VT * KS; ++i) {
-      const int vt = i / KS, ks = i % KS, n = i + RING - 1;
-      if (ks == 0) z[vt] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if (n < VT * KS) frag_z(n / KS, n % KS, w[n % RING]);
-      z[vt] = mfma6(w[i % RING], hf[ks], z[vt]);
-      __builtin_amdgcn_sched_barrier(0);   // no more of them than that
-    }
     float m = -INFINITY, s = 0.0f;
 #pragma unroll
     for (int vt = 0; vt < VT; ++vt) {
