@@ -43,8 +43,8 @@ struct NarrowArgs {
   const float* ent;
   const uint8_t* flag;
   float scale, out_scale;  // log2(e) / T, 1 / (T ln 2)
-  const uint16_t* wz;      // streamed W: [16 symbols][32 channels] fragments, then [16 channels][32 symbols]
-  const uint16_t* wd;
+  const uint16_t* wz;      // streamed W, in the order of use: fragments of 16 symbols x 32 channels for z,
+  const uint16_t* wd;      // of 16 channels x 32 symbols for dh
   float *bits, *lse, *dh;
   float* part;             // [blocks][C + waves / 2][V]: dw, shares of db
   int wide;                // rows of h in 16-byte pieces
@@ -121,7 +121,15 @@ __global__ void __launch_bounds__(64 * waves_of(CT), 2) k_narrow(NarrowArgs a) {
   __syncthreads();
   // What the loop over rows reads of W is the same every time, but does not fit the registers: with the lane and
   // the pointers opaque to the compiler it is not taken out of the loop (and spilled).
+  // Streamed fragments come in the order of their use.
   int lane_w = lane;
+  const s16x8 *pz = nullptr, *pd = nullptr;
+  const auto next = [](const s16x8*& p, s16x8 (&o)[3]) {
+#pragma unroll
+    for (int t = 0; t < 3; ++t) o[t] = p[t * 64];
+    p += 192;
+    asm volatile("" : "+v"(p));
+  };
   // LDS places: W for z (4 symbol groups, channels c and c + 4) and for dh, dz and h as written and as read back
   int az[4][2], ad[2][2], dw_at[2], dr_at[2], hw_at[2], hr_at[2];
   const int my_v = wave & 1, my_c = wave >> 1;   // this wave's tiles of dw: 16 of 32 symbols, every (NW / 2)th 16 channels
@@ -143,7 +151,6 @@ __global__ void __launch_bounds__(64 * waves_of(CT), 2) k_narrow(NarrowArgs a) {
       hr_at[q] = L::H + piece<CP * 2>(c + 4 * q, 4 * my_c + (l15 & 3));
     }
   }
-  const uint16_t *wz = a.wz, *wd = a.wd;
   // fragments of W: 16 symbols x 32 channels (z), and 16 channels x 32 symbols in the order of z's registers (dh)
   const auto frag_z = [&](int vt, int ks, s16x8 (&o)[3]) {
     if constexpr (L::W_HERE) {
@@ -152,9 +159,7 @@ __global__ void __launch_bounds__(64 * waves_of(CT), 2) k_narrow(NarrowArgs a) {
 #pragma unroll
       for (int t = 0; t < 3; ++t) o[t] = read_tr(p0 + t * L::W_PLANE, p1 + t * L::W_PLANE);
     } else {
-      const s16x8* p = reinterpret_cast<const s16x8*>(wz) + (vt * KS + ks) * 192 + lane_w;
-#pragma unroll
-      for (int t = 0; t < 3; ++t) o[t] = p[t * 64];
+      next(pz, o);
     }
   };
   const auto frag_d = [&](int u, int ct, s16x8 (&o)[3]) {
@@ -168,9 +173,7 @@ __global__ void __launch_bounds__(64 * waves_of(CT), 2) k_narrow(NarrowArgs a) {
         o[t] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
       }
     } else {
-      const s16x8* p = reinterpret_cast<const s16x8*>(wd) + (u * CT + ct) * 192 + lane_w;
-#pragma unroll
-      for (int t = 0; t < 3; ++t) o[t] = p[t * 64];
+      next(pd, o);
     }
   };
 
@@ -207,7 +210,11 @@ __global__ void __launch_bounds__(64 * waves_of(CT), 2) k_narrow(NarrowArgs a) {
   constexpr bool AHEAD = CT < 8;   // rows of the next step are loaded early where registers are left
   if (AHEAD && (int64_t)blockIdx.x < steps) load_h(blockIdx.x);
   for (int64_t step = blockIdx.x; step < steps; step += gridDim.x) {
-    asm volatile("" : "+v"(lane_w), "+s"(wz), "+s"(wd));
+    asm volatile("" : "+v"(lane_w));
+    if constexpr (!L::W_HERE) {
+      pz = reinterpret_cast<const s16x8*>(a.wz) + lane;
+      pd = reinterpret_cast<const s16x8*>(a.wd) + lane;
+    }
     const int64_t row = step * NB_ROWS + 16 * wave + l15;
     const bool in = row < a.N;
     int32_t target = -1;
@@ -465,8 +472,8 @@ __global__ void __launch_bounds__(256) k_narrow_pack(NarrowArgs a, int KS, int C
     float x[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const int v = z ? 16 * (f / KS) + l15 : 32 * (f / CT) + 16 * (e >> 2) + 4 * g + (e & 3);
-      const int c = z ? 32 * (f % KS) + 8 * g + e : 16 * (f % CT) + l15;
+      const int v = z ? 16 * (f % VT) + l15 : 32 * (f / CT) + 16 * (e >> 2) + 4 * g + (e & 3);
+      const int c = z ? 32 * (f / VT) + 8 * g + e : 16 * (f % CT) + l15;
       x[e] = c < a.C && v < a.V ? a.w[c * a.w_stride + v] : 0.0f;
     }
     s16x8 p[3];
