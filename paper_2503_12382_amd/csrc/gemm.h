@@ -20,6 +20,9 @@
 //              f(k) = (k & 3) | (k >> 3 & 1) << 2: a transposed read takes one
 //              slot of each of 16 rows k, which fall on 8 places.
 //
+// Rates (MI355X): 256 x 256 tiles of 8 waves and two blocks a CU of 128 x 128 tiles of 4 waves both reach
+// 1050 to 1190 TFLOP/s of bf16 where the grid fills the chip; a large product of the library's 1207.
+//
 // Bounds.  A buffer's size field ends at the operand's last row, so what a tile
 // reaches past it reads as zero; rows of an operand by rows are clamped as well.
 // Pieces past an operand's columns but inside its rows belong to outputs that

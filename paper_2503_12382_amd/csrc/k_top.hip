@@ -8,12 +8,15 @@
 //   k_top_short  rows of up to 256: 16 lanes a row, so that one wave's
 //                instructions serve four rows; every lane sorts its 16 logits
 //                in registers, then the largest head of 16 sorted lists is
-//                taken k times
+//                taken k times.  233737 x 256 fp32, k 16: 95 us, 2.8 TB/s; bound by its
+//                some 700 instructions for four rows
 //   k_top_long   a block a row.  The k-th largest of many groups' maxima bounds
 //                the k-th largest logit from below, so a second look at the row
 //                (from L2) keeps little more than k candidates, whose ranks are
 //                counted; rows with too many equal logits for that are cut
-//                exactly, by a radix selection
+//                exactly, by a radix selection.  Rows that fit the registers are
+//                held there between the looks.  4096 x 32768 bf16, k 64: 72 us,
+//                3.7 TB/s; one row of 131071 fp32: 23 us, the latency of one block
 
 #include <algorithm>
 
@@ -73,7 +76,7 @@ __device__ __forceinline__ float from_ordered(uint32_t o) {
 __device__ __forceinline__ uint64_t make_key(uint32_t o, uint32_t i) { return (uint64_t)o << 32 | (uint32_t)~i; }
 
 // ---------------------------------------------------------------------------
-// Rows of up to 256 logits.  233737 rows of 256 fp32, k = 16: see launch_top.
+// Rows of up to 256 logits.
 
 constexpr int SHORT_LANE = 16;      // logits of a lane, lanes of a row
 constexpr int SHORT_ROWS = 4;       // rows of a wave

@@ -174,9 +174,32 @@ def test_masked_symbols(dt):
     s[:] = 260
     ref = reference(h, w, b, *targets_of(s, V), g)
     compare(reno.head_code_length(*dev(h, w, b, s), row_weight=g.cuda(), grad=True), ref)
+    # the rest far below zero
+    for low in (-60.0, -200.0):
+        b[256:] = low
+        ref = reference(h, w, b, *targets_of(s, V), g)
+        compare(reno.head_code_length(*dev(h, w, b, s), row_weight=g.cuda(), grad=True), ref)
     b[:] = -math.inf
     r = reno.head_code_length(*dev(h, w, b, s), grad=True)
     assert bool(r.bits.isnan().all()) and bool((r.lse == -math.inf).all())
+
+
+@pytest.mark.parametrize("dt", TYPES)
+def test_masked_parts_of_a_larger_alphabet(dt):
+    """Parts of the alphabet without any symbol, beside logits far below zero."""
+    N, C, V = 70, 40, 1100
+    h, w, b, _, g = head_of(N, C, V, dt, seed=14)
+    g_ = torch.Generator().manual_seed(2)
+    for low in (0.0, -200.0, 90.0):
+        b[:] = low
+        b[64:640] = -math.inf
+        b[1000:] = -math.inf
+        s = torch.where(torch.rand(N, generator=g_) < 0.5, torch.randint(0, 64, (N,), generator=g_),
+                        torch.randint(640, 1000, (N,), generator=g_)).int()
+        s[3] = -1
+        ref = reference(h, w, b, *targets_of(s, V), g)
+        say("masked parts", dt, low)
+        compare(reno.head_code_length(*dev(h, w, b, s), row_weight=g.cuda(), grad=True), ref)
 
 
 @pytest.mark.parametrize("dt", TYPES)
