@@ -359,6 +359,7 @@ __global__ void __launch_bounds__(WM* WN * 64) k_head_logits(HeadArgs a, Operand
   // the entries of its own
   constexpr int MW = BM / WM, PR = 16384 / (MW * 4) / 16;   // symbols of the wave, groups of 16 rows in 16 KB
   static_assert(Tile::LDS >= WM * WN * 16384 && Tile::NF % PR == 0, "a wave's share of LDS holds 16 PR rows");
+  constexpr int AHEAD = 16;
   char* mine = lds + wave * 16384;
 #pragma unroll
   for (int j0 = 0; j0 < Tile::NF; j0 += PR) {
@@ -373,16 +374,18 @@ __global__ void __launch_bounds__(WM* WN * 64) k_head_logits(HeadArgs a, Operand
     const int all = rows * a.k;
     const float inv_k = 1.0f / (float)a.k;
     const int32_t* ix = a.index + (a.r0 + r0) * a.k;
-    for (int x0 = lane; x0 < all; x0 += 64 * 8) {   // 8 loads in flight
-      int id[8];
+    for (int x0 = 0; x0 < all; x0 += 64 * AHEAD) {
+      int id[AHEAD];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) id[u] = x0 + 64 * u < all ? ix[x0 + 64 * u] - v0 : -1;
+      for (int u = 0; u < AHEAD; ++u) id[u] = ix[min(x0 + 64 * u + lane, all - 1)];   // none waits for another
 #pragma unroll
-      for (int u = 0; u < 8; ++u)
-        if (id[u] >= 0 && id[u] < MW) {
-          const int x = x0 + 64 * u, rl = (int)(((float)x + 0.5f) * inv_k);   // x / k: x + 1/2 lies at least 1/2 off its multiples
-          a.tt[r0 * a.k + x] = *reinterpret_cast<const float*>(mine + rl * (MW * 4) + (((id[u] >> 2) ^ (rl & 15)) * 16) + (id[u] & 3) * 4);
+      for (int u = 0; u < AHEAD; ++u) {
+        const int x = x0 + 64 * u + lane, v = id[u] - v0;
+        if (x < all && id[u] >= v0 && v < MW) {
+          const int rl = (int)(((float)x + 0.5f) * inv_k);   // x / k: x + 1/2 lies at least 1/2 off its multiples
+          a.tt[r0 * a.k + x] = *reinterpret_cast<const float*>(mine + rl * (MW * 4) + (((v >> 2) ^ (rl & 15)) * 16) + (v & 3) * 4);
         }
+      }
     }
     wave_lds_fence();
   }
