@@ -210,10 +210,15 @@ template <int TYPE>
 __device__ __forceinline__ void pack8(const void* src, int64_t at, int n, uint16_t* dst, int64_t plane) {
   constexpr int P = planes_of(TYPE);
   uint16_t o[P][8];
+  float x[8] = {};
+  if (n > 0) {   // the loads of what is there, none waiting for another
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = load_as_float<TYPE>(src, at + min(e, n - 1));
+  }
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     uint16_t v[P];
-    to_planes<TYPE, P>(e < n ? load_as_float<TYPE>(src, at + e) : 0.0f, v);
+    to_planes<TYPE, P>(e < n ? x[e] : 0.0f, v);
 #pragma unroll
     for (int p = 0; p < P; ++p) o[p][e] = v[p];
   }
