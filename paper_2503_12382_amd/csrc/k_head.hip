@@ -716,49 +716,61 @@ __global__ void __launch_bounds__(WM* WN * 64) k_head_product(Operand A, Operand
   f32x4 acc[Tile::MF][Tile::NF];
   Tile::run(lds, A, B, (int64_t)tm * BM, (int64_t)tn * BN, k0, k1, terms, acc);
   const int lane = lane_id(), wave = threadIdx.x >> 6;
-  const int64_t m0 = (int64_t)tm * BM + (wave / WN) * (BM / WM) + 4 * (lane >> 4);
-  const int64_t n0 = (int64_t)tn * BN + (wave % WN) * (BN / WN) + (lane & 15);
+  const int l15 = lane & 15, g = lane >> 4;
+  const int64_t m0 = (int64_t)tm * BM + (wave / WN) * (BM / WM);
+  const int64_t n0 = (int64_t)tn * BN + (wave % WN) * (BN / WN);
   const float scale = o.scale * weight_scale(o.gpart);
   float* part = o.part ? o.part + split * o.M * o.N : nullptr;
   const bool typed = !o.part || (o.last && order.splits == 1);
-  const bool wide = o.M % 4 == 0;
+  const bool add = part && o.add;
+  // pieces of 4 outputs a lane, where they are aligned
+  const bool wide = o.M % 4 == 0 && (!typed || (uintptr_t)o.out % (o.type == RENO_T_FP32 ? 16 : 8) == 0);
+  // 16 PR rows n at a time through the wave's share of LDS: lanes hold 16 rows of 4 outputs each, memory wants
+  // whole lines of one row
+  constexpr int MW = BM / WM, PR = 16384 / (MW * 4) / 16, LR = MW / 4;   // LR lanes a row
+  static_assert(Tile::LDS >= WM * WN * 16384 && Tile::NF % PR == 0, "a wave's share of LDS holds 16 PR rows");
+  char* mine = lds + wave * 16384;
 #pragma unroll
-  for (int j = 0; j < Tile::NF; ++j) {
-    const int64_t n = n0 + 16 * j;
-    if (n >= o.N) continue;
+  for (int j0 = 0; j0 < Tile::NF; j0 += PR) {
 #pragma unroll
-    for (int i = 0; i < Tile::MF; ++i) {
-      const int64_t m = m0 + 16 * i;
-      if (m >= o.M) continue;
-      const int64_t at = n * o.M + m;
-      f32x4 x = acc[i][j];
-      if (wide) {
-        if (part && o.add) x += *reinterpret_cast<const f32x4*>(part + at);
+    for (int j = 0; j < PR; ++j)
+#pragma unroll
+      for (int i = 0; i < Tile::MF; ++i)   // pieces of 16 bytes, spread over the banks by the row
+        *reinterpret_cast<f32x4*>(mine + (16 * j + l15) * (MW * 4) + (((4 * i + g) ^ l15) * 16)) = acc[i][j0 + j];
+    wave_lds_fence();
+    if (wide) {
+#pragma unroll 4
+      for (int r = lane / LR; r < 16 * PR; r += 64 / LR) {
+        const int64_t n = n0 + 16 * j0 + r, m = m0 + 4 * (lane % LR), at = n * o.M + m;
+        if (n >= o.N || m >= o.M) continue;
+        f32x4 x = *reinterpret_cast<const f32x4*>(mine + r * (MW * 4) + (((lane % LR) ^ (r & 15)) * 16));
+        if (add) x += *reinterpret_cast<const f32x4*>(part + at);
         if (!typed) {
           *reinterpret_cast<f32x4*>(part + at) = x;
-          continue;
-        }
-        if (o.type == RENO_T_FP32 && (uintptr_t)o.out % 16 == 0) {
+        } else if (o.type == RENO_T_FP32) {
           *reinterpret_cast<f32x4*>(static_cast<float*>(o.out) + at) = x * scale;
-          continue;
-        }
-        if (o.type != RENO_T_FP32 && (uintptr_t)o.out % 8 == 0) {
+        } else {
           uint16_t h[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) h[e] = o.type == RENO_T_BF16 ? to_bf16(x[e] * scale) : to_fp16(x[e] * scale);
           *reinterpret_cast<uint2*>(static_cast<uint16_t*>(o.out) + at) = *reinterpret_cast<const uint2*>(h);
-          continue;
         }
-      } else if (part && o.add) {
-        for (int e = 0; e < 4; ++e)
-          if (m + e < o.M) x[e] += part[at + e];
       }
-      for (int e = 0; e < 4; ++e)
-        if (m + e < o.M) {
-          if (typed) store_typed(o.out, o.type, at + e, x[e] * scale);
-          else part[at + e] = x[e];
+    } else {
+#pragma unroll 4
+      for (int r = 0; r < 16 * PR; ++r)
+#pragma unroll
+        for (int i = 0; i < MW / 64; ++i) {
+          const int c = lane + 64 * i;
+          const int64_t n = n0 + 16 * j0 + r, m = m0 + c, at = n * o.M + m;
+          if (n >= o.N || m >= o.M) continue;
+          float x = *reinterpret_cast<const float*>(mine + r * (MW * 4) + (((c >> 2) ^ (r & 15)) * 16) + (c & 3) * 4);
+          if (add) x += part[at];
+          if (typed) store_typed(o.out, o.type, at, x * scale);
+          else part[at] = x;
         }
     }
+    wave_lds_fence();
   }
 }
 
