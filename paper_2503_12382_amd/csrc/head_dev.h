@@ -14,24 +14,18 @@ __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2
 __device__ __forceinline__ float log2_hw(float x) { return __builtin_amdgcn_logf(x); }
 
 // The three bf16 planes of x: each takes the leading 8 bits of what is left, cut off, so that
-// the parts add up to x exactly.  An infinity or NaN stays in the first.
+// the parts add up to x exactly.  An infinity leaves NaN in the lower planes (inf - inf): products
+// with it are NaN where fp32 might keep an infinity; NaN stays NaN.
 __device__ __forceinline__ void split3(float x, uint16_t (&o)[3]) {
   const uint32_t u = __float_as_uint(x);
-  o[0] = (uint16_t)(u >> 16);
-  if ((u & 0x7f800000u) == 0x7f800000u) {
-    if ((u & 0x007fffffu) != 0) o[0] |= 0x40;  // a NaN whose payload lies below stays one
-    o[1] = o[2] = 0;
-    return;
-  }
-  float r = x - __uint_as_float(u & 0xffff0000u);
+  const float r = x - __uint_as_float(u & 0xffff0000u);
   const uint32_t v = __float_as_uint(r);
+  o[0] = (uint16_t)(u >> 16);
   o[1] = (uint16_t)(v >> 16);
-  r -= __uint_as_float(v & 0xffff0000u);
-  o[2] = (uint16_t)(__float_as_uint(r) >> 16);
+  o[2] = (uint16_t)(__float_as_uint(r - __uint_as_float(v & 0xffff0000u)) >> 16);
 }
 
-// The planes of 8 values as three fragments.  An infinity leaves NaN in the lower planes (inf - inf), so
-// products with it are NaN where fp32 might keep an infinity; NaN stays NaN.
+// The planes of 8 values as three fragments.
 __device__ __forceinline__ void split_any8(const float (&x)[8], s16x8 (&o)[3]) {
   uint32_t w[3][4];
 #pragma unroll
