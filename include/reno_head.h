@@ -41,7 +41,8 @@ typedef enum {
   RENO_T_FP32 = 0, /* products of operands carried as three bf16 parts (24 bits, the range of
                       fp32), the six products above 2^-24 kept: fp32 accuracy */
   RENO_T_BF16 = 1, /* bf16 products, fp32 sums; logits' gradients are rounded to bf16 before
-                      they meet h and w (kept until then to 2^-12 of the probability) */
+                      they meet h and w (kept until then to 2^-12 of the probability; calls
+                      of up to 16 rows, where nothing averages, carry them in two parts) */
   RENO_T_FP16 = 2  /* the same in fp16, logits' gradients scaled by 2^14 over the largest
                       row weight so that none above 2^-38 of it is lost */
 } reno_type;

@@ -21,7 +21,7 @@
 //              slot of each of 16 rows k, which fall on 8 places.
 //
 // Rates (MI355X): 256 x 256 tiles of 8 waves and two blocks a CU of 128 x 128 tiles of 4 waves both reach
-// 1050 to 1190 TFLOP/s of bf16 where the grid fills the chip; a large product of the library's 1207.
+// 990 to 1220 TFLOP/s of bf16 where the grid fills the chip; a large product of the library's 1207.
 //
 // Bounds.  A buffer's size field ends at the operand's last row, so what a tile
 // reaches past it reads as zero; rows of an operand by rows are clamped as well.
@@ -56,11 +56,16 @@ struct Operand {
 };
 constexpr int64_t GEMM_MAX_LD = int64_t(1) << 22;  // 256 rows inside 32-bit offsets
 
-// fp32 operands are three bf16 planes x = x0 + x1 + x2 (8 bits each); the
-// products kept, smallest first.  One plane: the last one alone.
-constexpr int GEMM_TERMS = 6;
-__device__ __forceinline__ int term_a(int t) { return (0x052 >> 2 * t) & 3; }  // 2 0 1 1 0 0
-__device__ __forceinline__ int term_b(int t) { return (0x118 >> 2 * t) & 3; }  // 0 2 1 0 1 0
+// The products of planes that make one product: plane a (b) of term t in bits 2 t, 2 t + 1.  They follow
+// one another for each step of k, so that a plane read again is still in L2.
+struct Terms {
+  uint32_t a, b;
+  int n;
+};
+// fp32 operands are three bf16 planes x = x0 + x1 + x2 (8 bits each): those above 2^-24, smallest first
+constexpr Terms TERMS_FP32{0x052, 0x118, 6};   // 2 0 1 1 0 0 by 0 2 1 0 1 0
+constexpr Terms TERMS_ONE{0, 0, 1};
+constexpr Terms TERMS_A2{1, 0, 2}, TERMS_B2{0, 1, 2};   // two planes of one operand, the lower first
 
 template <bool HALF>
 __device__ __forceinline__ f32x4 mfma(s16x8 a, s16x8 b, f32x4 c) {
@@ -174,7 +179,7 @@ struct TileRead {
 
 // One block's tile: acc[i][j] of the wave (wm, wn) holds rows m = 16 i + 4 (lane
 // >> 4) + e, columns n = 16 j + (lane & 15) of its part.  k runs over [k0, k1) in steps
-// of BK for each of `terms` products of planes.
+// of BK, for each the products of planes `terms`.
 template <int BM, int BN, int WM, int WN, bool ACOL, bool BCOL, bool HALF>
 struct GemmTile {
   static constexpr int NW = WM * WN, MF = BM / WM / 16, NF = BN / WN / 16;
@@ -182,7 +187,7 @@ struct GemmTile {
   static constexpr int LDS = 2 * STAGE;
 
   __device__ static __forceinline__ void run(char* lds, const Operand& A, const Operand& B, int64_t m0, int64_t n0,
-                                             int64_t k0, int64_t k1, int terms, f32x4 (&acc)[MF][NF]) {
+                                             int64_t k0, int64_t k1, Terms terms, f32x4 (&acc)[MF][NF]) {
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / WN, wn = wave % WN;
@@ -199,17 +204,16 @@ struct GemmTile {
 #pragma unroll
       for (int j = 0; j < NF; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     const uint32_t lds0 = lds_offset(lds);
-    const int steps = (int)((k1 - k0) / GEMM_BK) * terms;
-    int term = GEMM_TERMS - terms;
+    const int steps = (int)((k1 - k0) / GEMM_BK) * terms.n;
+    int term = 0;
     int64_t k = k0;
     auto issue = [&](int stage) {
       const uint32_t at = lds0 + stage * STAGE;
-      la.issue(A, term_a(term) * A.plane, k, at, wave);
-      lb.issue(B, term_b(term) * B.plane, k, at + BM * GEMM_BK * 2, wave);
-      k += GEMM_BK;
-      if (k >= k1) {
-        k = k0;
-        ++term;
+      la.issue(A, (terms.a >> 2 * term & 3) * A.plane, k, at, wave);
+      lb.issue(B, (terms.b >> 2 * term & 3) * B.plane, k, at + BM * GEMM_BK * 2, wave);
+      if (++term == terms.n) {
+        term = 0;
+        k += GEMM_BK;
       }
     };
     if (steps > 0) issue(0);

@@ -22,9 +22,9 @@
 // dz is carried over the largest |g| (a power of two, G) and put right in the
 // products' results: fp16 and the low planes of fp32 lose nothing of it for small g.
 //
-// Bound: the three products.  8192 x 2048 x 65536 bf16 (6.6 TFLOP, two pieces) takes 6.62 ms, 996 TFLOP/s, where
-// one large product of the library's reaches 1207; of a piece of 4096 rows k_head_logits takes 1.16, the
-// products 1.11 and 1.19 (the second piece's dw reads and writes the first one's sums), k_head_dz 0.24 ms.
+// Bound: the three products.  8192 x 2048 x 65536 bf16 (6.6 TFLOP, two pieces) takes 6.6 ms, 1000 TFLOP/s, where
+// one large product of the library's reaches 1207; of a piece of 4096 rows k_head_logits takes 1.10 ms, dh 1.11,
+// dw 0.90 and (the second piece, which reads and writes the first one's sums) 1.25, k_head_dz 0.23.
 
 #include <algorithm>
 
@@ -52,9 +52,15 @@ __device__ __forceinline__ uint16_t to_fp16(float x) { return __builtin_bit_cast
 
 template <int TYPE, int PLANES>
 __device__ __forceinline__ void to_planes(float x, uint16_t (&o)[PLANES]) {
-  if constexpr (TYPE == RENO_T_FP32) split3(x, o);
-  else if constexpr (TYPE == RENO_T_BF16) o[0] = to_bf16(x);
-  else o[0] = to_fp16(x);
+  if constexpr (TYPE == RENO_T_FP32) {
+    split3(x, o);
+  } else if constexpr (TYPE == RENO_T_BF16) {
+    o[0] = to_bf16(x);
+    if constexpr (PLANES == 2) o[1] = to_bf16(x - __uint_as_float((uint32_t)o[0] << 16));
+  } else {
+    o[0] = to_fp16(x);
+    if constexpr (PLANES == 2) o[1] = to_fp16(x - (float)__builtin_bit_cast(_Float16, o[0]));
+  }
 }
 constexpr int planes_of(int type) { return type == RENO_T_FP32 ? 3 : 1; }
 
@@ -283,12 +289,12 @@ __global__ void __launch_bounds__(256) k_head_setup(HeadArgs a, SetupBlocks n, i
 }
 
 // ---- logits ----
-// 2048 x 2048 x 32768 bf16 forward: 232 us, 1185 TFLOP/s; fp32 (six products for one): 1.51 ms, 1091.
-// The epilogue costs some 3 us a tile, with 64 entries a row 10 more.
+// 2048 x 2048 x 32768 bf16 forward: 232 us, 1185 TFLOP/s; fp32 (six products for one): 1.33 ms, 1237.
+// The lookup of 64 entries a row adds 80 us to the 300 of 4096 x 1024 x 32768.
 // m runs over symbols, n over rows: a lane holds one row and 4 consecutive
 // symbols of each 16, so that a row's maximum and sum need two lane exchanges.
 template <int BM, int BN, int WM, int WN, bool HALF>
-__global__ void __launch_bounds__(WM* WN * 64) k_head_logits(HeadArgs a, Operand W, Operand H, TileOrder order, int terms) {
+__global__ void __launch_bounds__(WM* WN * 64) k_head_logits(HeadArgs a, Operand W, Operand H, TileOrder order, Terms terms) {
   using Tile = GemmTile<BM, BN, WM, WN, true, false, HALF>;
   __shared__ __attribute__((aligned(1024))) char lds[Tile::LDS];
   int tm, tn, split;
@@ -538,13 +544,13 @@ __global__ void __launch_bounds__(256) k_head_rows(HeadArgs a) {
   const float base = top > -INFINITY ? top : 0.0f;
   float sum = 0.0f;
   for (int p = 0; p < 16; ++p) sum += s_p[rl][p].y * exp2_hw(s_p[rl][p].x - base);
-  const float lse2 = base + log2_hw(sum);
+  const float over = log2_hw(sum), lse2 = base + over;
   const int flag = in ? row_flag(a, a.r0 + r) : 0;
   float b = 0.0f;
   if (flag == 1) {
     for (int j = pl; j < a.k; j += 16) {
       const float q = a.q ? a.q[(a.r0 + r) * a.k + j] : 1.0f;
-      if (q != 0.0f) b += q * (lse2 - a.tt[r * a.k + j]);
+      if (q != 0.0f) b += q * ((base - a.tt[r * a.k + j]) + over);   // not from lse2: where p is near 1 that rounds more than the bits
     }
   }
   s_b[rl][pl] = b;
@@ -558,12 +564,11 @@ __global__ void __launch_bounds__(256) k_head_rows(HeadArgs a) {
 }
 
 // ---- dz of a piece: a wave takes 512 symbols of dz_rows rows ----
-// Bound by memory: t read, dz written (bf16 in its place: 4 bytes a logit in all).  4096 x 65536 bf16: 238 us,
-// 4.5 TB/s.  bf16 keeps 2^(t - max + 15) in fp16 between the two: 2^-12 of itself down to 2^-29, an eighth of what
+// Bound by memory: t read, dz written (bf16 in its place: 4 bytes a logit in all).  4096 x 65536 bf16: 225 us,
+// 4.8 TB/s.  bf16 keeps 2^(t - max + 15) in fp16 between the two: 2^-12 of itself down to 2^-29, an eighth of what
 // rounding dz to bf16 takes; the targets' p - q come from their t in fp32.
-template <int TYPE>
+template <int TYPE, int P>
 __global__ void __launch_bounds__(256) k_head_dz(HeadArgs a) {
-  constexpr int P = planes_of(TYPE);
   constexpr bool T16 = TYPE == RENO_T_BF16;
   constexpr int U = 4;   // rows whose loads are in flight
   constexpr int S = DZ_COLS / 64;   // symbols of a lane
@@ -704,7 +709,7 @@ __device__ __forceinline__ void store_typed(void* out, int type, int64_t i, floa
 }
 
 template <int BM, int BN, int WM, int WN, bool ACOL, bool BCOL, bool HALF>
-__global__ void __launch_bounds__(WM* WN * 64) k_head_product(Operand A, Operand B, int64_t K, TileOrder order, int terms,
+__global__ void __launch_bounds__(WM* WN * 64) k_head_product(Operand A, Operand B, int64_t K, TileOrder order, Terms terms,
                                                               ProductOut o) {
   using Tile = GemmTile<BM, BN, WM, WN, ACOL, BCOL, HALF>;
   __shared__ __attribute__((aligned(1024))) char lds[Tile::LDS];
@@ -845,7 +850,7 @@ int few_width(const reno_head& p, bool grad) {
 }
 
 struct Plan {
-  int planes, terms;
+  int planes, dz_planes;
   int64_t Cp, Vp, Vb;   // Vb: padded to whole tiles
   int64_t R;            // rows of a piece
   int64_t pieces;
@@ -892,7 +897,11 @@ Plan make_plan(const reno_head& p, int k, bool grad) {
     return a;
   }
   a.planes = planes_of(p.type);
-  a.terms = p.type == RENO_T_FP32 ? GEMM_TERMS : 1;
+  // A second plane of dz for few rows: with many, the roundings of dz average out and leave as much as that of the
+  // result; in one row that of the target's dz is the whole result's.  Up to 16 rows the products wait for w and dw
+  // (1 x 2048 x 65536 bf16: 295 us, 252 with one plane).
+  a.dz_planes = p.type == RENO_T_FP32 ? 3 : p.rows <= 16 ? 2 : 1;
+  const int dz_terms = p.type == RENO_T_FP32 ? TERMS_FP32.n : a.dz_planes;
   a.Cp = up(p.channels, GEMM_BK);
   a.Vp = up(p.symbols, GEMM_BK);
   a.Vb = up(p.symbols, 256);
@@ -912,8 +921,8 @@ Plan make_plan(const reno_head& p, int k, bool grad) {
   a.big3 = big_tiles(p.symbols, p.channels);
   a.part_width = a.big1 ? 128 : 64;
   const int64_t parts = (p.symbols + a.part_width - 1) / a.part_width;
-  a.split2 = splits_for(a.big2, tiles_of(a.big2, p.channels, a.R), a.Vp, a.terms);
-  a.split3 = splits_for(a.big3, tiles_of(a.big3, p.symbols, p.channels), a.R, a.terms);
+  a.split2 = splits_for(a.big2, tiles_of(a.big2, p.channels, a.R), a.Vp, dz_terms);
+  a.split3 = splits_for(a.big3, tiles_of(a.big3, p.symbols, p.channels), a.R, dz_terms);
   a.bias = take(a.Vb * 4);
   a.wp = take(a.planes * (int64_t)p.channels * a.Vp * 2);
   a.gpart = take(GPARTS * 4);
@@ -923,7 +932,7 @@ Plan make_plan(const reno_head& p, int k, bool grad) {
   a.lse2 = take(a.R * 4);
   if (grad) {
     a.t = p.type == RENO_T_BF16 ? at : take(a.R * a.Vp * 4);
-    a.dz = take(a.planes * a.R * a.Vp * 2);
+    a.dz = take(a.dz_planes * a.R * a.Vp * 2);
     a.dbp = take((a.R + a.dz_rows - 1) / a.dz_rows * a.Vp * 4);
     a.dba = take(a.Vp * 4);
     a.dhp = a.split2 > 1 ? take(a.split2 * a.R * p.channels * 4) : at;
@@ -938,7 +947,7 @@ unsigned blocks_for(int64_t n, int64_t per, int64_t most = 8192) {
 }
 
 template <bool HALF>
-void run_logits(const HeadArgs& a, const Operand& W, const Operand& H, bool big, int terms, hipStream_t st) {
+void run_logits(const HeadArgs& a, const Operand& W, const Operand& H, bool big, Terms terms, hipStream_t st) {
   const int64_t b = big ? 256 : 128;
   const TileOrder o{(int)((a.V + b - 1) / b), (int)((a.R + b - 1) / b), 1};
   const dim3 grid((unsigned)((int64_t)o.tm * o.tn));
@@ -947,7 +956,7 @@ void run_logits(const HeadArgs& a, const Operand& W, const Operand& H, bool big,
 }
 
 template <bool ACOL, bool BCOL, bool HALF>
-void run_product(const Operand& A, const Operand& B, int64_t K, bool big, int splits, int terms, const ProductOut& po,
+void run_product(const Operand& A, const Operand& B, int64_t K, bool big, int splits, Terms terms, const ProductOut& po,
                  hipStream_t st) {
   const int64_t b = big ? 256 : 128;
   const TileOrder o{(int)((po.M + b - 1) / b), (int)((po.N + b - 1) / b), splits};
@@ -1062,17 +1071,21 @@ hipError_t run_head(const HeadCall& c, hipStream_t st) {
     const bool last = i + 1 == pl.pieces;
     if (i > 0) hipLaunchKernelGGL(k_head_pack_h<TYPE>, dim3(blocks_for(a.R * a.Cp / 8, 256)), dim3(256), 0, st, a);
     const Operand H{a.hp, pl.Cp, a.R, a.R * pl.Cp, a.h_plane};
-    run_logits<HALF>(a, W, H, pl.big1, pl.terms, st);
+    run_logits<HALF>(a, W, H, pl.big1, TYPE == RENO_T_FP32 ? TERMS_FP32 : TERMS_ONE, st);
     hipLaunchKernelGGL(k_head_rows, dim3((unsigned)((a.R + 15) / 16)), dim3(256), 0, st, a);
     if (!c.grad) continue;
     const int64_t row_blocks = (a.R + a.dz_rows - 1) / a.dz_rows;
-    hipLaunchKernelGGL(k_head_dz<TYPE>, dim3((unsigned)(((a.Vp + DZ_COLS - 1) / DZ_COLS * row_blocks + 3) / 4)), dim3(256), 0, st, a);
+    const Terms dz_b = TYPE == RENO_T_FP32 ? TERMS_FP32 : pl.dz_planes == 2 ? TERMS_B2 : TERMS_ONE;   // dz the second operand
+    const Terms dz_a = TYPE == RENO_T_FP32 ? TERMS_FP32 : pl.dz_planes == 2 ? TERMS_A2 : TERMS_ONE;   // the first
+    constexpr bool F32 = TYPE == RENO_T_FP32;
+    const auto make_dz = pl.dz_planes == 1 ? k_head_dz<TYPE, F32 ? 3 : 1> : k_head_dz<TYPE, F32 ? 3 : 2>;
+    hipLaunchKernelGGL(make_dz, dim3((unsigned)(((a.Vp + DZ_COLS - 1) / DZ_COLS * row_blocks + 3) / 4)), dim3(256), 0, st, a);
     const Operand D{a.dz, pl.Vp, a.R, a.R * pl.Vp, a.d_plane};
     if (c.d.dh) {
       void* out = static_cast<char*>(c.d.dh) + a.r0 * p.channels * size;
       float* part = reinterpret_cast<float*>(ws + pl.dhp);
       const ProductOut po{out, TYPE, scale_d, a.gpart, pl.split2 > 1 ? part : nullptr, 0, 1, p.channels, a.R};
-      run_product<false, false, HALF>(W, D, a.Vp, pl.big2, pl.split2, pl.terms, po, st);
+      run_product<false, false, HALF>(W, D, a.Vp, pl.big2, pl.split2, dz_b, po, st);
       if (pl.split2 > 1)
         hipLaunchKernelGGL(k_head_reduce, dim3(blocks_for(a.R * a.C, 256)), dim3(256), 0, st, part, (int64_t)pl.split2,
                            a.R * a.C, out, TYPE, scale_d, a.gpart);
@@ -1081,7 +1094,7 @@ hipError_t run_head(const HeadCall& c, hipStream_t st) {
       float* part = reinterpret_cast<float*>(ws + pl.dwp);
       const bool keep = pl.split3 > 1 || pl.pieces > 1;
       const ProductOut po{c.d.dw, TYPE, scale_d, a.gpart, keep ? part : nullptr, i > 0, last, p.symbols, p.channels};
-      run_product<true, true, HALF>(D, H, a.R, pl.big3, pl.split3, pl.terms, po, st);
+      run_product<true, true, HALF>(D, H, a.R, pl.big3, pl.split3, dz_a, po, st);
       if (last && pl.split3 > 1)
         hipLaunchKernelGGL(k_head_reduce, dim3(blocks_for((int64_t)a.C * a.V, 256)), dim3(256), 0, st, part,
                            (int64_t)pl.split3, (int64_t)a.C * a.V, c.d.dw, TYPE, scale_d, a.gpart);
