@@ -339,6 +339,52 @@ def test_pieces_of_rows(dt):
     check("db", r.db, db, edb + more * N * 1.5 / V)
 
 
+def test_features_past_32_bits():
+    """Rows whose offset in h and dh passes 2^31 elements."""
+    N, C, V, dt = 140000, 16384, 16, torch.bfloat16
+    g = torch.Generator(device="cuda").manual_seed(9)
+    h = torch.randn(N, C, generator=g, device="cuda", dtype=dt)
+    w = (torch.randn(C, V, generator=g, device="cuda") * math.sqrt(2.0 / C)).to(dt)
+    b = torch.zeros(V, device="cuda", dtype=dt)
+    s = torch.randint(-1, V, (N,), generator=g, device="cuda").int()
+    say("features past 32 bits", N, C, V)
+    r = reno.head_code_length(h, w, b, s, grad=True)
+    torch.cuda.synchronize()
+    dw, edw, size = 0.0, 0.0, 0.0
+    for i in range(0, N, 20000):
+        e = slice(i, min(N, i + 20000))
+        ref = reference(h[e], w, b, *targets_of(s[e], V))
+        for x in ("bits", "lse", "dh"):
+            check(x, getattr(r, x)[e], *ref[x])
+        dw, edw = dw + ref["dw"][0], edw + ref["dw"][1]
+        size = size + h[e].double().abs().sum(0)
+    # the bound of a part counts the sums of its 20000 rows; those of all N, with |dz| at most 1 / ln 2, come on top
+    check("dw", r.dw, dw, edw + (N + 16) * 2 * 2.0 ** -24 / math.log(2.0) * size[:, None])
+
+
+@pytest.mark.parametrize("N", [1, 2, 16, 17])
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float16])
+def test_few_rows_round_once(N, dt):
+    """Up to 16 rows dz has two parts: beside the bound in 32 bits only the result is rounded."""
+    C, V = 200, 700
+    h, w, b, s, g = head_of(N, C, V, dt, seed=15)
+    s = s.clamp(min=0)
+    say("few rows round once", N, dt)
+    r = reno.head_code_length(*dev(h, w, b, s), row_weight=g.cuda(), grad=True)
+    ref = reference(h, w, b, *targets_of(s, V), g)
+    compare(r, ref)
+    if N <= 16:
+        exact = reference(h.double().float(), w.float(), b.float(), *targets_of(s, V), g)   # bounds without the type
+        u = torch.finfo(dt).eps / 2
+        for x in ("dh", "dw", "db"):
+            value, bound = exact[x]
+            # dz in two parts of the type: 2^-16 (bf16), 2^-22 (fp16) of itself through the products' absolute values,
+            # which the bound of the type's own rounding, u |dz|, gives divided by u and multiplied by u^2
+            part = ref[x][1] * u * 2
+            low = 2.0 ** -25 if dt == torch.float16 else 0.0
+            check(x, getattr(r, x), value, bound + part + u * value.abs() * 1.01 + low)
+
+
 @pytest.mark.parametrize("dt", TYPES)
 def test_capture_streams_and_repeats(dt):
     N, C, V = 500, 64, 777
