@@ -65,9 +65,9 @@ struct Vec {
 
 // An unsigned integer in the order of the floats, from 1 (0: no logit).
 __device__ __forceinline__ uint32_t ordered(float x) {
-  if (x != x) return 0xfffffffeu;
   const uint32_t u = __float_as_uint(x + 0.0f);
-  return u & 0x80000000u ? ~u : u | 0x80000000u;
+  const uint32_t o = u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+  return x != x ? 0xfffffffeu : o;
 }
 __device__ __forceinline__ float from_ordered(uint32_t o) {
   if (o == 0xfffffffeu) return NAN;
@@ -121,8 +121,8 @@ __global__ void __launch_bounds__(256) k_top_short(const void* __restrict__ z, i
   const int64_t r = min(r0 + rw, rows - 1);
   const int64_t at = r * stride;
   const int v0 = l15 * PL;
-  uint64_t(*s_list)[64] = reinterpret_cast<uint64_t(*)[64]>(s_mem + wave * ((PL + 1) * 64 + SHORT_ROWS * k));   // [PL + 1]: a row of lanes for each place
-  uint64_t* s_out = s_list[PL + 1];
+  // a row of lanes for each of PL + 1 places, then [SHORT_ROWS][k] results
+  const int lists = wave * ((PL + 1) * 64 + SHORT_ROWS * k), out = lists + (PL + 1) * 64;
   float x[PL];
   if (PL == SHORT_LANE && wide && v0 + PL <= V) {
 #pragma unroll
@@ -150,8 +150,8 @@ __global__ void __launch_bounds__(256) k_top_short(const void* __restrict__ z, i
         for (int i = 0; i < q; ++i)
           if (i + j + q < PL && (i + j) / (2 * p) == (i + j + q) / (2 * p)) sort_pair(key[i + j], key[i + j + q]);
 #pragma unroll
-  for (int i = 0; i < PL; ++i) s_list[i][lane] = __builtin_bit_cast(uint64_t, key[i]);
-  s_list[PL][lane] = __builtin_bit_cast(uint64_t, sort_key(0, 0));
+  for (int i = 0; i < PL; ++i) s_mem[lists + i * 64 + lane] = __builtin_bit_cast(uint64_t, key[i]);
+  s_mem[lists + PL * 64 + lane] = __builtin_bit_cast(uint64_t, sort_key(0, 0));
   wave_lds_fence();
   if (lse) {
     const float m = from_ordered(row16_max(key_value(__builtin_bit_cast(uint64_t, key[0]))));
@@ -169,14 +169,14 @@ __global__ void __launch_bounds__(256) k_top_short(const void* __restrict__ z, i
     const uint32_t top = row16_max(o);
     const uint32_t tied = (uint32_t)(__ballot(o == top) >> (lane & 48)) & 0xffffu;
     const bool won = (tied & (0u - tied)) == 1u << l15;
-    if (won) s_out[rw * k + j] = head;
+    if (won) s_mem[out + rw * k + j] = head;
     place += won && place < PL ? 1 : 0;
-    head = s_list[place][lane];
+    head = s_mem[lists + place * 64 + lane];
   }
   wave_lds_fence();
   const int n = (int)min((int64_t)SHORT_ROWS, rows - r0) * k;
   for (int i = lane; i < n; i += 64) {
-    const uint64_t h = s_out[i];
+    const uint64_t h = s_mem[out + i];
     const uint32_t o = key_value(h);
     index[r0 * k + i] = o ? 255 - (int32_t)(h & 255) : -1;
     value[r0 * k + i] = from_ordered(o);
