@@ -127,8 +127,9 @@ __global__ void __launch_bounds__(64 * waves_of(CT), 2) k_narrow(NarrowArgs a) {
   // the pointers opaque to the compiler it is not taken out of the loop (and spilled).
   // Streamed fragments come in the order of their use.
   int lane_w = lane;
-  const s16x8 *pz = nullptr, *pd = nullptr;
-  const auto next = [](const s16x8*& p, s16x8 (&o)[3]) {
+  typedef const __attribute__((address_space(1))) s16x8* frag_ptr;   // stays a global pointer behind the asm
+  frag_ptr pz = nullptr, pd = nullptr;
+  const auto next = [](frag_ptr& p, s16x8 (&o)[3]) {
 #pragma unroll
     for (int t = 0; t < 3; ++t) o[t] = p[t * 64];
     p += 192;
@@ -216,8 +217,8 @@ __global__ void __launch_bounds__(64 * waves_of(CT), 2) k_narrow(NarrowArgs a) {
   for (int64_t step = blockIdx.x; step < steps; step += gridDim.x) {
     asm volatile("" : "+v"(lane_w));
     if constexpr (!L::W_HERE) {
-      pz = reinterpret_cast<const s16x8*>(a.wz) + lane;
-      pd = reinterpret_cast<const s16x8*>(a.wd) + lane;
+      pz = (frag_ptr)a.wz + lane;
+      pd = (frag_ptr)a.wd + lane;
     }
     const int64_t row = step * NB_ROWS + 16 * wave + l15;
     const bool in = row < a.N;
