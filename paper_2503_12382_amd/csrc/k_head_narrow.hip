@@ -20,7 +20,7 @@
 // 32 x 256) and the vector work of a logit (scaling, exponential, splitting:
 // some 20 instructions, 45 %) overlap little, since the waves of a SIMD do the
 // same at the same time; memory would allow several times the rate.  With all
-// gradients 233737 x 32 x 256 takes 100 us, 58711 x 128 x 256 122 (of which the weights'
+// gradients 233737 x 32 x 256 takes 100 us, 58711 x 128 x 256 120 (of which the weights'
 // way from L2 some 40), forward alone about a third.
 
 #include <algorithm>

@@ -8,8 +8,8 @@
 //   k_top_short  rows of up to 256: 16 lanes a row, so that one wave's
 //                instructions serve four rows; every lane sorts its 16 logits
 //                in registers, then the largest head of 16 sorted lists is
-//                taken k times.  233737 x 256 fp32, k 16: 95 us, 2.8 TB/s; bound by its
-//                some 700 instructions for four rows
+//                taken k times.  233737 x 256 fp32, k 16: 84 us, 3.2 TB/s; bound by its
+//                some 650 instructions for four rows
 //   k_top_long   a block a row.  The k-th largest of many groups' maxima bounds
 //                the k-th largest logit from below, so a second look at the row
 //                (from L2) keeps little more than k candidates, whose ranks are
@@ -162,16 +162,15 @@ __global__ void __launch_bounds__(256) k_top_short(const void* __restrict__ z, i
     s = row16_sum(s);
     if (l15 == 0 && r0 + rw < rows) lse[r] = m != m ? m : base + __builtin_amdgcn_logf(s) * LN2;
   }
-  uint64_t head = __builtin_bit_cast(uint64_t, key[0]);
   int place = 0;
   for (int j = 0; j < k; ++j) {
+    const uint64_t head = s_mem[lists + place * 64 + lane];
     const uint32_t o = key_value(head);
     const uint32_t top = row16_max(o);
     const uint32_t tied = (uint32_t)(__ballot(o == top) >> (lane & 48)) & 0xffffu;
     const bool won = (tied & (0u - tied)) == 1u << l15;
     if (won) s_mem[out + rw * k + j] = head;
     place += won && place < PL ? 1 : 0;
-    head = s_mem[lists + place * 64 + lane];
   }
   wave_lds_fence();
   const int n = (int)min((int64_t)SHORT_ROWS, rows - r0) * k;
