@@ -470,7 +470,8 @@ __global__ void __launch_bounds__(512) k_head_few(HeadArgs a, int wide) {
     for (int c = tid / LANES; c < a.C; c += SHARES) {
       float x[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = v + e < a.V ? load_as_float<TYPE>(a.w, c * a.w_stride + v + e) : 0.0f;
+      for (int e = 0; e < 8; ++e)   // past the alphabet: its last symbol again, whose sums are not used
+        x[e] = load_as_float<TYPE>(a.w, c * a.w_stride + min(v + e, a.V - 1));
       fma8(c, x);
     }
   }
