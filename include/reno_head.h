@@ -25,7 +25,9 @@
  *  - Outputs overlap neither each other nor inputs.
  *  - Logits are carried in powers of two over the temperature: |z / T| log2(e) of
  *    2^128 or more counts as infinite.  A symbol whose logit is -inf has
- *    probability 0; a row all of whose logits are -inf has NaN bits.
+ *    probability 0; a row all of whose logits are -inf has NaN bits.  That is for
+ *    biases: a weight that is infinite or NaN may make any gradient NaN, dh of
+ *    rows that are left out too.
  *  - The same call gives the same bits every time.
  */
 #ifndef RENO_HEAD_H
@@ -98,7 +100,7 @@ reno_status reno_head_code_length(const reno_head* head, const reno_head_data* d
  * An entry with a negative index is not there; one whose index occurs before
  * counts with it, as one entry of their summed probability.  A row without any
  * entry (or with logits of -inf only) is left out as above; an index of V or
- * more gives NaN as above.  temperature: positive and finite. */
+ * more gives NaN as above.  temperature: positive and finite, 2^-127 to 2^126. */
 reno_status reno_head_distill(const reno_head* head, const reno_head_data* data, const int32_t* top_index,
                               const float* top_logit, int k, float temperature, void* workspace,
                               int64_t workspace_bytes, void* hip_stream);

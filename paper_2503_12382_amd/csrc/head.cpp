@@ -76,8 +76,10 @@ reno_status reno_head_code_length(const reno_head* head, const reno_head_data* d
 reno_status reno_head_distill(const reno_head* head, const reno_head_data* data, const int32_t* top_index,
                               const float* top_logit, int k, float temperature, void* workspace,
                               int64_t workspace_bytes, void* hip_stream) {
-  if (!(temperature > 0.0f) || !std::isfinite(temperature) || !std::isnormal(1.0f / temperature))
-    return fail_thread(RENO_E_INVALID, "temperature must be positive and finite, and so its inverse");
+  // log2(e) / temperature, which logits are multiplied by, has to be a normal float
+  if (!(temperature > 0.0f) || !std::isfinite(temperature) ||
+      !std::isnormal((float)(1.4426950408889634 / (double)temperature)))
+    return fail_thread(RENO_E_INVALID, "temperature must be positive and finite, and so log2(e) over it");
   if (!top_logit && head && head->rows > 0) return fail_thread(RENO_E_INVALID, "null input");
   reno::HeadCall c;
   c.k = k;

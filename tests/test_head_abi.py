@@ -117,6 +117,14 @@ def test_distill_rejects_bad_arguments():
         assert L.reno_last_error(None)
 
 
+@pytest.mark.parametrize("T", [4e-39, 1e-39, 3e38])
+def test_distill_rejects_temperatures_whose_scale_is_not_a_normal_float(T):
+    """log2(e) / T multiplies the logits: at 4e-39 it is 3.6e38, past the largest float, though 1 / T is not."""
+    p, d = ctypes.c_void_p(256), reno.reno_head_data(h=256, w=256, bits=256)
+    assert reno.lib().reno_head_distill(ctypes.byref(head()), ctypes.byref(d), p, p, 4, T, p, 1 << 40,
+                                        None) == reno.RENO_E_INVALID
+
+
 def test_top_logits_rejects_bad_arguments():
     L = reno.lib()
     p = ctypes.c_void_p(256)
