@@ -50,6 +50,26 @@ __device__ __forceinline__ float load_as_float(const void* p, int64_t i) {
 __device__ __forceinline__ uint16_t to_bf16(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
 __device__ __forceinline__ uint16_t to_fp16(float x) { return __builtin_bit_cast(uint16_t, (_Float16)x); }
 
+// 8 values as they lie in memory (16 bytes, fp32: 32)
+template <int TYPE>
+__device__ __forceinline__ void widen8(const uint4 (&raw)[TYPE == RENO_T_FP32 ? 2 : 1], float (&x)[8]) {
+#pragma unroll
+  for (int q = 0; q < (TYPE == RENO_T_FP32 ? 2 : 1); ++q) {
+    const uint32_t b[4] = {raw[q].x, raw[q].y, raw[q].z, raw[q].w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if constexpr (TYPE == RENO_T_FP32) x[4 * q + e] = __uint_as_float(b[e]);
+      else if constexpr (TYPE == RENO_T_BF16) {
+        x[2 * e] = __uint_as_float(b[e] << 16);
+        x[2 * e + 1] = __uint_as_float(b[e] & 0xffff0000u);
+      } else {
+        x[2 * e] = (float)__builtin_bit_cast(_Float16, (uint16_t)b[e]);
+        x[2 * e + 1] = (float)__builtin_bit_cast(_Float16, (uint16_t)(b[e] >> 16));
+      }
+    }
+  }
+}
+
 template <int TYPE, int PLANES>
 __device__ __forceinline__ void to_planes(float x, uint16_t (&o)[PLANES]) {
   if constexpr (TYPE == RENO_T_FP32) {
@@ -217,7 +237,11 @@ __device__ __forceinline__ void pack8(const void* src, int64_t at, int n, uint16
   constexpr int P = planes_of(TYPE);
   uint16_t o[P][8];
   float x[8] = {};
-  if (n > 0) {   // the loads of what is there, none waiting for another
+  if (n >= 8) {   // whole loads, of any alignment
+    uint4 raw[TYPE == RENO_T_FP32 ? 2 : 1];
+    __builtin_memcpy(raw, static_cast<const char*>(src) + at * (TYPE == RENO_T_FP32 ? 4 : 2), sizeof raw);
+    widen8<TYPE>(raw, x);
+  } else if (n > 0) {   // what is there, no load waiting for another
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = load_as_float<TYPE>(src, at + min(e, n - 1));
   }
@@ -405,13 +429,14 @@ __global__ void __launch_bounds__(WM* WN * 64) k_head_logits(HeadArgs a, Operand
 // ---- few rows, no gradient: w is read once, by vector instructions ----
 // A block takes CB symbols and all channels; a lane 8 consecutive symbols of every (512 / (CB / 8))th
 // channel, so that a wave reads whole lines of w with 16-byte loads (fp32: two), FEW_AHEAD of them in
-// flight.  Bound by the read of w: 1 x 2048 x 65536 bf16 in 52 us, 5.1 TB/s.  FEW_ROWS: 4 rows take 55 us here
+// flight, wherever the rows start (1 x 2048 x 50021: fp32 88 us, bf16 60; element by element 234 and 124).
+// Bound by the read of w: 1 x 2048 x 65536 bf16 in 52 us, 5.1 TB/s.  FEW_ROWS: 4 rows take 55 us here
 // and 70 by k_head_logits, 8 rows 114 and 70.
 constexpr int FEW_ROWS = 4, FEW_AHEAD = 8;
 constexpr int FEW_H = 16384;   // values of h that are held in LDS
 
 template <int TYPE, int CB, int NR>
-__global__ void __launch_bounds__(512) k_head_few(HeadArgs a, int wide) {
+__global__ void __launch_bounds__(512) k_head_few(HeadArgs a) {
   constexpr int LANES = CB / 8, SHARES = 512 / LANES;
   __shared__ float s_h[FEW_H];
   __shared__ float s_sum[512 / 64][NR][CB];
@@ -431,7 +456,7 @@ __global__ void __launch_bounds__(512) k_head_few(HeadArgs a, int wide) {
       for (int e = 0; e < 8; ++e) acc[r][e] = fmaf(y, x[e], acc[r][e]);
     }
   };
-  if (wide && v + 8 <= a.V) {
+  if (v + 8 <= a.V) {
     constexpr int Q = TYPE == RENO_T_FP32 ? 2 : 1;
     const char* p = static_cast<const char*>(a.w) + (int64_t)v * (TYPE == RENO_T_FP32 ? 4 : 2);
     const int64_t ld = a.w_stride * (TYPE == RENO_T_FP32 ? 4 : 2);
@@ -441,27 +466,13 @@ __global__ void __launch_bounds__(512) k_head_few(HeadArgs a, int wide) {
       for (int u = 0; u < FEW_AHEAD; ++u) {
         const int c = min(c0 + u * SHARES, a.C - 1);
 #pragma unroll
-        for (int q = 0; q < Q; ++q) raw[u][q] = *reinterpret_cast<const uint4*>(p + c * ld + q * 16);
+        for (int q = 0; q < Q; ++q) __builtin_memcpy(&raw[u][q], p + c * ld + q * 16, 16);   // of any alignment
       }
 #pragma unroll
       for (int u = 0; u < FEW_AHEAD; ++u) {
         if (c0 + u * SHARES >= a.C) break;
         float x[8];
-#pragma unroll
-        for (int q = 0; q < Q; ++q) {
-          const uint32_t b[4] = {raw[u][q].x, raw[u][q].y, raw[u][q].z, raw[u][q].w};
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            if constexpr (TYPE == RENO_T_FP32) x[4 * q + e] = __uint_as_float(b[e]);
-            else if constexpr (TYPE == RENO_T_BF16) {
-              x[2 * e] = __uint_as_float(b[e] << 16);
-              x[2 * e + 1] = __uint_as_float(b[e] & 0xffff0000u);
-            } else {
-              x[2 * e] = (float)__builtin_bit_cast(_Float16, (uint16_t)b[e]);
-              x[2 * e + 1] = (float)__builtin_bit_cast(_Float16, (uint16_t)(b[e] >> 16));
-            }
-          }
-        }
+        widen8<TYPE>(raw[u], x);
         fma8(c0 + u * SHARES, x);
       }
     }
@@ -1040,9 +1051,8 @@ hipError_t run_head(const HeadCall& c, hipStream_t st) {
   a.flag = t.flag;
   if (const int few = few_width(p, c.grad)) {
     const dim3 grid((unsigned)a.parts);
-    const int wide = (uintptr_t)a.w % 16 == 0 && p.w_stride * size % 16 == 0;
     a.R = N;
-    const auto args = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(512), 0, st, a, wide); };
+    const auto args = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(512), 0, st, a); };
     if (few == 128) N <= 1 ? args(k_head_few<TYPE, 128, 1>) : args(k_head_few<TYPE, 128, 4>);
     else N <= 1 ? args(k_head_few<TYPE, 64, 1>) : args(k_head_few<TYPE, 64, 4>);
     hipLaunchKernelGGL(k_head_rows, dim3((unsigned)((N + 15) / 16)), dim3(256), 0, st, a);
