@@ -51,7 +51,6 @@ struct NarrowArgs {
   const uint16_t* wd;      // of 16 channels x 32 symbols for dh
   float *bits, *lse, *dh;
   float* part;             // [blocks][C + waves / 2][V]: dw, shares of db
-  int wide;                // rows of h in 16-byte pieces
 };
 
 // acc += the six terms of a b, the smallest first
@@ -202,10 +201,8 @@ __global__ void __launch_bounds__(64 * waves_of(CT), 2) k_narrow(NarrowArgs a) {
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
       const int c = 32 * ks + 8 * g;
-      if (a.wide && in && c + 8 <= a.C) {
-        const float4 u = *reinterpret_cast<const float4*>(p + c), v = *reinterpret_cast<const float4*>(p + c + 4);
-        x[ks][0] = u.x, x[ks][1] = u.y, x[ks][2] = u.z, x[ks][3] = u.w;
-        x[ks][4] = v.x, x[ks][5] = v.y, x[ks][6] = v.z, x[ks][7] = v.w;
+      if (in && c + 8 <= a.C) {
+        __builtin_memcpy(x[ks], p + c, 32);   // two loads, wherever the row starts
       } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[ks][e] = in && c + e < a.C ? p[c + e] : 0.0f;
@@ -566,7 +563,6 @@ hipError_t launch_head_narrow(const HeadCall& c, const HeadTargets& t, char* ws,
   a.bits = c.d.bits;
   a.lse = c.d.lse;
   a.dh = static_cast<float*>(c.d.dh);
-  a.wide = (uintptr_t)a.h % 16 == 0 && p.h_stride % 4 == 0;
   const int blocks = narrow_blocks(p);
   char* at = ws;
   if (c.grad) {
