@@ -8,7 +8,7 @@
 //   k_top_short  rows of up to 256: 16 lanes a row, so that one wave's
 //                instructions serve four rows; every lane sorts its 16 logits
 //                in registers, then the largest head of 16 sorted lists is
-//                taken k times.  233737 x 256 fp32, k 16: 84 us, 3.2 TB/s; bound by its
+//                taken k times.  233737 x 256 fp32, k 16: 86 us, 3.1 TB/s; bound by its
 //                some 650 instructions for four rows
 //   k_top_long   a block a row.  The k-th largest of many groups' maxima bounds
 //                the k-th largest logit from below, so a second look at the row
