@@ -124,7 +124,8 @@ __device__ __forceinline__ int row_flag(const HeadArgs& a, int64_t row) {
 }
 
 // ---- weights' scale ----
-// G: the power of two at or above the largest |g| (1 without weights), kept where its inverse is normal.
+// G: the power of two at or above the largest |g| of the rows that are taken (1 without weights), kept where its
+// inverse is normal.
 __device__ __forceinline__ float weight_scale(const float* gpart) {
   if (!gpart) return 1.0f;
   float m = gpart[lane_id()];
@@ -273,8 +274,8 @@ __global__ void __launch_bounds__(256) k_head_pack_h(HeadArgs a) {
   pack_h<TYPE>(a, blockIdx.x, gridDim.x);
 }
 
-// Blocks of the first launch, by what they do: the first piece's rows of h, GPARTS partial maxima of the finite
-// |g|, b * scale padded to whole tiles, the weights (where they cannot be read in place).
+// Blocks of the first launch, by what they do: the first piece's rows of h, GPARTS partial maxima of the finite |g|
+// of rows with a target (what the others weigh must not move the scale of dz), b * scale padded to whole tiles, the weights (where they cannot be read in place).
 struct SetupBlocks {
   unsigned h, g, b, w;
 };
@@ -289,8 +290,9 @@ __global__ void __launch_bounds__(256) k_head_setup(HeadArgs a, SetupBlocks n, i
     float m = 0.0f;
 #pragma unroll 4
     for (int64_t i = (int64_t)x * 256 + threadIdx.x; i < a.N; i += GPARTS * 256) {
+      const bool taken = row_flag(a, i) == 1;
       const float y = fabsf(a.g[i]);
-      if (y < INFINITY) m = fmaxf(m, y);
+      if (taken && y < INFINITY) m = fmaxf(m, y);
     }
     for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
     if (lane_id() == 0) s[threadIdx.x >> 6] = m;
