@@ -109,7 +109,8 @@ reno_status reno_head_distill(const reno_head* head, const reno_head_data* data,
  * rows row_stride >= V elements apart) in descending order, ties by ascending
  * index, NaN above everything: index int32 [N][k], value float [N][k]; with
  * k > V the entries from V on are -1 and -inf.  lse: NULL or float [N], the row's
- * log sum exp in natural log.  1 <= k <= RENO_HEAD_MAX_TOP.  Needs no workspace. */
+ * log sum exp in natural log (+inf with a logit of +inf, NaN with one of NaN).
+ * 1 <= k <= RENO_HEAD_MAX_TOP.  Needs no workspace. */
 reno_status reno_top_logits(const void* logits, int type, int64_t rows, int symbols, int64_t row_stride, int k,
                             int32_t* index, float* value, float* lse, void* hip_stream);
 

@@ -73,6 +73,9 @@ __device__ __forceinline__ float from_ordered(uint32_t o) {
   if (o == 0xfffffffeu) return NAN;
   return o == 0 ? -INFINITY : __uint_as_float(o & 0x80000000u ? o & 0x7fffffffu : ~o);
 }
+// What logits are taken off before their exponentials: the largest, where it is finite.  Without any the sum is 0
+// and the normaliser -inf; with one of +inf the sum is +inf (or NaN), where inf - inf would be NaN
+__device__ __forceinline__ float exp_base(float m) { return fabsf(m) < INFINITY ? m : 0.0f; }
 __device__ __forceinline__ uint64_t make_key(uint32_t o, uint32_t i) { return (uint64_t)o << 32 | (uint32_t)~i; }
 
 // ---------------------------------------------------------------------------
@@ -157,7 +160,7 @@ __global__ void __launch_bounds__(256) k_top_short(const void* __restrict__ z, i
   wave_lds_fence();
   if (lse) {
     const float m = from_ordered(row16_max(key_value(__builtin_bit_cast(uint64_t, key[0]))));
-    const float base = m > -INFINITY ? m : 0.0f;
+    const float base = exp_base(m);
     float s = 0.0f;
 #pragma unroll
     for (int i = 0; i < PL; ++i) s += v0 + i < V ? __builtin_amdgcn_exp2f((x[i] - base) * LOG2E) : 0.0f;
@@ -302,7 +305,7 @@ __global__ void __launch_bounds__(THREADS) k_top_long(const void* __restrict__ z
     for (int e = 1; e < N; ++e) top = e < n ? fmaxf(top, x[e]) : top;
     g = max(g, ordered(top));   // NaN beside a number does not count: it only lowers the bound
     const float next = fmaxf(m, top);
-    const float base = next > -INFINITY ? next : 0.0f;
+    const float base = exp_base(next);
     s *= __builtin_amdgcn_exp2f((m - base) * LOG2E);
 #pragma unroll
     for (int e = 0; e < N; ++e)
@@ -330,7 +333,7 @@ __global__ void __launch_bounds__(THREADS) k_top_long(const void* __restrict__ z
         m = fmaxf(m, top);
       }
     }
-    const float base = m > -INFINITY ? m : 0.0f;
+    const float base = exp_base(m);
 #pragma unroll
     for (int u = 0; u < KEEP; ++u)
       if (tid + u * THREADS < row.whole) {
@@ -359,7 +362,7 @@ __global__ void __launch_bounds__(THREADS) k_top_long(const void* __restrict__ z
   // the row's normaliser
   for (int o = 32; o > 0; o >>= 1) {
     const float om = __shfl_xor(m, o), os = __shfl_xor(s, o);
-    const float next = fmaxf(m, om), base = next > -INFINITY ? next : 0.0f;
+    const float next = fmaxf(m, om), base = exp_base(next);
     s = s * __builtin_amdgcn_exp2f((m - base) * LOG2E) + os * __builtin_amdgcn_exp2f((om - base) * LOG2E);
     m = next;
   }
@@ -368,11 +371,11 @@ __global__ void __launch_bounds__(THREADS) k_top_long(const void* __restrict__ z
   if (tid == 0 && lse) {
     for (int i = 1; i < WAVES; ++i) {
       const float2 o = s_ms[i];
-      const float next = fmaxf(m, o.x), base = next > -INFINITY ? next : 0.0f;
+      const float next = fmaxf(m, o.x), base = exp_base(next);
       s = s * __builtin_amdgcn_exp2f((m - base) * LOG2E) + o.y * __builtin_amdgcn_exp2f((o.x - base) * LOG2E);
       m = next;
     }
-    const float base = m > -INFINITY ? m : 0.0f;
+    const float base = exp_base(m);
     lse[r] = base + __builtin_amdgcn_logf(s) * LN2;
   }
   // the largest 16-bit prefix that at least k groups' maxima reach (0 where there are fewer groups)
