@@ -23,11 +23,13 @@
  *    statistics, bits and normalisers are fp32, gradients are rounded once to
  *    the type of what they belong to.
  *  - Outputs overlap neither each other nor inputs.
- *  - Logits are carried in powers of two over the temperature: |z / T| log2(e) of
- *    2^128 or more counts as infinite.  A symbol whose logit is -inf has
- *    probability 0; a row all of whose logits are -inf has NaN bits.  That is for
- *    biases: a weight that is infinite or NaN may make any gradient NaN, dh of
- *    rows that are left out too.
+ *  - Logits are carried in powers of two over the temperature: a bias or logit of
+ *    |z / T| log2(e) >= 2^128 counts as infinite.  A symbol whose logit is -inf has
+ *    probability 0; a row all of whose logits are -inf has lse -inf and NaN bits.
+ *    A row with a logit of +inf has lse +inf, bits of +inf, or NaN where the logit
+ *    of a target is +inf itself, and may have NaN in every gradient it reaches.
+ *    That is for biases: a weight that is infinite or NaN may make any gradient
+ *    NaN, dh of rows that are left out too.
  *  - The same call gives the same bits every time.
  */
 #ifndef RENO_HEAD_H

@@ -13,6 +13,10 @@ constexpr float LN2 = 0.6931471805599453f;
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float log2_hw(float x) { return __builtin_amdgcn_logf(x); }
 
+// What logits are taken off before their exponentials: the largest, where it is finite.  Without any the sum is 0
+// and the normaliser -inf; with one of +inf the sum is +inf (or NaN), where inf - inf would be NaN
+__device__ __forceinline__ float exp_base(float m) { return fabsf(m) < INFINITY ? m : 0.0f; }
+
 // The three bf16 planes of x: each takes the leading 8 bits of what is left, cut off, so that
 // the parts add up to x exactly.  An infinity leaves NaN in the lower planes (inf - inf): products
 // with it are NaN where fp32 might keep an infinity; NaN stays NaN.

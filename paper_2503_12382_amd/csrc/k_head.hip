@@ -351,7 +351,7 @@ __global__ void __launch_bounds__(WM* WN * 64) k_head_logits(HeadArgs a, Operand
       for (int e = 0; e < 4; ++e) m = fmaxf(m, acc[i][j][e]);
     m = fmaxf(m, __shfl_xor(m, 16));
     m = fmaxf(m, __shfl_xor(m, 32));
-    const float base = m > -INFINITY ? m : 0.0f;
+    const float base = exp_base(m);
 #pragma unroll
     for (int i = 0; i < Tile::MF; ++i)
 #pragma unroll
@@ -512,7 +512,7 @@ __global__ void __launch_bounds__(512) k_head_few(HeadArgs a) {
       m = fmaxf(m, t[i]);
     }
     for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-    const float base = m > -INFINITY ? m : 0.0f;
+    const float base = exp_base(m);
 #pragma unroll
     for (int i = 0; i < CB / 64; ++i) {
       s += exp2_hw(t[i] - base);
@@ -545,7 +545,7 @@ __global__ void __launch_bounds__(256) k_head_rows(HeadArgs a) {
       float n = m;
 #pragma unroll
       for (int u = 0; u < 8; ++u) n = fmaxf(n, x[u].x);
-      const float base = n > -INFINITY ? n : 0.0f;
+      const float base = exp_base(n);
       s *= exp2_hw(m - base);
 #pragma unroll
       for (int u = 0; u < 8; ++u) s += x[u].y * exp2_hw(x[u].x - base);
@@ -555,7 +555,7 @@ __global__ void __launch_bounds__(256) k_head_rows(HeadArgs a) {
   __syncthreads();
   float top = -INFINITY;
   for (int p = 0; p < 16; ++p) top = fmaxf(top, s_p[rl][p].x);
-  const float base = top > -INFINITY ? top : 0.0f;
+  const float base = exp_base(top);
   float sum = 0.0f;
   for (int p = 0; p < 16; ++p) sum += s_p[rl][p].y * exp2_hw(s_p[rl][p].x - base);
   const float over = log2_hw(sum), lse2 = base + over;

@@ -275,7 +275,7 @@ __global__ void __launch_bounds__(64 * waves_of(CT), 2) k_narrow(NarrowArgs a) {
     }
     m = fmaxf(m, __shfl_xor(m, 16));
     m = fmaxf(m, __shfl_xor(m, 32));
-    const float base = m > -INFINITY ? m : 0.0f;
+    const float base = exp_base(m);
     // the target is element sub of the 4 in register group tv, in the lane with its row and (target >> 2 & 3) = g
     f32x4 at_target = {0.f, 0.f, 0.f, 0.f};
     const int tv = DENSE || (target >> 2 & 3) != g ? -1 : target >> 4;

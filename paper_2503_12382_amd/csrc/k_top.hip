@@ -22,12 +22,12 @@
 
 #include "dev.h"
 #include "head.h"
+#include "head_dev.h"
 
 namespace reno {
 namespace {
 
 constexpr float LOG2E = 1.4426950408889634f;
-constexpr float LN2 = 0.6931471805599453f;
 
 template <int TYPE>
 __device__ __forceinline__ float logit(const void* p, int64_t i) {
@@ -73,9 +73,6 @@ __device__ __forceinline__ float from_ordered(uint32_t o) {
   if (o == 0xfffffffeu) return NAN;
   return o == 0 ? -INFINITY : __uint_as_float(o & 0x80000000u ? o & 0x7fffffffu : ~o);
 }
-// What logits are taken off before their exponentials: the largest, where it is finite.  Without any the sum is 0
-// and the normaliser -inf; with one of +inf the sum is +inf (or NaN), where inf - inf would be NaN
-__device__ __forceinline__ float exp_base(float m) { return fabsf(m) < INFINITY ? m : 0.0f; }
 __device__ __forceinline__ uint64_t make_key(uint32_t o, uint32_t i) { return (uint64_t)o << 32 | (uint32_t)~i; }
 
 // ---------------------------------------------------------------------------
