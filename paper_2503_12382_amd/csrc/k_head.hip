@@ -27,6 +27,7 @@
 // dw 0.90 and (the second piece, which reads and writes the first one's sums) 1.25, k_head_dz 0.23.
 
 #include <algorithm>
+#include <cmath>
 
 #include "dev.h"
 #include "gemm.h"
@@ -124,15 +125,25 @@ __device__ __forceinline__ int row_flag(const HeadArgs& a, int64_t row) {
 }
 
 // ---- weights' scale ----
-// G: the power of two at or above the largest |g| of the rows that are taken (1 without weights), kept where its
-// inverse is normal.
-__device__ __forceinline__ float weight_scale(const float* gpart) {
-  if (!gpart) return 1.0f;
+// e: the largest |g| of the rows that are taken is below 2^e and at least half of it (0 without weights, or with
+// none but 0).  dz is carried over G = 2^e.
+__device__ __forceinline__ int weight_exp(const float* gpart) {
+  if (!gpart) return 0;
   float m = gpart[lane_id()];
   for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-  if (m == 0.0f) return 1.0f;
-  const int e = min(max((int)(__float_as_uint(m) >> 23) + 1, 2), 252);
-  return __uint_as_float((uint32_t)e << 23);
+  return m == 0.0f ? 0 : __builtin_amdgcn_frexp_expf(m);
+}
+
+// What brings the sums of dz to gradients: 1 / (T ln 2), over 2^14 for fp16, as a number below 1 and a power of two.
+// That power and G may each be past the floats where the gradient is not; they meet as integers.
+struct OutScale {
+  float mant;
+  int exp;
+};
+__device__ __forceinline__ float scaled(float x, OutScale s) { return __builtin_amdgcn_ldexpf(x * s.mant, s.exp); }
+__device__ __forceinline__ OutScale with_weights(OutScale s, const float* gpart) {
+  s.exp += __builtin_amdgcn_readfirstlane(weight_exp(gpart));
+  return s;
 }
 
 // ---- targets of a distillation ----
@@ -588,7 +599,7 @@ __global__ void __launch_bounds__(256) k_head_dz(HeadArgs a) {
   constexpr int S = DZ_COLS / 64;   // symbols of a lane
   constexpr float SHIFT = TYPE == RENO_T_FP16 ? (float)(1 << HALF_SHIFT) : 1.0f;
   const int lane = lane_id();
-  const float inv_g = 1.0f / weight_scale(a.gpart);
+  const int ge = __builtin_amdgcn_readfirstlane(weight_exp(a.gpart));
   const int64_t groups = (a.Vp + 64 * S - 1) / (64 * S), blocks = (a.R + a.dz_rows - 1) / a.dz_rows;
   const int64_t task = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (task >= groups * blocks) return;
@@ -632,7 +643,7 @@ __global__ void __launch_bounds__(256) k_head_dz(HeadArgs a) {
       if (r >= end) break;
       float d[S] = {};
       if (flag[u]) {
-        const float wr = flag[u] == 2 ? NAN : a.g ? w[u] * inv_g : 1.0f;
+        const float wr = flag[u] == 2 ? NAN : a.g ? __builtin_amdgcn_ldexpf(w[u], -ge) : 1.0f;
         if constexpr (T16) {
           // a part without any logit adds nothing, however far below it the row's normaliser lies
           const float f = pm[u] > -INFINITY ? exp2_hw(pm[u] - lse2[u] - 15.0f) : lse2[u] > -INFINITY ? 0.0f : NAN;
@@ -709,7 +720,7 @@ __global__ void __launch_bounds__(256) k_head_dz(HeadArgs a) {
 struct ProductOut {
   void* out;
   int type;
-  float scale;
+  OutScale scale;
   const float* gpart;
   float* part;       // [splits][N][M], or null
   int add;           // part holds sums of earlier pieces
@@ -738,7 +749,7 @@ __global__ void __launch_bounds__(WM* WN * 64) k_head_product(Operand A, Operand
   const int l15 = lane & 15, g = lane >> 4;
   const int64_t m0 = (int64_t)tm * BM + (wave / WN) * (BM / WM);
   const int64_t n0 = (int64_t)tn * BN + (wave % WN) * (BN / WN);
-  const float scale = o.scale * weight_scale(o.gpart);
+  const OutScale scale = with_weights(o.scale, o.gpart);
   float* part = o.part ? o.part + split * o.M * o.N : nullptr;
   const bool typed = !o.part || (o.last && order.splits == 1);
   const bool add = part && o.add;
@@ -767,11 +778,14 @@ __global__ void __launch_bounds__(WM* WN * 64) k_head_product(Operand A, Operand
         if (!typed) {
           *reinterpret_cast<f32x4*>(part + at) = x;
         } else if (o.type == RENO_T_FP32) {
-          *reinterpret_cast<f32x4*>(static_cast<float*>(o.out) + at) = x * scale;
+          f32x4 y;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[e] = scaled(x[e], scale);
+          *reinterpret_cast<f32x4*>(static_cast<float*>(o.out) + at) = y;
         } else {
           uint16_t h[4];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) h[e] = o.type == RENO_T_BF16 ? to_bf16(x[e] * scale) : to_fp16(x[e] * scale);
+          for (int e = 0; e < 4; ++e) h[e] = o.type == RENO_T_BF16 ? to_bf16(scaled(x[e], scale)) : to_fp16(scaled(x[e], scale));
           *reinterpret_cast<uint2*>(static_cast<uint16_t*>(o.out) + at) = *reinterpret_cast<const uint2*>(h);
         }
       }
@@ -785,7 +799,7 @@ __global__ void __launch_bounds__(WM* WN * 64) k_head_product(Operand A, Operand
           if (n >= o.N || m >= o.M) continue;
           float x = *reinterpret_cast<const float*>(mine + r * (MW * 4) + (((c >> 2) ^ (r & 15)) * 16) + (c & 3) * 4);
           if (add) x += part[at];
-          if (typed) store_typed(o.out, o.type, at, x * scale);
+          if (typed) store_typed(o.out, o.type, at, scaled(x, scale));
           else part[at] = x;
         }
     }
@@ -795,22 +809,22 @@ __global__ void __launch_bounds__(WM* WN * 64) k_head_product(Operand A, Operand
 
 // out[i] = scale G (sum over s of part[s][i]), i < n; rows of `width` values of which `cols` are stored
 __global__ void __launch_bounds__(256) k_head_reduce(const float* __restrict__ part, int64_t count, int64_t n, void* out,
-                                                     int type, float scale, const float* __restrict__ gpart) {
-  const float s = scale * weight_scale(gpart);
+                                                     int type, OutScale scale, const float* __restrict__ gpart) {
+  const OutScale s = with_weights(scale, gpart);
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
     float x = 0.0f;
     for (int64_t p = 0; p < count; ++p) x += part[p * n + i];
-    store_typed(out, type, i, x * s);
+    store_typed(out, type, i, scaled(x, s));
   }
 }
 
 // Column sums of dz: acc[v] (+)= sum over the piece's row blocks, four lanes'
 // worth of blocks at a time; the last piece stores db.
 __global__ void __launch_bounds__(256) k_head_db(const float* __restrict__ dbp, int64_t blocks, int64_t Vp, int V,
-                                                 float* __restrict__ acc, int add, int last, void* out, int type, float scale,
+                                                 float* __restrict__ acc, int add, int last, void* out, int type, OutScale scale,
                                                  const float* __restrict__ gpart) {
   __shared__ float s[4][64];
-  const float sc = scale * weight_scale(gpart);
+  const OutScale sc = with_weights(scale, gpart);
   const int lane = lane_id(), w = threadIdx.x >> 6;
   const int64_t v = (int64_t)blockIdx.x * 64 + lane;
   float x = 0.0f;
@@ -822,7 +836,7 @@ __global__ void __launch_bounds__(256) k_head_db(const float* __restrict__ dbp, 
   x = s[0][lane] + s[1][lane] + s[2][lane] + s[3][lane];
   if (add) x += acc[v];
   if (!last) acc[v] = x;
-  else if (v < V) store_typed(out, type, v, x * sc);
+  else if (v < V) store_typed(out, type, v, scaled(x, sc));
 }
 
 __global__ void __launch_bounds__(256) k_head_zero(void* out, int64_t bytes) {
@@ -1076,8 +1090,9 @@ hipError_t run_head(const HeadCall& c, hipStream_t st) {
   const int64_t wl = in_place ? p.w_stride : pl.Vp;
   const Operand W{in_place ? static_cast<const uint16_t*>(c.d.w) : a.wp, wl, p.channels,
                   (p.channels - 1) * wl + (in_place ? p.symbols : pl.Vp), a.w_plane};
-  const float scale = (float)(1.0 / (0.6931471805599453 * (double)c.temperature));
-  const float scale_d = HALF ? scale / (float)(1 << HALF_SHIFT) : scale;
+  OutScale scale;
+  scale.mant = (float)std::frexp(1.0 / (0.6931471805599453 * (double)c.temperature), &scale.exp);
+  const OutScale scale_d{scale.mant, scale.exp - (HALF ? HALF_SHIFT : 0)};
   for (int64_t i = 0; i < pl.pieces; ++i) {
     a.r0 = i * pl.R;
     a.R = std::min(pl.R, N - a.r0);

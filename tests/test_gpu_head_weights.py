@@ -1,5 +1,6 @@
-"""Row weights at the ends of their range: what a row that is left out weighs
-changes nothing of the others."""
+"""Row weights and temperatures at the ends of their ranges: what a row that is
+left out weighs changes nothing of the others, and gradients whose weight over
+the temperature lies far from 1 keep their bits."""
 import math
 
 import pytest
@@ -7,6 +8,7 @@ import torch
 
 import paper_2503_12382_amd as reno
 from gpu_helpers import say
+from head_ref import check, reference, targets_of_top
 
 pytestmark = pytest.mark.gpu
 TYPES = [torch.float32, torch.bfloat16, torch.float16]
@@ -61,3 +63,71 @@ def test_weights_of_rows_without_a_valid_target_stay_with_them(N, C, V, dt):
     for got, ref in zip(both(h, w, b, s, index, logit, weight), want):
         assert bool(got.dh[1].isnan().all()) and bool(got.dw.isnan().all())
         assert torch.equal(got.dh[2:], ref.dh[2:]) and bool(ref.dh[2:].any())
+
+
+@pytest.mark.parametrize("V", [300])
+def test_large_weights_at_a_low_temperature(V):
+    """g / T is past the largest float, dh = g / (T ln 2) sum (p - q) w is not."""
+    N, C, T, G = 40, 48, 2.0 ** -100, 2.0 ** 40
+    h, w, _, _, index, logit, weight = inputs(N, C, V, torch.float32, 3)
+    h, w, logit, weight = h * 2.0 ** -10, w * 2.0 ** -90, logit * T, weight * G
+    say("large weights, low temperature", V)
+    r = reno.head_distill(h, w, None, index, logit, temperature=T, row_weight=weight, grad=("dh",))
+    ref = reference(h, w, None, *targets_of_top(index, logit, T, V), weight, T)
+    assert 2.0 ** 40 < float(ref["dh"][0].abs().max()) < 2.0 ** 60
+    for x in ("bits", "dh"):
+        check(x, getattr(r, x), *ref[x])
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("V", [300])
+def test_gradients_of_zero_at_a_low_temperature(V, dt):
+    """One symbol's worth of teacher and student: p - q is 0, and so is every gradient, however large g / T."""
+    N, C, T = 20, 48, 2.0 ** -100
+    h = torch.ones(N, C, dtype=dt, device="cuda")
+    w = torch.zeros(C, V, dtype=dt, device="cuda")
+    b = torch.full((V,), -math.inf, dtype=dt, device="cuda")
+    b[7] = 0.0
+    index = torch.full((N, 1), 7, dtype=torch.int32, device="cuda")
+    weight = torch.full((N,), 2.0 ** 40, device="cuda")
+    say("gradients of zero", V, dt)
+    r = reno.head_distill(h, w, b, index, torch.zeros(N, 1, device="cuda"), temperature=T, row_weight=weight, grad=True)
+    for x in (r.bits, r.dh, r.dw, r.db):
+        assert not bool(x.any())
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float16])
+def test_large_weights_at_a_high_temperature(dt):
+    """1 / (T ln 2) over fp16's 2^14 lies below the normal floats, the gradients do not."""
+    N, C, V = 16, 48, 300
+    T = float(torch.tensor(2.0 ** 135 / (math.log(2.0) * 530.5), dtype=torch.float32))   # half a step between two of them
+    h, w, b, _, index, logit, weight = inputs(N, C, V, dt, 4)
+    weight = weight * 2.0 ** 125
+    say("large weights, high temperature", dt)
+    r = reno.head_distill(h, w, b, index, logit, temperature=T, row_weight=weight, grad=True)
+    q, taken, bad = targets_of_top(index, logit, T, V)
+    exact = reference(h.float(), w.float(), b.float(), q, taken, bad, weight, T)
+    # of the type's: the result's rounding, and dz in two parts (2^-16 of itself, fp16 2^-22) through |w| and |h|
+    u = torch.finfo(dt).eps / 2
+    dz = (weight.double() / (T * math.log(2.0)))[:, None] * (1.0 / V - q).abs() * 1.01 * taken[:, None]
+    part = {"dh": dz @ w.double().abs().T, "dw": h.double().abs().T @ dz, "db": 0.0}
+    for x in ("dh", "dw", "db"):
+        value, bound = exact[x]
+        check(x, getattr(r, x), value, bound + 2 * u * u * part[x] + u * value.abs() * 1.01 + 2.0 ** -25)
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("V", [300])
+def test_weights_at_the_ends_of_fp32(V, dt):
+    """The largest float and the smallest normal one as every row's weight, brought to size by the temperature."""
+    N, C = 40, 48
+    h, w, b, _, index, logit, weight = inputs(N, C, V, dt, 5)
+    for e, T in ((126.9, 2.0 ** 125), (-125.0, 2.0 ** -120)):
+        scale = 1.0 if T > 1 else 2.0 ** -60 if dt == torch.float32 else 0.0   # logits of 0 where T leaves no others
+        weight = torch.full((N,), 2.0 ** e, device="cuda")
+        a, c = (h * scale).to(dt), (w * scale if scale else w).to(dt)
+        say("weights at the ends", V, dt, e)
+        r = reno.head_distill(a, c, None, index, logit * min(T, 1.0), temperature=T, row_weight=weight, grad=True)
+        ref = reference(a, c, None, *targets_of_top(index, logit * min(T, 1.0), T, V), weight, T)
+        for x in ("bits", "dh", "dw", "db"):
+            check(x, getattr(r, x), *ref[x])
