@@ -38,7 +38,8 @@ struct HeadTargets {
 // fp32 heads that one kernel takes whole (k_head_narrow.hip)
 bool head_is_narrow(const reno_head& p);
 int64_t head_narrow_bytes(const reno_head& p, bool grad);
-hipError_t launch_head_narrow(const HeadCall& c, const HeadTargets& t, char* ws, hipStream_t stream);
+// gpart: partial maxima of the rows' weights, over which dz is carried, or null
+hipError_t launch_head_narrow(const HeadCall& c, const HeadTargets& t, const float* gpart, char* ws, hipStream_t stream);
 
 int64_t head_workspace(const reno_head& p, int k, bool grad);
 hipError_t launch_head(const HeadCall& c, hipStream_t stream);

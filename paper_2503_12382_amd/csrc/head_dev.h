@@ -4,6 +4,9 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <cmath>
+
+#include "dev.h"
 #include "gemm.h"
 
 namespace reno {
@@ -16,6 +19,34 @@ __device__ __forceinline__ float log2_hw(float x) { return __builtin_amdgcn_logf
 // What logits are taken off before their exponentials: the largest, where it is finite.  Without any the sum is 0
 // and the normaliser -inf; with one of +inf the sum is +inf (or NaN), where inf - inf would be NaN
 __device__ __forceinline__ float exp_base(float m) { return fabsf(m) < INFINITY ? m : 0.0f; }
+
+constexpr int GPARTS = 64;   // partial maxima of |g|, in the workspace
+
+// e: the largest |g| of the rows that are taken is below 2^e and at least half of it (0 without weights, or with
+// none but 0).  dz is carried over G = 2^e.
+__device__ __forceinline__ int weight_exp(const float* gpart) {
+  if (!gpart) return 0;
+  float m = gpart[lane_id()];
+  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+  return m == 0.0f ? 0 : __builtin_amdgcn_frexp_expf(m);
+}
+
+// What brings the sums of dz to gradients: 1 / (T ln 2), over 2^14 for fp16, as a number below 1 and a power of two.
+// That power and G may each be past the floats where the gradient is not; they meet as integers.
+struct OutScale {
+  float mant;
+  int exp;
+};
+inline OutScale out_scale(float temperature) {
+  OutScale s;
+  s.mant = (float)std::frexp(1.0 / (0.6931471805599453 * (double)temperature), &s.exp);
+  return s;
+}
+__device__ __forceinline__ float scaled(float x, OutScale s) { return __builtin_amdgcn_ldexpf(x * s.mant, s.exp); }
+__device__ __forceinline__ OutScale with_weights(OutScale s, const float* gpart) {
+  s.exp += __builtin_amdgcn_readfirstlane(weight_exp(gpart));
+  return s;
+}
 
 // The three bf16 planes of x: each takes the leading 8 bits of what is left, cut off, so that
 // the parts add up to x exactly.  An infinity leaves NaN in the lower planes (inf - inf): products

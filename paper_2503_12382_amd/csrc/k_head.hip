@@ -27,7 +27,6 @@
 // dw 0.90 and (the second piece, which reads and writes the first one's sums) 1.25, k_head_dz 0.23.
 
 #include <algorithm>
-#include <cmath>
 
 #include "dev.h"
 #include "gemm.h"
@@ -37,7 +36,6 @@
 namespace reno {
 namespace {
 
-constexpr int GPARTS = 64;       // partial maxima of |g|
 constexpr int DZ_COLS = 512;     // symbols of a wave of k_head_dz
 constexpr int HALF_SHIFT = 14;   // dz in fp16 is scaled by 2^14
 
@@ -122,28 +120,6 @@ __device__ __forceinline__ int row_flag(const HeadArgs& a, int64_t row) {
   if (a.flag) return a.flag[row];
   const int32_t s = a.index[row];
   return s < 0 ? 0 : s < a.V ? 1 : 2;
-}
-
-// ---- weights' scale ----
-// e: the largest |g| of the rows that are taken is below 2^e and at least half of it (0 without weights, or with
-// none but 0).  dz is carried over G = 2^e.
-__device__ __forceinline__ int weight_exp(const float* gpart) {
-  if (!gpart) return 0;
-  float m = gpart[lane_id()];
-  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-  return m == 0.0f ? 0 : __builtin_amdgcn_frexp_expf(m);
-}
-
-// What brings the sums of dz to gradients: 1 / (T ln 2), over 2^14 for fp16, as a number below 1 and a power of two.
-// That power and G may each be past the floats where the gradient is not; they meet as integers.
-struct OutScale {
-  float mant;
-  int exp;
-};
-__device__ __forceinline__ float scaled(float x, OutScale s) { return __builtin_amdgcn_ldexpf(x * s.mant, s.exp); }
-__device__ __forceinline__ OutScale with_weights(OutScale s, const float* gpart) {
-  s.exp += __builtin_amdgcn_readfirstlane(weight_exp(gpart));
-  return s;
 }
 
 // ---- targets of a distillation ----
@@ -911,8 +887,9 @@ Plan make_plan(const reno_head& p, int k, bool grad) {
   a.q = take(N * k * 4);
   a.ent = take(N * 4);
   a.flag = take(N);
-  a.narrow = at;
   if (head_is_narrow(p)) {
+    a.gpart = take(GPARTS * 4);
+    a.narrow = at;
     a.bytes = at + std::max<int64_t>(256, head_narrow_bytes(p, grad));
     return a;
   }
@@ -1032,12 +1009,25 @@ hipError_t run_head(const HeadCall& c, hipStream_t st) {
     else args(k_head_targets<64, 2>);
     t = HeadTargets{idx, q, ent, flag};
   }
-  if (head_is_narrow(p)) return launch_head_narrow(c, t, ws + pl.narrow, st);
   HeadArgs a{};
   a.N = N;
   a.C = p.channels;
   a.V = p.symbols;
   a.k = c.k;
+  a.g = c.d.row_weight;
+  a.index = t.index;
+  a.q = t.q;
+  a.ent = t.ent;
+  a.flag = t.flag;
+  if (head_is_narrow(p)) {
+    // These carry dz as g (p - q), as long as 1 / T leaves that within 2^24 of the gradients' own size; beyond,
+    // over the largest weight too (233737 rows: 5 us).
+    const bool far = c.grad && c.d.row_weight && !(c.temperature >= 0x1p-24f && c.temperature <= 0x1p24f);
+    float* gpart = far ? reinterpret_cast<float*>(ws + pl.gpart) : nullptr;
+    if (far)
+      hipLaunchKernelGGL(k_head_setup<TYPE>, dim3(GPARTS), dim3(256), 0, st, a, SetupBlocks{0, GPARTS, 0, 0}, int64_t(0), gpart);
+    return launch_head_narrow(c, t, gpart, ws + pl.narrow, st);
+  }
   a.Cp = pl.Cp;
   a.Vp = pl.Vp;
   a.h_stride = p.h_stride;
@@ -1045,7 +1035,6 @@ hipError_t run_head(const HeadCall& c, hipStream_t st) {
   a.h = c.d.h;
   a.w = c.d.w;
   a.b = c.d.b;
-  a.g = c.d.row_weight;
   a.scale = (float)(1.4426950408889634 / (double)c.temperature);
   a.bias = reinterpret_cast<float*>(ws + pl.bias);
   a.hp = reinterpret_cast<uint16_t*>(ws + pl.hp);
@@ -1061,10 +1050,6 @@ hipError_t run_head(const HeadCall& c, hipStream_t st) {
   a.lse2 = reinterpret_cast<float*>(ws + pl.lse2);
   a.bits = c.d.bits;
   a.lse = c.d.lse;
-  a.index = t.index;
-  a.q = t.q;
-  a.ent = t.ent;
-  a.flag = t.flag;
   if (const int few = few_width(p, c.grad)) {
     const dim3 grid((unsigned)a.parts);
     a.R = N;
@@ -1090,8 +1075,7 @@ hipError_t run_head(const HeadCall& c, hipStream_t st) {
   const int64_t wl = in_place ? p.w_stride : pl.Vp;
   const Operand W{in_place ? static_cast<const uint16_t*>(c.d.w) : a.wp, wl, p.channels,
                   (p.channels - 1) * wl + (in_place ? p.symbols : pl.Vp), a.w_plane};
-  OutScale scale;
-  scale.mant = (float)std::frexp(1.0 / (0.6931471805599453 * (double)c.temperature), &scale.exp);
+  const OutScale scale = out_scale(c.temperature);
   const OutScale scale_d{scale.mant, scale.exp - (HALF ? HALF_SHIFT : 0)};
   for (int64_t i = 0; i < pl.pieces; ++i) {
     a.r0 = i * pl.R;

@@ -46,7 +46,9 @@ struct NarrowArgs {
   const float* q;          // [N][k] joined probabilities, or null: one entry with 1
   const float* ent;
   const uint8_t* flag;
-  float scale, out_scale;  // log2(e) / T, 1 / (T ln 2)
+  float scale;             // log2(e) / T
+  OutScale out_scale;      // 1 / (T ln 2)
+  const float* gpart;      // partial maxima of |g| that dz is carried over, or null: as it is
   const uint16_t* wz;      // streamed W, in the order of use: fragments of 16 symbols x 32 channels for z,
   const uint16_t* wd;      // of 16 channels x 32 symbols for dh
   float *bits, *lse, *dh;
@@ -191,6 +193,8 @@ __global__ void __launch_bounds__(64 * waves_of(CT), 2) k_narrow(NarrowArgs a) {
       for (int j = 0; j < DW_N; ++j) dw[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
   }
+  const int g_exp = GRAD ? __builtin_amdgcn_readfirstlane(weight_exp(a.gpart)) : 0;
+  const OutScale out_scale{a.out_scale.mant, a.out_scale.exp + g_exp};
   const int64_t steps = (a.N + NB_ROWS - 1) / NB_ROWS;
   // this lane's piece of its row: channels 32 ks + 8 g .. + 7
   float x[KS][8];
@@ -230,7 +234,7 @@ __global__ void __launch_bounds__(64 * waves_of(CT), 2) k_narrow(NarrowArgs a) {
       }
     }
     float weight = 1.0f;
-    if (GRAD && a.g && flag) weight = a.g[row];
+    if (GRAD && a.g && flag) weight = __builtin_amdgcn_ldexpf(a.g[row], -g_exp);
     if (!AHEAD) load_h(step);
     // logits, 32 channels at a time.  Fragments of W on their way: one or two ahead
     constexpr int RING = L::W_HERE && DENSE ? 2 : 3;
@@ -434,8 +438,9 @@ __global__ void __launch_bounds__(64 * waves_of(CT), 2) k_narrow(NarrowArgs a) {
         for (int ct = 0; ct < CT; ++ct) {
           const int c = 16 * ct + 4 * g;
           float* o = a.dh + row * a.C + c;
-          f32x4 y = dh[ct] * a.out_scale;
-          if (!flag) y = f32x4{0.f, 0.f, 0.f, 0.f};   // also where weights that are NaN reach it
+          f32x4 y;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[e] = flag ? scaled(dh[ct][e], out_scale) : 0.0f;   // 0 also where weights that are NaN reach it
           if (a.C % 4 == 0 && (uintptr_t)a.dh % 16 == 0) {
             if (c < a.C) *reinterpret_cast<f32x4*>(o) = y;
           } else {
@@ -488,8 +493,10 @@ __global__ void __launch_bounds__(256) k_narrow_pack(NarrowArgs a, int KS, int C
 
 // dw and db from the blocks' sums: 16 values a block, 16 shares of the blocks each.
 __global__ void __launch_bounds__(256) k_narrow_join(const float* __restrict__ part, int blocks, int C, int V, int DB,
-                                                     float scale, float* __restrict__ dw, float* __restrict__ db) {
+                                                     OutScale out_scale, const float* __restrict__ gpart,
+                                                     float* __restrict__ dw, float* __restrict__ db) {
   __shared__ float s[16][17];
+  const OutScale scale = with_weights(out_scale, gpart);
   const int i = threadIdx.x & 15, share = threadIdx.x >> 4;
   const int64_t n = (int64_t)C * V, all = n + (int64_t)DB * V, at = (int64_t)blockIdx.x * 16 + i;
   float x = 0.0f;
@@ -507,8 +514,8 @@ __global__ void __launch_bounds__(256) k_narrow_join(const float* __restrict__ p
   x = 0.0f;
   for (int k = 0; k < 16; ++k) x += s[k][i];
   if (at < n) {
-    if (dw) dw[at] = x * scale;
-  } else if (db) db[at - n] = x * scale;
+    if (dw) dw[at] = scaled(x, scale);
+  } else if (db) db[at - n] = scaled(x, scale);
 }
 
 int width_of(int channels) { return channels <= 32 ? 2 : channels <= 64 ? 4 : 8; }
@@ -541,7 +548,7 @@ int64_t head_narrow_bytes(const reno_head& p, bool grad) {
   return n;
 }
 
-hipError_t launch_head_narrow(const HeadCall& c, const HeadTargets& t, char* ws, hipStream_t st) {
+hipError_t launch_head_narrow(const HeadCall& c, const HeadTargets& t, const float* gpart, char* ws, hipStream_t st) {
   const reno_head& p = c.p;
   NarrowArgs a{};
   a.N = p.rows;
@@ -559,7 +566,8 @@ hipError_t launch_head_narrow(const HeadCall& c, const HeadTargets& t, char* ws,
   a.ent = t.ent;
   a.flag = t.flag;
   a.scale = (float)(1.4426950408889634 / (double)c.temperature);
-  a.out_scale = (float)(1.0 / (0.6931471805599453 * (double)c.temperature));
+  a.out_scale = out_scale(c.temperature);
+  a.gpart = gpart;
   a.bits = c.d.bits;
   a.lse = c.d.lse;
   a.dh = static_cast<float*>(c.d.dh);
@@ -590,7 +598,7 @@ hipError_t launch_head_narrow(const HeadCall& c, const HeadTargets& t, char* ws,
   if (c.d.dw || c.d.db) {
     const int64_t n = (int64_t)(a.C + 1) * a.V;
     hipLaunchKernelGGL(k_narrow_join, dim3((unsigned)((n + 15) / 16)), dim3(256), 0, st, a.part, blocks, a.C, a.V,
-                       waves_of(CT) / 2, a.out_scale, static_cast<float*>(c.d.dw), static_cast<float*>(c.d.db));
+                       waves_of(CT) / 2, a.out_scale, a.gpart, static_cast<float*>(c.d.dw), static_cast<float*>(c.d.db));
   }
   return hipGetLastError();
 }

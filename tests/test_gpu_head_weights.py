@@ -131,3 +131,28 @@ def test_weights_at_the_ends_of_fp32(V, dt):
         ref = reference(a, c, None, *targets_of_top(index, logit * min(T, 1.0), T, V), weight, T)
         for x in ("bits", "dh", "dw", "db"):
             check(x, getattr(r, x), *ref[x])
+
+
+@pytest.mark.parametrize("C", [24, 48, 128])
+@pytest.mark.parametrize("e,T", [(126.9, 2.0 ** 125), (-125.0, 2.0 ** -120), (40.0, 2.0 ** -100), (-100.0, 2.0 ** -90)])
+def test_narrow_heads_at_the_ends_of_fp32(C, e, T):
+    N, V = 300, 200
+    h, w, b, _, index, logit, _ = inputs(N, C, V, torch.float32, 6)
+    weight = torch.full((N,), 2.0 ** e, device="cuda")
+    scale = 1.0 if T > 1 else math.sqrt(T)       # logits of order 1 over T
+    h, w, logit = h * scale, w * scale, logit * min(T, 1.0)
+    say("narrow heads at the ends", C, e, T)
+    r = reno.head_distill(h, w, None, index, logit, temperature=T, row_weight=weight, grad=True)
+    ref = reference(h, w, None, *targets_of_top(index, logit, T, V), weight, T)
+    big = torch.finfo(torch.float32).max
+    for x in ("bits", "dh", "dw", "db"):
+        value, bound = ref[x]
+        over = value.abs() > big                 # past fp32: infinite
+        assert bool((getattr(r, x)[over].abs() == math.inf).all()) and not (x == "dh" and bool(over.any()))
+        check(x, torch.where(over, 0.0, getattr(r, x).double()), torch.where(over, 0.0, value), bound)
+
+
+def test_narrow_gradients_of_zero_at_a_low_temperature():
+    test_gradients_of_zero_at_a_low_temperature(200, torch.float32)
+    test_large_weights_at_a_low_temperature(200)
+    test_weights_at_the_ends_of_fp32(200, torch.float32)
