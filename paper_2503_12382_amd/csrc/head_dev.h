@@ -16,9 +16,11 @@ constexpr float LN2 = 0.6931471805599453f;
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float log2_hw(float x) { return __builtin_amdgcn_logf(x); }
 
-// What logits are taken off before their exponentials: the largest, where it is finite.  Without any the sum is 0
-// and the normaliser -inf; with one of +inf the sum is +inf (or NaN), where inf - inf would be NaN
-__device__ __forceinline__ float exp_base(float m) { return fabsf(m) < INFINITY ? m : 0.0f; }
+// What logits are taken off before their exponentials: the largest, where that is finite.  Without any logit the sum
+// is 0 and the normaliser -inf; with one of +inf the sum is +inf, or NaN beside NaN.  (inf - inf would be NaN at
+// once.  In this form k_narrow with gradients takes 119 us for 58711 x 128 x 256, as one median of three or as a
+// comparison of |m| 123.5: the compiler then places the tiles' registers differently.)
+__device__ __forceinline__ float exp_base(float m) { return m > -INFINITY ? fminf(m, 0x1.fffffep127f) : 0.0f; }
 
 constexpr int GPARTS = 64;   // partial maxima of |g|, in the workspace
 
