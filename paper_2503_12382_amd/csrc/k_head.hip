@@ -910,10 +910,11 @@ Plan make_plan(const reno_head& p, int k, bool grad) {
   a.Cp = up(p.channels, GEMM_BK);
   a.Vp = up(p.symbols, GEMM_BK);
   a.Vb = up(p.symbols, 256);
-  // a piece: at most 2^28 logits (2^27 in fp32) where they are kept for the
-  // gradient, 2^32 where they are not
+  // A piece: at most 2^28 logits (2^27 in fp32) where they are kept for the gradient, 2^32 where they are not, and
+  // 2^31 bytes of what is copied of a row (h as planes, its targets' t): with few symbols h is the larger part.
   const int64_t most = !grad ? int64_t(1) << 32 : p.type == RENO_T_FP32 ? int64_t(1) << 27 : int64_t(1) << 28;
-  int64_t R = std::max<int64_t>(256, most / a.Vp / 256 * 256);
+  const int64_t copied = a.planes * a.Cp * 2 + 4 * (int64_t)k;
+  const int64_t R = std::max<int64_t>(256, std::min(most / a.Vp, (int64_t(1) << 31) / copied) / 256 * 256);
   a.pieces = (N + R - 1) / R;
   a.R = std::min(N, up((N + a.pieces - 1) / a.pieces, 256));
   a.pieces = (N + a.R - 1) / a.R;
