@@ -118,9 +118,13 @@ reno_status reno_top_logits(const void* logits, int type, int64_t rows, int symb
 
 /* FEATURES of a model scale (b0 < scale < B) that the head is applied to, as
  * the last reno_predict_probs of that scale left them (Sec. 3.2, h of the last
- * layer): fp32 [N_scale][C].  RENO_ALL_SCALES: every model scale, concatenated
- * in order.  Channels whose head weights are all zero are not kept by the
- * model kernels and come back as NaN.  RENO_E_STATE before predict_probs. */
+ * layer; two-stage: of the first head, the second's are h + Emb(S1)): fp32
+ * [N_scale][C].  RENO_ALL_SCALES: every model scale, concatenated in order.
+ * A channel that no weight reads (its rows of the head, of both heads, are all
+ * zero; the full predictor's own layers read every channel) is not kept by the
+ * model kernels and comes back as NaN.  The features do not depend on the head:
+ * to train one from zero, or one with rows that are zero, take them under a
+ * head without such rows.  RENO_E_STATE before predict_probs. */
 reno_status reno_features(reno_ctx* ctx, int scale, float* features);
 
 #ifdef __cplusplus

@@ -393,7 +393,9 @@ class Context:
     def features(self, scale: int):
         """Features [N_scale][C] (fp32) that the head is applied to, as the last
         predict_probs of the scale left them; RENO_ALL_SCALES concatenates the
-        model scales.  Channels that no head weight reads come back as NaN."""
+        model scales.  They do not depend on the head, but channels that no
+        weight reads (rows of zeros in it) come back as NaN: to train a head
+        that starts from zero, take them under one without such rows."""
         if scale == RENO_ALL_SCALES:
             n = sum(self.num_voxels(b) for b in range(self.b0 + 1, self.B))
         else:
