@@ -549,13 +549,21 @@ def _head_check(rc):
         raise RenoError(rc, lib().reno_last_error(None).decode())
 
 
+def _entries(k):
+    """Entries a row, checked here: the C ABI takes an int, which ctypes would cut to 32 bits."""
+    k = int(k)
+    if not 1 <= k <= RENO_HEAD_MAX_TOP:
+        raise RenoError(RENO_E_INVALID, "k must be in [1, RENO_HEAD_MAX_TOP]")
+    return k
+
+
 def head_workspace(rows: int, channels: int, symbols: int, dtype, top_k: int = 1, grad: bool = False) -> int:
     """Bytes of workspace for such a call (reno_head_workspace)."""
     kind = _type_of(dtype)
     _need(kind is not None, "dtype must be float32, bfloat16 or float16")
     p = reno_head(rows, channels, symbols, kind, channels, symbols)
     n = ctypes.c_int64()
-    _head_check(lib().reno_head_workspace(ctypes.byref(p), top_k, int(bool(grad)), ctypes.byref(n)))
+    _head_check(lib().reno_head_workspace(ctypes.byref(p), _entries(top_k), int(bool(grad)), ctypes.byref(n)))
     return n.value
 
 
@@ -646,7 +654,7 @@ def head_distill(h, w, b, top_index, top_logit, temperature: float = 1.0, row_we
     other arguments and the results as for head_code_length."""
     import torch
     _need(top_index.dim() == 2, "top_index must be [N][k]")
-    k = int(top_index.shape[1])
+    k = _entries(top_index.shape[1])
     shape = (h.shape[0], k)
 
     def call(p, d, ix, lg, ws, nbytes, st):
@@ -663,13 +671,13 @@ def top_logits(logits, k: int, stream=None) -> TopLogits:
     import torch
     _need(logits.dim() == 2 and logits.is_cuda, "logits must be a device tensor [N][V]")
     _need(_type_of(logits.dtype) is not None, "logits must be float32, bfloat16 or float16")
-    k, dev = int(k), logits.device
+    k, dev = _entries(k), logits.device
     n, v = logits.shape
 
     def run(st):
         x = _rows(logits, "logits", logits.dtype, dev, (n, v))
-        index = torch.empty((n, max(k, 0)), dtype=torch.int32, device=dev)
-        value = torch.empty((n, max(k, 0)), dtype=torch.float32, device=dev)
+        index = torch.empty((n, k), dtype=torch.int32, device=dev)
+        value = torch.empty((n, k), dtype=torch.float32, device=dev)
         lse = torch.empty(n, dtype=torch.float32, device=dev)
         _head_check(lib().reno_top_logits(x.data_ptr(), _type_of(x.dtype), n, v, _stride(x), k, index.data_ptr(),
                                           value.data_ptr(), lse.data_ptr(), st.cuda_stream))
