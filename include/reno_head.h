@@ -6,7 +6,9 @@
  * They stand beside reno_code_length and reno_predict_probs (reno.h), whose
  * head they train: z = w^T h + b (Eq. 10), bits = -log2 softmax(z)[symbol]
  * (Eq. 4).  The features may be the framework's own (reno_features) or any
- * others, and the alphabet any size: the logits are never kept whole.
+ * others, and the alphabet any size.  Without gradients no logits are kept; with
+ * them, those of one piece of rows at a time are, in the workspace: all of a call
+ * of up to 2^28 (fp32: 2^27) logits or 256 rows, at most so many of a larger one.
  *
  * Conventions: those of reno.h (device pointers, status codes, nothing thrown
  * or aborted), and
@@ -42,11 +44,17 @@ extern "C" {
 #endif
 
 typedef enum {
-  RENO_T_FP32 = 0, /* products of operands carried as three bf16 parts (24 bits, the range of
-                      fp32), the six products above 2^-24 kept: fp32 accuracy */
+  RENO_T_FP32 = 0, /* products of operands carried as three bf16 parts, cut off: 24 bits, down to
+                      2^-133 (operands below 2^-110, in heads of up to 128 channels and 256
+                      symbols g (p - q) too, keep fewer).  Of the nine products of parts six
+                      are kept; the others are below 2^-21 of the whole together, 2^-24.6 on
+                      average, and of its sign.  (Up to 4 rows without gradients, in wider heads:
+                      plain fp32 sums.) */
   RENO_T_BF16 = 1, /* bf16 products, fp32 sums; logits' gradients are rounded to bf16 before
-                      they meet h and w (kept until then to 2^-12 of the probability; calls
-                      of up to 16 rows, where nothing averages, carry them in two parts) */
+                      they meet h and w (kept until then to 2^-12 of the probability, and
+                      as 0 below 2^-39 of the largest of 64 or 128 symbols), so that
+                      gradients have two roundings, 1.4 times the error of one; calls of up
+                      to 16 rows, where nothing averages, carry them in two parts and have one */
   RENO_T_FP16 = 2  /* the same in fp16, logits' gradients scaled by 2^14 over the largest
                       row weight so that none above 2^-38 of it is lost */
 } reno_type;
@@ -80,7 +88,10 @@ typedef struct {
 
 /* Bytes of workspace (into *bytes_host) for a call on such a head with top_k
  * entries a row (reno_head_code_length: 1), with any gradient (grad != 0) or
- * none.  No device work. */
+ * none: every row's targets (8 top_k + 5 bytes a row), a copy of w as 16-bit
+ * parts (reserved also for weights that turn out to be read in place), one piece
+ * of rows (copies of h: 2^31 bytes or 256 rows at most) and, with gradients, its
+ * logits (fp32 10 bytes each, fp16 6, bf16 2) and fp32 sums of dw.  No device work. */
 reno_status reno_head_workspace(const reno_head* head, int top_k, int grad, int64_t* bytes_host);
 
 /* CODE LENGTH of a head with its gradient (Eqs. 4, 10):

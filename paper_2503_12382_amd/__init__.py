@@ -630,13 +630,24 @@ def _head_call(h, w, b, targets, row_weight, grad, workspace, stream, k, call):
 
 def head_code_length(h, w, b, symbol, row_weight=None, grad=False, workspace=None, stream=None) -> HeadResult:
     """Ideal code length of the linear head z = h w + b and its gradient
-    (reno_head_code_length), without keeping the logits: h [N][C], w [C][V], b [V]
-    or None (float32, bfloat16 or float16, one type), symbol int32 [N] (negative:
-    the row is left out), row_weight float32 [N] or None.  grad: True or a
+    (reno_head_code_length); logits are kept only with a gradient, a piece of
+    rows at a time, in the workspace.  h [N][C], w [C][V], b [V] or None
+    (float32, bfloat16 or float16, one type), symbol int32 [N] (negative: the
+    row is left out), row_weight float32 [N] or None.  grad: True or a
     selection of "dh", "dw", "db", the gradients of sum_r row_weight_r bits_r.
     workspace: a uint8 tensor of head_workspace bytes, or None to take it from
     torch's allocator.  Enqueued on ``stream`` (default: the current stream of
-    the tensors' device); rows may be strided."""
+    the tensors' device); rows may be strided.
+
+    Sums are fp32 for every type.  Gradients of bfloat16 and float16 have two
+    roundings to the type, of the logits' gradient before it meets h and w and
+    of the result (up to 16 rows: one); bfloat16 keeps the softmax to 2^-12 in
+    between.  float32 has products to about 2^-24 (include/reno_head.h).
+
+    Nothing is recorded for autograd: arguments that require a gradient are
+    read as they are, and the results have no grad_fn.  The gradients of
+    sum_r row_weight_r bits_r come with the call; pass dh on (h.backward(dh))
+    and add dw and db to the parameters' own."""
     import torch
 
     def call(p, d, s, ws, nbytes, st):
@@ -651,7 +662,8 @@ def head_distill(h, w, b, top_index, top_logit, temperature: float = 1.0, row_we
     top_index int32 [N][k] (negative: no entry) and top_logit float32 [N][k], as
     top_logits gives them.  bits are the divergence of the student's
     distribution at the temperature from the teacher's over its entries; the
-    other arguments and the results as for head_code_length."""
+    other arguments, the results, their precision and what autograd sees as for
+    head_code_length."""
     import torch
     _need(top_index.dim() == 2, "top_index must be [N][k]")
     k = _entries(top_index.shape[1])

@@ -23,8 +23,8 @@
 // products' results: fp16 and the low planes of fp32 lose nothing of it for small g.
 //
 // Bound: the three products.  8192 x 2048 x 65536 bf16 (6.6 TFLOP, two pieces) takes 6.6 ms, 1000 TFLOP/s, where
-// one large product of the library's reaches 1207; of a piece of 4096 rows k_head_logits takes 1.10 ms, dh 1.11,
-// dw 0.90 and (the second piece, which reads and writes the first one's sums) 1.25, k_head_dz 0.23.
+// one large product of the library's reaches 1207; of a piece of 4096 rows k_head_logits takes 1.13 ms, dh 1.10,
+// dw 0.97 and (the second piece, which reads and writes the first one's sums) 1.27, k_head_dz 0.23.
 
 #include <algorithm>
 
@@ -904,7 +904,7 @@ Plan make_plan(const reno_head& p, int k, bool grad) {
   a.planes = planes_of(p.type);
   // A second plane of dz for few rows: with many, the roundings of dz average out and leave as much as that of the
   // result; in one row that of the target's dz is the whole result's.  Up to 16 rows the products wait for w and dw
-  // (1 x 2048 x 65536 bf16: 295 us, 252 with one plane).
+  // (1 x 2048 x 65536 bf16: 280 us; 17 rows, with one plane, 251).
   a.dz_planes = p.type == RENO_T_FP32 ? 3 : p.rows <= 16 ? 2 : 1;
   const int dz_terms = p.type == RENO_T_FP32 ? TERMS_FP32.n : a.dz_planes;
   a.Cp = up(p.channels, GEMM_BK);
