@@ -114,7 +114,8 @@ reno_status reno_head_code_length(const reno_head* head, const reno_head_data* d
  * An entry with a negative index is not there; one whose index occurs before
  * counts with it, as one entry of their summed probability.  A row without any
  * entry (or with logits of -inf only) is left out as above; an index of V or
- * more, or an entry's logit of +inf or NaN, gives NaN as above.  temperature: positive and finite, 2^-127 to 2^126. */
+ * more, or an entry's logit of +inf or NaN, gives NaN as above.  temperature:
+ * positive and finite, 2^-127 to 2^126. */
 reno_status reno_head_distill(const reno_head* head, const reno_head_data* data, const int32_t* top_index,
                               const float* top_logit, int k, float temperature, void* workspace,
                               int64_t workspace_bytes, void* hip_stream);
