@@ -262,7 +262,8 @@ __global__ void __launch_bounds__(256) k_head_pack_h(HeadArgs a) {
 }
 
 // Blocks of the first launch, by what they do: the first piece's rows of h, GPARTS partial maxima of the finite |g|
-// of rows with a target (what the others weigh must not move the scale of dz), b * scale padded to whole tiles, the weights (where they cannot be read in place).
+// of rows with a target (what the others weigh must not move the scale of dz), b * scale padded to whole tiles, the
+// weights (where they cannot be read in place).
 struct SetupBlocks {
   unsigned h, g, b, w;
 };
@@ -1022,7 +1023,7 @@ hipError_t run_head(const HeadCall& c, hipStream_t st) {
   a.flag = t.flag;
   if (head_is_narrow(p)) {
     // These carry dz as g (p - q), as long as 1 / T leaves that within 2^24 of the gradients' own size; beyond,
-    // over the largest weight too (233737 rows: 5 us).
+    // over the largest weight too (233737 x 32 x 256, 16 entries a row: 187 us for 180).
     const bool far = c.grad && c.d.row_weight && !(c.temperature >= 0x1p-24f && c.temperature <= 0x1p24f);
     float* gpart = far ? reinterpret_cast<float*>(ws + pl.gpart) : nullptr;
     if (far)
