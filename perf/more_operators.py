@@ -1,0 +1,329 @@
+"""Performance cases of drawing symbols from logits and of the step that follows a gradient: its global norm, clipping
+by it, and the AdamW update of the weights.
+
+A case names the operator (``op``) and its sizes:
+
+  sample  a symbol of each row of logits, by a given random number u of the row, from the distribution at the
+          temperature cut to the top_k largest, to the shortest prefix of mass top_p of those, and to those of at
+          least min_p of the largest; -log2 of its probability there.  Symbols that ``allowed`` leaves out are never
+          drawn; rows whose u lies outside [0, 1) are left out (-1 and 0)
+  norm    the 2-norm over all tensors of a model's gradients, which carry a loss scale
+  clip    the same, and the gradients over the loss scale, scaled down to the largest norm that is allowed
+  adamw   the norm, and one AdamW update by the clipped gradients: weights, their 32-bit copies where they have 16 bits,
+          and both moments
+
+The tensors of a model lie in one buffer a kind, as training programs lay them out, each on 512 bytes or, ``packed``,
+one right behind the other.  ``run`` computes the plain form, or with ``own`` calls the framework; ``exact`` recomputes
+the results in float64 from the definitions.
+"""
+import math
+
+import torch
+
+own = False
+DEV = "cuda" if torch.cuda.is_available() else "cpu"
+TYPES = {"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16}
+SIZES = {"fp32": 4, "bf16": 2, "fp16": 2}
+MOST_LOGITS = 4096 * 32768
+MOST_WEIGHTS = 1 << 27
+LR, BETA1, BETA2, EPS, DECAY, MOST_NORM = 1e-3, 0.9, 0.999, 1e-8, 0.01, 1.0
+
+
+def _sample(name, rows, symbols, *, dtype="fp32", temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, mask="none", each=False):
+    c = dict(op="sample", rows=rows, symbols=symbols, dtype=dtype, temperature=temperature, top_k=top_k, top_p=top_p,
+             min_p=min_p, mask=mask, each=each)
+    return dict(c, name=name) if name else c
+
+
+def _step(name, op, model, channels, symbols, *, layers=0, kernel=3, dtype="fp32", packed=False):
+    c = dict(op=op, model=model, channels=channels, symbols=symbols, layers=layers, kernel=kernel, dtype=dtype,
+             packed=packed)
+    return dict(c, name=name) if name else c
+
+
+def listed():
+    return [
+        # one coarse scale of the 16-beam 10-bit scan, codes drawn from the whole distribution: launches count
+        _sample("sample 87 rows 256", 87, 256, mask="shared"),
+        # the codes of all model voxels of the 64-beam 14-bit scan; code 0 stands for no child and is never drawn
+        _sample("sample 14-bit 256", 233737, 256, top_p=0.95, mask="shared"),
+        # one answer over a large odd alphabet
+        _sample("sample one row 131071", 1, 131071, temperature=0.8, top_k=50, top_p=0.95),
+        # a serving batch whose requests have settings and masks of their own
+        _sample("sample 64 rows 50021", 64, 50021, dtype="fp16", mask="rows", each=True),
+        # drawn targets of a training batch over a large alphabet
+        _sample("sample 4096 rows 32768", 4096, 32768, dtype="bf16", top_p=0.9, min_p=0.001),
+        # gradients of the 14-bit scan's model, 32 channels and four layers: latency
+        _step("norm c32 model", "norm", "layers", 32, 256, layers=4),
+        # gradients of a head over a large alphabet
+        _step("norm head 65536", "norm", "head", 2048, 65536, dtype="bf16"),
+        # the widest predictor, 5x5x5 kernels
+        _step("clip top c128 k5", "clip", "top", 128, 256, kernel=5),
+        # a ragged head in 16 bits, its tensors packed: nothing is aligned
+        _step("clip head 50021", "clip", "head", 1000, 50021, dtype="fp16", packed=True),
+        # training steps: the scan's model, the widest predictor, a large head with 32-bit copies
+        _step("adamw c32 model", "adamw", "layers", 32, 256, layers=4),
+        _step("adamw top c128 k5", "adamw", "top", 128, 256, kernel=5),
+        _step("adamw head 65536", "adamw", "head", 2048, 65536, dtype="bf16"),
+    ]
+
+
+def draw(rng):
+    """One more case of the same ranges: scans' rows of 16 or 256 codes, 1 to 8192 rows over alphabets up to 131071;
+    models of the framework's sizes and heads of up to 2^27 weights."""
+
+    def log_int(lo, hi):
+        return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+    op = rng.choice(["sample", "sample", "sample", "norm", "clip", "adamw", "adamw"])
+    if op != "sample":
+        dtype, packed = rng.choice(["fp32", "fp32", "bf16", "fp16"]), rng.random() < 0.3
+        model = rng.choice(["layers", "top", "head", "head"])
+        if model == "layers":
+            return _step(None, op, model, rng.choice([16, 32, 64, 128]), 256, layers=rng.randint(1, 8), dtype=dtype, packed=packed)
+        if model == "top":
+            return _step(None, op, model, rng.choice([16, 32, 64, 128]), 256, kernel=rng.choice([3, 5]), dtype=dtype, packed=packed)
+        channels = log_int(16, 2048)
+        most = MOST_WEIGHTS // (2 if dtype == "fp32" else 1)
+        return _step(None, op, model, channels, log_int(16, min(131071, most // channels - 1)), dtype=dtype, packed=packed)
+    small = rng.random() < 0.4
+    symbols = rng.choice([16, 255, 256, 256]) if small else log_int(300, 131071)
+    rows = max(1, min(log_int(1, 233737 if small else 8192), MOST_LOGITS // symbols))
+    return _sample(None, rows, symbols, dtype=rng.choice(["fp32", "bf16", "fp16"]),
+                   temperature=rng.choice([0.0, 0.7, 1.0, 1.0, 1.3]), top_k=rng.choice([0, 0, log_int(1, symbols)]),
+                   top_p=rng.choice([1.0, round(rng.uniform(0.05, 0.999), 3), round(rng.uniform(0.8, 0.99), 3)]),
+                   min_p=rng.choice([0.0, 0.0, round(10 ** rng.uniform(-4, -0.5), 5)]),
+                   mask=rng.choice(["none", "shared", "rows"]), each=rng.random() < 0.25)
+
+
+def _shapes(case):
+    """The model's tensors: the codec's layers, the full predictor, or a head alone."""
+    C, V = case["channels"], case["symbols"]
+    shapes = []
+    if case["model"] == "layers":
+        for i in range(case["layers"]):
+            shapes += [(27, C if i else 11, C), (C,)]
+    if case["model"] == "top":
+        shapes += [(256, C), (8, C)] + [(case["kernel"] ** 3, C, C), (C,)] * 4
+    return shapes + [(C, V), (V,)]
+
+
+def _places(case):
+    """Where each tensor starts in its buffer, and the buffer's length."""
+    step = 1 if case["packed"] else 512 // SIZES[case["dtype"]]
+    at, starts = 0, []
+    for shape in _shapes(case):
+        starts.append(at)
+        at += -(-math.prod(shape) // step) * step
+    return starts, at
+
+
+# ---- inputs ----
+
+def prepare(case, seed):
+    g = torch.Generator(device=DEV).manual_seed(1000003 * int(seed) + 29)
+    dt = TYPES[case["dtype"]]
+
+    def normal(*shape):
+        return torch.randn(*shape, generator=g, device=DEV)
+
+    def uniform(*shape):
+        return torch.rand(*shape, generator=g, device=DEV)
+
+    if case["op"] == "sample":
+        N, V = case["rows"], case["symbols"]
+        s = {"case": case, "logits": (normal(N, V) * 3).to(dt), "u": torch.where(uniform(N) < 1 / 16, -1.0, uniform(N)),
+             "allowed": None, "temperature": case["temperature"], "top_k": case["top_k"], "top_p": case["top_p"],
+             "min_p": case["min_p"]}
+        if N == 1:
+            s["u"] = s["u"].abs() * (1 - 2.0 ** -24)   # a lone row is not left out
+        if case["mask"] == "shared":
+            s["allowed"] = torch.arange(V, device=DEV) > 0
+        elif case["mask"] == "rows":
+            s["allowed"] = uniform(N, V) < uniform(N, 1)
+        if case["each"]:
+            kind = torch.randint(0, 4, (N,), generator=g, device=DEV)
+            s["temperature"] = torch.where(kind == 0, 0.0, 0.5 + uniform(N))
+            s["top_k"] = torch.where(kind == 1, torch.randint(1, 101, (N,), generator=g, device=DEV), case["top_k"]).int()
+            s["top_p"] = torch.where(kind >= 2, 0.8 + 0.2 * uniform(N), case["top_p"]).float()
+            s["min_p"] = torch.where(kind == 3, 0.05 * uniform(N), case["min_p"]).float()
+        return s
+
+    starts, total = _places(case)
+    shapes = _shapes(case)
+    scale = 1024.0 if case["dtype"] == "fp16" else 1.0   # the loss scale that 16 bits of range ask for
+    used = torch.zeros(total, dtype=torch.bool, device=DEV)
+    views = {}
+
+    def split(buffer):
+        return [buffer[a:a + math.prod(shape)].view(shape) for a, shape in zip(starts, shapes)]
+
+    for x in split(used):
+        x.fill_(True)
+    size = 4.0 ** (uniform(1) - 0.25) / math.sqrt(sum(math.prod(x) for x in shapes))   # norms on both sides of the largest
+    grad = (normal(total) * (size * scale) * used).to(dt)
+    s = {"case": case, "grad": grad, "scale": 1.0 / scale, "out": torch.empty_like(grad)}
+    if case["op"] == "adamw":
+        weight = normal(total) * used * 0.05
+        s["param"] = weight.to(dt)
+        s["exp_avg"] = normal(total) * (0.3 * size) * used
+        s["exp_avg_sq"] = (size * size) * (0.2 + uniform(total)) * used
+        s["master"] = weight if case["dtype"] != "fp32" else None
+        s["steps"] = torch.stack([torch.randint(1, 2000, (), generator=g, device=DEV), torch.zeros((), device=DEV).long()]).int()
+    views.update({k: split(x) for k, x in s.items() if k in ("grad", "out", "param", "exp_avg", "exp_avg_sq", "master") and x is not None})
+    s["lists"] = views
+    return s
+
+
+# ---- the operators in plain torch operations, and the framework's calls ----
+
+def _column(x):
+    """A setting of all rows or of each, in 64 bits."""
+    return x.double()[:, None] if torch.is_tensor(x) else x
+
+
+def _plain_sample(s):
+    # 64 bits: symbols are decided next to borders of sums
+    z = s["logits"].double()
+    N, V = z.shape
+    there = z > -math.inf if s["allowed"] is None else (z > -math.inf) & s["allowed"]
+    z, order = torch.where(there, z, -math.inf).sort(dim=1, descending=True, stable=True)
+    full = z[:, :1] > -math.inf
+    T, k, p, least = (_column(s[x]) for x in ("temperature", "top_k", "top_p", "min_p"))
+    T, k, p, least = (torch.as_tensor(x, dtype=torch.float64, device=z.device) for x in (T, k, p, least))
+    greedy = T == 0
+    w = ((z - z[:, :1].clamp(min=-3e38)) / torch.where(greedy, 1.0, T)).exp()
+    k = torch.where(greedy, 1, torch.where(k > 0, k, V))
+    w = torch.where(torch.arange(V, device=z.device) < k, w, 0.0)
+    mass = w.cumsum(1)
+    before = torch.nn.functional.pad(mass[:, :-1], (1, 0))
+    w = torch.where((p >= 1) | (before < p * mass[:, -1:]), w, 0.0)
+    w[:, 1:] = torch.where(w[:, 1:] >= least, w[:, 1:], 0.0)
+    w = torch.zeros_like(w).scatter_(1, order, w)
+    mass = w.cumsum(1)
+    total = mass[:, -1:]
+    u = s["u"].double()[:, None]
+    symbol = (mass <= u * total).sum(1, keepdim=True).clamp(max=V - 1)
+    bits = (total / w.gather(1, symbol)).log2()
+    taken = (u >= 0) & (u < 1) & full
+    return {"symbol": torch.where(taken, symbol, -1)[:, 0].int(), "bits": torch.where(taken, bits, 0.0)[:, 0].float()}
+
+
+def _plain_step(s):
+    case = s["case"]
+    g = s["grad"].float()
+    norm = (g.square().sum(dtype=torch.float64).sqrt() * s["scale"]).float()   # a long sum
+    if case["op"] == "norm":
+        return {"norm": norm}
+    g = g * (s["scale"] * (MOST_NORM / norm).clamp(max=1.0))
+    if case["op"] == "clip":
+        s["out"].copy_(g)
+        return {"norm": norm, "out": s["out"]}
+    s["steps"][0] += 1
+    t = s["steps"][0].double()
+    m, v = s["exp_avg"], s["exp_avg_sq"]
+    w = s["param"] if s["master"] is None else s["master"]
+    m.mul_(BETA1).add_(g * (1 - BETA1))
+    v.mul_(BETA2).add_(g * g * (1 - BETA2))
+    step = m / (1 - BETA1 ** t).float() / ((v / (1 - BETA2 ** t).float()).sqrt() + EPS)
+    w.sub_(LR * (step + DECAY * w))
+    if s["master"] is not None:
+        s["param"].copy_(w)
+    return dict({k: s[k] for k in ("param", "exp_avg", "exp_avg_sq", "master", "steps") if s[k] is not None}, norm=norm)
+
+
+def run(s):
+    case = s["case"]
+    if not own:
+        return _plain_sample(s) if case["op"] == "sample" else _plain_step(s)
+    import paper_2503_12382_amd as reno
+    if case["op"] == "sample":
+        r = reno.sample_symbols(s["logits"], s["u"], temperature=s["temperature"], top_k=s["top_k"], top_p=s["top_p"],
+                                min_p=s["min_p"], allowed=s["allowed"])
+        return {"symbol": r.symbol, "bits": r.bits}
+    x = s["lists"]
+    norm = reno.grad_norm(x["grad"], scale=s["scale"])
+    if case["op"] == "norm":
+        return {"norm": norm}
+    if case["op"] == "clip":
+        reno.clip_grads(x["grad"], norm, MOST_NORM, scale=s["scale"], out=x["out"])
+        return {"norm": norm, "out": s["out"]}
+    reno.adamw_step(x["param"], x["grad"], x["exp_avg"], x["exp_avg_sq"], s["steps"], master=x.get("master"), lr=LR,
+                    betas=(BETA1, BETA2), eps=EPS, weight_decay=DECAY, norm=norm, max_norm=MOST_NORM, scale=s["scale"])
+    return dict({k: s[k] for k in ("param", "exp_avg", "exp_avg_sq", "master", "steps") if s[k] is not None}, norm=norm)
+
+
+def work(case):
+    if case["op"] == "sample":
+        N, V = case["rows"], case["symbols"]
+        mask = {"none": 0, "shared": V, "rows": N * V}[case["mask"]]
+        return {"bytes": SIZES[case["dtype"]] * N * V + mask + (12 + (16 if case["each"] else 0)) * N, "flops": 0}
+    n = sum(math.prod(x) for x in _shapes(case))
+    size = SIZES[case["dtype"]]
+    # adamw: gradient, moments and the weight or its 32-bit copy in, moments, weight and copy out: 28 of either type
+    each = {"norm": size, "clip": 2 * size, "adamw": 28}[case["op"]]
+    return {"bytes": each * n, "flops": 0}
+
+
+# ---- the definitions in float64 ----
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    if case["op"] == "sample":
+        step = max(1, (1 << 25) // case["symbols"])
+        parts = [_exact_rows(s, slice(r, min(case["rows"], r + step))) for r in range(0, case["rows"], step)]
+        return {"symbol": torch.cat([a for a, _ in parts]), "bits": torch.cat([b for _, b in parts])}
+    norm = torch.linalg.vector_norm(s["grad"].double()) * s["scale"]
+    if case["op"] == "norm":
+        return {"norm": norm}
+    factor = s["scale"] * min(1.0, MOST_NORM / float(norm))
+    if case["op"] == "clip":
+        return {"norm": norm, "out": s["grad"].double() * factor}
+    t = int(s["steps"][0]) + 1
+    new = {k: [] for k in ("param", "exp_avg", "exp_avg_sq", "master")}
+    weights = s["param"] if s["master"] is None else s["master"]
+    for g, m, v, w in zip(*(x.split(1 << 24) for x in (s["grad"], s["exp_avg"], s["exp_avg_sq"], weights))):
+        g = g.double() * factor
+        m = BETA1 * m.double() + (1 - BETA1) * g
+        v = BETA2 * v.double() + (1 - BETA2) * g ** 2
+        w = w.double() * (1 - LR * DECAY) - LR * (m / (1 - BETA1 ** t)) / (torch.sqrt(v / (1 - BETA2 ** t)) + EPS)
+        for k, x in zip(new, (w, m, v, w)):
+            new[k].append(x)
+    out = {k: torch.cat(x) for k, x in new.items() if s[k] is not None}
+    return dict(out, norm=norm, steps=torch.stack([s["steps"][0] + 1, s["steps"][1]]))
+
+
+def _exact_rows(s, rows):
+    """Rows' symbols by the value and the number of ties that cut the distribution."""
+    n = s["u"][rows].shape[0]
+
+    def setting(name):
+        x = s[name]
+        return x[rows].double() if torch.is_tensor(x) else torch.full((n,), float(x), dtype=torch.float64, device=DEV)
+
+    z = s["logits"][rows].double()
+    V = z.shape[1]
+    if s["allowed"] is not None:
+        allowed = s["allowed"] if s["allowed"].dim() == 1 else s["allowed"][rows]
+        z = z.masked_fill(~allowed, -math.inf)
+    T, k, p, least, u = setting("temperature"), setting("top_k"), setting("top_p"), setting("min_p"), s["u"][rows].double()
+    live = z.isfinite().sum(1)
+    k = torch.where(T == 0, 1, torch.where(k <= 0, V, k)).minimum(live.clamp(min=1)).long()
+    w = torch.softmax(z.masked_fill((live == 0)[:, None], 0.0) / torch.where(T == 0, 1.0, T)[:, None], 1)
+    w = w / w.amax(1, keepdim=True)
+    down = w.flip(1).sort(dim=1, descending=True)[0]
+    sums = torch.cumsum(down, 1)
+    whole = sums.gather(1, k[:, None] - 1)[:, 0]
+    # as many as it takes to reach the share
+    count = torch.where(p >= 1, k, torch.searchsorted(sums, (p * whole)[:, None])[:, 0] + 1).minimum(k)
+    count = torch.minimum(count, (down >= least[:, None]).sum(1).clamp(min=1))
+    cut = z.sort(dim=1, descending=True)[0].gather(1, count[:, None] - 1)
+    ties = count - (z > cut).sum(1)
+    kept = (z > cut) | ((z == cut) & ((z == cut).cumsum(1) <= ties[:, None]))
+    share = torch.where(kept, w, 0.0)
+    share = share / share.sum(1, keepdim=True)
+    at = torch.cumsum(share, 1)
+    symbol = torch.searchsorted(at, (u.clamp(0, 1)[:, None] * at[:, -1:]), right=True)[:, 0].clamp(max=V - 1)
+    taken = (u >= 0) & (u < 1) & (live > 0)
+    bits = -share.gather(1, symbol[:, None])[:, 0].log2()
+    return torch.where(taken, symbol, -1).int(), torch.where(taken, bits, 0.0)
