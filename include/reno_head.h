@@ -1,7 +1,8 @@
 /*
  * reno_head.h - training operators of the codec's head: the ideal code length
  * of a linear head with its gradient, distillation of a head from a teacher's
- * top logits with its gradient, and the selection of those top logits.
+ * top logits with its gradient, and the selection of those top logits; and
+ * symbols drawn from logits.
  *
  * They stand beside reno_code_length and reno_predict_probs (reno.h), whose
  * head they train: z = w^T h + b (Eq. 10), bits = -log2 softmax(z)[symbol]
@@ -128,6 +129,43 @@ reno_status reno_head_distill(const reno_head* head, const reno_head_data* data,
  * 1 <= k <= RENO_HEAD_MAX_TOP.  Needs no workspace. */
 reno_status reno_top_logits(const void* logits, int type, int64_t rows, int symbols, int64_t row_stride, int k,
                             int32_t* index, float* value, float* lse, void* hip_stream);
+
+/* Rows of logits to draw from, and how. */
+typedef struct {
+  int64_t rows;        /* N, 0 <= N < 2^31 */
+  int symbols;         /* V, 1 .. RENO_HEAD_MAX_SYMBOLS */
+  int type;            /* reno_type of the logits */
+  int64_t row_stride;  /* elements from one row of logits to the next, >= V */
+  double temperature;  /* T: 0 (the largest logit, of equal ones the first), or 2^-126 to 2^126 */
+  double top_p;        /* 0 .. 1; 1: all */
+  double min_p;        /* 0 .. 1; 0: all */
+  int top_k;           /* 0 or more; 0: all */
+  const float* temperature_rows; /* [N] device, each row's own T, or NULL; top_p_rows, min_p_rows and */
+  const float* top_p_rows;       /* top_k_rows the same.  Nothing checks them before the call: a      */
+  const float* min_p_rows;       /* temperature that is negative, infinite or NaN, or a NaN, gives    */
+  const int32_t* top_k_rows;     /* NaN bits, others outside their range count as its end             */
+  const uint8_t* allowed;        /* [V], or [N][V] with rows allowed_stride apart: symbols whose byte is 0
+                                    are not there, their logits (NaN included) count for nothing; NULL: all are */
+  int64_t allowed_stride;        /* 0: one [V] for all rows, else >= V */
+} reno_sample;
+
+/* SYMBOLS DRAWN from rows of logits [N][V] by given random numbers u float [N]
+ * in [0, 1).  A row's symbols are those allowed whose logit is above -inf, in
+ * descending order, ties by ascending index, with weights w = exp((z - max) / T):
+ *   the first top_k of them; of these the shortest run from the first on that
+ *   has top_p of their weight (one at least); of these those with w >= min_p.
+ * With W the weight of what is left: symbol = the lowest index up to which
+ * (inclusive) those that are left weigh more than u W together, and bits =
+ * -log2(w_symbol / W), fp32.  Weights are computed in 64 bits and summed
+ * exactly in units of 2^-51 of the largest for V up to 2048, 2^-42 for 2^20;
+ * a u W below one unit counts as none.  A u outside [0, 1) or NaN leaves its
+ * row out, and one without symbols is: symbol -1, bits 0.  A logit of +inf or
+ * NaN that is allowed, and settings that are none: symbol -1, bits NaN. */
+reno_status reno_sample_symbols(const reno_sample* how, const void* logits, const float* u, int32_t* symbol, float* bits,
+                                void* workspace, int64_t workspace_bytes, void* hip_stream);
+
+/* Bytes of workspace (into *bytes_host) for such a call. */
+reno_status reno_sample_workspace(const reno_sample* how, int64_t* bytes_host);
 
 /* FEATURES of a model scale (b0 < scale < B) that the head is applied to, as
  * the last reno_predict_probs of that scale left them (Sec. 3.2, h of the last

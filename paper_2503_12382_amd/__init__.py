@@ -1,7 +1,9 @@
 """MI355X (gfx950) hot path of the RENO LiDAR geometry codec.
 
-Thin ctypes binding over the C ABI of libreno.so (declared in include/reno.h
-and, for the head's training operators, include/reno_head.h):
+Thin ctypes binding over the C ABI of libreno.so (declared in include/reno.h,
+for the head's training operators and symbols drawn from logits
+include/reno_head.h, and for the step that follows a gradient
+include/reno_step.h):
 argument marshalling only.  Device memory and streams come from PyTorch; every
 step of the codec runs in the library's HIP kernels.  Importing works without
 a GPU; creating a context needs one, and the library must have been built
@@ -9,6 +11,7 @@ a GPU; creating a context needs one, and the library must have been built
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import os
 import typing
@@ -126,6 +129,14 @@ class reno_head_data(ctypes.Structure):
                 ("dh", ctypes.c_void_p), ("dw", ctypes.c_void_p), ("db", ctypes.c_void_p)]
 
 
+class reno_sample(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("symbols", ctypes.c_int), ("type", ctypes.c_int),
+                ("row_stride", ctypes.c_int64), ("temperature", ctypes.c_double), ("top_p", ctypes.c_double),
+                ("min_p", ctypes.c_double), ("top_k", ctypes.c_int), ("temperature_rows", ctypes.c_void_p),
+                ("top_p_rows", ctypes.c_void_p), ("min_p_rows", ctypes.c_void_p), ("top_k_rows", ctypes.c_void_p),
+                ("allowed", ctypes.c_void_p), ("allowed_stride", ctypes.c_int64)]
+
+
 # the same for include/reno_head.h
 _HEAD_SIGS = {
     "reno_head_workspace": (_int, [ctypes.POINTER(reno_head), _int, _int, ctypes.POINTER(_i64)]),
@@ -133,7 +144,37 @@ _HEAD_SIGS = {
     "reno_head_distill": (_int, [ctypes.POINTER(reno_head), ctypes.POINTER(reno_head_data), _vp, _vp, _int,
                                  ctypes.c_float, _vp, _i64, _vp]),
     "reno_top_logits": (_int, [_vp, _int, _i64, _int, _i64, _int, _vp, _vp, _vp, _vp]),
+    "reno_sample_symbols": (_int, [ctypes.POINTER(reno_sample), _vp, _vp, _vp, _vp, _vp, _i64, _vp]),
+    "reno_sample_workspace": (_int, [ctypes.POINTER(reno_sample), ctypes.POINTER(_i64)]),
     "reno_features": (_int, [_vp, _int, _vp]),
+}
+
+RENO_STEP_MAX_TENSORS = 1 << 20
+
+
+class reno_gradient(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int64), ("type", ctypes.c_int64), ("grad", ctypes.c_void_p), ("out", ctypes.c_void_p)]
+
+
+class reno_parameter(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int64), ("type", ctypes.c_int64), ("grad_type", ctypes.c_int64),
+                ("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("master", ctypes.c_void_p),
+                ("exp_avg", ctypes.c_void_p), ("exp_avg_sq", ctypes.c_void_p)]
+
+
+class reno_adamw(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
+                ("eps", ctypes.c_double), ("weight_decay", ctypes.c_double), ("scale", ctypes.c_double),
+                ("max_norm", ctypes.c_double), ("lr_factor", ctypes.c_void_p), ("norm", ctypes.c_void_p),
+                ("steps", ctypes.c_void_p)]
+
+
+# and for include/reno_step.h (lists: arrays of reno_gradient or reno_parameter)
+_STEP_SIGS = {
+    "reno_grad_workspace": (_int, [_vp, _i64, ctypes.POINTER(_i64)]),
+    "reno_grad_norm": (_int, [_vp, _i64, ctypes.c_double, _vp, _vp, _i64, _vp]),
+    "reno_grad_clip": (_int, [_vp, _i64, _vp, ctypes.c_double, ctypes.c_double, _vp]),
+    "reno_adamw_step": (_int, [_vp, _i64, ctypes.POINTER(reno_adamw), _vp]),
 }
 
 KERNELS = ["zero", "quantize", "sort", "pyramid", "codes", "set_base", "expand", "conv_first",
@@ -154,7 +195,7 @@ def lib():
             raise RuntimeError(f"{LIB_PATH} is missing: build it with "
                                "`python -m paper_2503_12382_amd.build` (no CPU fallback exists)")
         L = ctypes.CDLL(LIB_PATH)
-        for name, (res, args) in {**_SIGS, **_HEAD_SIGS}.items():
+        for name, (res, args) in {**_SIGS, **_HEAD_SIGS, **_STEP_SIGS}.items():
             f = getattr(L, name)
             f.restype = res
             f.argtypes = args
@@ -696,6 +737,215 @@ def top_logits(logits, k: int, stream=None) -> TopLogits:
         _read_on(stream, x)
         return TopLogits(index, value, lse)
     return _on(dev, stream, run)
+
+
+class Samples(typing.NamedTuple):
+    symbol: object        # int32 [N], -1: none
+    bits: object          # float32 [N], -log2 of the symbol's probability
+
+
+def sample_symbols(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, allowed=None, workspace=None,
+                   stream=None) -> Samples:
+    """A symbol of each row of logits [N][V] (float32, bfloat16 or float16, rows
+    may be strided), drawn by the row's random number u float32 [N] in [0, 1)
+    (reno_sample_symbols): from the distribution at the temperature (0: the
+    largest logit), cut to the top_k largest logits (0: all), of those to the
+    shortest run of mass top_p from the largest on, and to those of at least
+    min_p of the largest's probability.  Each setting is a number, or a tensor
+    [N] on the device (float32, top_k int32) with every row's own.  allowed:
+    bool [V] or [N][V], the symbols that may be drawn; logits of -inf are not.
+    Rows whose u lies outside [0, 1) (-1, say) are left out, and rows without
+    any symbol have none: symbol -1 and 0 bits.  Allowed logits of +inf or NaN
+    give symbol -1 and NaN bits.
+
+    The same u gives the same symbol every time, whatever the other rows are:
+    masses are exact sums (include/reno_head.h).  workspace: a uint8 tensor of
+    sample_workspace bytes, or None to take it from torch's allocator."""
+    import torch
+    _need(logits.dim() == 2 and logits.is_cuda, "logits must be a device tensor [N][V]")
+    kind = _type_of(logits.dtype)
+    _need(kind is not None, "logits must be float32, bfloat16 or float16")
+    dev = logits.device
+    n, v = logits.shape
+
+    def run(st):
+        x = _rows(logits, "logits", logits.dtype, dev, (n, v))
+        uu = _rows(u, "u", torch.float32, dev, (n,))
+        p = reno_sample(n, v, kind, _stride(x), 1.0, 1.0, 0.0, 0)
+        keep = [x, uu]
+        for name, value, dt in (("temperature", temperature, torch.float32), ("top_p", top_p, torch.float32),
+                                ("min_p", min_p, torch.float32), ("top_k", top_k, torch.int32)):
+            if torch.is_tensor(value):
+                t = _rows(value, name, dt, dev, (n,))
+                keep.append(t)
+                setattr(p, name + "_rows", t.data_ptr())
+            elif dt is torch.int32:
+                k = int(value)
+                _need(k == value and 0 <= k < 1 << 31, "top_k must be a whole number in [0, 2^31)")
+                p.top_k = k
+            else:
+                setattr(p, name, float(value))
+        if allowed is not None:
+            _need(allowed.dim() in (1, 2), "allowed must be [V] or [N][V]")
+            t = _rows(allowed, "allowed", torch.bool, dev, (v,) if allowed.dim() == 1 else (n, v))
+            keep.append(t)
+            p.allowed = t.data_ptr()
+            p.allowed_stride = 0 if t.dim() == 1 else _stride(t)
+        need = ctypes.c_int64()
+        _head_check(lib().reno_sample_workspace(ctypes.byref(p), ctypes.byref(need)))
+        ws = workspace
+        if ws is None and need.value:
+            ws = torch.empty(need.value, dtype=torch.uint8, device=dev)
+        if ws is not None:
+            _need(ws.device == dev and ws.is_contiguous(), "workspace must be contiguous and on the device of the arguments")
+            keep.append(ws)
+        symbol = torch.empty(n, dtype=torch.int32, device=dev)
+        bits = torch.empty(n, dtype=torch.float32, device=dev)
+        _head_check(lib().reno_sample_symbols(ctypes.byref(p), x.data_ptr(), uu.data_ptr(), symbol.data_ptr(),
+                                              bits.data_ptr(), 0 if ws is None else ws.data_ptr(),
+                                              0 if ws is None else ws.numel() * ws.element_size(), st.cuda_stream))
+        _read_on(stream, *keep)
+        return Samples(symbol, bits)
+    return _on(dev, stream, run)
+
+
+def sample_workspace(rows: int, symbols: int, dtype) -> int:
+    """Bytes of workspace for such a call (reno_sample_workspace)."""
+    kind = _type_of(dtype)
+    _need(kind is not None, "dtype must be float32, bfloat16 or float16")
+    p = reno_sample(rows, symbols, kind, symbols, 1.0, 1.0, 0.0, 0)
+    n = ctypes.c_int64()
+    _head_check(lib().reno_sample_workspace(ctypes.byref(p), ctypes.byref(n)))
+    return n.value
+
+
+def _list_of(tensors, name, like=None, dtype=None):
+    """The tensors of a list as they are, checked: dense, on one device, of a known type (of `dtype`), and of the
+    shapes of `like`."""
+    _need(like is None or len(tensors) == len(like), f"{name} must have as many tensors as the list")
+    dev = (tensors if like is None else like)[0].device if len(tensors) else None
+    for i, t in enumerate(tensors):
+        if not t.is_cuda or t.device != dev or not t.is_contiguous():
+            raise ValueError(f"{name} must be dense tensors on one device")
+        if (t.dtype is not dtype) if dtype is not None else (t.dtype not in _TYPES):
+            raise ValueError(f"{name} must be " + (str(dtype) if dtype is not None else "float32, bfloat16 or float16"))
+        if like is not None and t.shape != like[i].shape:
+            raise ValueError(f"{name} must have the shapes of the list")
+    return tensors
+
+
+def _scalar_on(t, name, dtype, dev, n=1):
+    """The address of a scalar (n words) on the device, or None."""
+    if t is None:
+        return None
+    _need(t.device == dev and t.dtype == dtype and t.numel() == n and t.is_contiguous(),
+          f"{name} must be {n} {dtype} on {dev}")
+    return t.data_ptr()
+
+
+def _dense(grads):
+    return [g if g.is_contiguous() else g.contiguous() for g in grads]
+
+
+def grad_norm(grads, scale: float = 1.0, workspace=None, stream=None):
+    """scale times the 2-norm over all the tensors (float32, bfloat16 or float16,
+    mixed; reno_grad_norm), as a float32 scalar on their device.  scale: one over
+    a loss scale.  Sums are carried in 64 bits.  workspace: a uint8 tensor that
+    is large enough (reno_grad_workspace), or None to take it from torch's
+    allocator."""
+    import torch
+    grads = list(grads)
+    _need(len(grads) and grads[0].is_cuda, "grads must be device tensors, one at least")
+    dev = grads[0].device
+
+    def run(st):
+        _type_of(None)
+        g = _list_of(_dense(grads), "grads")
+        words = []
+        for t in g:
+            words += (t.numel(), _TYPES[t.dtype], t.data_ptr(), 0)
+        arr = array.array("q", words)
+        at, count = arr.buffer_info()[0], len(g)
+        need = ctypes.c_int64()
+        L = lib()
+        _head_check(L.reno_grad_workspace(at, count, ctypes.byref(need)))
+        ws = workspace
+        if ws is None:
+            ws = torch.empty(need.value, dtype=torch.uint8, device=dev)
+        _need(ws.device == dev and ws.is_contiguous(), "workspace must be contiguous and on the device of the arguments")
+        norm = torch.empty((), dtype=torch.float32, device=dev)
+        _head_check(L.reno_grad_norm(at, count, float(scale), norm.data_ptr(), ws.data_ptr(),
+                                     ws.numel() * ws.element_size(), st.cuda_stream))
+        _read_on(stream, ws, *g)
+        return norm
+    return _on(dev, stream, run)
+
+
+def clip_grads(grads, norm, max_norm: float, scale: float = 1.0, out=None, stream=None):
+    """The gradients times scale min(1, max_norm / norm) (reno_grad_clip), written
+    to the tensors of ``out`` (default: in place; then they must be dense), which
+    is returned.  norm: grad_norm of the same gradients with the same scale."""
+    import torch
+    grads = list(grads)
+    _need(len(grads) and grads[0].is_cuda, "grads must be device tensors, one at least")
+    dev = grads[0].device
+
+    def run(st):
+        _type_of(None)
+        g = _list_of(grads if out is None else _dense(grads), "grads")
+        o = g if out is None else _list_of(list(out), "out", g)
+        words = []
+        for a, b in zip(g, o):
+            _need(a.dtype is b.dtype, "out must have the gradients' types")
+            words += (a.numel(), _TYPES[a.dtype], a.data_ptr(), b.data_ptr())
+        arr = array.array("q", words)
+        at = _scalar_on(norm, "norm", torch.float32, dev)
+        _head_check(lib().reno_grad_clip(arr.buffer_info()[0], len(g), at, float(scale), float(max_norm), st.cuda_stream))
+        _read_on(stream, norm, *g, *(o if out is not None else ()))
+        return o
+    return _on(dev, stream, run)
+
+
+def adamw_step(params, grads, exp_avg, exp_avg_sq, steps, master=None, lr: float = 1e-3, betas=(0.9, 0.999),
+               eps: float = 1e-8, weight_decay: float = 0.01, norm=None, max_norm: float = float("inf"),
+               scale: float = 1.0, lr_factor=None, stream=None) -> None:
+    """One AdamW step in place (reno_adamw_step): lists of weights (float32,
+    bfloat16 or float16, mixed), their gradients (of the weight's type or
+    float32), and their float32 moments.  steps: int32 [2] on the device, zeros
+    before the first step: the steps made so far, which the call counts up, and a
+    word of its own.  master: None, or a list with the float32 copies of weights
+    of 16 bits, and None for those without.  With ``norm`` (grad_norm with the
+    same scale) gradients count scaled down to max_norm, and a norm that is not
+    finite leaves everything as it is.  lr_factor: a float32 scalar on the device
+    that multiplies lr, or None.  Weights may require gradients; nothing is
+    recorded for autograd."""
+    import torch
+    params = list(params)
+    _need(len(params) and params[0].is_cuda, "params must be device tensors, one at least")
+    dev = params[0].device
+
+    def run(st):
+        _type_of(None)
+        p = _list_of(params, "params")
+        g = _list_of(_dense(grads), "grads", p)
+        m = _list_of(list(exp_avg), "exp_avg", p, torch.float32)
+        v = _list_of(list(exp_avg_sq), "exp_avg_sq", p, torch.float32)
+        w = [None] * len(p) if master is None else list(master)
+        _need(len(w) == len(p), "master must have as many tensors as the list")
+        if master is not None:
+            pairs = [(x, y) for x, y in zip(w, p) if x is not None]
+            _list_of([x for x, _ in pairs], "master", [y for _, y in pairs], torch.float32)
+        words = []
+        for i, t in enumerate(p):
+            words += (t.numel(), _TYPES[t.dtype], _TYPES[g[i].dtype], t.data_ptr(), g[i].data_ptr(),
+                      0 if w[i] is None else w[i].data_ptr(), m[i].data_ptr(), v[i].data_ptr())
+        arr = array.array("q", words)
+        how = reno_adamw(float(lr), float(betas[0]), float(betas[1]), float(eps), float(weight_decay), float(scale),
+                         float(max_norm), _scalar_on(lr_factor, "lr_factor", torch.float32, dev),
+                         _scalar_on(norm, "norm", torch.float32, dev), _scalar_on(steps, "steps", torch.int32, dev, 2))
+        _head_check(lib().reno_adamw_step(arr.buffer_info()[0], len(p), ctypes.byref(how), st.cuda_stream))
+        _read_on(stream, steps, norm, lr_factor, *p, *g, *m, *v, *w)
+    _on(dev, stream, run)
 
 
 def rans_encode(sym: np.ndarray, freq: np.ndarray) -> np.ndarray:

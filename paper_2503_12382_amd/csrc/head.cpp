@@ -54,6 +54,25 @@ reno_status run(reno::HeadCall& c, const reno_head* p, const reno_head_data* d, 
   return RENO_OK;
 }
 
+reno_status check_sample(const reno_sample* p) {
+  if (!p) return fail_thread(RENO_E_INVALID, "null argument");
+  if (p->rows < 0 || p->rows >= (int64_t(1) << 31)) return fail_thread(RENO_E_INVALID, "rows must be in [0, 2^31)");
+  if (p->symbols < 1 || p->symbols > RENO_HEAD_MAX_SYMBOLS)
+    return fail_thread(RENO_E_INVALID, "symbols must be in [1, RENO_HEAD_MAX_SYMBOLS]");
+  if (p->type != RENO_T_FP32 && p->type != RENO_T_BF16 && p->type != RENO_T_FP16)
+    return fail_thread(RENO_E_INVALID, "type must be a reno_type");
+  if (p->row_stride < p->symbols || p->row_stride >= (int64_t(1) << 31))
+    return fail_thread(RENO_E_INVALID, "row_stride must be in [symbols, 2^31)");
+  if (!(p->temperature == 0.0 || (p->temperature >= 0x1p-126 && p->temperature <= 0x1p126)))
+    return fail_thread(RENO_E_INVALID, "temperature must be 0 or in [2^-126, 2^126]");
+  if (!(p->top_p >= 0.0 && p->top_p <= 1.0)) return fail_thread(RENO_E_INVALID, "top_p must be in [0, 1]");
+  if (!(p->min_p >= 0.0 && p->min_p <= 1.0)) return fail_thread(RENO_E_INVALID, "min_p must be in [0, 1]");
+  if (p->top_k < 0) return fail_thread(RENO_E_INVALID, "top_k must be 0 or more");
+  if (p->allowed && p->allowed_stride != 0 && (p->allowed_stride < p->symbols || p->allowed_stride >= (int64_t(1) << 31)))
+    return fail_thread(RENO_E_INVALID, "allowed_stride must be 0 or in [symbols, 2^31)");
+  return RENO_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -108,6 +127,30 @@ reno_status reno_top_logits(const void* logits, int type, int64_t rows, int symb
     return fail_thread(RENO_E_INVALID, "an operand is not aligned to its type");
   const hipError_t e = reno::launch_top(logits, type, rows, symbols, row_stride, k, index, value, lse,
                                         static_cast<hipStream_t>(hip_stream));
+  if (e != hipSuccess) return fail_thread(RENO_E_HIP, hipGetErrorString(e));
+  return RENO_OK;
+}
+
+reno_status reno_sample_workspace(const reno_sample* how, int64_t* bytes_host) {
+  const reno_status s = check_sample(how);
+  if (s != RENO_OK) return s;
+  if (!bytes_host) return fail_thread(RENO_E_INVALID, "null argument");
+  *bytes_host = 0;
+  return RENO_OK;
+}
+
+reno_status reno_sample_symbols(const reno_sample* how, const void* logits, const float* u, int32_t* symbol, float* bits,
+                                void* ws, int64_t bytes, void* hip_stream) {
+  const reno_status s = check_sample(how);
+  if (s != RENO_OK) return s;
+  if (how->rows == 0) return RENO_OK;
+  if (!logits || !u || !symbol || !bits) return fail_thread(RENO_E_INVALID, "null argument");
+  const void* words[] = {u, symbol, bits, how->temperature_rows, how->top_p_rows, how->min_p_rows, how->top_k_rows};
+  for (const void* q : words)
+    if ((uintptr_t)q % 4) return fail_thread(RENO_E_INVALID, "an operand is not aligned to its type");
+  if ((uintptr_t)logits % (how->type == RENO_T_FP32 ? 4 : 2))
+    return fail_thread(RENO_E_INVALID, "an operand is not aligned to its type");
+  const hipError_t e = reno::launch_sample(*how, logits, u, symbol, bits, static_cast<hipStream_t>(hip_stream));
   if (e != hipSuccess) return fail_thread(RENO_E_HIP, hipGetErrorString(e));
   return RENO_OK;
 }

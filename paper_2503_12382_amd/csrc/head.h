@@ -1,5 +1,5 @@
 // The head's training operators: what the C entry points (head.cpp) hand to
-// the kernels' launchers (k_head.hip, k_top.hip).
+// the kernels' launchers (k_head.hip, k_top.hip, k_sample.hip).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -45,5 +45,7 @@ int64_t head_workspace(const reno_head& p, int k, bool grad);
 hipError_t launch_head(const HeadCall& c, hipStream_t stream);
 hipError_t launch_top(const void* logits, int type, int64_t rows, int symbols, int64_t stride, int k, int32_t* index,
                       float* value, float* lse, hipStream_t stream);
+hipError_t launch_sample(const reno_sample& p, const void* logits, const float* u, int32_t* symbol, float* bits,
+                         hipStream_t stream);
 
 }  // namespace reno

@@ -1,0 +1,545 @@
+// Symbols drawn from rows of logits (reno_head.h).
+//
+// Decisions next to borders have to be those of exact sums, so masses are
+// integers: a symbol's weight 2^y, y = (z - max) log2(e) / T, is computed in 64
+// bits to 2^-48 and counted in units of 2^-S of the largest, 2^S V < 2^63.  Sums
+// of them are exact in any order, LDS atomics among it.
+//
+// What is kept is a prefix of the row in descending order, ties by index, so it
+// is given by a cut: the ordered value of the last logit kept, and the index up
+// to which logits equal to it are.  The cut of a count or of a mass is found
+// without sorting: a histogram over the row, the bin that holds the cut, a
+// histogram over that bin's range of values, until a bin is one value.
+//
+//   k_sample_long  a block a row, held in LDS where it fits
+
+#include <algorithm>
+#include <cmath>
+
+#include "dev.h"
+#include "head.h"
+#include "head_dev.h"
+#include "logits.h"
+
+namespace reno {
+namespace {
+
+constexpr uint32_t FIRST_LIVE = 0x00800000u;   // ordered(-inf) + 1
+constexpr uint32_t ALL = 0xffffffffu;
+
+// 2^y in units of 2^-S, to the nearest; y <= 0, S <= 51.
+__device__ __forceinline__ uint64_t units(double y, int S) {
+  y = fmax(y, -1000.0);
+  constexpr double ROUND = 0x1.8p52;
+  const double t = y + ROUND;
+  const double f = y - (t - ROUND);
+  // (2^f - 1) / f on [-1/2, 1/2], interpolated at the zeros of a Chebyshev polynomial; 1 + f q is right to 2^-50
+  double q = 0x1.e5e9ef7b8cd7ap-28;
+  q = __builtin_fma(q, f, 0x1.b6571e5ac5dabp-24);
+  q = __builtin_fma(q, f, 0x1.62bfe465e6f1bp-20);
+  q = __builtin_fma(q, f, 0x1.ffcb7678282dfp-17);
+  q = __builtin_fma(q, f, 0x1.4309130375a29p-13);
+  q = __builtin_fma(q, f, 0x1.5d87fe908fa7dp-10);
+  q = __builtin_fma(q, f, 0x1.3b2ab6fba3871p-7);
+  q = __builtin_fma(q, f, 0x1.c6b08d7044119p-5);
+  q = __builtin_fma(q, f, 0x1.ebfbdff82c590p-3);
+  q = __builtin_fma(q, f, 0x1.62e42fefa39f7p-1);
+  q = __builtin_fma(q, f, 1.0);
+  const int n = (int)(uint32_t)__builtin_bit_cast(uint64_t, t) + S;
+  const double p = __builtin_bit_cast(double, (uint64_t)(uint32_t)(1023 + n) << 52);
+  // rounded to a whole number by the sum with 2^52, whose fraction it then is
+  return __builtin_bit_cast(uint64_t, __builtin_fma(q, p, 0x1p52)) & 0xfffffffffffffull;
+}
+
+// The units of a row of V: the sum of V of them stays below 2^63.
+int unit_bits(int V) {
+  int lg = 0;
+  while ((int64_t(1) << lg) < V) ++lg;
+  return std::min(51, 62 - lg);
+}
+
+// ceil(p m), 1 at least, for p < 1, and floor(u m) for 0 <= u < 1, the products as 64-bit floats: so that a share of
+// equal weights is what it says (0.9 of 3000 is 2700, though the float next to 0.9 lies above it).
+__device__ __forceinline__ uint64_t share_up(double p, uint64_t m) {
+  return max(min((uint64_t)__builtin_ceil(fmax(p, 0.0) * (double)m), m), (uint64_t)1);
+}
+__device__ __forceinline__ uint64_t share_down(float u, uint64_t m) { return (uint64_t)((double)u * (double)m); }
+
+// A row's settings.
+struct Row {
+  double T, p, least;
+  int64_t k;        // 0: all
+  float u;
+  bool valid;
+};
+
+struct SampleArgs {
+  const void* z;
+  int64_t stride;
+  int V, S;
+  double T, p, least;
+  int k;
+  const float *T_rows, *p_rows, *least_rows;
+  const int32_t* k_rows;
+  const uint8_t* allowed;
+  int64_t allowed_stride;
+  const float* u;
+  int32_t* symbol;
+  float* bits;
+};
+
+__device__ __forceinline__ Row settings(const SampleArgs& a, int64_t r) {
+  Row s;
+  s.u = a.u[r];
+  s.T = a.T_rows ? (double)a.T_rows[r] : a.T;
+  s.p = a.p_rows ? (double)a.p_rows[r] : a.p;
+  s.least = a.least_rows ? (double)a.least_rows[r] : a.least;
+  s.k = max(a.k_rows ? a.k_rows[r] : a.k, 0);
+  s.valid = s.T >= 0.0 && s.T < (double)INFINITY && s.p == s.p && s.least == s.least;
+  s.least = fmin(s.least, 1.0);
+  if (s.T == 0.0) {   // the largest alone
+    s.k = 1;
+    s.p = 1.0;
+    s.least = 0.0;
+  }
+  return s;
+}
+
+constexpr double LOG2E_D = 1.4426950408889634;
+
+// The ordered value from which on logits have a weight of `least` of the largest, m.
+__device__ __forceinline__ uint32_t least_key(double least, float m, double T) {
+  if (!(least > 0.0)) return FIRST_LIVE;
+  const double z = (double)m + T * log(least);
+  float f = (float)z;
+  if ((double)f < z) f = nextafterf(f, INFINITY);
+  return max(ordered(f), FIRST_LIVE);
+}
+
+// ---------------------------------------------------------------------------
+// A block a row.
+
+constexpr int BINS = 1024;
+
+__device__ __forceinline__ uint64_t wave_sum(uint64_t v) {
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+  return v;
+}
+__device__ __forceinline__ uint64_t wave_scan(uint64_t v) {   // inclusive
+  for (int o = 1; o < 64; o <<= 1) {
+    const uint64_t w = __shfl_up(v, o);
+    if (lane_id() >= o) v += w;
+  }
+  return v;
+}
+
+// THREADS a row; KEEP: the row is held in LDS (else read again each time).  A wave's pieces of 16 bytes follow one
+// another: the row's order is by wave, then by turn, then by lane.  A thread reads only what it wrote itself.
+template <int TYPE, int THREADS, bool KEEP>
+struct Long {
+  static constexpr int N = Vec<TYPE>::N, WAVES = THREADS / 64, SIZE = 16 / N;
+  static constexpr uint32_t DEAD = TYPE == RENO_T_FP32 ? 0xff800000u : TYPE == RENO_T_BF16 ? 0xff80ff80u : 0xfc00fc00u;
+  const char* z;
+  const uint8_t* allowed;
+  uint4* kept;
+  int V, turns, first;      // first: this thread's first piece
+
+  __device__ __forceinline__ uint4 read(int piece) const {
+    uint32_t w[4] = {DEAD, DEAD, DEAD, DEAD};
+    const int v = piece * N;
+    if (v + N <= V) {
+      __builtin_memcpy(w, z + (int64_t)v * SIZE, 16);   // one load, wherever the row starts
+      if (allowed) {
+        uint8_t a[N];
+        __builtin_memcpy(a, allowed + v, N);
+#pragma unroll
+        for (int e = 0; e < N; ++e) put(w, e, a[e] != 0);
+      }
+    } else if (v < V) {
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        if (v + e < V) {
+          if constexpr (N == 4) w[e] = reinterpret_cast<const uint32_t*>(z)[v + e];
+          else w[e / 2] = (w[e / 2] & (e & 1 ? 0xffffu : 0xffff0000u)) |
+                          (uint32_t)reinterpret_cast<const uint16_t*>(z)[v + e] << (16 * (e & 1));
+          if (allowed) put(w, e, allowed[v + e] != 0);
+        }
+      }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  __device__ static __forceinline__ void put(uint32_t (&w)[4], int e, bool there) {
+    if constexpr (N == 4) w[e] = there ? w[e] : DEAD;
+    else {
+      const uint32_t mask = e & 1 ? 0xffff0000u : 0xffffu;
+      w[e / 2] = there ? w[e / 2] : (w[e / 2] & ~mask) | (DEAD & mask);
+    }
+  }
+  __device__ __forceinline__ int index(int turn, int e) const { return (first + turn * 64) * N + e; }
+  // f(turn, logits) for every turn of the thread
+  template <typename F>
+  __device__ __forceinline__ void each(const F& f) const {
+    for (int t = 0; t < turns; ++t) {
+      Vec<TYPE> x;
+      if constexpr (KEEP) x.from(kept[t * THREADS + threadIdx.x]);
+      else x.from(read(first + t * 64));
+      f(t, x.x);
+    }
+  }
+};
+
+// Shared memory of a row.
+template <int WAVES>
+struct Shared {
+  uint64_t hist[BINS];
+  uint64_t part[WAVES];
+  float top[WAVES], low[WAVES];
+  uint32_t lo, hi;
+  uint64_t total, above, at;
+  int bin, live[WAVES], index;
+};
+
+template <int THREADS>
+__device__ __forceinline__ void clear(uint64_t* hist) {
+  for (int i = threadIdx.x; i < BINS; i += THREADS) hist[i] = 0;
+}
+
+// Wave 0: the first bin at whose end `want` of what `above` and the bins hold is reached.  want(total) is asked
+// with what all bins hold; false: more than there is, nothing is set but s.total.
+template <int WAVES, typename F>
+__device__ __forceinline__ void find_bin(Shared<WAVES>& s, uint64_t above, const F& want) {
+  if (threadIdx.x < 64) {
+    constexpr int PER = BINS / 64;
+    const int lane = lane_id();
+    uint64_t mine = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) mine += s.hist[lane * PER + i];
+    const uint64_t upto = wave_scan(mine);
+    const uint64_t total = __shfl(upto, 63);
+    const uint64_t w = want(total);
+    uint64_t a = above + upto - mine;
+    if (lane == 0) {
+      s.total = total;
+      if (w > above + total) s.bin = -1;
+    }
+    if (a < w && a + mine >= w) {
+      int i = lane * PER;
+      while (a + s.hist[i] < w) a += s.hist[i++];
+      s.bin = i;
+      s.above = a;
+      s.at = s.hist[i];
+    }
+  }
+}
+
+// The largest ordered value, from `lo` up, that leaves `want` of the measure (logits, or with MASS their weights) at
+// it and above.  False: all of them are less.  above: what lies above it.
+template <bool MASS, typename L, typename S, typename F>
+__device__ __forceinline__ bool search(const L& row, S& s, uint32_t lo, float m, float low, double c, int bits, const F& want,
+                       uint32_t* cut, uint64_t* above, uint64_t* total) {
+  constexpr int N = L::N, THREADS = L::WAVES * 64;
+  // first histogram: by value, over 40 octaves of weight at most
+  const float range = fminf(m - low, (float)fmin(40.0 / c, 3e38));
+  const float scale = range > 0.0f ? fminf((float)BINS / range, 3e38f) : 0.0f;
+  const auto bin_of = [&](float x) { return (int)fminf((m - x) * scale, (float)(BINS - 1)); };
+  const auto measure = [&](float x) -> uint64_t { return MASS ? units(((double)x - (double)m) * c, bits) : 1ull; };
+  clear<THREADS>(s.hist);
+  __syncthreads();
+  row.each([&](int, const float (&x)[N]) {
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      if (ordered(x[e]) >= lo) atomicAdd((unsigned long long*)&s.hist[bin_of(x[e])], (unsigned long long)measure(x[e]));
+  });
+  __syncthreads();
+  uint64_t wanted = 0;
+  find_bin(s, 0, [&](uint64_t t) { return wanted = want(t); });
+  if (threadIdx.x == 0) {
+    s.lo = ALL;
+    s.hi = 0;
+  }
+  __syncthreads();
+  *total = s.total;
+  if (s.bin < 0) return false;
+  const int bin = s.bin;
+  uint64_t a = s.above;
+  if (threadIdx.x == 0) s.part[0] = wanted;
+  // the bin's own range of ordered values
+  uint32_t kmin = ALL, kmax = 0;
+  row.each([&](int, const float (&x)[N]) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const uint32_t o = ordered(x[e]);
+      const bool in = o >= lo && bin_of(x[e]) == bin;
+      kmin = in ? min(kmin, o) : kmin;
+      kmax = in ? max(kmax, o) : kmax;
+    }
+  });
+  if (kmax) {
+    atomicMin(&s.lo, kmin);
+    atomicMax(&s.hi, kmax);
+  }
+  __syncthreads();
+  uint32_t from = s.lo, to = s.hi;
+  wanted = s.part[0];
+  // histograms of ordered values, each over one bin of the last
+  while (from != to) {
+    const int width = 32 - __builtin_clz(to - from);   // to - from < 2^width
+    const int shift = max(0, width - 10);
+    __syncthreads();
+    clear<THREADS>(s.hist);
+    __syncthreads();
+    row.each([&](int, const float (&x)[N]) {
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const uint32_t o = ordered(x[e]);
+        if (o >= from && o <= to) atomicAdd((unsigned long long*)&s.hist[(to - o) >> shift], (unsigned long long)measure(x[e]));
+      }
+    });
+    __syncthreads();
+    find_bin(s, a, [&](uint64_t) { return wanted; });
+    __syncthreads();
+    a = s.above;
+    const uint32_t b = (uint32_t)s.bin;
+    const uint32_t top = to - (b << shift);
+    from = max(from, top - ((1u << shift) - 1u));
+    to = top;
+  }
+  __syncthreads();
+  *cut = to;
+  *above = a;
+  return true;
+}
+
+// The index of the logit at which the sum of value(index, logit) along the row reaches want (at least 1), and that
+// logit.  total: the sum of all, by which want is asked for.
+template <typename L, typename S, typename V, typename W>
+__device__ __forceinline__ void locate(const L& row, S& s, const V& value, const W& want, int* index, float* logit, uint64_t* total) {
+  constexpr int N = L::N, WAVES = L::WAVES;
+  const int lane = lane_id(), wave = threadIdx.x >> 6;
+  uint64_t mine = 0;
+  row.each([&](int t, const float (&x)[N]) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) mine += value(row.index(t, e), x[e]);
+  });
+  mine = wave_sum(mine);
+  __syncthreads();
+  if (lane == 0) s.part[wave] = mine;
+  __syncthreads();
+  uint64_t all = 0;
+  for (int i = 0; i < WAVES; ++i) all += s.part[i];
+  *total = all;
+  const uint64_t w = want(all);
+  uint64_t before = 0;
+  int at = 0;
+  while (at < WAVES - 1 && before + s.part[at] < w) before += s.part[at++];
+  if (wave == at) {
+    bool found = false;
+    row.each([&](int t, const float (&x)[N]) {
+      if (found) return;
+      uint64_t part = 0;
+#pragma unroll
+      for (int e = 0; e < N; ++e) part += value(row.index(t, e), x[e]);
+      const uint64_t upto = wave_scan(part);
+      const uint64_t turn = __shfl(upto, 63);
+      if (before + turn >= w) {
+        found = true;
+        uint64_t a = before + upto - part;
+        if (a < w && a + part >= w) {
+          bool here = false;
+#pragma unroll
+          for (int e = 0; e < N; ++e) {
+            a += value(row.index(t, e), x[e]);
+            if (!here && a >= w) {
+              here = true;
+              s.index = row.index(t, e);
+              s.top[0] = x[e];
+            }
+          }
+        }
+      }
+      before += turn;
+    });
+  }
+  __syncthreads();
+  *index = s.index;
+  *logit = s.top[0];
+}
+
+template <int TYPE, int THREADS, bool KEEP>
+__global__ void __launch_bounds__(THREADS) k_sample_long(SampleArgs a) {
+  typedef Long<TYPE, THREADS, KEEP> L;
+  constexpr int N = L::N, WAVES = L::WAVES;
+  __shared__ Shared<WAVES> s;
+  const int64_t r = blockIdx.x;
+  const int tid = threadIdx.x, lane = lane_id(), wave = tid >> 6;
+  const Row set = settings(a, r);
+  if (!(set.u >= 0.0f && set.u < 1.0f) || !set.valid) {
+    if (tid == 0) {
+      a.symbol[r] = -1;
+      a.bits[r] = set.u >= 0.0f && set.u < 1.0f ? NAN : 0.0f;
+    }
+    return;
+  }
+  L row;
+  row.z = static_cast<const char*>(a.z) + r * a.stride * L::SIZE;
+  row.allowed = a.allowed ? a.allowed + r * a.allowed_stride : nullptr;
+  row.V = a.V;
+  row.turns = (a.V + N * THREADS - 1) / (N * THREADS);
+  row.first = wave * row.turns * 64 + lane;
+  extern __shared__ uint4 s_row[];
+  row.kept = s_row;
+  if constexpr (KEEP) {
+    for (int t = 0; t < row.turns; ++t) s_row[t * THREADS + tid] = row.read(row.first + t * 64);
+  }
+  // the largest and the smallest logit, how many there are
+  float m = -INFINITY, low = INFINITY;
+  int live = 0;
+  bool bad = false;
+  row.each([&](int, const float (&x)[N]) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const bool there = x[e] > -INFINITY;
+      bad |= !(x[e] < INFINITY);
+      m = fmaxf(m, x[e]);
+      low = there ? fminf(low, x[e]) : low;
+      live += there ? 1 : 0;
+    }
+  });
+  for (int o = 32; o > 0; o >>= 1) {
+    m = fmaxf(m, __shfl_xor(m, o));
+    low = fminf(low, __shfl_xor(low, o));
+    live += __shfl_xor(live, o);
+  }
+  const bool any_bad = __ballot(bad) != 0;
+  if (lane == 0) {
+    s.top[wave] = m;
+    s.low[wave] = low;
+    s.live[wave] = any_bad ? -1 : live;
+  }
+  __syncthreads();
+  live = 0;
+  bad = false;
+  for (int i = 0; i < WAVES; ++i) {
+    m = fmaxf(m, s.top[i]);
+    low = fminf(low, s.low[i]);
+    bad |= s.live[i] < 0;
+    live += s.live[i];
+  }
+  if (bad || live == 0) {
+    if (tid == 0) {
+      a.symbol[r] = -1;
+      a.bits[r] = bad ? NAN : 0.0f;
+    }
+    return;
+  }
+  const double c = set.T > 0.0 ? LOG2E_D / set.T : 0.0;
+  const auto weight = [&](float x) { return units(((double)x - (double)m) * c, a.S); };
+
+  // the cut: logits of an ordered value above `cut` are kept, of those that equal it the first `ties` (ALL: all)
+  uint32_t cut = FIRST_LIVE, ties = ALL;
+  uint64_t above = 0, total = 0;
+  if (set.k == 1) {
+    cut = ordered(m);
+    ties = 1;
+  } else if (set.k > 0 && set.k < live) {
+    search<false>(row, s, FIRST_LIVE, m, low, c > 0.0 ? c : 1.0, 0, [&](uint64_t) { return (uint64_t)set.k; }, &cut, &above,
+                  &total);
+    ties = (uint32_t)(set.k - (int64_t)above);
+  }
+  if (set.p < 1.0 && set.k != 1) {
+    const uint32_t k_cut = cut, k_ties = ties;
+    const bool limited = ties != ALL;
+    const uint64_t each_tie = limited ? weight(from_ordered(k_cut)) : 0;
+    const bool found = search<true>(row, s, limited ? k_cut + 1 : FIRST_LIVE, m, low, c, a.S, [&](uint64_t t) {
+      return share_up(set.p, t + each_tie * (limited ? k_ties : 0));
+    }, &cut, &above, &total);
+    const uint64_t wanted = share_up(set.p, total + each_tie * (limited ? k_ties : 0));
+    if (!found) {   // among the logits that equal the last of the k
+      cut = k_cut;
+      above = total;
+    }
+    const uint64_t w = weight(from_ordered(cut));
+    ties = (uint32_t)min((wanted - above + w - 1) / w, (uint64_t)(ALL - 1));
+  }
+  const uint32_t least = least_key(set.least, m, set.T);
+  if (least > cut) {
+    cut = least;
+    ties = ALL;
+  }
+
+  int index;
+  float z;
+  // the index of the last of the ties
+  int last = a.V;
+  if (ties != ALL) {
+    uint64_t n;
+    locate(row, s, [&](int, float x) -> uint64_t { return ordered(x) == cut ? 1 : 0; },
+           [&](uint64_t all) { return min((uint64_t)ties, all); }, &last, &z, &n);
+  }
+  // a share of nothing: the first symbol of any weight, though it be less than a unit
+  for (bool any = false;; any = true) {
+    uint64_t sum;
+    locate(row, s, [&](int v, float x) -> uint64_t {
+      const uint32_t o = ordered(x);
+      if (!(o > cut || (o == cut && v <= last))) return 0;
+      return any ? (((double)x - (double)m) * c >= -1074.0 ? 1 : 0) : weight(x);
+    }, [&](uint64_t all) { return any ? 1 : share_down(set.u, all) + 1; }, &index, &z, &sum);
+    if (any) break;
+    total = sum;
+    if (share_down(set.u, total) > 0) break;
+  }
+  if (tid == 0) {
+    a.symbol[r] = index;
+    a.bits[r] = (float)(log2((double)total) - a.S - ((double)z - (double)m) * c);
+  }
+}
+
+template <int TYPE>
+void run(const SampleArgs& a, int64_t rows, hipStream_t st) {
+  const int pieces = (a.V + Vec<TYPE>::N - 1) / Vec<TYPE>::N;
+  const auto go = [&](auto kern, int threads, bool keep) {
+    const unsigned lds = keep ? 16 * ((pieces + threads - 1) / threads * threads) : 0;
+    hipLaunchKernelGGL(kern, dim3((unsigned)rows), dim3(threads), lds, st, a);
+  };
+  if (pieces <= 512) go(k_sample_long<TYPE, 64, true>, 64, true);
+  else if (pieces <= 2048) go(k_sample_long<TYPE, 256, true>, 256, true);
+  else if (pieces <= 4096) go(k_sample_long<TYPE, 512, true>, 512, true);
+  else if (pieces <= 8192) go(k_sample_long<TYPE, 1024, true>, 1024, true);
+  else go(k_sample_long<TYPE, 1024, false>, 1024, false);
+}
+
+}  // namespace
+
+hipError_t launch_sample(const reno_sample& p, const void* logits, const float* u, int32_t* symbol, float* bits,
+                         hipStream_t st) {
+  // a row is given up to 1024 threads
+  for (int64_t r = 0; r < p.rows; r += LAUNCH_ROWS / 4) {
+    const int64_t n = std::min(LAUNCH_ROWS / 4, p.rows - r);
+    SampleArgs a;
+    a.z = static_cast<const char*>(logits) + r * p.row_stride * (p.type == RENO_T_FP32 ? 4 : 2);
+    a.stride = p.row_stride;
+    a.V = p.symbols;
+    a.S = unit_bits(p.symbols);
+    a.T = p.temperature;
+    a.p = p.top_p;
+    a.least = p.min_p;
+    a.k = p.top_k;
+    a.T_rows = p.temperature_rows ? p.temperature_rows + r : nullptr;
+    a.p_rows = p.top_p_rows ? p.top_p_rows + r : nullptr;
+    a.least_rows = p.min_p_rows ? p.min_p_rows + r : nullptr;
+    a.k_rows = p.top_k_rows ? p.top_k_rows + r : nullptr;
+    a.allowed = p.allowed ? p.allowed + r * p.allowed_stride : nullptr;
+    a.allowed_stride = p.allowed_stride;
+    a.u = u + r;
+    a.symbol = symbol + r;
+    a.bits = bits + r;
+    switch (p.type) {
+      case RENO_T_FP32: run<RENO_T_FP32>(a, n, st); break;
+      case RENO_T_BF16: run<RENO_T_BF16>(a, n, st); break;
+      default: run<RENO_T_FP16>(a, n, st);
+    }
+  }
+  return hipGetLastError();
+}
+
+}  // namespace reno

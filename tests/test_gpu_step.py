@@ -1,0 +1,290 @@
+"""Norm, clipping and AdamW against the formulas in 64 bits: types, sizes, alignments, long lists, norms that are not
+finite, streams, graphs; then a head trained by them."""
+import math
+
+import pytest
+import torch
+
+import paper_2503_12382_amd as reno
+from gpu_helpers import say
+
+pytestmark = pytest.mark.gpu
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+HALF = {F32: 2.0 ** -24, BF16: 2.0 ** -8, F16: 2.0 ** -11}   # half a step of the type, relative
+TINY = {F32: 2.0 ** -150, BF16: 2.0 ** -134, F16: 2.0 ** -25}   # half a step of its smallest values
+LISTS = {
+    "one": [((1,), F32)],
+    "empty ones": [((0,), F32), ((3,), BF16), ((0, 5), F16), ((7,), F32)],
+    "model": [((27, 11, 32), F32), ((32,), F32), ((27, 32, 32), F32), ((32,), F32), ((32, 256), F32), ((256,), F32)],
+    "mixed": [((1001,), F32), ((513, 3), BF16), ((4097,), F16), ((8,), BF16), ((4095,), F32)],
+    "long": [((300007,), BF16), ((5,), F32), ((70001,), F32)],
+    "many": [((1 + 7 * (i % 13),), (F32, BF16, F16)[i % 3]) for i in range(150)],
+}
+
+
+def tensors(shapes, seed, spread=1.0, packed=False):
+    """Random tensors; packed: at odd places of one buffer a type."""
+    g = torch.Generator().manual_seed(seed)
+    out = []
+    for shape, dt in shapes:
+        x = (torch.randn(shape, generator=g) * spread).to(dt)
+        if packed:
+            buf = torch.zeros(x.numel() + 3, dtype=dt, device="cuda")
+            v = buf[1 + len(out) % 3:][:x.numel()].view(shape)
+            v.copy_(x)
+            out.append(v)
+        else:
+            out.append(x.cuda())
+    return out
+
+
+def norm64(ts):
+    return math.sqrt(math.fsum(float(t.double().square().sum()) for t in ts))
+
+
+def near(name, got, want, bound):
+    got, want = got.double(), want.double()
+    bad = ~((got - want).abs() <= bound)
+    assert not bool(bad.any()), (name, got[bad][:3].tolist(), want[bad][:3].tolist(), int(bad.sum()))
+
+
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("name", list(LISTS))
+def test_norm_and_clip(name, packed):
+    g = tensors(LISTS[name], 1, packed=packed)
+    before = [t.clone() for t in g]
+    for scale in (1.0, 1 / 1024, 1e-30, 3.0):
+        want = norm64(g) * scale
+        say("norm", name, packed, scale)
+        n = reno.grad_norm(g, scale=scale)
+        # sums of 64 bits, one rounding
+        assert n.shape == () and abs(float(n) - want) <= 2.0 ** -24 * want * 1.01
+        assert torch.equal(n, reno.grad_norm(g, scale=scale))
+        for most in (want / 2 if want else 1.0, want * 2 + 1.0, math.inf):
+            c = scale * min(1.0, most / float(n)) if float(n) > 0 else scale
+            out = [torch.full_like(t, 77.0) for t in g]
+            r = reno.clip_grads(g, n, most, scale=scale, out=out)
+            assert all(a is b for a, b in zip(r, out))
+            for a, b, t in zip(out, g, before):
+                assert torch.equal(b, t)
+                x = b.double() * c
+                # the product is rounded to fp32, then to the type
+                near("clip", a, x, x.abs() * (HALF[b.dtype] + 2.0 ** -24) * 1.01 + TINY[b.dtype] + 2.0 ** -150)
+    n = reno.grad_norm(g)
+    reno.clip_grads(g, n, 0.25)
+    if float(n) > 0.25:
+        for a, t in zip(g, before):
+            x = t.double() * (0.25 / float(n))
+            near("in place", a, x, x.abs() * (HALF[t.dtype] + 2.0 ** -24) * 1.01 + TINY[t.dtype] + 2.0 ** -150)
+
+
+def test_norms_at_the_ends_of_the_range():
+    for dt, big in ((F32, 3e38), (BF16, 3e38), (F16, 65504.0)):
+        x = torch.full((5000,), big).to(dt).cuda()
+        want = float(x[0].double()) * math.sqrt(5000)
+        n = float(reno.grad_norm([x], scale=1e-3))
+        assert n == pytest.approx(want * 1e-3, rel=2.0 ** -23)
+    assert math.isinf(float(reno.grad_norm([torch.full((5000,), 3e38).cuda()])))
+    tiny = torch.full((9,), 1e-44).cuda()
+    assert float(reno.grad_norm([tiny], scale=1e40)) == pytest.approx(float(tiny[0].double()) * 3e40, rel=2.0 ** -23)
+    for bad in (math.nan, math.inf, -math.inf):
+        for dt in (F32, BF16, F16):
+            x = torch.ones(4099, dtype=dt, device="cuda")
+            x[4097] = bad
+            n = reno.grad_norm([torch.ones(3, device="cuda"), x])
+            assert math.isnan(float(n)) if math.isnan(bad) else math.isinf(float(n))
+    out = reno.clip_grads([torch.ones(5, device="cuda")], torch.tensor(math.nan, device="cuda"), 1.0)
+    assert bool(out[0].isnan().all())
+    out = reno.clip_grads([torch.ones(5, device="cuda")], torch.tensor(math.inf, device="cuda"), 1.0)
+    assert bool((out[0] == 0).all())
+    out = reno.clip_grads([torch.zeros(5, device="cuda")], torch.zeros((), device="cuda"), 1.0)
+    assert bool((out[0] == 0).all())
+    # gradients that are not rows of one another: columns are copied
+    x = torch.randn(30, 40, device="cuda")
+    assert torch.equal(reno.grad_norm([x.t()]), reno.grad_norm([x.t().contiguous()]))
+
+
+def test_long_tensor():
+    """Elements past 2^31, in the last of which alone something is."""
+    n = (1 << 31) + 4099
+    x = torch.zeros(n, dtype=F16, device="cuda")
+    x[-1], x[5] = 3.0, 4.0
+    say("norm, long", n)
+    assert float(reno.grad_norm([x])) == 5.0
+    reno.clip_grads([x], torch.tensor(10.0, device="cuda"), 5.0)
+    assert float(x[-1]) == 1.5 and float(x[5]) == 2.0 and float(x[n // 2]) == 0.0
+
+
+def reference(w, g, m, v, t, factor, lr, b1, b2, eps, decay):
+    w, g, m, v = (x.double() for x in (w, g, m, v))
+    g = g * factor
+    m = b1 * m + (1 - b1) * g
+    v = b2 * v + (1 - b2) * g * g
+    step = m / (1 - b1 ** t) / ((v / (1 - b2 ** t)).sqrt() + eps)
+    return w - lr * (step + decay * w), m, v, step
+
+
+@pytest.mark.parametrize("kind", ["own", "grad32", "master", "master grad32"])
+@pytest.mark.parametrize("name", list(LISTS))
+def test_adamw(name, kind):
+    shapes = LISTS[name]
+    packed = name in ("mixed", "long")
+    p = tensors(shapes, 2, packed=packed)
+    g = tensors([(s, F32 if "grad32" in kind else dt) for s, dt in shapes], 3, packed=packed)
+    m = tensors([(s, F32) for s, _ in shapes], 4, 0.1, packed=packed)
+    v = [x.square_() for x in tensors([(s, F32) for s, _ in shapes], 5, packed=packed)]
+    master = [(t.float() + 1e-4 * torch.randn_like(t, dtype=F32)) if "master" in kind and t.dtype != F32 else None for t in p]
+    steps = torch.tensor([7, 0], dtype=torch.int32, device="cuda")
+    lr, b1, b2, eps, decay, scale = 0.02, 0.9, 0.995, 1e-6, 0.1, 0.5
+    for most in (math.inf, 0.3):
+        t = int(steps[0]) + 1
+        norm = reno.grad_norm(g, scale=scale)
+        factor = scale * min(1.0, most / float(norm))
+        old = [(a.clone(), b.clone(), c.clone(), d.clone(), None if x is None else x.clone())
+               for a, b, c, d, x in zip(p, g, m, v, master)]
+        say("adamw", name, kind, most)
+        reno.adamw_step(p, g, m, v, steps, master=master, lr=lr, betas=(b1, b2), eps=eps, weight_decay=decay, norm=norm,
+                        max_norm=most, scale=scale)
+        assert steps.tolist() == [t, 0]
+        e = 2.0 ** -24
+        for i, (w0, g0, m0, v0, x0) in enumerate(old):
+            assert torch.equal(g[i], g0)
+            w, m1, v1, step = reference(w0 if x0 is None else x0, g0, m0, v0, t, factor, lr, b1, b2, eps, decay)
+            gx = g0.double().abs() * factor
+            # g', its product, beta and the sum: a rounding each
+            bm = e * 1.01 * (2 * b1 * m0.double().abs() + 4 * (1 - b1) * gx) + 2.0 ** -148
+            bv = e * 1.01 * (3 * b2 * v0.double() + 7 * (1 - b2) * gx * gx) + 2.0 ** -148
+            near("exp_avg", m[i], m1, bm)
+            near("exp_avg_sq", v[i], v1, bv)
+            # the step: m, its scaling (2), the quotient; the root has half of v's error, 3 roundings and eps's 2
+            root = (v1 / (1 - b2 ** t)).sqrt() + eps
+            bs = bm / (1 - b1 ** t) / root + step.abs() * (e * 10 + bv / (2 * v1 + 1e-30))
+            x = w0 if x0 is None else x0
+            # lr and decay are rounded, their products with the sum: 4 roundings; the new weight's one
+            bw = lr * (bs + 5 * e * (step.abs() + 2 * decay * x.double().abs())) + e * w.abs() * 1.01 + 2.0 ** -148
+            if x0 is None:
+                near("param", p[i], w, bw + HALF[w0.dtype] * 1.01 * w.abs() + TINY[w0.dtype])
+            else:
+                near("master", master[i], w, bw)
+                assert torch.equal(p[i], master[i].to(w0.dtype))
+
+
+def test_adamw_without_a_norm_and_not_finite():
+    p, g = [torch.randn(4097, device="cuda")], [torch.randn(4097, device="cuda")]
+    m, v = [torch.zeros(4097, device="cuda")], [torch.zeros(4097, device="cuda")]
+    steps = torch.zeros(2, dtype=torch.int32, device="cuda")
+    for bad in (math.nan, math.inf):
+        keep = [t[0].clone() for t in (p, m, v)]
+        reno.adamw_step(p, g, m, v, steps, norm=torch.tensor(bad, device="cuda"), max_norm=1.0)
+        assert all(torch.equal(a[0], b) for a, b in zip((p, m, v), keep)) and steps.tolist() == [0, 0]
+    w, m1, v1, _ = reference(p[0], g[0], m[0], v[0], 1, 1.0, 1e-3, 0.9, 0.999, 1e-8, 0.01)
+    reno.adamw_step(p, g, m, v, steps)
+    assert torch.allclose(p[0].double(), w, rtol=2.0 ** -22, atol=1e-3 * 2.0 ** -19) and steps.tolist() == [1, 0]
+    # the factor of a schedule, a captured step: replays count on
+    half = torch.tensor(0.5, device="cuda")
+    q, n, s = [p[0].clone()], [m[0].clone()], [v[0].clone()]
+    st = steps.clone()
+    reno.adamw_step(q, g, n, s, st, lr=2e-3, lr_factor=half)
+    reno.adamw_step(p, g, m, v, steps)
+    assert torch.equal(p[0], q[0]) and torch.equal(steps, st)
+    # no elements: the step counts all the same
+    z = [torch.empty(0, device="cuda")]
+    reno.adamw_step(z, z, z, z, steps)
+    assert steps.tolist() == [3, 0]
+
+
+def test_step_in_a_graph_and_on_a_stream():
+    shapes = LISTS["mixed"]
+
+    def state():
+        return tensors(shapes, 2), tensors([(s, F32) for s, _ in shapes], 4, 0.1), [
+            x.square_() for x in tensors([(s, F32) for s, _ in shapes], 5)], torch.zeros(2, dtype=torch.int32, device="cuda")
+
+    g = tensors(shapes, 3)
+    a, b = state(), state()
+
+    def step(x):
+        norm = reno.grad_norm(g)
+        reno.adamw_step(x[0], g, x[1], x[2], x[3], norm=norm, max_norm=1.0)
+        return norm
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        norm = step(a)
+    for i in range(3):
+        graph.replay()
+        want = step(b)
+        torch.cuda.synchronize()
+        assert torch.equal(norm, want)
+        for x, y in zip(a, b):
+            for s, t in zip(x, y):
+                assert torch.equal(s, t)
+        g[0].mul_(1.5)       # the replay reads the gradients as they are
+    assert a[3].tolist() == [3, 0]
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    norm = reno.grad_norm(g, stream=s)
+    reno.adamw_step(a[0], g, a[1], a[2], a[3], norm=norm, max_norm=1.0, stream=s)
+    s.synchronize()
+    step(b)
+    assert all(torch.equal(x, y) for x, y in zip(a[0], b[0]))
+
+
+def test_refusals():
+    x = torch.ones(8, device="cuda")
+    n = torch.ones((), device="cuda")
+    steps = torch.zeros(2, dtype=torch.int32, device="cuda")
+    for bad in ([x.cpu()], [x.double()], [x, x.cpu()], []):
+        with pytest.raises(ValueError):
+            reno.grad_norm(bad)
+    with pytest.raises(ValueError):
+        reno.clip_grads([torch.ones(4, 4, device="cuda").t()], n, 1.0)     # in place
+    for kw in (dict(scale=0.0), dict(scale=math.inf), dict(max_norm=0.0), dict(max_norm=math.nan)):
+        with pytest.raises(reno.RenoError):
+            reno.clip_grads([x], n, **{"max_norm": 1.0, **kw})
+    with pytest.raises(reno.RenoError):
+        reno.clip_grads([x, x], n, 1.0)                                    # the same tensor twice
+    y = torch.ones(9, device="cuda")
+    with pytest.raises(reno.RenoError):
+        reno.clip_grads([y[:8]], n, 1.0, out=[y[1:]])
+    a, b, c, d = (torch.ones(8, device="cuda") for _ in range(4))
+    for bad in (([a], [b], [c], [c]), ([a, a], [b, b], [c, d], [x, y[:8]]), ([a], [a], [c], [d])):
+        with pytest.raises(reno.RenoError):
+            reno.adamw_step(*bad, steps)
+    for kw in (dict(lr=-1.0), dict(betas=(1.0, 0.9)), dict(betas=(0.9, -0.1)), dict(eps=0.0), dict(weight_decay=math.nan),
+               dict(scale=-1.0), dict(max_norm=-1.0), dict(master=[torch.ones(8, device="cuda")])):
+        with pytest.raises(reno.RenoError):
+            reno.adamw_step([a], [b], [c], [d], steps, **kw)
+    for bad in (dict(steps=steps[:1]), dict(steps=steps.float()), dict(norm=n.double()), dict(grads=[b.half()]),
+                dict(exp_avg=[c.half()]), dict(exp_avg_sq=[d[:7]]), dict(grads=[b, b])):
+        with pytest.raises((ValueError, reno.RenoError)):
+            reno.adamw_step(**{**dict(params=[a], grads=[b], exp_avg=[c], exp_avg_sq=[d], steps=steps), **bad})
+    assert bool((a == 1).all()) and steps.tolist() == [0, 0]
+
+
+def test_a_head_trained_on_drawn_symbols():
+    """The operators in the order that a program uses them in: symbols drawn from a teacher's logits, their code length
+    under a head with its gradient, the gradients' norm, the clipped step.  Each link against its formula."""
+    N, C, V = 600, 32, 256
+    g = torch.Generator().manual_seed(11)
+    h = torch.randn(N, C, generator=g).relu().cuda()
+    teacher = (h @ torch.randn(C, V, generator=g).cuda() * 0.5).contiguous()
+    w, b = (torch.randn(C, V, generator=g) * 0.1).cuda(), torch.zeros(V, device="cuda")
+    state = [[torch.zeros_like(x) for x in (w, b)] for _ in range(2)]
+    steps = torch.zeros(2, dtype=torch.int32, device="cuda")
+    allowed = torch.arange(V, device="cuda") > 0
+    weight = torch.full((N,), 1.0 / N, device="cuda")
+    for i in range(3):
+        u = torch.rand(N, generator=g)
+        u[::7] = -1.0                                       # padding
+        drawn = reno.sample_symbols(teacher, u.cuda(), top_p=0.9, allowed=allowed)
+        r = reno.head_code_length(h, w, b, drawn.symbol, row_weight=weight, grad=("dw", "db"))
+        assert bool((r.bits[::7] == 0).all()) and bool((drawn.symbol[::7] == -1).all())
+        norm = reno.grad_norm([r.dw, r.db])
+        assert float(norm) == pytest.approx(norm64([r.dw, r.db]), rel=2.0 ** -23)
+        want = [reference(x, d, m, v, i + 1, min(1.0, 0.05 / float(norm)), 0.01, 0.9, 0.999, 1e-8, 0.01)[0]
+                for x, d, m, v in zip((w, b), (r.dw, r.db), *state)]
+        reno.adamw_step([w, b], [r.dw, r.db], *state, steps, lr=0.01, norm=norm, max_norm=0.05)
+        for x, y in zip((w, b), want):
+            # a moment's relative error of 2^-22 moves the step, of size 1, by as much
+            assert torch.allclose(x.double(), y, rtol=2.0 ** -22, atol=0.01 * 2.0 ** -18)
+    assert steps.tolist() == [3, 0]
