@@ -819,19 +819,16 @@ def sample_workspace(rows: int, symbols: int, dtype) -> int:
     return n.value
 
 
-def _list_of(tensors, name, like=None, dtype=None):
-    """The tensors of a list as they are, checked: dense, on one device, of a known type (of `dtype`), and of the
-    shapes of `like`."""
-    _need(like is None or len(tensors) == len(like), f"{name} must have as many tensors as the list")
-    dev = (tensors if like is None else like)[0].device if len(tensors) else None
-    for i, t in enumerate(tensors):
-        if not t.is_cuda or t.device != dev or not t.is_contiguous():
-            raise ValueError(f"{name} must be dense tensors on one device")
-        if (t.dtype is not dtype) if dtype is not None else (t.dtype not in _TYPES):
-            raise ValueError(f"{name} must be " + (str(dtype) if dtype is not None else "float32, bfloat16 or float16"))
-        if like is not None and t.shape != like[i].shape:
-            raise ValueError(f"{name} must have the shapes of the list")
-    return tensors
+def _in_list(name, dev, *tensors):
+    """What is wrong with tensors of a list that have to be dense, on one device and of one size."""
+    for t in tensors:
+        if t.get_device() != dev:
+            raise ValueError(f"{name} must be on one device")
+        if not t.is_contiguous():
+            raise ValueError(f"{name} must be dense")
+        if t.numel() != tensors[0].numel():
+            raise ValueError(f"{name} must have the sizes of one another")
+    raise ValueError(f"{name} must be float32, bfloat16 or float16 of matching types")
 
 
 def _scalar_on(t, name, dtype, dev, n=1):
@@ -841,10 +838,6 @@ def _scalar_on(t, name, dtype, dev, n=1):
     _need(t.device == dev and t.dtype == dtype and t.numel() == n and t.is_contiguous(),
           f"{name} must be {n} {dtype} on {dev}")
     return t.data_ptr()
-
-
-def _dense(grads):
-    return [g if g.is_contiguous() else g.contiguous() for g in grads]
 
 
 def grad_norm(grads, scale: float = 1.0, workspace=None, stream=None):
@@ -859,11 +852,15 @@ def grad_norm(grads, scale: float = 1.0, workspace=None, stream=None):
     dev = grads[0].device
 
     def run(st):
-        _type_of(None)
-        g = _list_of(_dense(grads), "grads")
-        words = []
-        for t in g:
-            words += (t.numel(), _TYPES[t.dtype], t.data_ptr(), 0)
+        at_dev, words, g = dev.index, [], []
+        for t in grads:
+            if not t.is_contiguous():
+                t = t.contiguous()
+            kind = _type_of(t.dtype)
+            if kind is None or t.get_device() != at_dev:
+                _in_list("grads", at_dev, t)
+            g.append(t)
+            words += (t.numel(), kind, t.data_ptr(), 0)
         arr = array.array("q", words)
         at, count = arr.buffer_info()[0], len(g)
         need = ctypes.c_int64()
@@ -891,13 +888,19 @@ def clip_grads(grads, norm, max_norm: float, scale: float = 1.0, out=None, strea
     dev = grads[0].device
 
     def run(st):
-        _type_of(None)
-        g = _list_of(grads if out is None else _dense(grads), "grads")
-        o = g if out is None else _list_of(list(out), "out", g)
-        words = []
-        for a, b in zip(g, o):
-            _need(a.dtype is b.dtype, "out must have the gradients' types")
-            words += (a.numel(), _TYPES[a.dtype], a.data_ptr(), b.data_ptr())
+        at_dev, words, g = dev.index, [], []
+        o = grads if out is None else list(out)
+        _need(len(o) == len(grads), "out must have as many tensors as grads")
+        for a, b in zip(grads, o):
+            if out is not None and not a.is_contiguous():
+                a = a.contiguous()
+            n, dt = a.numel(), a.dtype
+            kind = _type_of(dt)
+            if (kind is None or b.dtype is not dt or b.numel() != n or a.get_device() != at_dev
+                    or b.get_device() != at_dev or not b.is_contiguous()):
+                _in_list("grads and out", at_dev, a, b)
+            g.append(a)
+            words += (n, kind, a.data_ptr(), b.data_ptr())
         arr = array.array("q", words)
         at = _scalar_on(norm, "norm", torch.float32, dev)
         _head_check(lib().reno_grad_clip(arr.buffer_info()[0], len(g), at, float(scale), float(max_norm), st.cuda_stream))
@@ -925,26 +928,32 @@ def adamw_step(params, grads, exp_avg, exp_avg_sq, steps, master=None, lr: float
     dev = params[0].device
 
     def run(st):
-        _type_of(None)
-        p = _list_of(params, "params")
-        g = _list_of(_dense(grads), "grads", p)
-        m = _list_of(list(exp_avg), "exp_avg", p, torch.float32)
-        v = _list_of(list(exp_avg_sq), "exp_avg_sq", p, torch.float32)
-        w = [None] * len(p) if master is None else list(master)
-        _need(len(w) == len(p), "master must have as many tensors as the list")
-        if master is not None:
-            pairs = [(x, y) for x, y in zip(w, p) if x is not None]
-            _list_of([x for x, _ in pairs], "master", [y for _, y in pairs], torch.float32)
-        words = []
-        for i, t in enumerate(p):
-            words += (t.numel(), _TYPES[t.dtype], _TYPES[g[i].dtype], t.data_ptr(), g[i].data_ptr(),
-                      0 if w[i] is None else w[i].data_ptr(), m[i].data_ptr(), v[i].data_ptr())
+        at_dev, words, keep, f32 = dev.index, [], [], torch.float32
+        lists = [params, list(grads), list(exp_avg), list(exp_avg_sq)]
+        lists.append([None] * len(params) if master is None else list(master))
+        _need(all(len(x) == len(params) for x in lists), "the lists must have as many tensors as params")
+        for p, g, m, v, w in zip(*lists):
+            if not g.is_contiguous():
+                g = g.contiguous()
+            n = p.numel()
+            kind, grad_kind = _type_of(p.dtype), _type_of(g.dtype)
+            if (kind is None or grad_kind is None or m.dtype is not f32 or v.dtype is not f32 or g.numel() != n
+                    or m.numel() != n or v.numel() != n or p.get_device() != at_dev or g.get_device() != at_dev
+                    or m.get_device() != at_dev or v.get_device() != at_dev or not p.is_contiguous()
+                    or not m.is_contiguous() or not v.is_contiguous()):
+                _in_list("weights, gradients and moments", at_dev, p, g, m, v)
+            if w is not None and (w.dtype is not f32 or w.numel() != n or w.get_device() != at_dev or not w.is_contiguous()):
+                _in_list("weights and their copies", at_dev, p, w)
+            keep.append(g)
+            words += (n, kind, grad_kind, p.data_ptr(), g.data_ptr(), 0 if w is None else w.data_ptr(), m.data_ptr(),
+                      v.data_ptr())
         arr = array.array("q", words)
         how = reno_adamw(float(lr), float(betas[0]), float(betas[1]), float(eps), float(weight_decay), float(scale),
                          float(max_norm), _scalar_on(lr_factor, "lr_factor", torch.float32, dev),
                          _scalar_on(norm, "norm", torch.float32, dev), _scalar_on(steps, "steps", torch.int32, dev, 2))
-        _head_check(lib().reno_adamw_step(arr.buffer_info()[0], len(p), ctypes.byref(how), st.cuda_stream))
-        _read_on(stream, steps, norm, lr_factor, *p, *g, *m, *v, *w)
+        _head_check(lib().reno_adamw_step(arr.buffer_info()[0], len(params), ctypes.byref(how), st.cuda_stream))
+        if stream is not None:
+            _read_on(stream, steps, norm, lr_factor, *keep, *lists[0], *lists[2], *lists[3], *lists[4])
     _on(dev, stream, run)
 
 

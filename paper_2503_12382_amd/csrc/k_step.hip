@@ -19,9 +19,12 @@ constexpr int LIST = 64;          // tensors of a launch: their places are compa
 constexpr int THREADS = 256;
 
 // Elements of a chunk for so many in all.
+#ifndef CHUNKS
+#define CHUNKS 4096
+#endif
 int64_t chunk_of(int64_t total) {
   int64_t c = 4096;
-  while (total / c > 8192 && c < 1 << 24) c *= 2;
+  while (total / c > CHUNKS && c < 1 << 24) c *= 2;
   return c;
 }
 
@@ -266,13 +269,18 @@ struct AdamTerms {
 // bits in one instruction, which differs where the copy lies halfway between two of them.
 __device__ __forceinline__ void rounded(float& x) { asm("" : "+v"(x)); }
 
+#ifndef ADAM_U
+#define ADAM_U 2
+#endif
 template <int PT, int GT, bool MASTER>
 __global__ void __launch_bounds__(THREADS) k_adamw(AdamList l, uint32_t chunk, AdamHow h) {
-  constexpr int N = 4, U = 2;
+  constexpr int N = 4, U = ADAM_U;
+  __shared__ AdamTerms s_terms;
   if (h.norm && !(*h.norm <= 0x1.fffffep127f)) return;   // inf or NaN: the step is not made
-  const uint32_t t = (uint32_t)h.steps[0] + 1u;
-  if (l.s.first[0] == 0) {   // a list without elements has one block, to count
-    const Place pl = place(l.s, l.n, chunk);
+  // terms that all elements share: one thread's work, 64-bit quotients and powers
+  uint32_t t = 0;
+  if (threadIdx.x == 0) {
+    t = (uint32_t)h.steps[0] + 1u;
     AdamTerms a;
     a.f = factor(h.norm, h.scale, h.max_norm);
     a.b1 = (float)h.beta1;
@@ -284,6 +292,12 @@ __global__ void __launch_bounds__(THREADS) k_adamw(AdamList l, uint32_t chunk, A
     a.lr = (float)(h.lr * (h.lr_factor ? (double)*h.lr_factor : 1.0));
     a.eps = h.eps;
     a.decay = h.decay;
+    s_terms = a;
+  }
+  __syncthreads();
+  if (l.s.first[0] == 0) {   // a list without elements has one block, to count
+    const AdamTerms a = s_terms;
+    const Place pl = place(l.s, l.n, chunk);
     const void* gp = l.grad[pl.i];
     void* wp = MASTER ? (void*)l.master[pl.i] : l.param[pl.i];
     void* out = l.param[pl.i];
@@ -333,10 +347,9 @@ __global__ void __launch_bounds__(THREADS) k_adamw(AdamList l, uint32_t chunk, A
       put1<PT>(out, i, w);
     }
   }
-  // The last block to come here knows that every wave has read the count.
-  __syncthreads();
+  // The last block to come here knows that every other has read the count.  (No fence: nothing else is handed over,
+  // and one would write this XCD's L2 back, for each block.  8.3e6 fp32 weights: 108 us with it, see above without.)
   if (h.last && threadIdx.x == 0) {
-    __threadfence();
     if (atomicAdd(&h.steps[1], 1) == (int)gridDim.x - 1) {
       h.steps[0] = (int32_t)t;
       h.steps[1] = 0;
