@@ -11,6 +11,7 @@
 // without sorting: a histogram over the row, the bin that holds the cut, a
 // histogram over that bin's range of values, until a bin is one value.
 //
+//   k_sample_short rows of up to 256: 16 lanes a row, in registers
 //   k_sample_long  a block a row, held in LDS where it fits
 
 #include <algorithm>
@@ -27,28 +28,36 @@ namespace {
 constexpr uint32_t FIRST_LIVE = 0x00800000u;   // ordered(-inf) + 1
 constexpr uint32_t ALL = 0xffffffffu;
 
-// 2^y in units of 2^-S, to the nearest; y <= 0, S <= 51.
-__device__ __forceinline__ uint64_t units(double y, int S) {
-  y = fmax(y, -1000.0);
+// a b + c with c from scalar registers: the compiler would copy a constant to the result's registers first, two moves
+// for each step of a polynomial.
+__device__ __forceinline__ double fma_s(double a, double b, double c) {
+  double r;
+  asm("v_fma_f64 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "s"(c));
+  return r;
+}
+
+// 2^(d c) in units of 2^-S, to the nearest; d <= 0 <= c, S <= 51 a whole number.  0 for a d that is NaN.
+__device__ __forceinline__ uint64_t units(double d, double c, double S) {
   constexpr double ROUND = 0x1.8p52;
+  const double y = fmax(__builtin_fma(d, c, S), -900.0);
   const double t = y + ROUND;
   const double f = y - (t - ROUND);
   // (2^f - 1) / f on [-1/2, 1/2], interpolated at the zeros of a Chebyshev polynomial; 1 + f q is right to 2^-50
-  double q = 0x1.e5e9ef7b8cd7ap-28;
-  q = __builtin_fma(q, f, 0x1.b6571e5ac5dabp-24);
-  q = __builtin_fma(q, f, 0x1.62bfe465e6f1bp-20);
-  q = __builtin_fma(q, f, 0x1.ffcb7678282dfp-17);
-  q = __builtin_fma(q, f, 0x1.4309130375a29p-13);
-  q = __builtin_fma(q, f, 0x1.5d87fe908fa7dp-10);
-  q = __builtin_fma(q, f, 0x1.3b2ab6fba3871p-7);
-  q = __builtin_fma(q, f, 0x1.c6b08d7044119p-5);
-  q = __builtin_fma(q, f, 0x1.ebfbdff82c590p-3);
-  q = __builtin_fma(q, f, 0x1.62e42fefa39f7p-1);
+  double q = fma_s(f, 0x1.e5e9ef7b8cd7ap-28, 0x1.b6571e5ac5dabp-24);
+  q = fma_s(q, f, 0x1.62bfe465e6f1bp-20);
+  q = fma_s(q, f, 0x1.ffcb7678282dfp-17);
+  q = fma_s(q, f, 0x1.4309130375a29p-13);
+  q = fma_s(q, f, 0x1.5d87fe908fa7dp-10);
+  q = fma_s(q, f, 0x1.3b2ab6fba3871p-7);
+  q = fma_s(q, f, 0x1.c6b08d7044119p-5);
+  q = fma_s(q, f, 0x1.ebfbdff82c590p-3);
+  q = fma_s(q, f, 0x1.62e42fefa39f7p-1);
   q = __builtin_fma(q, f, 1.0);
-  const int n = (int)(uint32_t)__builtin_bit_cast(uint64_t, t) + S;
-  const double p = __builtin_bit_cast(double, (uint64_t)(uint32_t)(1023 + n) << 52);
-  // rounded to a whole number by the sum with 2^52, whose fraction it then is
-  return __builtin_bit_cast(uint64_t, __builtin_fma(q, p, 0x1p52)) & 0xfffffffffffffull;
+  // the whole part goes to the exponent; the sum with 2^52 rounds to a whole number, which its fraction then is
+  const uint32_t n = (uint32_t)__builtin_bit_cast(uint64_t, t) << 20;
+  const uint64_t b = __builtin_bit_cast(uint64_t, q);
+  const double w = __builtin_bit_cast(double, (uint64_t)((uint32_t)(b >> 32) + n) << 32 | (uint32_t)b);
+  return __builtin_bit_cast(uint64_t, w + 0x1p52) & 0xfffffffffffffull;
 }
 
 // The units of a row of V: the sum of V of them stays below 2^63.
@@ -114,6 +123,404 @@ __device__ __forceinline__ uint32_t least_key(double least, float m, double T) {
   float f = (float)z;
   if ((double)f < z) f = nextafterf(f, INFINITY);
   return max(ordered(f), FIRST_LIVE);
+}
+
+// ---------------------------------------------------------------------------
+// Rows of up to 256 logits: 16 lanes a row.
+
+constexpr int SHORT_LANE = 16;      // logits of a lane, lanes of a row
+constexpr int SHORT_ROWS = 4;       // rows of a wave
+constexpr int SHORT_BINS = 64;
+
+template <int CTRL>
+__device__ __forceinline__ uint64_t dpp64(uint64_t v) {   // lanes without a source: 0
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, 0xF, 0xF, false);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(v >> 32), CTRL, 0xF, 0xF, false);
+  return (uint64_t)hi << 32 | lo;
+}
+__device__ __forceinline__ uint64_t row16_scan(uint64_t v) {   // inclusive
+  v += dpp64<0x111>(v);
+  v += dpp64<0x112>(v);
+  v += dpp64<0x114>(v);
+  return v + dpp64<0x118>(v);
+}
+__device__ __forceinline__ uint32_t row16_scan(uint32_t v) {
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xF, 0xF, false);
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xF, 0xF, false);
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xF, 0xF, false);
+  return v + (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xF, 0xF, false);
+}
+__device__ __forceinline__ uint32_t row16_max(uint32_t v) {
+  v = max(v, dpp<0x128>(v));
+  v = max(v, dpp<0x124>(v));
+  v = max(v, dpp<0x122>(v));
+  return max(v, dpp<0x121>(v));
+}
+__device__ __forceinline__ float row16_max(float v) {
+  v = fmaxf(v, __uint_as_float(dpp<0x128>(__float_as_uint(v))));
+  v = fmaxf(v, __uint_as_float(dpp<0x124>(__float_as_uint(v))));
+  v = fmaxf(v, __uint_as_float(dpp<0x122>(__float_as_uint(v))));
+  return fmaxf(v, __uint_as_float(dpp<0x121>(__float_as_uint(v))));
+}
+__device__ __forceinline__ float row16_min(float v) {
+  v = fminf(v, __uint_as_float(dpp<0x128>(__float_as_uint(v))));
+  v = fminf(v, __uint_as_float(dpp<0x124>(__float_as_uint(v))));
+  v = fminf(v, __uint_as_float(dpp<0x122>(__float_as_uint(v))));
+  return fminf(v, __uint_as_float(dpp<0x121>(__float_as_uint(v))));
+}
+template <typename T>
+__device__ __forceinline__ T row16_last(T v) { return __shfl(v, lane_id() | 15); }
+// The lane of this row whose condition holds (one of them; 15 where none does).
+__device__ __forceinline__ int row16_which(bool here) {
+  const uint32_t b = (uint32_t)(__ballot(here) >> (lane_id() & 48)) & 0xffffu;
+  return (lane_id() & 48) | (b ? __builtin_ctz(b) : 15);
+}
+
+// Shared memory of a wave.
+struct ShortShared {
+  uint64_t hist[SHORT_ROWS][SHORT_BINS];
+  ulonglong2 cand[SHORT_ROWS][16];
+  float x[SHORT_ROWS][16 * SHORT_LANE];   // the rows, for the turns that are rare
+};
+
+// A row's logits in registers, -inf where there is none, with their weights.
+template <int PL>
+struct Short {
+  float x[PL];
+  uint64_t w[PL];
+  int v0;             // the lane's first symbol
+};
+
+// The last logit of the row's order that is kept: logits above x, and those that equal it up to symbol v.
+struct ShortCut {
+  float x;
+  int v;
+};
+
+// A search under way: `above` lies above the range that still holds the cut, `wanted` is what it has to reach.
+struct ShortSearch {
+  uint64_t above, wanted;
+  bool active;
+};
+
+// A place in the row's order: the ordered value, then the index complemented.
+__device__ __forceinline__ uint64_t place_of(float x, int v) { return (uint64_t)ordered(x) << 8 | (uint32_t)(255 - v); }
+
+__device__ __forceinline__ float next_below(float x) { return __uint_as_float(__float_as_uint(x) - 1u); }   // x > 0
+__device__ __forceinline__ float next_above(float x) {
+  return x == 0.0f ? 0x1p-149f : __uint_as_float(__float_as_uint(x) + (x > 0.0f ? 1u : ~0u));
+}
+
+// The bin of a histogram at which what is wanted is reached; q.above becomes what lies above it.
+__device__ __forceinline__ int short_bin(const ShortShared& s, ShortSearch& q, uint64_t (&h)[SHORT_BINS / 16], uint64_t mine,
+                                         uint64_t upto) {
+  constexpr int PER = SHORT_BINS / 16;
+  uint64_t a = q.above + upto - mine;
+  const int owner = row16_which(a < q.wanted && a + mine >= q.wanted);
+  int bin = (lane_id() & 15) * PER;
+  bool past = false;
+#pragma unroll
+  for (int i = 0; i < PER - 1; ++i) {
+    past |= a + h[i] >= q.wanted;
+    bin += past ? 0 : 1;
+    a += past ? 0 : h[i];
+  }
+  const uint64_t above = __shfl(a, owner);
+  q.above = q.active ? above : q.above;
+  return __shfl(bin, owner);
+}
+
+// The cut among the `n` <= 16 candidates that lie in LDS, for rows with `few`: ranks and sums of all pairs.
+__device__ __forceinline__ void short_pairs(const ShortShared& s, ShortSearch& q, bool few, uint32_t n, ShortCut* cut) {
+  const int lane = lane_id(), l15 = lane & 15, rw = lane >> 4;
+  wave_lds_fence();
+  const bool there = few && l15 < (int)n;
+  const ulonglong2 me = s.cand[rw][l15];
+  uint64_t sum = q.above;
+  for (int j = 0; __any(few && j < (int)n); ++j) {
+    const ulonglong2 o = s.cand[rw][j];
+    sum += j < (int)n && o.x >= me.x ? o.y : 0;
+  }
+  const int who = row16_which(there && sum >= q.wanted && sum - me.y < q.wanted);
+  const uint32_t o = __shfl((uint32_t)(me.x >> 8), who);
+  const int v = 255 - (__shfl((int)me.x, who) & 255);
+  cut->x = few ? from_ordered(o) : cut->x;
+  cut->v = few ? v : cut->v;
+  q.active = q.active && !few;
+  wave_lds_fence();
+}
+
+// The rare turns, for rows whose bin holds more than 16 logits (from what `in` says first): a histogram over what the
+// bin spans until few are left or all are equal.  One logit at a time from LDS.
+template <bool MASS, int PL, typename In>
+__device__ __forceinline__ void short_more(ShortShared& s, ShortSearch& q, int v0, float m, double c, double S, const In& in,
+                                        ShortCut* cut) {
+  constexpr int PER = SHORT_BINS / 16;
+  const int lane = lane_id(), l15 = lane & 15, rw = lane >> 4;
+  uint32_t lo = 0, top = ALL;   // the ordered values that are left
+  int shift = 0;
+  bool first = true;
+  const auto measure = [&](float x) -> uint64_t { return MASS ? units((double)x - (double)m, c, S) : 1; };
+  const auto left = [&](float x) {
+    const uint32_t o = ordered(x);
+    return q.active && (first ? in(x) : o >= lo && o <= top);
+  };
+  while (__any(q.active)) {
+    uint32_t n = 0, kmax = 0, kmin = ALL;
+#pragma unroll 1
+    for (int i = 0; i < PL; ++i) {
+      const float x = s.x[rw][v0 + i];
+      if (left(x)) {
+        ++n;
+        kmax = max(kmax, ordered(x));
+        kmin = min(kmin, ordered(x));
+      }
+    }
+    const uint32_t upto_n = row16_scan(n);
+    const uint32_t all_n = row16_last(upto_n);
+    kmax = row16_max(kmax);
+    kmin = ~row16_max(~kmin);
+    const bool few = q.active && all_n <= 16;
+    if (__any(few)) {
+      uint32_t at = upto_n - n;
+#pragma unroll 1
+      for (int i = 0; i < PL; ++i) {
+        const float x = s.x[rw][v0 + i];
+        if (few && left(x)) s.cand[rw][at++] = make_ulonglong2(place_of(x, v0 + i), measure(x));
+      }
+      short_pairs(s, q, few, all_n, cut);
+    }
+    const bool same = q.active && kmin == kmax;
+    if (__any(same)) {   // equal logits: the symbol by their number
+      const uint64_t each = max(measure(from_ordered(kmax)), (uint64_t)1);
+      const uint32_t ties = (uint32_t)((q.wanted - q.above + each - 1) / each);   // the cut's place among them
+      uint32_t to_go = ties - (upto_n - n);                                       // ... among the lane's
+      const int who = row16_which(upto_n >= ties && upto_n - n < ties);
+      int v = 0;
+#pragma unroll 1
+      for (int i = 0; i < PL; ++i)
+        if (same && left(s.x[rw][v0 + i])) {
+          v = to_go == 1 ? v0 + i : v;
+          --to_go;
+        }
+      v = __shfl(v, who);
+      cut->x = same ? from_ordered(kmax) : cut->x;
+      cut->v = same ? v : cut->v;
+      q.active = q.active && !same;
+    }
+    if (!__any(q.active)) break;
+    lo = kmin;
+    top = kmax;
+    shift = max(0, 26 - (int)__builtin_clz((kmax - kmin) | 1u));
+    first = false;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) s.hist[rw][l15 * PER + i] = 0;
+    wave_lds_fence();
+#pragma unroll 1
+    for (int i = 0; i < PL; ++i) {
+      const float x = s.x[rw][v0 + i];
+      if (left(x)) atomicAdd((unsigned long long*)&s.hist[rw][(top - ordered(x)) >> shift], (unsigned long long)measure(x));
+    }
+    wave_lds_fence();
+    uint64_t h[PER], mine = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) mine += h[i] = s.hist[rw][l15 * PER + i];
+    const int bin = short_bin(s, q, h, mine, row16_scan(mine));
+    top -= (uint32_t)bin << shift;
+    lo = max(lo, top - min(top, (1u << shift) - 1u));
+  }
+}
+
+// For rows that are `active`: the last logit at which `want` of the measure (logits, or with MASS their weights) is
+// reached from the largest, m, on; want(total) is asked with the measure of all, and more than that changes no `cut`.
+// range: how far below m the cut lies at most, or is worth bins.
+template <bool MASS, int PL, typename F>
+__device__ __forceinline__ void short_search(const Short<PL>& row, ShortShared& s, bool active, float m, float range,
+                                             double c, double S, const F& want, ShortCut* cut) {
+  constexpr int PER = SHORT_BINS / 16;
+  const int lane = lane_id(), l15 = lane & 15, rw = lane >> 4;
+  ShortSearch q;
+  q.above = 0;
+  // (a range of 0: all are equal, and any scale puts them first and what is not there last)
+  const float scale = active ? (range > 0.0f ? fminf((float)SHORT_BINS / fminf(range, 3e38f), 3e38f) : 1.0f) : NAN;
+  const auto bin_of = [&](float x) { return (m - x) * scale; };   // NaN where the row is not searched
+#pragma unroll
+  for (int i = 0; i < PER; ++i) s.hist[rw][l15 * PER + i] = 0;
+  wave_lds_fence();
+#pragma unroll
+  for (int i = 0; i < PL; ++i)   // (a row that is not searched adds to its last bin)
+    atomicAdd((unsigned long long*)&s.hist[rw][(uint32_t)fminf(bin_of(row.x[i]), (float)(SHORT_BINS - 1))],
+              MASS ? (unsigned long long)row.w[i] : 1ull);
+  wave_lds_fence();
+  uint64_t h[PER], mine = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) mine += h[i] = s.hist[rw][l15 * PER + i];
+  const uint64_t upto = row16_scan(mine);
+  const uint64_t all = row16_last(upto);
+  q.wanted = want(all);
+  q.active = active && q.wanted <= all;
+  const int bin = short_bin(s, q, h, mine, upto);
+  // the bin's logits
+  const float b0 = q.active ? (float)bin : NAN;
+  const float b1 = bin == SHORT_BINS - 1 ? INFINITY : next_below((float)(bin + 1));
+  const auto in = [&](float x) {
+    const float b = bin_of(x);
+    return b >= b0 && b <= b1;
+  };
+  uint32_t n = 0;
+#pragma unroll
+  for (int i = 0; i < PL; ++i) n += in(row.x[i]) ? 1 : 0;
+  const uint32_t upto_n = row16_scan(n);
+  const uint32_t all_n = row16_last(upto_n);
+  const bool few = q.active && all_n <= 16;
+  uint32_t at = upto_n - n;
+#pragma unroll
+  for (int i = 0; i < PL; ++i)
+    if (in(row.x[i]) && few) s.cand[rw][at++] = make_ulonglong2(place_of(row.x[i], row.v0 + i), MASS ? row.w[i] : 1);
+  short_pairs(s, q, few, all_n, cut);
+  if (__any(q.active)) short_more<MASS, PL>(s, q, row.v0, m, c, S, in, cut);
+}
+
+// Whether logit i of the lane is kept: `lim`, the last of the lane whose ties are, is cut.v - v0.
+__device__ __forceinline__ bool is_kept(float x, int i, float cut, float above, int lim) {
+  return x >= (i <= lim ? cut : above);
+}
+
+template <int TYPE, int PL>
+__device__ __forceinline__ void short_load(const SampleArgs& a, int64_t at, int v0, float (&x)[PL]) {
+  const int V = a.V;
+  if (PL == SHORT_LANE && v0 + PL <= V) {
+#pragma unroll
+    for (int i = 0; i < PL; i += Vec<TYPE>::N) {
+      Vec<TYPE> t;
+      uint4 raw;   // one load, wherever the row starts
+      __builtin_memcpy(&raw, static_cast<const char*>(a.z) + (at + v0 + i) * (16 / Vec<TYPE>::N), 16);
+      t.from(raw);
+#pragma unroll
+      for (int e = 0; e < Vec<TYPE>::N && i + e < PL; ++e) x[i + e] = t.x[e];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < PL; ++i) {
+      x[i] = logit<TYPE>(a.z, at + min(v0 + i, V - 1));
+      x[i] = v0 + i < V ? x[i] : -INFINITY;
+    }
+  }
+}
+template <int PL>
+__device__ __forceinline__ void short_mask(const uint8_t* allowed, int V, int v0, float (&x)[PL]) {
+  if (PL == SHORT_LANE && v0 + PL <= V) {
+    uint32_t there[(PL + 3) / 4];
+    __builtin_memcpy(there, allowed + v0, PL);
+#pragma unroll
+    for (int i = 0; i < PL; ++i) x[i] = there[i / 4] & (0xffu << (8 * (i & 3))) ? x[i] : -INFINITY;
+  } else {
+#pragma unroll
+    for (int i = 0; i < PL; ++i) x[i] = allowed[min(v0 + i, V - 1)] ? x[i] : -INFINITY;
+  }
+}
+
+#ifndef SHORT_OCC
+#define SHORT_OCC 4
+#endif
+template <int TYPE, int PL>
+__global__ void __launch_bounds__(256, SHORT_OCC) k_sample_short(SampleArgs a, int64_t rows) {
+  __shared__ ShortShared s_all[4];
+  const int lane = lane_id(), wave = threadIdx.x >> 6, l15 = lane & 15, rw = lane >> 4;
+  const int64_t r0 = ((int64_t)blockIdx.x * 4 + wave) * SHORT_ROWS;
+  if (r0 >= rows) return;
+  ShortShared& s = s_all[wave];
+  const int64_t r = min(r0 + rw, rows - 1);
+  const double S = (double)a.S;
+  Short<PL> row;
+  row.v0 = l15 * PL;
+  short_load<TYPE, PL>(a, r * a.stride, row.v0, row.x);
+  const Row set = settings(a, r);
+  const bool taken = r0 + rw < rows && set.u >= 0.0f && set.u < 1.0f;
+  if (a.allowed) short_mask<PL>(a.allowed + r * a.allowed_stride, a.V, row.v0, row.x);
+  bool odd = false;
+  float m = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < PL; ++i) {
+    odd |= !(row.x[i] < INFINITY);
+    m = fmaxf(m, row.x[i]);
+    s.x[rw][row.v0 + i] = row.x[i];
+  }
+  m = row16_max(m);
+  const bool bad = taken && (!set.valid || (__ballot(odd) >> (lane & 48) & 0xffffu) != 0);
+  const bool live = taken && !bad && m > -INFINITY;
+  const double c = set.T > 0.0 ? LOG2E_D / set.T : 0.0;
+#pragma unroll
+  for (int i = 0; i < PL; ++i) row.w[i] = row.x[i] > -INFINITY ? units((double)row.x[i] - (double)m, c, S) : 0;
+  ShortCut cut{-INFINITY, 255};
+  const bool by_count = live && set.k > 0 && set.k < a.V;
+  if (__any(by_count)) {
+    float low = INFINITY;
+#pragma unroll
+    for (int i = 0; i < PL; ++i) low = fminf(low, row.x[i] > -INFINITY ? row.x[i] : INFINITY);
+    short_search<false>(row, s, by_count, m, m - row16_min(low), c, S, [&](uint64_t) { return (uint64_t)set.k; }, &cut);
+    // what is cut off has no part in the shares
+    const float over = next_above(cut.x);
+#pragma unroll
+    for (int i = 0; i < PL; ++i)
+      if (!is_kept(row.x[i], i, cut.x, over, cut.v - row.v0)) {
+        row.x[i] = -INFINITY;
+        row.w[i] = 0;
+        s.x[rw][row.v0 + i] = -INFINITY;
+      }
+  }
+  const bool by_mass = live && set.p < 1.0;
+  if (__any(by_mass)) {
+    // V weights below (1 - p) / V of the largest are together less than what may be missing
+    const float range = (__builtin_amdgcn_logf((float)a.V) - __builtin_amdgcn_logf((float)(1.0 - set.p)) + 1.0f) / (float)c;
+    short_search<true>(row, s, by_mass, m, range, c, S, [&](uint64_t t) { return share_up(set.p, t); }, &cut);
+  }
+  if (__any(live && set.least > 0.0)) {
+    const float least = from_ordered(least_key(set.least, m, set.T));
+    if (live && set.least > 0.0 && least > cut.x) cut = ShortCut{least, 255};
+  }
+  uint64_t mine = 0;
+  const float over = next_above(cut.x);
+#pragma unroll
+  for (int i = 0; i < PL; ++i) {
+    row.w[i] = is_kept(row.x[i], i, cut.x, over, cut.v - row.v0) ? row.w[i] : 0;
+    mine += row.w[i];
+  }
+  uint64_t upto = row16_scan(mine);
+  const uint64_t total = row16_last(upto);
+  const uint64_t want = share_down(set.u, total) + 1;
+  if (__any(live && want == 1)) {   // a share of nothing: the first symbol of any weight, though it be less than a unit
+    const bool any = live && want == 1;
+    uint64_t ones = 0;
+#pragma unroll
+    for (int i = 0; i < PL; ++i) {
+      const bool some = is_kept(row.x[i], i, cut.x, over, cut.v - row.v0) && ((double)row.x[i] - (double)m) * c >= -1074.0;
+      row.w[i] = any ? (some ? 1 : 0) : row.w[i];
+      ones += row.w[i];
+    }
+    mine = any ? ones : mine;
+    upto = row16_scan(mine);
+  }
+  // the lane that holds the symbol hands its weights to the row's lanes
+  const int who = row16_which(upto - mine < want && upto >= want);
+  uint64_t* wl = s.hist[rw];
+  if (lane == who) {
+#pragma unroll
+    for (int i = 0; i < PL; ++i) wl[i] = row.w[i];
+  }
+  wave_lds_fence();
+  const uint64_t w = l15 < PL ? wl[l15] : 0;
+  const uint64_t before = __shfl(upto - mine, who);
+  const uint64_t at = before + row16_scan(w);
+  if (live && at >= want && at - w < want) {
+    const int v = (who & 15) * PL + l15;
+    a.symbol[r] = v;
+    a.bits[r] = (float)(log2((double)total) - S - ((double)s.x[rw][v] - (double)m) * c);
+  }
+  if (!live && l15 == 0 && r0 + rw < rows) {
+    a.symbol[r] = -1;
+    a.bits[r] = bad ? NAN : 0.0f;
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -242,7 +649,7 @@ __device__ __forceinline__ bool search(const L& row, S& s, uint32_t lo, float m,
   const float range = fminf(m - low, (float)fmin(40.0 / c, 3e38));
   const float scale = range > 0.0f ? fminf((float)BINS / range, 3e38f) : 0.0f;
   const auto bin_of = [&](float x) { return (int)fminf((m - x) * scale, (float)(BINS - 1)); };
-  const auto measure = [&](float x) -> uint64_t { return MASS ? units(((double)x - (double)m) * c, bits) : 1ull; };
+  const auto measure = [&](float x) -> uint64_t { return MASS ? units((double)x - (double)m, c, (double)bits) : 1ull; };
   clear<THREADS>(s.hist);
   __syncthreads();
   row.each([&](int, const float (&x)[N]) {
@@ -433,7 +840,7 @@ __global__ void __launch_bounds__(THREADS) k_sample_long(SampleArgs a) {
     return;
   }
   const double c = set.T > 0.0 ? LOG2E_D / set.T : 0.0;
-  const auto weight = [&](float x) { return units(((double)x - (double)m) * c, a.S); };
+  const auto weight = [&](float x) { return units((double)x - (double)m, c, (double)a.S); };
 
   // the cut: logits of an ordered value above `cut` are kept, of those that equal it the first `ties` (ALL: all)
   uint32_t cut = FIRST_LIVE, ties = ALL;
@@ -496,6 +903,14 @@ __global__ void __launch_bounds__(THREADS) k_sample_long(SampleArgs a) {
 
 template <int TYPE>
 void run(const SampleArgs& a, int64_t rows, hipStream_t st) {
+  if (a.V <= 16 * SHORT_LANE) {
+    const dim3 grid((unsigned)((rows + 4 * SHORT_ROWS - 1) / (4 * SHORT_ROWS)));
+    const auto go = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(256), 0, st, a, rows); };
+    if (a.V <= 16) go(k_sample_short<TYPE, 1>);
+    else if (a.V <= 64) go(k_sample_short<TYPE, 4>);
+    else go(k_sample_short<TYPE, 16>);
+    return;
+  }
   const int pieces = (a.V + Vec<TYPE>::N - 1) / Vec<TYPE>::N;
   const auto go = [&](auto kern, int threads, bool keep) {
     const unsigned lds = keep ? 16 * ((pieces + threads - 1) / threads * threads) : 0;
