@@ -36,28 +36,60 @@ __device__ __forceinline__ double fma_s(double a, double b, double c) {
   return r;
 }
 
-// 2^(d c) in units of 2^-S, to the nearest; d <= 0 <= c, S <= 51 a whole number.  0 for a d that is NaN.
-__device__ __forceinline__ uint64_t units(double d, double c, double S) {
+// 2^y for N values of y >= -900, below 2^52.  All steps of the values side by side: one chain would wait for itself.
+template <int N>
+__device__ __forceinline__ void exp2_all(const double (&y)[N], double (&w)[N]) {
   constexpr double ROUND = 0x1.8p52;
-  const double y = fmax(__builtin_fma(d, c, S), -900.0);
-  const double t = y + ROUND;
-  const double f = y - (t - ROUND);
+  double t[N], f[N];
+#pragma unroll
+  for (int e = 0; e < N; ++e) {
+    t[e] = y[e] + ROUND;
+    f[e] = y[e] - (t[e] - ROUND);
+    w[e] = 0x1.e5e9ef7b8cd7ap-28;
+  }
   // (2^f - 1) / f on [-1/2, 1/2], interpolated at the zeros of a Chebyshev polynomial; 1 + f q is right to 2^-50
-  double q = fma_s(f, 0x1.e5e9ef7b8cd7ap-28, 0x1.b6571e5ac5dabp-24);
-  q = fma_s(q, f, 0x1.62bfe465e6f1bp-20);
-  q = fma_s(q, f, 0x1.ffcb7678282dfp-17);
-  q = fma_s(q, f, 0x1.4309130375a29p-13);
-  q = fma_s(q, f, 0x1.5d87fe908fa7dp-10);
-  q = fma_s(q, f, 0x1.3b2ab6fba3871p-7);
-  q = fma_s(q, f, 0x1.c6b08d7044119p-5);
-  q = fma_s(q, f, 0x1.ebfbdff82c590p-3);
-  q = fma_s(q, f, 0x1.62e42fefa39f7p-1);
-  q = __builtin_fma(q, f, 1.0);
-  // the whole part goes to the exponent; the sum with 2^52 rounds to a whole number, which its fraction then is
-  const uint32_t n = (uint32_t)__builtin_bit_cast(uint64_t, t) << 20;
-  const uint64_t b = __builtin_bit_cast(uint64_t, q);
-  const double w = __builtin_bit_cast(double, (uint64_t)((uint32_t)(b >> 32) + n) << 32 | (uint32_t)b);
-  return __builtin_bit_cast(uint64_t, w + 0x1p52) & 0xfffffffffffffull;
+  constexpr double C[9] = {0x1.b6571e5ac5dabp-24, 0x1.62bfe465e6f1bp-20, 0x1.ffcb7678282dfp-17,
+                           0x1.4309130375a29p-13, 0x1.5d87fe908fa7dp-10, 0x1.3b2ab6fba3871p-7,
+                           0x1.c6b08d7044119p-5,  0x1.ebfbdff82c590p-3,  0x1.62e42fefa39f7p-1};
+#pragma unroll
+  for (int k = 0; k < 9; ++k)
+#pragma unroll
+    for (int e = 0; e < N; ++e) w[e] = fma_s(w[e], f[e], C[k]);
+#pragma unroll
+  for (int e = 0; e < N; ++e) {
+    // the whole part goes to the exponent
+    const uint64_t b = __builtin_bit_cast(uint64_t, __builtin_fma(w[e], f[e], 1.0));
+    const uint32_t n = (uint32_t)__builtin_bit_cast(uint64_t, t[e]) << 20;
+    w[e] = __builtin_bit_cast(double, (uint64_t)((uint32_t)(b >> 32) + n) << 32 | (uint32_t)b);
+  }
+}
+
+// 2^((x - m) c) in units of 2^-S, to the nearest; x <= m, c >= 0, S <= 51 a whole number.  -inf and NaN give 0.
+template <int N>
+__device__ __forceinline__ void units_all(const float* x, double m, double c, double S, uint64_t* u) {
+  double y[N], w[N];
+#pragma unroll
+  for (int e = 0; e < N; ++e) y[e] = fmax(__builtin_fma((double)x[e] - m, c, S), -900.0);
+  exp2_all<N>(y, w);
+  // the sum with 2^52 rounds to a whole number, which its fraction then is
+#pragma unroll
+  for (int e = 0; e < N; ++e) u[e] = __builtin_bit_cast(uint64_t, w[e] + 0x1p52) & 0xfffffffffffffull;
+}
+__device__ __forceinline__ uint64_t units(float x, double m, double c, double S) {
+  uint64_t u;
+  units_all<1>(&x, m, c, S, &u);
+  return u;
+}
+
+// log2 of a whole number from 1, to 2^-44: fp32's logarithm, and what 2 to its power lacks.
+__device__ __forceinline__ double log2_of(uint64_t n) {
+  const int e = 63 - __builtin_clzll(n);
+  const double f = __builtin_ldexp((double)n, -e);           // 1 .. 2
+  const double l = (double)__builtin_amdgcn_logf((float)f);
+  const double y[1] = {-l};
+  double w[1];
+  exp2_all<1>(y, w);
+  return (double)e + l + __builtin_fma(f, w[0], -1.0) * 1.4426950408889634;
 }
 
 // The units of a row of V: the sum of V of them stays below 2^63.
@@ -76,7 +108,8 @@ __device__ __forceinline__ uint64_t share_down(float u, uint64_t m) { return (ui
 
 // A row's settings.
 struct Row {
-  double T, p, least;
+  double T, c, p, least;   // c: log2(e) / T, 0 for a T of 0
+  float octaves;           // below the largest weight: the cut by p lies above
   int64_t k;        // 0: all
   float u;
   bool valid;
@@ -86,7 +119,8 @@ struct SampleArgs {
   const void* z;
   int64_t stride;
   int V, S;
-  double T, p, least;
+  double T, c, p, least;
+  float octaves;
   int k;
   const float *T_rows, *p_rows, *least_rows;
   const int32_t* k_rows;
@@ -97,6 +131,13 @@ struct SampleArgs {
   float* bits;
 };
 
+constexpr double LOG2E_D = 1.4426950408889634;
+
+// V weights below (1 - p) / V of the largest are together less than what a share of p may miss.
+__host__ __device__ __forceinline__ float octaves_of(int V, double p) {
+  return log2f((float)V) - log2f(fmaxf((float)(1.0 - p), 0x1p-60f)) + 1.0f;
+}
+
 __device__ __forceinline__ Row settings(const SampleArgs& a, int64_t r) {
   Row s;
   s.u = a.u[r];
@@ -104,6 +145,10 @@ __device__ __forceinline__ Row settings(const SampleArgs& a, int64_t r) {
   s.p = a.p_rows ? (double)a.p_rows[r] : a.p;
   s.least = a.least_rows ? (double)a.least_rows[r] : a.least;
   s.k = max(a.k_rows ? a.k_rows[r] : a.k, 0);
+  s.c = a.c;
+  if (a.T_rows) s.c = s.T > 0.0 ? LOG2E_D / s.T : 0.0;
+  s.octaves = a.octaves;
+  if (a.p_rows) s.octaves = octaves_of(a.V, fmax(s.p, 0.0));
   s.valid = s.T >= 0.0 && s.T < (double)INFINITY && s.p == s.p && s.least == s.least;
   s.least = fmin(s.least, 1.0);
   if (s.T == 0.0) {   // the largest alone
@@ -113,8 +158,6 @@ __device__ __forceinline__ Row settings(const SampleArgs& a, int64_t r) {
   }
   return s;
 }
-
-constexpr double LOG2E_D = 1.4426950408889634;
 
 // The ordered value from which on logits have a weight of `least` of the largest, m.
 __device__ __forceinline__ uint32_t least_key(double least, float m, double T) {
@@ -180,7 +223,7 @@ __device__ __forceinline__ int row16_which(bool here) {
 struct ShortShared {
   uint64_t hist[SHORT_ROWS][SHORT_BINS];
   ulonglong2 cand[SHORT_ROWS][16];
-  float x[SHORT_ROWS][16 * SHORT_LANE];   // the rows, for the turns that are rare
+  float x[SHORT_ROWS][16 * SHORT_LANE];   // the rows, for the turns that are rare: logit i of lane l at 16 i + l
 };
 
 // A row's logits in registers, -inf where there is none, with their weights.
@@ -260,7 +303,7 @@ __device__ __forceinline__ void short_more(ShortShared& s, ShortSearch& q, int v
   uint32_t lo = 0, top = ALL;   // the ordered values that are left
   int shift = 0;
   bool first = true;
-  const auto measure = [&](float x) -> uint64_t { return MASS ? units((double)x - (double)m, c, S) : 1; };
+  const auto measure = [&](float x) -> uint64_t { return MASS ? units(x, (double)m, c, S) : 1; };
   const auto left = [&](float x) {
     const uint32_t o = ordered(x);
     return q.active && (first ? in(x) : o >= lo && o <= top);
@@ -269,7 +312,7 @@ __device__ __forceinline__ void short_more(ShortShared& s, ShortSearch& q, int v
     uint32_t n = 0, kmax = 0, kmin = ALL;
 #pragma unroll 1
     for (int i = 0; i < PL; ++i) {
-      const float x = s.x[rw][v0 + i];
+      const float x = s.x[rw][i * 16 + l15];
       if (left(x)) {
         ++n;
         kmax = max(kmax, ordered(x));
@@ -285,7 +328,7 @@ __device__ __forceinline__ void short_more(ShortShared& s, ShortSearch& q, int v
       uint32_t at = upto_n - n;
 #pragma unroll 1
       for (int i = 0; i < PL; ++i) {
-        const float x = s.x[rw][v0 + i];
+        const float x = s.x[rw][i * 16 + l15];
         if (few && left(x)) s.cand[rw][at++] = make_ulonglong2(place_of(x, v0 + i), measure(x));
       }
       short_pairs(s, q, few, all_n, cut);
@@ -299,7 +342,7 @@ __device__ __forceinline__ void short_more(ShortShared& s, ShortSearch& q, int v
       int v = 0;
 #pragma unroll 1
       for (int i = 0; i < PL; ++i)
-        if (same && left(s.x[rw][v0 + i])) {
+        if (same && left(s.x[rw][i * 16 + l15])) {
           v = to_go == 1 ? v0 + i : v;
           --to_go;
         }
@@ -318,7 +361,7 @@ __device__ __forceinline__ void short_more(ShortShared& s, ShortSearch& q, int v
     wave_lds_fence();
 #pragma unroll 1
     for (int i = 0; i < PL; ++i) {
-      const float x = s.x[rw][v0 + i];
+      const float x = s.x[rw][i * 16 + l15];
       if (left(x)) atomicAdd((unsigned long long*)&s.hist[rw][(top - ordered(x)) >> shift], (unsigned long long)measure(x));
     }
     wave_lds_fence();
@@ -444,14 +487,14 @@ __global__ void __launch_bounds__(256, SHORT_OCC) k_sample_short(SampleArgs a, i
   for (int i = 0; i < PL; ++i) {
     odd |= !(row.x[i] < INFINITY);
     m = fmaxf(m, row.x[i]);
-    s.x[rw][row.v0 + i] = row.x[i];
+    s.x[rw][i * 16 + l15] = row.x[i];
   }
   m = row16_max(m);
   const bool bad = taken && (!set.valid || (__ballot(odd) >> (lane & 48) & 0xffffu) != 0);
   const bool live = taken && !bad && m > -INFINITY;
-  const double c = set.T > 0.0 ? LOG2E_D / set.T : 0.0;
+  const double c = set.c;
 #pragma unroll
-  for (int i = 0; i < PL; ++i) row.w[i] = row.x[i] > -INFINITY ? units((double)row.x[i] - (double)m, c, S) : 0;
+  for (int i = 0; i < PL; i += PL < 4 ? 1 : 4) units_all<PL < 4 ? 1 : 4>(row.x + i, (double)m, c, S, row.w + i);
   ShortCut cut{-INFINITY, 255};
   const bool by_count = live && set.k > 0 && set.k < a.V;
   if (__any(by_count)) {
@@ -466,14 +509,12 @@ __global__ void __launch_bounds__(256, SHORT_OCC) k_sample_short(SampleArgs a, i
       if (!is_kept(row.x[i], i, cut.x, over, cut.v - row.v0)) {
         row.x[i] = -INFINITY;
         row.w[i] = 0;
-        s.x[rw][row.v0 + i] = -INFINITY;
+        s.x[rw][i * 16 + l15] = -INFINITY;
       }
   }
   const bool by_mass = live && set.p < 1.0;
   if (__any(by_mass)) {
-    // V weights below (1 - p) / V of the largest are together less than what may be missing
-    const float range = (__builtin_amdgcn_logf((float)a.V) - __builtin_amdgcn_logf((float)(1.0 - set.p)) + 1.0f) / (float)c;
-    short_search<true>(row, s, by_mass, m, range, c, S, [&](uint64_t t) { return share_up(set.p, t); }, &cut);
+    short_search<true>(row, s, by_mass, m, set.octaves * __builtin_amdgcn_rcpf((float)c), c, S, [&](uint64_t t) { return share_up(set.p, t); }, &cut);
   }
   if (__any(live && set.least > 0.0)) {
     const float least = from_ordered(least_key(set.least, m, set.T));
@@ -515,7 +556,7 @@ __global__ void __launch_bounds__(256, SHORT_OCC) k_sample_short(SampleArgs a, i
   if (live && at >= want && at - w < want) {
     const int v = (who & 15) * PL + l15;
     a.symbol[r] = v;
-    a.bits[r] = (float)(log2((double)total) - S - ((double)s.x[rw][v] - (double)m) * c);
+    a.bits[r] = (float)(log2_of(total) - S - ((double)s.x[rw][l15 * 16 + (who & 15)] - (double)m) * c);
   }
   if (!live && l15 == 0 && r0 + rw < rows) {
     a.symbol[r] = -1;
@@ -649,7 +690,7 @@ __device__ __forceinline__ bool search(const L& row, S& s, uint32_t lo, float m,
   const float range = fminf(m - low, (float)fmin(40.0 / c, 3e38));
   const float scale = range > 0.0f ? fminf((float)BINS / range, 3e38f) : 0.0f;
   const auto bin_of = [&](float x) { return (int)fminf((m - x) * scale, (float)(BINS - 1)); };
-  const auto measure = [&](float x) -> uint64_t { return MASS ? units((double)x - (double)m, c, (double)bits) : 1ull; };
+  const auto measure = [&](float x) -> uint64_t { return MASS ? units(x, (double)m, c, (double)bits) : 1ull; };
   clear<THREADS>(s.hist);
   __syncthreads();
   row.each([&](int, const float (&x)[N]) {
@@ -839,8 +880,8 @@ __global__ void __launch_bounds__(THREADS) k_sample_long(SampleArgs a) {
     }
     return;
   }
-  const double c = set.T > 0.0 ? LOG2E_D / set.T : 0.0;
-  const auto weight = [&](float x) { return units((double)x - (double)m, c, (double)a.S); };
+  const double c = set.c;
+  const auto weight = [&](float x) { return units(x, (double)m, c, (double)a.S); };
 
   // the cut: logits of an ordered value above `cut` are kept, of those that equal it the first `ties` (ALL: all)
   uint32_t cut = FIRST_LIVE, ties = ALL;
@@ -897,7 +938,7 @@ __global__ void __launch_bounds__(THREADS) k_sample_long(SampleArgs a) {
   }
   if (tid == 0) {
     a.symbol[r] = index;
-    a.bits[r] = (float)(log2((double)total) - a.S - ((double)z - (double)m) * c);
+    a.bits[r] = (float)(log2_of(total) - a.S - ((double)z - (double)m) * c);
   }
 }
 
@@ -936,6 +977,8 @@ hipError_t launch_sample(const reno_sample& p, const void* logits, const float* 
     a.V = p.symbols;
     a.S = unit_bits(p.symbols);
     a.T = p.temperature;
+    a.c = a.T > 0.0 ? LOG2E_D / a.T : 0.0;
+    a.octaves = octaves_of(a.V, p.top_p);
     a.p = p.top_p;
     a.least = p.min_p;
     a.k = p.top_k;
