@@ -221,7 +221,7 @@ __device__ __forceinline__ int row16_which(bool here) {
 
 // Shared memory of a wave.
 struct ShortShared {
-  uint64_t hist[SHORT_ROWS][SHORT_BINS];
+  uint64_t hist[SHORT_ROWS][SHORT_BINS + 16];   // 63 bins, then the last one of each lane: what lies far below meets there
   ulonglong2 cand[SHORT_ROWS][16];
   float x[SHORT_ROWS][16 * SHORT_LANE];   // the rows, for the turns that are rare: logit i of lane l at 16 i + l
 };
@@ -234,10 +234,12 @@ struct Short {
   int v0;             // the lane's first symbol
 };
 
-// The last logit of the row's order that is kept: logits above x, and those that equal it up to symbol v.
+// The last logit of the row's order that is kept: logits above x, and those that equal it up to symbol v.  split: there
+// are others that equal it behind v.
 struct ShortCut {
   float x;
   int v;
+  bool split;
 };
 
 // A search under way: `above` lies above the range that still holds the cut, `wanted` is what it has to reach.
@@ -285,10 +287,11 @@ __device__ __forceinline__ void short_pairs(const ShortShared& s, ShortSearch& q
     sum += j < (int)n && o.x >= me.x ? o.y : 0;
   }
   const int who = row16_which(there && sum >= q.wanted && sum - me.y < q.wanted);
-  const uint32_t o = __shfl((uint32_t)(me.x >> 8), who);
-  const int v = 255 - (__shfl((int)me.x, who) & 255);
-  cut->x = few ? from_ordered(o) : cut->x;
-  cut->v = few ? v : cut->v;
+  const uint64_t last = __shfl((uint64_t)me.x, who);
+  const bool behind = there && me.x < last && me.x >> 8 == last >> 8;
+  cut->x = few ? from_ordered((uint32_t)(last >> 8)) : cut->x;
+  cut->v = few ? 255 - (int)(last & 255) : cut->v;
+  cut->split = few ? (__ballot(behind) >> (lane & 48) & 0xffffu) != 0 : cut->split;
   q.active = q.active && !few;
   wave_lds_fence();
 }
@@ -349,6 +352,7 @@ __device__ __forceinline__ void short_more(ShortShared& s, ShortSearch& q, int v
       v = __shfl(v, who);
       cut->x = same ? from_ordered(kmax) : cut->x;
       cut->v = same ? v : cut->v;
+      cut->split |= same;
       q.active = q.active && !same;
     }
     if (!__any(q.active)) break;
@@ -388,18 +392,27 @@ __device__ __forceinline__ void short_search(const Short<PL>& row, ShortShared& 
   const float scale = active ? (range > 0.0f ? fminf((float)SHORT_BINS / fminf(range, 3e38f), 3e38f) : 1.0f) : NAN;
   const auto bin_of = [&](float x) { return (m - x) * scale; };   // NaN where the row is not searched
 #pragma unroll
-  for (int i = 0; i < PER; ++i) s.hist[rw][l15 * PER + i] = 0;
+  for (int i = 0; i < PER + 1; ++i) s.hist[rw][i * 16 + l15] = 0;
   wave_lds_fence();
+  const float last = (float)(SHORT_BINS - 1 + l15);
 #pragma unroll
-  for (int i = 0; i < PL; ++i)   // (a row that is not searched adds to its last bin)
-    atomicAdd((unsigned long long*)&s.hist[rw][(uint32_t)fminf(bin_of(row.x[i]), (float)(SHORT_BINS - 1))],
-              MASS ? (unsigned long long)row.w[i] : 1ull);
+  for (int i = 0; i < PL; ++i)
+    atomicAdd((unsigned long long*)&s.hist[rw][(uint32_t)fminf(bin_of(row.x[i]), last)], MASS ? (unsigned long long)row.w[i] : 1ull);
   wave_lds_fence();
   uint64_t h[PER], mine = 0;
 #pragma unroll
-  for (int i = 0; i < PER; ++i) mine += h[i] = s.hist[rw][l15 * PER + i];
-  const uint64_t upto = row16_scan(mine);
-  const uint64_t all = row16_last(upto);
+  for (int i = 0; i < PER; ++i) {
+    h[i] = i < PER - 1 || l15 < 15 ? s.hist[rw][l15 * PER + i] : 0;
+    mine += h[i];
+  }
+  uint64_t upto = row16_scan(mine);
+  const uint64_t far = row16_last(row16_scan(s.hist[rw][SHORT_BINS - 1 + l15]));
+  const uint64_t all = row16_last(upto) + far;
+  if (l15 == 15) {
+    h[PER - 1] += far;
+    mine += far;
+    upto += far;
+  }
   q.wanted = want(all);
   q.active = active && q.wanted <= all;
   const int bin = short_bin(s, q, h, mine, upto);
@@ -410,16 +423,26 @@ __device__ __forceinline__ void short_search(const Short<PL>& row, ShortShared& 
     const float b = bin_of(x);
     return b >= b0 && b <= b1;
   };
-  uint32_t n = 0;
+  uint32_t which = 0;
 #pragma unroll
-  for (int i = 0; i < PL; ++i) n += in(row.x[i]) ? 1 : 0;
+  for (int i = 0; i < PL; ++i) which |= in(row.x[i]) ? 1u << i : 0u;
+  const uint32_t n = (uint32_t)__builtin_popcount(which);
   const uint32_t upto_n = row16_scan(n);
   const uint32_t all_n = row16_last(upto_n);
   const bool few = q.active && all_n <= 16;
-  uint32_t at = upto_n - n;
-#pragma unroll
-  for (int i = 0; i < PL; ++i)
-    if (in(row.x[i]) && few) s.cand[rw][at++] = make_ulonglong2(place_of(row.x[i], row.v0 + i), MASS ? row.w[i] : 1);
+  uint32_t* list = reinterpret_cast<uint32_t*>(s.hist[rw]);   // the bins are done with
+  wave_lds_fence();
+  which = few ? which : 0;
+  for (uint32_t at = upto_n - n; __any(which != 0); ++at) {
+    if (which) list[at] = (uint32_t)__builtin_ctz(which) * 16u + (uint32_t)l15;
+    which &= which - 1u;
+  }
+  wave_lds_fence();
+  if (few && l15 < (int)all_n) {
+    const uint32_t p = list[l15];
+    const float x = s.x[rw][p];
+    s.cand[rw][l15] = make_ulonglong2(place_of(x, (int)(p & 15u) * PL + (int)(p >> 4)), MASS ? units(x, (double)m, c, S) : 1);
+  }
   short_pairs(s, q, few, all_n, cut);
   if (__any(q.active)) short_more<MASS, PL>(s, q, row.v0, m, c, S, in, cut);
 }
@@ -495,7 +518,7 @@ __global__ void __launch_bounds__(256, SHORT_OCC) k_sample_short(SampleArgs a, i
   const double c = set.c;
 #pragma unroll
   for (int i = 0; i < PL; i += PL < 4 ? 1 : 4) units_all<PL < 4 ? 1 : 4>(row.x + i, (double)m, c, S, row.w + i);
-  ShortCut cut{-INFINITY, 255};
+  ShortCut cut{-INFINITY, 255, false};
   const bool by_count = live && set.k > 0 && set.k < a.V;
   if (__any(by_count)) {
     float low = INFINITY;
@@ -518,15 +541,19 @@ __global__ void __launch_bounds__(256, SHORT_OCC) k_sample_short(SampleArgs a, i
   }
   if (__any(live && set.least > 0.0)) {
     const float least = from_ordered(least_key(set.least, m, set.T));
-    if (live && set.least > 0.0 && least > cut.x) cut = ShortCut{least, 255};
+    if (live && set.least > 0.0 && least > cut.x) cut = ShortCut{least, 255, false};
   }
   uint64_t mine = 0;
   const float over = next_above(cut.x);
+  if (__any(cut.split)) {   // among logits that equal the last one
 #pragma unroll
-  for (int i = 0; i < PL; ++i) {
-    row.w[i] = is_kept(row.x[i], i, cut.x, over, cut.v - row.v0) ? row.w[i] : 0;
-    mine += row.w[i];
+    for (int i = 0; i < PL; ++i) row.w[i] = is_kept(row.x[i], i, cut.x, over, cut.v - row.v0) ? row.w[i] : 0;
+  } else {
+#pragma unroll
+    for (int i = 0; i < PL; ++i) row.w[i] = row.x[i] >= cut.x ? row.w[i] : 0;
   }
+#pragma unroll
+  for (int i = 0; i < PL; ++i) mine += row.w[i];
   uint64_t upto = row16_scan(mine);
   const uint64_t total = row16_last(upto);
   const uint64_t want = share_down(set.u, total) + 1;
