@@ -177,8 +177,8 @@ constexpr int SHORT_BINS = 64;
 
 template <int CTRL>
 __device__ __forceinline__ uint64_t dpp64(uint64_t v) {   // lanes without a source: 0
-  const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, 0xF, 0xF, false);
-  const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(v >> 32), CTRL, 0xF, 0xF, false);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, 0xF, 0xF, true);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(v >> 32), CTRL, 0xF, 0xF, true);
   return (uint64_t)hi << 32 | lo;
 }
 __device__ __forceinline__ uint64_t row16_scan(uint64_t v) {   // inclusive
@@ -188,10 +188,10 @@ __device__ __forceinline__ uint64_t row16_scan(uint64_t v) {   // inclusive
   return v + dpp64<0x118>(v);
 }
 __device__ __forceinline__ uint32_t row16_scan(uint32_t v) {
-  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xF, 0xF, false);
-  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xF, 0xF, false);
-  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xF, 0xF, false);
-  return v + (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xF, 0xF, false);
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xF, 0xF, true);
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xF, 0xF, true);
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xF, 0xF, true);
+  return v + (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xF, 0xF, true);
 }
 __device__ __forceinline__ uint32_t row16_max(uint32_t v) {
   v = max(v, dpp<0x128>(v));
@@ -425,7 +425,7 @@ __device__ __forceinline__ void short_search(const Short<PL>& row, ShortShared& 
   };
   uint32_t which = 0;
 #pragma unroll
-  for (int i = 0; i < PL; ++i) which |= in(row.x[i]) ? 1u << i : 0u;
+  for (int i = PL - 1; i >= 0; --i) which = which + which + (in(row.x[i]) ? 1u : 0u);
   const uint32_t n = (uint32_t)__builtin_popcount(which);
   const uint32_t upto_n = row16_scan(n);
   const uint32_t all_n = row16_last(upto_n);
