@@ -595,30 +595,43 @@ __global__ void __launch_bounds__(256, SHORT_OCC) k_sample_short(SampleArgs a, i
 // A block a row.
 
 constexpr int BINS = 1024;
+constexpr int LIST = 512;       // logits that are compared with one another
+constexpr int LIST_K = 256;     // counts up to this are cut in a list of what the maxima of groups bound from below
 
-__device__ __forceinline__ uint64_t wave_sum(uint64_t v) {
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
-  return v;
+__device__ __forceinline__ uint64_t wave_sum(uint64_t v) {   // in every lane
+  v = row16_scan(v);
+  v = __shfl(v, lane_id() | 15);
+  v += __shfl_xor(v, 16);
+  return v + __shfl_xor(v, 32);
 }
 __device__ __forceinline__ uint64_t wave_scan(uint64_t v) {   // inclusive
-  for (int o = 1; o < 64; o <<= 1) {
-    const uint64_t w = __shfl_up(v, o);
-    if (lane_id() >= o) v += w;
-  }
-  return v;
+  v = row16_scan(v);
+  const uint64_t rows = v;
+  const uint64_t r0 = __shfl(rows, 15), r1 = __shfl(rows, 31), r2 = __shfl(rows, 47);
+  const int rw = lane_id() >> 4;
+  return v + (rw > 0 ? r0 : 0) + (rw > 1 ? r1 : 0) + (rw > 2 ? r2 : 0);
 }
+
+// A row's last logit that is kept: those above x are, and those equal to it up to symbol v.
+struct Cut {
+  float x;
+  int v;
+  __device__ __forceinline__ bool keeps(float z, int i) const { return z > x || (z == x && i <= v); }
+};
 
 // THREADS a row; KEEP: the row is held in LDS (else read again each time).  A wave's pieces of 16 bytes follow one
 // another: the row's order is by wave, then by turn, then by lane.  A thread reads only what it wrote itself.
 template <int TYPE, int THREADS, bool KEEP>
 struct Long {
   static constexpr int N = Vec<TYPE>::N, WAVES = THREADS / 64, SIZE = 16 / N;
+  static constexpr bool KEPT = KEEP;
   static constexpr uint32_t DEAD = TYPE == RENO_T_FP32 ? 0xff800000u : TYPE == RENO_T_BF16 ? 0xff80ff80u : 0xfc00fc00u;
   const char* z;
   const uint8_t* allowed;
   uint4* kept;
   int V, turns, first;      // first: this thread's first piece
 
+  // a piece; -inf where there is no logit
   __device__ __forceinline__ uint4 read(int piece) const {
     uint32_t w[4] = {DEAD, DEAD, DEAD, DEAD};
     const int v = piece * N;
@@ -651,13 +664,17 @@ struct Long {
     }
   }
   __device__ __forceinline__ int index(int turn, int e) const { return (first + turn * 64) * N + e; }
+  __device__ __forceinline__ Vec<TYPE> at(int turn) const {
+    Vec<TYPE> x;
+    if constexpr (KEEP) x.from(kept[turn * THREADS + threadIdx.x]);
+    else x.from(read(first + turn * 64));
+    return x;
+  }
   // f(turn, logits) for every turn of the thread
   template <typename F>
   __device__ __forceinline__ void each(const F& f) const {
     for (int t = 0; t < turns; ++t) {
-      Vec<TYPE> x;
-      if constexpr (KEEP) x.from(kept[t * THREADS + threadIdx.x]);
-      else x.from(read(first + t * 64));
+      const Vec<TYPE> x = at(t);
       f(t, x.x);
     }
   }
@@ -666,29 +683,32 @@ struct Long {
 // Shared memory of a row.
 template <int WAVES>
 struct Shared {
-  uint64_t hist[BINS];
+  uint64_t hist[BINS + 64];   // the last bin is one of each lane's: what lies far below meets there; then weights
+  uint64_t list[LIST];        // places: the ordered value, then the index complemented
   uint64_t part[WAVES];
-  float top[WAVES], low[WAVES];
+  uint64_t above, total, before;
   uint32_t lo, hi;
-  uint64_t total, above, at;
-  int bin, live[WAVES], index;
+  float top[WAVES], x;
+  int odd[WAVES], count[2 * WAVES];
+  int bin, n, wave, turn, index;
 };
 
-template <int THREADS>
-__device__ __forceinline__ void clear(uint64_t* hist) {
-  for (int i = threadIdx.x; i < BINS; i += THREADS) hist[i] = 0;
-}
+__device__ __forceinline__ uint64_t place64(float x, int v) { return (uint64_t)ordered(x) << 32 | (uint32_t)~v; }
+__device__ __forceinline__ float x_of(uint64_t place) { return from_ordered((uint32_t)(place >> 32)); }
+__device__ __forceinline__ int v_of(uint64_t place) { return (int)~(uint32_t)place; }
 
-// Wave 0: the first bin at whose end `want` of what `above` and the bins hold is reached.  want(total) is asked
-// with what all bins hold; false: more than there is, nothing is set but s.total.
+// Wave 0: the first bin at whose end `want` of what `above` and the bins hold is reached, and what lies above it.
+// want(total) is asked with what all bins hold; bin -1: more than there is.
 template <int WAVES, typename F>
 __device__ __forceinline__ void find_bin(Shared<WAVES>& s, uint64_t above, const F& want) {
   if (threadIdx.x < 64) {
     constexpr int PER = BINS / 64;
     const int lane = lane_id();
-    uint64_t mine = 0;
+    const uint64_t far = wave_sum(s.hist[BINS - 1 + lane]);   // (slot BINS - 1 + 64 lies past the lanes')
+    uint64_t mine = lane == 63 ? far : 0;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) mine += s.hist[lane * PER + i];
+    for (int i = 0; i < PER - 1; ++i) mine += s.hist[lane * PER + i];
+    if (lane < 63) mine += s.hist[lane * PER + PER - 1];
     const uint64_t upto = wave_scan(mine);
     const uint64_t total = __shfl(upto, 63);
     const uint64_t w = want(total);
@@ -699,160 +719,227 @@ __device__ __forceinline__ void find_bin(Shared<WAVES>& s, uint64_t above, const
     }
     if (a < w && a + mine >= w) {
       int i = lane * PER;
-      while (a + s.hist[i] < w) a += s.hist[i++];
+      while (i < BINS - 1 && a + s.hist[i] < w) a += s.hist[i++];
       s.bin = i;
       s.above = a;
-      s.at = s.hist[i];
     }
   }
 }
 
-// The largest ordered value, from `lo` up, that leaves `want` of the measure (logits, or with MASS their weights) at
-// it and above.  False: all of them are less.  above: what lies above it.
-template <bool MASS, typename L, typename S, typename F>
-__device__ __forceinline__ bool search(const L& row, S& s, uint32_t lo, float m, float low, double c, int bits, const F& want,
-                       uint32_t* cut, uint64_t* above, uint64_t* total) {
-  constexpr int N = L::N, THREADS = L::WAVES * 64;
-  // first histogram: by value, over 40 octaves of weight at most
-  const float range = fminf(m - low, (float)fmin(40.0 / c, 3e38));
-  const float scale = range > 0.0f ? fminf((float)BINS / range, 3e38f) : 0.0f;
-  const auto bin_of = [&](float x) { return (int)fminf((m - x) * scale, (float)(BINS - 1)); };
-  const auto measure = [&](float x) -> uint64_t { return MASS ? units(x, (double)m, c, (double)bits) : 1ull; };
-  clear<THREADS>(s.hist);
+// The symbol at which the sum of the measure (COUNT: 1, else the weight) along the row of logits that are kept reaches
+// want(total), at least 1, and its logit.
+template <bool COUNT, typename L, typename S, typename K, typename W>
+__device__ __forceinline__ void pick(const L& row, S& s, const K& keeps, double m, double c, double bits, const W& want,
+                                     int* index, float* logit, uint64_t* total) {
+  constexpr int N = L::N, WAVES = L::WAVES;
+  extern __shared__ uint4 s_row[];
+  // a sum of each turn of a wave, behind the row; and place for a turn's logits, where the histogram was
+  uint64_t* sums = reinterpret_cast<uint64_t*>(s_row + (L::KEPT ? row.turns * WAVES * 64 : 0));
+  const int lane = lane_id(), wave = threadIdx.x >> 6;
   __syncthreads();
-  row.each([&](int, const float (&x)[N]) {
+  for (int t = 0; t < row.turns; ++t) {
+    const auto x = row.at(t);
+    uint64_t mine = 0;
+    if constexpr (COUNT) {
+#pragma unroll
+      for (int e = 0; e < N; ++e) mine += keeps(x.x[e], row.index(t, e)) ? 1 : 0;
+    } else {
+#pragma unroll
+      for (int e0 = 0; e0 < N; e0 += 4) {
+        bool k[4], some = false;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) some |= k[e] = keeps(x.x[e0 + e], row.index(t, e0 + e));
+        if (__any(some)) {
+          uint64_t w[4];
+          units_all<4>(x.x + e0, m, c, bits, w);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) mine += k[e] ? w[e] : 0;
+        }
+      }
+    }
+    mine = wave_sum(mine);
+    if (lane == 0) sums[wave * row.turns + t] = mine;
+  }
+  __syncthreads();
+  if (wave == 0) {
+    const int n = WAVES * row.turns, per = (n + 63) / 64;
+    uint64_t mine = 0;
+    for (int i = lane * per; i < min(n, (lane + 1) * per); ++i) mine += sums[i];
+    const uint64_t upto = wave_scan(mine);
+    const uint64_t all = __shfl(upto, 63);
+    const uint64_t w = want(all);
+    uint64_t a = upto - mine;
+    if (lane == 0) s.total = all;
+    if (a < w && a + mine >= w) {
+      int i = lane * per;
+      while (a + sums[i] < w) a += sums[i++];
+      s.wave = i / row.turns;
+      s.turn = i % row.turns;
+      s.before = a;
+    }
+  }
+  __syncthreads();
+  *total = s.total;
+  const uint64_t w = want(s.total);
+  if (wave == s.wave) {
+    const int t = s.turn;
+    const auto x = row.at(t);
+    uint64_t v[N], mine = 0;
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      v[e] = keeps(x.x[e], row.index(t, e)) ? (COUNT ? 1 : units(x.x[e], m, c, bits)) : 0;
+      mine += v[e];
+    }
+    uint64_t a = s.before + wave_scan(mine) - mine;
+    if (a < w && a + mine >= w) {
+      bool here = false;
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        a += v[e];
+        if (!here && a >= w) {
+          here = true;
+          s.index = row.index(t, e);
+          s.x = x.x[e];
+        }
+      }
+    }
+  }
+  __syncthreads();
+  *index = s.index;
+  *logit = s.x;
+}
+
+// The logit of the row's order at which `want` of the measure (logits, or with MASS their weights) of those that
+// `from` keeps is reached; want(total) is asked with the measure of all, and more than that leaves `from`.
+// range: how far below the largest, m, the cut lies at most, or is worth bins.
+template <bool MASS, typename L, typename S, typename F>
+__device__ __forceinline__ Cut search(const L& row, S& s, const Cut from, float m, float range, double c, double bits,
+                                      const F& want) {
+  constexpr int N = L::N, THREADS = L::WAVES * 64;
+  const int tid = threadIdx.x;
+  const float scale = range > 0.0f ? fminf((float)BINS / fminf(range, 3e38f), 3e38f) : 1.0f;
+  const auto bin_of = [&](float x) { return (m - x) * scale; };
+  const auto clear = [&] {
+    for (int i = tid; i < BINS + 64; i += THREADS) s.hist[i] = 0;
+    __syncthreads();
+  };
+  clear();
+  const float last = (float)(BINS - 1 + lane_id());
+  row.each([&](int t, const float (&x)[N]) {
+#pragma unroll
+    for (int e0 = 0; e0 < N; e0 += 4) {
+      uint64_t w[4];
+      if constexpr (MASS) units_all<4>(x + e0, (double)m, c, bits, w);
+#pragma unroll
+      for (int e = e0; e < e0 + 4; ++e)
+        if (from.keeps(x[e], row.index(t, e)))
+          atomicAdd((unsigned long long*)&s.hist[(uint32_t)fminf(bin_of(x[e]), last)], MASS ? (unsigned long long)w[e - e0] : 1ull);
+    }
+  });
+  if (tid == 0) s.n = 0;
+  __syncthreads();
+  find_bin(s, 0, want);
+  __syncthreads();
+  const uint64_t wanted = want(s.total);
+  const int bin = s.bin;
+  if (bin < 0) return from;
+  uint64_t above = s.above;
+  // the bin's logits
+  const float b0 = (float)bin, b1 = bin == BINS - 1 ? INFINITY : next_below((float)(bin + 1));
+  const auto in_bin = [&](float x, int v) {
+    const float b = bin_of(x);
+    return b >= b0 && b <= b1 && from.keeps(x, v);
+  };
+  row.each([&](int t, const float (&x)[N]) {
 #pragma unroll
     for (int e = 0; e < N; ++e)
-      if (ordered(x[e]) >= lo) atomicAdd((unsigned long long*)&s.hist[bin_of(x[e])], (unsigned long long)measure(x[e]));
+      if (in_bin(x[e], row.index(t, e))) {
+        const int i = atomicAdd(&s.n, 1);
+        if (i < LIST) s.list[i] = place64(x[e], row.index(t, e));
+      }
   });
   __syncthreads();
-  uint64_t wanted = 0;
-  find_bin(s, 0, [&](uint64_t t) { return wanted = want(t); });
-  if (threadIdx.x == 0) {
+  const int n = s.n;
+  if (n <= LIST) {   // sums of all pairs
+    for (int i = tid; i < n; i += THREADS) s.hist[i] = MASS ? units(x_of(s.list[i]), (double)m, c, bits) : 1;
+    __syncthreads();
+    for (int i = tid; i < n; i += THREADS) {
+      const uint64_t me = s.list[i];
+      uint64_t sum = above;
+      for (int j = 0; j < n; ++j) sum += s.list[j] >= me ? s.hist[j] : 0;
+      if (sum >= wanted && sum - s.hist[i] < wanted) {
+        s.x = x_of(me);
+        s.index = v_of(me);
+      }
+    }
+    __syncthreads();
+    return Cut{s.x, s.index};
+  }
+  // too many: histograms of ordered values over what the bin spans, until one value is left
+  if (tid == 0) {
     s.lo = ALL;
     s.hi = 0;
   }
   __syncthreads();
-  *total = s.total;
-  if (s.bin < 0) return false;
-  const int bin = s.bin;
-  uint64_t a = s.above;
-  if (threadIdx.x == 0) s.part[0] = wanted;
-  // the bin's own range of ordered values
   uint32_t kmin = ALL, kmax = 0;
-  row.each([&](int, const float (&x)[N]) {
+  row.each([&](int t, const float (&x)[N]) {
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-      const uint32_t o = ordered(x[e]);
-      const bool in = o >= lo && bin_of(x[e]) == bin;
-      kmin = in ? min(kmin, o) : kmin;
-      kmax = in ? max(kmax, o) : kmax;
-    }
+    for (int e = 0; e < N; ++e)
+      if (in_bin(x[e], row.index(t, e))) {
+        kmin = min(kmin, ordered(x[e]));
+        kmax = max(kmax, ordered(x[e]));
+      }
   });
   if (kmax) {
     atomicMin(&s.lo, kmin);
     atomicMax(&s.hi, kmax);
   }
   __syncthreads();
-  uint32_t from = s.lo, to = s.hi;
-  wanted = s.part[0];
-  // histograms of ordered values, each over one bin of the last
-  while (from != to) {
-    const int width = 32 - __builtin_clz(to - from);   // to - from < 2^width
-    const int shift = max(0, width - 10);
-    __syncthreads();
-    clear<THREADS>(s.hist);
-    __syncthreads();
-    row.each([&](int, const float (&x)[N]) {
+  uint32_t lo = s.lo, hi = s.hi;
+  while (lo != hi) {
+    const int shift = max(0, 22 - (int)__builtin_clz(hi - lo));   // hi - lo < BINS << shift
+    clear();
+    row.each([&](int t, const float (&x)[N]) {
 #pragma unroll
       for (int e = 0; e < N; ++e) {
-        const uint32_t o = ordered(x[e]);
-        if (o >= from && o <= to) atomicAdd((unsigned long long*)&s.hist[(to - o) >> shift], (unsigned long long)measure(x[e]));
+        const uint32_t o = ordered(x[e]), b = (hi - o) >> shift;
+        if (o >= lo && o <= hi && from.keeps(x[e], row.index(t, e)))
+          atomicAdd((unsigned long long*)&s.hist[b], MASS ? (unsigned long long)units(x[e], (double)m, c, bits) : 1ull);
       }
     });
     __syncthreads();
-    find_bin(s, a, [&](uint64_t) { return wanted; });
+    find_bin(s, above, [&](uint64_t) { return wanted; });
     __syncthreads();
-    a = s.above;
-    const uint32_t b = (uint32_t)s.bin;
-    const uint32_t top = to - (b << shift);
-    from = max(from, top - ((1u << shift) - 1u));
-    to = top;
+    above = s.above;
+    hi -= (uint32_t)s.bin << shift;
+    lo = max(lo, hi - min(hi, (1u << shift) - 1u));
+    __syncthreads();
   }
-  __syncthreads();
-  *cut = to;
-  *above = a;
-  return true;
-}
-
-// The index of the logit at which the sum of value(index, logit) along the row reaches want (at least 1), and that
-// logit.  total: the sum of all, by which want is asked for.
-template <typename L, typename S, typename V, typename W>
-__device__ __forceinline__ void locate(const L& row, S& s, const V& value, const W& want, int* index, float* logit, uint64_t* total) {
-  constexpr int N = L::N, WAVES = L::WAVES;
-  const int lane = lane_id(), wave = threadIdx.x >> 6;
-  uint64_t mine = 0;
-  row.each([&](int t, const float (&x)[N]) {
-#pragma unroll
-    for (int e = 0; e < N; ++e) mine += value(row.index(t, e), x[e]);
-  });
-  mine = wave_sum(mine);
-  __syncthreads();
-  if (lane == 0) s.part[wave] = mine;
-  __syncthreads();
-  uint64_t all = 0;
-  for (int i = 0; i < WAVES; ++i) all += s.part[i];
-  *total = all;
-  const uint64_t w = want(all);
-  uint64_t before = 0;
-  int at = 0;
-  while (at < WAVES - 1 && before + s.part[at] < w) before += s.part[at++];
-  if (wave == at) {
-    bool found = false;
-    row.each([&](int t, const float (&x)[N]) {
-      if (found) return;
-      uint64_t part = 0;
-#pragma unroll
-      for (int e = 0; e < N; ++e) part += value(row.index(t, e), x[e]);
-      const uint64_t upto = wave_scan(part);
-      const uint64_t turn = __shfl(upto, 63);
-      if (before + turn >= w) {
-        found = true;
-        uint64_t a = before + upto - part;
-        if (a < w && a + part >= w) {
-          bool here = false;
-#pragma unroll
-          for (int e = 0; e < N; ++e) {
-            a += value(row.index(t, e), x[e]);
-            if (!here && a >= w) {
-              here = true;
-              s.index = row.index(t, e);
-              s.top[0] = x[e];
-            }
-          }
-        }
-      }
-      before += turn;
-    });
-  }
-  __syncthreads();
-  *index = s.index;
-  *logit = s.top[0];
+  const float x = from_ordered(hi);
+  const uint64_t each = MASS ? units(x, (double)m, c, bits) : 1;
+  const uint64_t ties = (wanted - above + each - 1) / max(each, (uint64_t)1);
+  int index;
+  float z;
+  uint64_t all;
+  pick<true>(row, s, [&](float y, int v) { return y == x && from.keeps(y, v); }, 0.0, 0.0, 0.0,
+             [&](uint64_t) { return ties; }, &index, &z, &all);
+  return Cut{x, index};
 }
 
 template <int TYPE, int THREADS, bool KEEP>
 __global__ void __launch_bounds__(THREADS) k_sample_long(SampleArgs a) {
   typedef Long<TYPE, THREADS, KEEP> L;
-  constexpr int N = L::N, WAVES = L::WAVES;
+  constexpr int N = L::N, WAVES = L::WAVES, GROUPS = 4;
   __shared__ Shared<WAVES> s;
   const int64_t r = blockIdx.x;
   const int tid = threadIdx.x, lane = lane_id(), wave = tid >> 6;
   const Row set = settings(a, r);
+  const auto answer = [&](int symbol, float bits) {
+    a.symbol[r] = symbol;
+    a.bits[r] = bits;
+  };
   if (!(set.u >= 0.0f && set.u < 1.0f) || !set.valid) {
-    if (tid == 0) {
-      a.symbol[r] = -1;
-      a.bits[r] = set.u >= 0.0f && set.u < 1.0f ? NAN : 0.0f;
-    }
+    if (tid == 0) answer(-1, set.u >= 0.0f && set.u < 1.0f ? NAN : 0.0f);
     return;
   }
   L row;
@@ -863,110 +950,201 @@ __global__ void __launch_bounds__(THREADS) k_sample_long(SampleArgs a) {
   row.first = wave * row.turns * 64 + lane;
   extern __shared__ uint4 s_row[];
   row.kept = s_row;
-  if constexpr (KEEP) {
-    for (int t = 0; t < row.turns; ++t) s_row[t * THREADS + tid] = row.read(row.first + t * 64);
-  }
-  // the largest and the smallest logit, how many there are
-  float m = -INFINITY, low = INFINITY;
-  int live = 0;
-  bool bad = false;
-  row.each([&](int, const float (&x)[N]) {
+  // the largest logit, and the largest of the thread's groups
+  float group[GROUPS] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+  bool odd = false;
+  const auto look = [&](const uint4& raw) {
+    Vec<TYPE> x;
+    x.from(raw);
+    float top = -INFINITY;
 #pragma unroll
     for (int e = 0; e < N; ++e) {
-      const bool there = x[e] > -INFINITY;
-      bad |= !(x[e] < INFINITY);
-      m = fmaxf(m, x[e]);
-      low = there ? fminf(low, x[e]) : low;
-      live += there ? 1 : 0;
+      odd |= !(x.x[e] < INFINITY);
+      top = fmaxf(top, x.x[e]);
     }
-  });
-  for (int o = 32; o > 0; o >>= 1) {
-    m = fmaxf(m, __shfl_xor(m, o));
-    low = fminf(low, __shfl_xor(low, o));
-    live += __shfl_xor(live, o);
+    const float first = fmaxf(group[0], top);
+#pragma unroll
+    for (int g = 0; g + 1 < GROUPS; ++g) group[g] = group[g + 1];
+    group[GROUPS - 1] = first;
+  };
+  for (int t0 = 0; t0 < row.turns; t0 += 4) {   // four loads under way
+    uint4 raw[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (t0 + i < row.turns) raw[i] = row.read(row.first + (t0 + i) * 64);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (t0 + i < row.turns) {
+        if constexpr (KEEP) s_row[(t0 + i) * THREADS + tid] = raw[i];
+        look(raw[i]);
+      }
   }
-  const bool any_bad = __ballot(bad) != 0;
+  float m = fmaxf(fmaxf(group[0], group[1]), fmaxf(group[2], group[3]));
+  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+  const bool any_odd = __ballot(odd) != 0;
   if (lane == 0) {
     s.top[wave] = m;
-    s.low[wave] = low;
-    s.live[wave] = any_bad ? -1 : live;
+    s.odd[wave] = any_odd;
   }
+  if (tid == 0) s.n = 0;
   __syncthreads();
-  live = 0;
-  bad = false;
+  odd = false;
   for (int i = 0; i < WAVES; ++i) {
     m = fmaxf(m, s.top[i]);
-    low = fminf(low, s.low[i]);
-    bad |= s.live[i] < 0;
-    live += s.live[i];
+    odd |= s.odd[i] != 0;
   }
-  if (bad || live == 0) {
-    if (tid == 0) {
-      a.symbol[r] = -1;
-      a.bits[r] = bad ? NAN : 0.0f;
-    }
+  if (odd || m == -INFINITY) {
+    if (tid == 0) answer(-1, odd ? NAN : 0.0f);
     return;
   }
-  const double c = set.c;
-  const auto weight = [&](float x) { return units(x, (double)m, c, (double)a.S); };
+  const double c = set.c, S = (double)a.S;
+  const float least = from_ordered(least_key(set.least, m, set.T));
+  Cut cut{-INFINITY, -1};   // nothing is cut off
 
-  // the cut: logits of an ordered value above `cut` are kept, of those that equal it the first `ties` (ALL: all)
-  uint32_t cut = FIRST_LIVE, ties = ALL;
-  uint64_t above = 0, total = 0;
-  if (set.k == 1) {
-    cut = ordered(m);
-    ties = 1;
-  } else if (set.k > 0 && set.k < live) {
-    search<false>(row, s, FIRST_LIVE, m, low, c > 0.0 ? c : 1.0, 0, [&](uint64_t) { return (uint64_t)set.k; }, &cut, &above,
-                  &total);
-    ties = (uint32_t)(set.k - (int64_t)above);
-  }
-  if (set.p < 1.0 && set.k != 1) {
-    const uint32_t k_cut = cut, k_ties = ties;
-    const bool limited = ties != ALL;
-    const uint64_t each_tie = limited ? weight(from_ordered(k_cut)) : 0;
-    const bool found = search<true>(row, s, limited ? k_cut + 1 : FIRST_LIVE, m, low, c, a.S, [&](uint64_t t) {
-      return share_up(set.p, t + each_tie * (limited ? k_ties : 0));
-    }, &cut, &above, &total);
-    const uint64_t wanted = share_up(set.p, total + each_tie * (limited ? k_ties : 0));
-    if (!found) {   // among the logits that equal the last of the k
-      cut = k_cut;
-      above = total;
+  if (set.k > 0 && set.k <= LIST_K && set.k < a.V) {
+    // the largest 16-bit prefix that at least k groups' maxima reach bounds the k-th largest logit from below
+    uint32_t bound = 0;
+    for (int bit = 31; bit >= 16; --bit) {
+      const uint32_t next = bound | 1u << bit;
+      int n = 0;
+#pragma unroll
+      for (int g = 0; g < GROUPS; ++g) n += (int)__popcll(__ballot(ordered(group[g]) >= next));
+      int* b = s.count + (bit & 1) * WAVES;   // two buffers: one barrier a turn
+      if (lane == 0) b[wave] = n;
+      __syncthreads();
+      n = 0;
+      for (int i = 0; i < WAVES; ++i) n += b[i];
+      if (n >= (int)set.k) bound = next;
     }
-    const uint64_t w = weight(from_ordered(cut));
-    ties = (uint32_t)min((wanted - above + w - 1) / w, (uint64_t)(ALL - 1));
+    const float low = from_ordered(max(bound, FIRST_LIVE));
+    row.each([&](int t, const float (&x)[N]) {
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (x[e] >= low) {
+          const int i = atomicAdd(&s.n, 1);
+          if (i < LIST) s.list[i] = place64(x[e], row.index(t, e));
+        }
+    });
+    __syncthreads();
+    const int n = s.n;
+    if (n <= LIST) {   // all that is left to do concerns the list: ranks and sums of all pairs
+      for (int i = tid; i < n; i += THREADS) s.hist[i] = units(x_of(s.list[i]), (double)m, c, S);
+      __syncthreads();
+      // what each thread's logits weigh with all above them (two of a thread at most)
+      constexpr int PER = (LIST + THREADS - 1) / THREADS;
+      uint64_t upto[PER], mine = 0;
+      int rank[PER];
+#pragma unroll
+      for (int q = 0; q < PER; ++q) {
+        const int i = tid + q * THREADS;
+        upto[q] = 0;
+        rank[q] = 0;
+        if (i < n) {
+          const uint64_t me = s.list[i];
+          for (int j = 0; j < n; ++j) {
+            const bool up = s.list[j] >= me;
+            upto[q] += up ? s.hist[j] : 0;
+            rank[q] += up ? 1 : 0;
+          }
+          if (rank[q] <= set.k) mine += s.hist[i];
+        }
+      }
+      const auto block_total = [&](uint64_t v) {
+        v = wave_sum(v);
+        __syncthreads();
+        if (lane == 0) s.part[wave] = v;
+        __syncthreads();
+        v = 0;
+        for (int i = 0; i < WAVES; ++i) v += s.part[i];
+        return v;
+      };
+      const uint64_t mass = block_total(mine);
+      const uint64_t wanted = set.p < 1.0 ? share_up(set.p, mass) : mass;
+      mine = 0;
+#pragma unroll
+      for (int q = 0; q < PER; ++q) {
+        const int i = tid + q * THREADS;
+        if (i < n) {
+          const uint64_t w = s.hist[i];
+          const bool kept = rank[q] <= set.k && (set.p >= 1.0 || upto[q] - w < wanted) &&
+                            (x_of(s.list[i]) >= least || rank[q] == 1);
+          rank[q] = kept;
+          mine += kept ? w : 0;
+        } else {
+          rank[q] = 0;
+        }
+      }
+      const uint64_t total = block_total(mine);   // (its barriers: everyone has read the weights)
+      const uint64_t want = share_down(set.u, total) + 1;
+#pragma unroll
+      for (int q = 0; q < PER; ++q) {
+        const int i = tid + q * THREADS;
+        if (i < n && !rank[q]) s.list[i] = 0;   // no place: what is not kept
+      }
+      if (tid == 0) s.index = a.V;
+      __syncthreads();
+#pragma unroll
+      for (int q = 0; q < PER; ++q) {
+        const int i = tid + q * THREADS;
+        if (i < n && rank[q]) {
+          const uint64_t me = s.list[i];
+          if (want == 1) {   // a share of nothing: the first symbol of any weight, though it be less than a unit
+            if (((double)x_of(me) - (double)m) * c >= -1074.0) atomicMin(&s.index, v_of(me));
+          } else {
+            uint64_t sum = 0;
+            for (int j = 0; j < n; ++j) sum += s.list[j] && v_of(s.list[j]) <= v_of(me) ? s.hist[j] : 0;
+            if (sum >= want && sum - s.hist[i] < want) s.index = v_of(me);
+          }
+        }
+      }
+      __syncthreads();
+#pragma unroll
+      for (int q = 0; q < PER; ++q) {
+        const int i = tid + q * THREADS;
+        if (i < n && rank[q] && v_of(s.list[i]) == s.index)
+          answer(s.index, (float)(log2_of(total) - S - ((double)x_of(s.list[i]) - (double)m) * c));
+      }
+      return;
+    }
   }
-  const uint32_t least = least_key(set.least, m, set.T);
-  if (least > cut) {
-    cut = least;
-    ties = ALL;
+  if (set.k > 0 && set.k < a.V) {
+    if (set.k == 1) {
+      cut = Cut{m, -1};
+      int index;
+      float z;
+      uint64_t n;
+      pick<true>(row, s, [&](float x, int) { return x == m; }, 0.0, 0.0, 0.0, [&](uint64_t) { return (uint64_t)1; }, &index,
+                 &z, &n);
+      cut.v = index;
+    } else {
+      cut = search<false>(row, s, cut, m, (float)fmin(40.0 / c, 3e38), c, S, [&](uint64_t) { return (uint64_t)set.k; });
+    }
   }
-
+  if (set.p < 1.0)
+    cut = search<true>(row, s, cut, m, set.octaves * __builtin_amdgcn_rcpf((float)c), c, S,
+                       [&](uint64_t t) { return share_up(set.p, t); });
+  if (set.least > 0.0 && least > cut.x) cut = Cut{least, a.V};
   int index;
   float z;
-  // the index of the last of the ties
-  int last = a.V;
-  if (ties != ALL) {
-    uint64_t n;
-    locate(row, s, [&](int, float x) -> uint64_t { return ordered(x) == cut ? 1 : 0; },
-           [&](uint64_t all) { return min((uint64_t)ties, all); }, &last, &z, &n);
+  uint64_t total;
+  pick<false>(row, s, [&](float x, int v) { return cut.keeps(x, v); }, (double)m, c, S,
+              [&](uint64_t all) { return share_down(set.u, all) + 1; }, &index, &z, &total);
+  if (share_down(set.u, total) == 0) {   // a share of nothing: the first symbol of any weight, though it be less than a unit
+    int first = a.V;
+    row.each([&](int t, const float (&x)[N]) {
+#pragma unroll
+      for (int e = N - 1; e >= 0; --e)
+        if (cut.keeps(x[e], row.index(t, e)) && ((double)x[e] - (double)m) * c >= -1074.0) first = min(first, row.index(t, e));
+    });
+    __syncthreads();
+    if (tid == 0) s.index = a.V;
+    __syncthreads();
+    atomicMin(&s.index, first);
+    __syncthreads();
+    index = s.index;
+    z = logit<TYPE>(row.z, index);
   }
-  // a share of nothing: the first symbol of any weight, though it be less than a unit
-  for (bool any = false;; any = true) {
-    uint64_t sum;
-    locate(row, s, [&](int v, float x) -> uint64_t {
-      const uint32_t o = ordered(x);
-      if (!(o > cut || (o == cut && v <= last))) return 0;
-      return any ? (((double)x - (double)m) * c >= -1074.0 ? 1 : 0) : weight(x);
-    }, [&](uint64_t all) { return any ? 1 : share_down(set.u, all) + 1; }, &index, &z, &sum);
-    if (any) break;
-    total = sum;
-    if (share_down(set.u, total) > 0) break;
-  }
-  if (tid == 0) {
-    a.symbol[r] = index;
-    a.bits[r] = (float)(log2_of(total) - a.S - ((double)z - (double)m) * c);
-  }
+  if (tid == 0) answer(index, (float)(log2_of(total) - S - ((double)z - (double)m) * c));
 }
 
 template <int TYPE>
@@ -981,7 +1159,8 @@ void run(const SampleArgs& a, int64_t rows, hipStream_t st) {
   }
   const int pieces = (a.V + Vec<TYPE>::N - 1) / Vec<TYPE>::N;
   const auto go = [&](auto kern, int threads, bool keep) {
-    const unsigned lds = keep ? 16 * ((pieces + threads - 1) / threads * threads) : 0;
+    const int turns = (pieces + threads - 1) / threads;
+    const unsigned lds = (keep ? 16 * turns * threads : 0) + 8 * turns * (threads / 64);   // the row, a sum of each turn
     hipLaunchKernelGGL(kern, dim3((unsigned)rows), dim3(threads), lds, st, a);
   };
   if (pieces <= 512) go(k_sample_long<TYPE, 64, true>, 64, true);
