@@ -617,6 +617,8 @@ struct Cut {
   float x;
   int v;
   __device__ __forceinline__ bool keeps(float z, int i) const { return z > x || (z == x && i <= v); }
+  // from where on logits are kept whose symbols are v0 .. v0 + n - 1, all of them on one side of v; else NaN
+  __device__ __forceinline__ float from(int v0, int n) const { return v >= v0 + n - 1 ? x : v < v0 ? next_above(x) : NAN; }
 };
 
 // THREADS a row; KEEP: the row is held in LDS (else read again each time).  A wave's pieces of 16 bytes follow one
@@ -726,34 +728,57 @@ __device__ __forceinline__ void find_bin(Shared<WAVES>& s, uint64_t above, const
   }
 }
 
-// The symbol at which the sum of the measure (COUNT: 1, else the weight) along the row of logits that are kept reaches
-// want(total), at least 1, and its logit.
-template <bool COUNT, typename L, typename S, typename K, typename W>
-__device__ __forceinline__ void pick(const L& row, S& s, const K& keeps, double m, double c, double bits, const W& want,
+// f(e, kept) for the N logits of a lane in a turn; in the turn that holds the cut's symbol each is asked for itself.
+template <typename L, typename F>
+__device__ __forceinline__ void kept_of(const L& row, const Cut& cut, int t, const float (&x)[L::N], const F& f) {
+  constexpr int N = L::N;
+  const float from = cut.from(__builtin_amdgcn_readfirstlane(row.index(t, 0)), 64 * N);
+  if (from == from) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) f(e, x[e] >= from);
+  } else {
+#pragma unroll
+    for (int e = 0; e < N; ++e) f(e, cut.keeps(x[e], row.index(t, e)));
+  }
+}
+
+// The symbol at which the sum along the row of logits that are kept (EQUAL: that equal the cut's, each 1; else all
+// that the cut keeps, by weight) reaches want(total), at least 1, and its logit.
+template <bool EQUAL, typename L, typename S, typename W>
+__device__ __forceinline__ void pick(const L& row, S& s, const Cut& cut, double m, double c, double bits, const W& want,
                                      int* index, float* logit, uint64_t* total) {
-  constexpr int N = L::N, WAVES = L::WAVES;
+  constexpr int N = L::N, WAVES = L::WAVES, PUSHED = (int)(sizeof(s.hist) + sizeof(s.list)) / 4 / WAVES;
   extern __shared__ uint4 s_row[];
-  // a sum of each turn of a wave, behind the row; and place for a turn's logits, where the histogram was
+  // a sum of each turn of a wave, behind the row; where the histogram and the list were, a turn's logits that are kept
   uint64_t* sums = reinterpret_cast<uint64_t*>(s_row + (L::KEPT ? row.turns * WAVES * 64 : 0));
   const int lane = lane_id(), wave = threadIdx.x >> 6;
+  float* pushed = reinterpret_cast<float*>(s.hist) + wave * PUSHED;
   __syncthreads();
   for (int t = 0; t < row.turns; ++t) {
     const auto x = row.at(t);
     uint64_t mine = 0;
-    if constexpr (COUNT) {
+    if constexpr (EQUAL) {
 #pragma unroll
-      for (int e = 0; e < N; ++e) mine += keeps(x.x[e], row.index(t, e)) ? 1 : 0;
+      for (int e = 0; e < N; ++e) mine += x.x[e] == cut.x && row.index(t, e) <= cut.v ? 1 : 0;
     } else {
+      // few are kept as a rule: they are pushed together first, so that a weight is computed by every lane
+      int n = 0;
+      kept_of(row, cut, t, x.x, [&](int e, bool kept) {
+        const uint64_t which = __ballot(kept);
+        const int at = n + (int)rank_below(which);
+        if (kept && at < PUSHED) pushed[at] = x.x[e];
+        n += (int)__popcll(which);
+      });
+      if (n <= PUSHED) {
+        wave_lds_fence();
+        for (int i = lane; i < n; i += 64) mine += units(pushed[i], m, c, bits);
+        wave_lds_fence();
+      } else {
 #pragma unroll
-      for (int e0 = 0; e0 < N; e0 += 4) {
-        bool k[4], some = false;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) some |= k[e] = keeps(x.x[e0 + e], row.index(t, e0 + e));
-        if (__any(some)) {
+        for (int e0 = 0; e0 < N; e0 += 4) {
           uint64_t w[4];
           units_all<4>(x.x + e0, m, c, bits, w);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) mine += k[e] ? w[e] : 0;
+          for (int e = 0; e < 4; ++e) mine += cut.keeps(x.x[e0 + e], row.index(t, e0 + e)) ? w[e] : 0;
         }
       }
     }
@@ -787,7 +812,8 @@ __device__ __forceinline__ void pick(const L& row, S& s, const K& keeps, double 
     uint64_t v[N], mine = 0;
 #pragma unroll
     for (int e = 0; e < N; ++e) {
-      v[e] = keeps(x.x[e], row.index(t, e)) ? (COUNT ? 1 : units(x.x[e], m, c, bits)) : 0;
+      if constexpr (EQUAL) v[e] = x.x[e] == cut.x && row.index(t, e) <= cut.v ? 1 : 0;
+      else v[e] = cut.keeps(x.x[e], row.index(t, e)) ? units(x.x[e], m, c, bits) : 0;
       mine += v[e];
     }
     uint64_t a = s.before + wave_scan(mine) - mine;
@@ -810,15 +836,16 @@ __device__ __forceinline__ void pick(const L& row, S& s, const K& keeps, double 
 }
 
 // The logit of the row's order at which `want` of the measure (logits, or with MASS their weights) of those that
-// `from` keeps is reached; want(total) is asked with the measure of all, and more than that leaves `from`.
+// `from` keeps (LIMITED, else all) is reached; want(total) is asked with the measure of all, and more than that leaves `from`.
 // range: how far below the largest, m, the cut lies at most, or is worth bins.
-template <bool MASS, typename L, typename S, typename F>
+template <bool MASS, bool LIMITED, typename L, typename S, typename F>
 __device__ __forceinline__ Cut search(const L& row, S& s, const Cut from, float m, float range, double c, double bits,
                                       const F& want) {
   constexpr int N = L::N, THREADS = L::WAVES * 64;
   const int tid = threadIdx.x;
   const float scale = range > 0.0f ? fminf((float)BINS / fminf(range, 3e38f), 3e38f) : 1.0f;
   const auto bin_of = [&](float x) { return (m - x) * scale; };
+  const auto there = [&](float x, int v) { return LIMITED ? from.keeps(x, v) : x > -INFINITY; };
   const auto clear = [&] {
     for (int i = tid; i < BINS + 64; i += THREADS) s.hist[i] = 0;
     __syncthreads();
@@ -832,7 +859,7 @@ __device__ __forceinline__ Cut search(const L& row, S& s, const Cut from, float 
       if constexpr (MASS) units_all<4>(x + e0, (double)m, c, bits, w);
 #pragma unroll
       for (int e = e0; e < e0 + 4; ++e)
-        if (from.keeps(x[e], row.index(t, e)))
+        if ((MASS && !LIMITED) || there(x[e], row.index(t, e)))   // (-inf weighs nothing)
           atomicAdd((unsigned long long*)&s.hist[(uint32_t)fminf(bin_of(x[e]), last)], MASS ? (unsigned long long)w[e - e0] : 1ull);
     }
   });
@@ -848,7 +875,7 @@ __device__ __forceinline__ Cut search(const L& row, S& s, const Cut from, float 
   const float b0 = (float)bin, b1 = bin == BINS - 1 ? INFINITY : next_below((float)(bin + 1));
   const auto in_bin = [&](float x, int v) {
     const float b = bin_of(x);
-    return b >= b0 && b <= b1 && from.keeps(x, v);
+    return b >= b0 && b <= b1 && there(x, v);
   };
   row.each([&](int t, const float (&x)[N]) {
 #pragma unroll
@@ -903,7 +930,7 @@ __device__ __forceinline__ Cut search(const L& row, S& s, const Cut from, float 
 #pragma unroll
       for (int e = 0; e < N; ++e) {
         const uint32_t o = ordered(x[e]), b = (hi - o) >> shift;
-        if (o >= lo && o <= hi && from.keeps(x[e], row.index(t, e)))
+        if (o >= lo && o <= hi && there(x[e], row.index(t, e)))
           atomicAdd((unsigned long long*)&s.hist[b], MASS ? (unsigned long long)units(x[e], (double)m, c, bits) : 1ull);
       }
     });
@@ -921,8 +948,8 @@ __device__ __forceinline__ Cut search(const L& row, S& s, const Cut from, float 
   int index;
   float z;
   uint64_t all;
-  pick<true>(row, s, [&](float y, int v) { return y == x && from.keeps(y, v); }, 0.0, 0.0, 0.0,
-             [&](uint64_t) { return ties; }, &index, &z, &all);
+  const Cut equal{x, LIMITED && x == from.x ? from.v : row.V};
+  pick<true>(row, s, equal, 0.0, 0.0, 0.0, [&](uint64_t) { return ties; }, &index, &z, &all);
   return Cut{x, index};
 }
 
@@ -1109,26 +1136,27 @@ __global__ void __launch_bounds__(THREADS) k_sample_long(SampleArgs a) {
   }
   if (set.k > 0 && set.k < a.V) {
     if (set.k == 1) {
-      cut = Cut{m, -1};
       int index;
       float z;
       uint64_t n;
-      pick<true>(row, s, [&](float x, int) { return x == m; }, 0.0, 0.0, 0.0, [&](uint64_t) { return (uint64_t)1; }, &index,
-                 &z, &n);
-      cut.v = index;
+      pick<true>(row, s, Cut{m, a.V}, 0.0, 0.0, 0.0, [&](uint64_t) { return (uint64_t)1; }, &index, &z, &n);
+      cut = Cut{m, index};
     } else {
-      cut = search<false>(row, s, cut, m, (float)fmin(40.0 / c, 3e38), c, S, [&](uint64_t) { return (uint64_t)set.k; });
+      cut = search<false, false>(row, s, cut, m, (float)fmin(40.0 / c, 3e38), c, S, [&](uint64_t) { return (uint64_t)set.k; });
     }
   }
-  if (set.p < 1.0)
-    cut = search<true>(row, s, cut, m, set.octaves * __builtin_amdgcn_rcpf((float)c), c, S,
-                       [&](uint64_t t) { return share_up(set.p, t); });
+  if (set.p < 1.0) {
+    const auto want = [&](uint64_t t) { return share_up(set.p, t); };
+    const float range = set.octaves * __builtin_amdgcn_rcpf((float)c);
+    cut = cut.x > -INFINITY ? search<true, true>(row, s, cut, m, range, c, S, want)
+                            : search<true, false>(row, s, cut, m, range, c, S, want);
+  }
   if (set.least > 0.0 && least > cut.x) cut = Cut{least, a.V};
   int index;
   float z;
   uint64_t total;
-  pick<false>(row, s, [&](float x, int v) { return cut.keeps(x, v); }, (double)m, c, S,
-              [&](uint64_t all) { return share_down(set.u, all) + 1; }, &index, &z, &total);
+  pick<false>(row, s, cut, (double)m, c, S, [&](uint64_t all) { return share_down(set.u, all) + 1; }, &index, &z,
+              &total);
   if (share_down(set.u, total) == 0) {   // a share of nothing: the first symbol of any weight, though it be less than a unit
     int first = a.V;
     row.each([&](int t, const float (&x)[N]) {
