@@ -108,7 +108,7 @@ __device__ __forceinline__ uint64_t share_down(float u, uint64_t m) { return (ui
 
 // A row's settings.
 struct Row {
-  double T, c, p, least;   // c: log2(e) / T, 0 for a T of 0
+  double T, c, p, least, log_least;   // c: log2(e) / T, 0 for a T of 0
   float octaves;           // below the largest weight: the cut by p lies above
   int64_t k;        // 0: all
   float u;
@@ -119,7 +119,7 @@ struct SampleArgs {
   const void* z;
   int64_t stride;
   int V, S;
-  double T, c, p, least;
+  double T, c, p, least, log_least;
   float octaves;
   int k;
   const float *T_rows, *p_rows, *least_rows;
@@ -151,6 +151,8 @@ __device__ __forceinline__ Row settings(const SampleArgs& a, int64_t r) {
   if (a.p_rows) s.octaves = octaves_of(a.V, fmax(s.p, 0.0));
   s.valid = s.T >= 0.0 && s.T < (double)INFINITY && s.p == s.p && s.least == s.least;
   s.least = fmin(s.least, 1.0);
+  s.log_least = a.log_least;
+  if (a.least_rows) s.log_least = s.least > 0.0 ? log(s.least) : 0.0;
   if (s.T == 0.0) {   // the largest alone
     s.k = 1;
     s.p = 1.0;
@@ -159,10 +161,10 @@ __device__ __forceinline__ Row settings(const SampleArgs& a, int64_t r) {
   return s;
 }
 
-// The ordered value from which on logits have a weight of `least` of the largest, m.
-__device__ __forceinline__ uint32_t least_key(double least, float m, double T) {
-  if (!(least > 0.0)) return FIRST_LIVE;
-  const double z = (double)m + T * log(least);
+// The ordered value from which on logits have a weight of set.least of the largest, m.
+__device__ __forceinline__ uint32_t least_key(const Row& set, float m) {
+  if (!(set.least > 0.0)) return FIRST_LIVE;
+  const double z = (double)m + set.T * set.log_least;
   float f = (float)z;
   if ((double)f < z) f = nextafterf(f, INFINITY);
   return max(ordered(f), FIRST_LIVE);
@@ -540,7 +542,7 @@ __global__ void __launch_bounds__(256, SHORT_OCC) k_sample_short(SampleArgs a, i
     short_search<true>(row, s, by_mass, m, set.octaves * __builtin_amdgcn_rcpf((float)c), c, S, [&](uint64_t t) { return share_up(set.p, t); }, &cut);
   }
   if (__any(live && set.least > 0.0)) {
-    const float least = from_ordered(least_key(set.least, m, set.T));
+    const float least = from_ordered(least_key(set, m));
     if (live && set.least > 0.0 && least > cut.x) cut = ShortCut{least, 255, false};
   }
   uint64_t mine = 0;
@@ -764,12 +766,19 @@ __device__ __forceinline__ void pick(const L& row, S& s, const Cut& cut, double 
   for (int t = 0; t < row.turns; ++t) {
     const auto x = row.at(t);
     uint64_t mine = 0;
+    int n = 0;
     if constexpr (EQUAL) {
+      const float y = cut.x;
+      if (__builtin_amdgcn_readfirstlane(row.index(t, 0)) + 64 * N - 1 <= cut.v) {
 #pragma unroll
-      for (int e = 0; e < N; ++e) mine += x.x[e] == cut.x && row.index(t, e) <= cut.v ? 1 : 0;
+        for (int e = 0; e < N; ++e) n += (int)__popcll(__ballot(x.x[e] == y));
+      } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e) n += (int)__popcll(__ballot(x.x[e] == y && row.index(t, e) <= cut.v));
+      }
+      mine = lane == 0 ? (uint64_t)n : 0;
     } else {
       // few are kept as a rule: they are pushed together first, so that a weight is computed by every lane
-      int n = 0;
       kept_of(row, cut, t, x.x, [&](int e, bool kept) {
         const uint64_t which = __ballot(kept);
         const int at = n + (int)rank_below(which);
@@ -788,15 +797,20 @@ __device__ __forceinline__ void pick(const L& row, S& s, const Cut& cut, double 
           for (int e = 0; e < 4; ++e) mine += cut.keeps(x.x[e0 + e], row.index(t, e0 + e)) ? w[e] : 0;
         }
       }
+      mine = row16_scan(mine);
     }
-    mine = wave_sum(mine);
-    if (lane == 0) sums[wave * row.turns + t] = mine;
+    // a turn's sum in four parts, one of 16 lanes
+    if ((lane & 15) == (EQUAL ? 0 : 15)) sums[(wave * row.turns + t) * 4 + (lane >> 4)] = mine;
   }
   __syncthreads();
   if (wave == 0) {
     const int n = WAVES * row.turns, per = (n + 63) / 64;
+    const auto sum_of = [&](int i) {
+      const ulonglong2* p = reinterpret_cast<const ulonglong2*>(sums + i * 4);
+      return p[0].x + p[0].y + p[1].x + p[1].y;
+    };
     uint64_t mine = 0;
-    for (int i = lane * per; i < min(n, (lane + 1) * per); ++i) mine += sums[i];
+    for (int i = lane * per; i < min(n, (lane + 1) * per); ++i) mine += sum_of(i);
     const uint64_t upto = wave_scan(mine);
     const uint64_t all = __shfl(upto, 63);
     const uint64_t w = want(all);
@@ -804,7 +818,7 @@ __device__ __forceinline__ void pick(const L& row, S& s, const Cut& cut, double 
     if (lane == 0) s.total = all;
     if (a < w && a + mine >= w) {
       int i = lane * per;
-      while (a + sums[i] < w) a += sums[i++];
+      while (a + sum_of(i) < w) a += sum_of(i++);
       s.wave = i / row.turns;
       s.turn = i % row.turns;
       s.before = a;
@@ -1169,7 +1183,7 @@ __global__ void __launch_bounds__(THREADS) k_sample_long(SampleArgs a) {
     return;
   }
   const double c = set.c, S = (double)a.S;
-  const float least = from_ordered(least_key(set.least, m, set.T));
+  const float least = from_ordered(least_key(set, m));
   Cut cut{-INFINITY, -1};   // nothing is cut off
 
   if (set.k > 0 && set.k <= LIST_K && set.k < a.V) {
@@ -1336,7 +1350,7 @@ void run(const SampleArgs& a, int64_t rows, hipStream_t st) {
   const int pieces = (a.V + Vec<TYPE>::N - 1) / Vec<TYPE>::N;
   const auto go = [&](auto kern, int threads, bool keep) {
     const int turns = (pieces + threads - 1) / threads;
-    const unsigned lds = (keep ? 16 * turns * threads : 0) + 8 * turns * (threads / 64);   // the row, a sum of each turn
+    const unsigned lds = (keep ? 16 * turns * threads : 0) + 32 * turns * (threads / 64);   // the row, sums of each turn
     hipLaunchKernelGGL(kern, dim3((unsigned)rows), dim3(threads), lds, st, a);
   };
   if (pieces <= 512) go(k_sample_long<TYPE, 64, true>, 64, true);
@@ -1361,6 +1375,7 @@ hipError_t launch_sample(const reno_sample& p, const void* logits, const float* 
     a.T = p.temperature;
     a.c = a.T > 0.0 ? LOG2E_D / a.T : 0.0;
     a.octaves = octaves_of(a.V, p.top_p);
+    a.log_least = p.min_p > 0.0 ? std::log(p.min_p) : 0.0;
     a.p = p.top_p;
     a.least = p.min_p;
     a.k = p.top_k;
