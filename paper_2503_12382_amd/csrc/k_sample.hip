@@ -12,7 +12,7 @@
 // histogram over that bin's range of values, until a bin is one value.
 //
 //   k_sample_short rows of up to 256: 16 lanes a row, in registers
-//   k_sample_long  a block a row, held in LDS where it fits
+//   k_sample_long  a block a row, read again for each look at it
 
 #include <algorithm>
 #include <cmath>
@@ -626,16 +626,15 @@ struct Cut {
   __device__ __forceinline__ float from(int v0, int n) const { return v >= v0 + n - 1 ? x : v < v0 ? next_above(x) : NAN; }
 };
 
-// THREADS a row; KEEP: the row is held in LDS (else read again each time).  A wave's pieces of 16 bytes follow one
-// another: the row's order is by wave, then by turn, then by lane.  A thread reads only what it wrote itself.
-template <int TYPE, int THREADS, bool KEEP>
+// THREADS a row.  A wave's pieces of 16 bytes follow one another: the row's order is by wave, then by turn, then by
+// lane.  The row is read anew for each look at it, from L2: held in LDS it leaves place for fewer blocks a CU, whose
+// waits for one another then show (4096 rows of 32768 bf16: 247 us, against 210).
+template <int TYPE, int THREADS>
 struct Long {
   static constexpr int N = Vec<TYPE>::N, WAVES = THREADS / 64, SIZE = 16 / N;
-  static constexpr bool KEPT = KEEP;
   static constexpr uint32_t DEAD = TYPE == RENO_T_FP32 ? 0xff800000u : TYPE == RENO_T_BF16 ? 0xff80ff80u : 0xfc00fc00u;
   const char* z;
   const uint8_t* allowed;
-  uint4* kept;
   int V, turns, first;      // first: this thread's first piece
 
   // a piece; -inf where there is no logit
@@ -671,10 +670,7 @@ struct Long {
     }
   }
   __device__ __forceinline__ int index(int turn, int e) const { return (first + turn * 64) * N + e; }
-  __device__ __forceinline__ uint4 raw(int turn) const {
-    if constexpr (KEEP) return kept[turn * THREADS + threadIdx.x];
-    else return read(first + turn * 64);
-  }
+  __device__ __forceinline__ uint4 raw(int turn) const { return read(first + turn * 64); }
   __device__ __forceinline__ Vec<TYPE> at(int turn) const {
     Vec<TYPE> x;
     x.from(raw(turn));
@@ -757,9 +753,8 @@ template <bool EQUAL, typename L, typename S, typename W>
 __device__ __forceinline__ void pick(const L& row, S& s, const Cut& cut, double m, double c, double bits, const W& want,
                                      int* index, float* logit, uint64_t* total) {
   constexpr int N = L::N, WAVES = L::WAVES, PUSHED = (int)(sizeof(s.hist) + sizeof(s.list)) / 4 / WAVES;
-  extern __shared__ uint4 s_row[];
-  // a sum of each turn of a wave, behind the row; where the histogram and the list were, a turn's logits that are kept
-  uint64_t* sums = reinterpret_cast<uint64_t*>(s_row + (L::KEPT ? row.turns * WAVES * 64 : 0));
+  extern __shared__ uint64_t sums[];   // of each turn of a wave, in four parts
+  // where the histogram and the list were, a turn's logits that are kept
   const int lane = lane_id(), wave = threadIdx.x >> 6;
   float* pushed = reinterpret_cast<float*>(s.hist) + wave * PUSHED;
   __syncthreads();
@@ -779,7 +774,8 @@ __device__ __forceinline__ void pick(const L& row, S& s, const Cut& cut, double 
       mine = lane == 0 ? (uint64_t)n : 0;
     } else {
       // few are kept as a rule: they are pushed together first, so that a weight is computed by every lane
-      kept_of(row, cut, t, x.x, [&](int e, bool kept) {
+      if (cut.x == -INFINITY) n = PUSHED + 1;
+      else kept_of(row, cut, t, x.x, [&](int e, bool kept) {
         const uint64_t which = __ballot(kept);
         const int at = n + (int)rank_below(which);
         if (kept && at < PUSHED) pushed[at] = x.x[e];
@@ -794,7 +790,8 @@ __device__ __forceinline__ void pick(const L& row, S& s, const Cut& cut, double 
         for (int e0 = 0; e0 < N; e0 += 4) {
           uint64_t w[4];
           units_all<4>(x.x + e0, m, c, bits, w);
-          for (int e = 0; e < 4; ++e) mine += cut.keeps(x.x[e0 + e], row.index(t, e0 + e)) ? w[e] : 0;
+          for (int e = 0; e < 4; ++e)   // (-inf weighs nothing)
+            mine += cut.x == -INFINITY || cut.keeps(x.x[e0 + e], row.index(t, e0 + e)) ? w[e] : 0;
         }
       }
       mine = row16_scan(mine);
@@ -1111,9 +1108,12 @@ __device__ __forceinline__ bool by_counts(const L& row, S& s, float m, double c,
   return true;
 }
 
-template <int TYPE, int THREADS, bool KEEP>
-__global__ void __launch_bounds__(THREADS) k_sample_long(SampleArgs a) {
-  typedef Long<TYPE, THREADS, KEEP> L;
+#ifndef LOCC
+#define LOCC 1
+#endif
+template <int TYPE, int THREADS>
+__global__ void __launch_bounds__(THREADS, LOCC) k_sample_long(SampleArgs a) {
+  typedef Long<TYPE, THREADS> L;
   constexpr int N = L::N, WAVES = L::WAVES, GROUPS = 4;
   __shared__ Shared<WAVES> s;
   const int64_t r = blockIdx.x;
@@ -1133,8 +1133,6 @@ __global__ void __launch_bounds__(THREADS) k_sample_long(SampleArgs a) {
   row.V = a.V;
   row.turns = (a.V + N * THREADS - 1) / (N * THREADS);
   row.first = wave * row.turns * 64 + lane;
-  extern __shared__ uint4 s_row[];
-  row.kept = s_row;
   // the largest logit, and the largest of the thread's groups
   float group[GROUPS] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
   bool odd = false;
@@ -1156,13 +1154,10 @@ __global__ void __launch_bounds__(THREADS) k_sample_long(SampleArgs a) {
     uint4 raw[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      if (t0 + i < row.turns) raw[i] = row.read(row.first + (t0 + i) * 64);
+      if (t0 + i < row.turns) raw[i] = row.raw(t0 + i);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      if (t0 + i < row.turns) {
-        if constexpr (KEEP) s_row[(t0 + i) * THREADS + tid] = raw[i];
-        look(raw[i]);
-      }
+      if (t0 + i < row.turns) look(raw[i]);
   }
   float m = fmaxf(fmaxf(group[0], group[1]), fmaxf(group[2], group[3]));
   for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
@@ -1348,16 +1343,23 @@ void run(const SampleArgs& a, int64_t rows, hipStream_t st) {
     return;
   }
   const int pieces = (a.V + Vec<TYPE>::N - 1) / Vec<TYPE>::N;
-  const auto go = [&](auto kern, int threads, bool keep) {
+  const auto go = [&](auto kern, int threads) {
     const int turns = (pieces + threads - 1) / threads;
-    const unsigned lds = (keep ? 16 * turns * threads : 0) + 32 * turns * (threads / 64);   // the row, sums of each turn
-    hipLaunchKernelGGL(kern, dim3((unsigned)rows), dim3(threads), lds, st, a);
+    hipLaunchKernelGGL(kern, dim3((unsigned)rows), dim3(threads), 32 * turns * (threads / 64), st, a);   // sums of each turn
   };
-  if (pieces <= 512) go(k_sample_long<TYPE, 64, true>, 64, true);
-  else if (pieces <= 2048) go(k_sample_long<TYPE, 256, true>, 256, true);
-  else if (pieces <= 4096) go(k_sample_long<TYPE, 512, true>, 512, true);
-  else if (pieces <= 8192) go(k_sample_long<TYPE, 1024, true>, 1024, true);
-  else go(k_sample_long<TYPE, 1024, false>, 1024, false);
+  // Threads of a row.  With rows for every CU several blocks share one, and fewer threads wait less for one another
+  // (2048 rows of 32768 fp32, top_p, with 128, 256, 512, 1024: 209, 203, 183, 256 us; 8192 of 4096: 107, 102, 136, 307);
+  // else a row is as quick as its threads are many (64 rows of 50021 fp16: 119, 69, 49, 42).
+  int threads = pieces <= 128 ? 64 : pieces <= 512 ? 128 : pieces <= 4096 ? 256 : 512;
+  if (rows <= 256)
+    while (threads < 1024 && threads * 2 < pieces) threads *= 2;
+  switch (threads) {
+    case 64: go(k_sample_long<TYPE, 64>, 64); break;
+    case 128: go(k_sample_long<TYPE, 128>, 128); break;
+    case 256: go(k_sample_long<TYPE, 256>, 256); break;
+    case 512: go(k_sample_long<TYPE, 512>, 512); break;
+    default: go(k_sample_long<TYPE, 1024>, 1024);
+  }
 }
 
 }  // namespace
