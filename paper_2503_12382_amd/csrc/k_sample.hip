@@ -450,7 +450,7 @@ __device__ __forceinline__ void short_search(const Short<PL>& row, ShortShared& 
 }
 
 // Whether logit i of the lane is kept: `lim`, the last of the lane whose ties are, is cut.v - v0.
-__device__ __forceinline__ bool is_kept(float x, int i, float cut, float above, int lim) {
+__device__ __forceinline__ bool itimesept(float x, int i, float cut, float above, int lim) {
   return x >= (i <= lim ? cut : above);
 }
 
@@ -531,7 +531,7 @@ __global__ void __launch_bounds__(256, SHORT_OCC) k_sample_short(SampleArgs a, i
     const float over = next_above(cut.x);
 #pragma unroll
     for (int i = 0; i < PL; ++i)
-      if (!is_kept(row.x[i], i, cut.x, over, cut.v - row.v0)) {
+      if (!itimesept(row.x[i], i, cut.x, over, cut.v - row.v0)) {
         row.x[i] = -INFINITY;
         row.w[i] = 0;
         s.x[rw][i * 16 + l15] = -INFINITY;
@@ -549,7 +549,7 @@ __global__ void __launch_bounds__(256, SHORT_OCC) k_sample_short(SampleArgs a, i
   const float over = next_above(cut.x);
   if (__any(cut.split)) {   // among logits that equal the last one
 #pragma unroll
-    for (int i = 0; i < PL; ++i) row.w[i] = is_kept(row.x[i], i, cut.x, over, cut.v - row.v0) ? row.w[i] : 0;
+    for (int i = 0; i < PL; ++i) row.w[i] = itimesept(row.x[i], i, cut.x, over, cut.v - row.v0) ? row.w[i] : 0;
   } else {
 #pragma unroll
     for (int i = 0; i < PL; ++i) row.w[i] = row.x[i] >= cut.x ? row.w[i] : 0;
@@ -564,7 +564,7 @@ __global__ void __launch_bounds__(256, SHORT_OCC) k_sample_short(SampleArgs a, i
     uint64_t ones = 0;
 #pragma unroll
     for (int i = 0; i < PL; ++i) {
-      const bool some = is_kept(row.x[i], i, cut.x, over, cut.v - row.v0) && ((double)row.x[i] - (double)m) * c >= -1074.0;
+      const bool some = itimesept(row.x[i], i, cut.x, over, cut.v - row.v0) && ((double)row.x[i] - (double)m) * c >= -1074.0;
       row.w[i] = any ? (some ? 1 : 0) : row.w[i];
       ones += row.w[i];
     }
@@ -600,41 +600,49 @@ constexpr int BINS = 1024;
 constexpr int LIST = 512;       // logits that are compared with one another
 constexpr int LIST_K = 256;     // counts up to this are cut in a list of what the maxima of groups bound from below
 
-__device__ __forceinline__ uint64_t wave_sum(uint64_t v) {   // in every lane
-  v = row16_scan(v);
-  v = __shfl(v, lane_id() | 15);
-  v += __shfl_xor(v, 16);
-  return v + __shfl_xor(v, 32);
+// Of each row of lanes in ROWS: the value of lane 15 of the row before (0x142), or of lane 31 (0x143); else 0.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint64_t dpp_rows(uint64_t v) {
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, ROWS, 0xF, false);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(v >> 32), CTRL, ROWS, 0xF, false);
+  return (uint64_t)hi << 32 | lo;
 }
 __device__ __forceinline__ uint64_t wave_scan(uint64_t v) {   // inclusive
   v = row16_scan(v);
-  const uint64_t rows = v;
-  const uint64_t r0 = __shfl(rows, 15), r1 = __shfl(rows, 31), r2 = __shfl(rows, 47);
-  const int rw = lane_id() >> 4;
-  return v + (rw > 0 ? r0 : 0) + (rw > 1 ? r1 : 0) + (rw > 2 ? r2 : 0);
+  v += dpp_rows<0x142, 0xA>(v);
+  return v + dpp_rows<0x143, 0xC>(v);
 }
-
+__device__ __forceinline__ uint64_t wave_sum(uint64_t v) {   // in every lane
+  v = wave_scan(v);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, 63);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), 63);
+  return (uint64_t)hi << 32 | lo;
+}
 // bf16 logits of 2^-6 to 2^6 are counted by value, one of 12 times 128 values of either sign.
 constexpr int ZONE = 12 * 128, ZONE_FIRST = (127 - 6) << 7, OTHERS = 512;
 
-// A row's last logit that is kept: those above x are, and those equal to it up to symbol v.
+// What a row keeps: logits above x, and of those that equal it the first `ties` (ALL: all).
 struct Cut {
   float x;
-  int v;
-  __device__ __forceinline__ bool keeps(float z, int i) const { return z > x || (z == x && i <= v); }
-  // from where on logits are kept whose symbols are v0 .. v0 + n - 1, all of them on one side of v; else NaN
-  __device__ __forceinline__ float from(int v0, int n) const { return v >= v0 + n - 1 ? x : v < v0 ? next_above(x) : NAN; }
+  uint32_t ties;
+};
+
+// A wave's turn: what its logits above the cut weigh, and how many equal it.
+struct Turn {
+  uint64_t above, equal;
 };
 
 // THREADS a row.  A wave's pieces of 16 bytes follow one another: the row's order is by wave, then by turn, then by
-// lane.  The row is read anew for each look at it, from L2: held in LDS it leaves place for fewer blocks a CU, whose
-// waits for one another then show (4096 rows of 32768 bf16: 247 us, against 210).
-template <int TYPE, int THREADS>
+// lane.  KEEP: the first look leaves the row in LDS, where a thread reads what it wrote itself.  Else the row is read
+// anew for each look: with rows for every CU LDS has no place for enough of them (4096 rows of 32768 bf16, two looks
+// more than now: 247 us, against 210).
+template <int TYPE, int THREADS, bool KEEP>
 struct Long {
   static constexpr int N = Vec<TYPE>::N, WAVES = THREADS / 64, SIZE = 16 / N;
   static constexpr uint32_t DEAD = TYPE == RENO_T_FP32 ? 0xff800000u : TYPE == RENO_T_BF16 ? 0xff80ff80u : 0xfc00fc00u;
   const char* z;
   const uint8_t* allowed;
+  uint4* kept;
   int V, turns, first;      // first: this thread's first piece
 
   // a piece; -inf where there is no logit
@@ -669,8 +677,19 @@ struct Long {
       w[e / 2] = there ? w[e / 2] : (w[e / 2] & ~mask) | (DEAD & mask);
     }
   }
+  __device__ __forceinline__ Turn* sums() const {
+    return reinterpret_cast<Turn*>(kept + (KEEP ? turns * THREADS : 0));
+  }
   __device__ __forceinline__ int index(int turn, int e) const { return (first + turn * 64) * N + e; }
-  __device__ __forceinline__ uint4 raw(int turn) const { return read(first + turn * 64); }
+  __device__ __forceinline__ uint4 load(int turn) const {   // the first look
+    const uint4 r = read(first + turn * 64);
+    if constexpr (KEEP) kept[turn * THREADS + threadIdx.x] = r;
+    return r;
+  }
+  __device__ __forceinline__ uint4 raw(int turn) const {
+    if constexpr (KEEP) return kept[turn * THREADS + threadIdx.x];
+    else return read(first + turn * 64);
+  }
   __device__ __forceinline__ Vec<TYPE> at(int turn) const {
     Vec<TYPE> x;
     x.from(raw(turn));
@@ -690,11 +709,11 @@ struct Long {
 template <int WAVES>
 struct Shared {
   uint64_t hist[BINS + 64];   // the last bin is one of each lane's: what lies far below meets there; then weights
-  uint64_t list[LIST];        // places: the ordered value, then the index complemented
+  uint64_t list[LIST];        // places: the ordered value, then the index complemented; or ordered values
   uint16_t other[OTHERS];     // bf16 values outside the table of counts, which lies over both of the above
   uint64_t part[WAVES];
   uint64_t above, total, before;
-  uint32_t lo, hi;
+  uint32_t lo, hi, left;
   float top[WAVES], x;
   int odd[WAVES], count[2 * WAVES];
   int bin, n, wave, turn, index;
@@ -703,6 +722,18 @@ struct Shared {
 __device__ __forceinline__ uint64_t place64(float x, int v) { return (uint64_t)ordered(x) << 32 | (uint32_t)~v; }
 __device__ __forceinline__ float x_of(uint64_t place) { return from_ordered((uint32_t)(place >> 32)); }
 __device__ __forceinline__ int v_of(uint64_t place) { return (int)~(uint32_t)place; }
+
+// The sum of a value a thread, in every thread.
+template <int WAVES>
+__device__ __forceinline__ uint64_t block_total(Shared<WAVES>& s, uint64_t v) {
+  v = wave_sum(v);
+  __syncthreads();
+  if (lane_id() == 0) s.part[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = 0;
+  for (int i = 0; i < WAVES; ++i) v += s.part[i];
+  return v;
+}
 
 // Wave 0: the first bin at whose end `want` of what `above` and the bins hold is reached, and what lies above it.
 // want(total) is asked with what all bins hold; bin -1: more than there is.
@@ -733,92 +764,82 @@ __device__ __forceinline__ void find_bin(Shared<WAVES>& s, uint64_t above, const
   }
 }
 
-// f(e, kept) for the N logits of a lane in a turn; in the turn that holds the cut's symbol each is asked for itself.
-template <typename L, typename F>
-__device__ __forceinline__ void kept_of(const L& row, const Cut& cut, int t, const float (&x)[L::N], const F& f) {
-  constexpr int N = L::N;
-  const float from = cut.from(__builtin_amdgcn_readfirstlane(row.index(t, 0)), 64 * N);
-  if (from == from) {
-#pragma unroll
-    for (int e = 0; e < N; ++e) f(e, x[e] >= from);
-  } else {
-#pragma unroll
-    for (int e = 0; e < N; ++e) f(e, cut.keeps(x[e], row.index(t, e)));
-  }
-}
-
-// The symbol at which the sum along the row of logits that are kept (EQUAL: that equal the cut's, each 1; else all
-// that the cut keeps, by weight) reaches want(total), at least 1, and its logit.
-template <bool EQUAL, typename L, typename S, typename W>
+// The symbol at which the weights along the row of what the cut keeps reach want(total), at least 1, and its logit.
+template <typename L, typename S, typename W>
 __device__ __forceinline__ void pick(const L& row, S& s, const Cut& cut, double m, double c, double bits, const W& want,
                                      int* index, float* logit, uint64_t* total) {
   constexpr int N = L::N, WAVES = L::WAVES, PUSHED = (int)(sizeof(s.hist) + sizeof(s.list)) / 4 / WAVES;
-  extern __shared__ uint64_t sums[];   // of each turn of a wave, in four parts
-  // where the histogram and the list were, a turn's logits that are kept
+  Turn* turns = row.sums();
   const int lane = lane_id(), wave = threadIdx.x >> 6;
-  float* pushed = reinterpret_cast<float*>(s.hist) + wave * PUSHED;
+  float* pushed = reinterpret_cast<float*>(s.hist) + wave * PUSHED;   // a turn's logits, where histogram and list were
+  const bool whole = cut.ties == ALL;                // of those that equal the cut too
+  const float from = whole ? cut.x : next_above(cut.x);
   __syncthreads();
   for (int t = 0; t < row.turns; ++t) {
     const auto x = row.at(t);
     uint64_t mine = 0;
-    int n = 0;
-    if constexpr (EQUAL) {
-      const float y = cut.x;
-      if (__builtin_amdgcn_readfirstlane(row.index(t, 0)) + 64 * N - 1 <= cut.v) {
+    int n = 0, equal = 0;
+    // few are kept as a rule: they are pushed together first, so that a weight is computed by every lane
+    const bool all = from == -INFINITY;
+    if (!all) {
 #pragma unroll
-        for (int e = 0; e < N; ++e) n += (int)__popcll(__ballot(x.x[e] == y));
-      } else {
-#pragma unroll
-        for (int e = 0; e < N; ++e) n += (int)__popcll(__ballot(x.x[e] == y && row.index(t, e) <= cut.v));
-      }
-      mine = lane == 0 ? (uint64_t)n : 0;
-    } else {
-      // few are kept as a rule: they are pushed together first, so that a weight is computed by every lane
-      if (cut.x == -INFINITY) n = PUSHED + 1;
-      else kept_of(row, cut, t, x.x, [&](int e, bool kept) {
-        const uint64_t which = __ballot(kept);
-        const int at = n + (int)rank_below(which);
-        if (kept && at < PUSHED) pushed[at] = x.x[e];
+      for (int e = 0; e < N; ++e) {
+        const uint64_t which = __ballot(x.x[e] >= from);
+        const uint32_t at = __builtin_amdgcn_mbcnt_hi((uint32_t)(which >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)which, (uint32_t)n));
+        if (x.x[e] >= from && (PUSHED >= 64 * N || at < PUSHED)) pushed[at] = x.x[e];
         n += (int)__popcll(which);
-      });
-      if (n <= PUSHED) {
-        wave_lds_fence();
-        for (int i = lane; i < n; i += 64) mine += units(pushed[i], m, c, bits);
-        wave_lds_fence();
-      } else {
-#pragma unroll
-        for (int e0 = 0; e0 < N; e0 += 4) {
-          uint64_t w[4];
-          units_all<4>(x.x + e0, m, c, bits, w);
-          for (int e = 0; e < 4; ++e)   // (-inf weighs nothing)
-            mine += cut.x == -INFINITY || cut.keeps(x.x[e0 + e], row.index(t, e0 + e)) ? w[e] : 0;
-        }
       }
-      mine = row16_scan(mine);
     }
-    // a turn's sum in four parts, one of 16 lanes
-    if ((lane & 15) == (EQUAL ? 0 : 15)) sums[(wave * row.turns + t) * 4 + (lane >> 4)] = mine;
+    if (!whole) {
+#pragma unroll
+      for (int e = 0; e < N; ++e) equal += (int)__popcll(__ballot(x.x[e] == cut.x));
+    }
+    if (!all && (PUSHED >= 64 * N || n <= PUSHED)) {
+      wave_lds_fence();
+      for (int i = lane; i < n; i += 64) mine += units(pushed[i], m, c, bits);
+      wave_lds_fence();
+    } else {
+#pragma unroll
+      for (int e0 = 0; e0 < N; e0 += 4) {
+        uint64_t w[4];
+        units_all<4>(x.x + e0, m, c, bits, w);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) mine += x.x[e0 + e] >= from ? w[e] : 0;   // (-inf weighs nothing)
+      }
+    }
+    mine = wave_sum(mine);
+    if (lane == 0) turns[wave * row.turns + t] = Turn{mine, (uint64_t)equal};
   }
   __syncthreads();
+  const uint64_t each = whole ? 0 : units(cut.x, m, c, bits);
   if (wave == 0) {
-    const int n = WAVES * row.turns, per = (n + 63) / 64;
-    const auto sum_of = [&](int i) {
-      const ulonglong2* p = reinterpret_cast<const ulonglong2*>(sums + i * 4);
-      return p[0].x + p[0].y + p[1].x + p[1].y;
-    };
-    uint64_t mine = 0;
-    for (int i = lane * per; i < min(n, (lane + 1) * per); ++i) mine += sum_of(i);
+    const int n = WAVES * row.turns, per = (n + 63) / 64, first = lane * per, end = min(n, first + per);
+    uint64_t mine = 0, equal = 0;
+    for (int i = first; i < end; ++i) {
+      mine += turns[i].above;
+      equal += turns[i].equal;
+    }
+    // of what equals the cut, what is left to those from the lane's first turn on
+    const uint64_t before = wave_scan(equal) - equal;
+    uint64_t left = cut.ties > before ? cut.ties - before : 0;
+    mine += min(left, equal) * each;
     const uint64_t upto = wave_scan(mine);
     const uint64_t all = __shfl(upto, 63);
     const uint64_t w = want(all);
     uint64_t a = upto - mine;
     if (lane == 0) s.total = all;
     if (a < w && a + mine >= w) {
-      int i = lane * per;
-      while (a + sum_of(i) < w) a += sum_of(i++);
+      int i = first;
+      for (; i < end; ++i) {
+        const uint64_t here = turns[i].above + min(left, turns[i].equal) * each;
+        if (a + here >= w) break;
+        a += here;
+        left -= min(left, turns[i].equal);
+      }
       s.wave = i / row.turns;
       s.turn = i % row.turns;
       s.before = a;
+      s.left = (uint32_t)left;
     }
   }
   __syncthreads();
@@ -827,11 +848,16 @@ __device__ __forceinline__ void pick(const L& row, S& s, const Cut& cut, double 
   if (wave == s.wave) {
     const int t = s.turn;
     const auto x = row.at(t);
+    uint32_t equal = 0;
+#pragma unroll
+    for (int e = 0; e < N; ++e) equal += !whole && x.x[e] == cut.x ? 1 : 0;
+    uint32_t place = (uint32_t)wave_scan((uint64_t)equal) - equal;   // among the turn's that equal the cut
     uint64_t v[N], mine = 0;
 #pragma unroll
     for (int e = 0; e < N; ++e) {
-      if constexpr (EQUAL) v[e] = x.x[e] == cut.x && row.index(t, e) <= cut.v ? 1 : 0;
-      else v[e] = cut.keeps(x.x[e], row.index(t, e)) ? units(x.x[e], m, c, bits) : 0;
+      bool kept = x.x[e] >= from;
+      if (!whole && x.x[e] == cut.x) kept = place++ < s.left;
+      v[e] = kept ? units(x.x[e], m, c, bits) : 0;
       mine += v[e];
     }
     uint64_t a = s.before + wave_scan(mine) - mine;
@@ -853,72 +879,83 @@ __device__ __forceinline__ void pick(const L& row, S& s, const Cut& cut, double 
   *logit = s.x;
 }
 
-// The logit of the row's order at which `want` of the measure (logits, or with MASS their weights) of those that
-// `from` keeps (LIMITED, else all) is reached; want(total) is asked with the measure of all, and more than that leaves `from`.
+// Where `want` of the measure (logits, or with MASS their weights) is reached in the row's order, of what `from` keeps;
+// want(total) is asked with the measure of all of it, and more than that leaves `from`.
 // range: how far below the largest, m, the cut lies at most, or is worth bins.
-template <bool MASS, bool LIMITED, typename L, typename S, typename F>
+template <bool MASS, typename L, typename S, typename F>
 __device__ __forceinline__ Cut search(const L& row, S& s, const Cut from, float m, float range, double c, double bits,
                                       const F& want) {
   constexpr int N = L::N, THREADS = L::WAVES * 64;
   const int tid = threadIdx.x;
   const float scale = range > 0.0f ? fminf((float)BINS / fminf(range, 3e38f), 3e38f) : 1.0f;
   const auto bin_of = [&](float x) { return (m - x) * scale; };
-  const auto there = [&](float x, int v) { return LIMITED ? from.keeps(x, v) : x > -INFINITY; };
+  const auto measure = [&](float x) -> uint64_t { return MASS ? units(x, (double)m, c, bits) : 1; };
   const auto clear = [&] {
     for (int i = tid; i < BINS + 64; i += THREADS) s.hist[i] = 0;
     __syncthreads();
   };
+  // the cut at x: as many of the logits that equal it, `equal` together, as it takes after what lies above
+  const auto cut_at = [&](float x, uint64_t wanted, uint64_t above, uint64_t equal) {
+    const uint64_t w = max(measure(x), (uint64_t)1), ties = (wanted - above + w - 1) / w;
+    return Cut{x, MASS && ties * w >= equal ? ALL : (uint32_t)ties};   // (a search by mass asks a count for its number)
+  };
   clear();
   const float last = (float)(BINS - 1 + lane_id());
-  row.each([&](int t, const float (&x)[N]) {
+  row.each([&](int, const float (&x)[N]) {
 #pragma unroll
     for (int e0 = 0; e0 < N; e0 += 4) {
       uint64_t w[4];
       if constexpr (MASS) units_all<4>(x + e0, (double)m, c, bits, w);
 #pragma unroll
       for (int e = e0; e < e0 + 4; ++e)
-        if ((MASS && !LIMITED) || there(x[e], row.index(t, e)))   // (-inf weighs nothing)
+        if (x[e] > from.x)
           atomicAdd((unsigned long long*)&s.hist[(uint32_t)fminf(bin_of(x[e]), last)], MASS ? (unsigned long long)w[e - e0] : 1ull);
     }
   });
   if (tid == 0) s.n = 0;
   __syncthreads();
-  find_bin(s, 0, want);
+  const uint64_t tail = from.x > -INFINITY ? from.ties * measure(from.x) : 0;   // what equals from.x and is kept
+  find_bin(s, 0, [&](uint64_t t) { return want(t + tail); });
   __syncthreads();
-  const uint64_t wanted = want(s.total);
+  const uint64_t wanted = want(s.total + tail);
   const int bin = s.bin;
-  if (bin < 0) return from;
+  if (bin < 0) return tail ? (wanted >= s.total + tail ? from : cut_at(from.x, wanted, s.total, ~0ull)) : from;
   uint64_t above = s.above;
   // the bin's logits
   const float b0 = (float)bin, b1 = bin == BINS - 1 ? INFINITY : next_below((float)(bin + 1));
-  const auto in_bin = [&](float x, int v) {
+  const auto in_bin = [&](float x) {
     const float b = bin_of(x);
-    return b >= b0 && b <= b1 && there(x, v);
+    return b >= b0 && b <= b1 && x > from.x;
   };
-  row.each([&](int t, const float (&x)[N]) {
+  uint32_t* list = reinterpret_cast<uint32_t*>(s.list);   // ordered values
+  row.each([&](int, const float (&x)[N]) {
 #pragma unroll
     for (int e = 0; e < N; ++e)
-      if (in_bin(x[e], row.index(t, e))) {
+      if (in_bin(x[e])) {
         const int i = atomicAdd(&s.n, 1);
-        if (i < LIST) s.list[i] = place64(x[e], row.index(t, e));
+        if (i < LIST) list[i] = ordered(x[e]);
       }
   });
   __syncthreads();
   const int n = s.n;
   if (n <= LIST) {   // sums of all pairs
-    for (int i = tid; i < n; i += THREADS) s.hist[i] = MASS ? units(x_of(s.list[i]), (double)m, c, bits) : 1;
+    for (int i = tid; i < n; i += THREADS) s.hist[i] = measure(from_ordered(list[i]));
     __syncthreads();
     for (int i = tid; i < n; i += THREADS) {
-      const uint64_t me = s.list[i];
-      uint64_t sum = above;
-      for (int j = 0; j < n; ++j) sum += s.list[j] >= me ? s.hist[j] : 0;
-      if (sum >= wanted && sum - s.hist[i] < wanted) {
-        s.x = x_of(me);
-        s.index = v_of(me);
+      const uint32_t me = list[i];
+      uint64_t more = above, equal = 0;
+      for (int j = 0; j < n; ++j) {
+        more += list[j] > me ? s.hist[j] : 0;
+        equal += list[j] == me ? s.hist[j] : 0;
+      }
+      if (more < wanted && more + equal >= wanted) {   // (all that are equal write the same)
+        s.x = from_ordered(me);
+        s.before = more;
+        s.total = equal;
       }
     }
     __syncthreads();
-    return Cut{s.x, s.index};
+    return cut_at(s.x, wanted, s.before, s.total);
   }
   // too many: histograms of ordered values over what the bin spans, until one value is left
   if (tid == 0) {
@@ -927,10 +964,10 @@ __device__ __forceinline__ Cut search(const L& row, S& s, const Cut from, float 
   }
   __syncthreads();
   uint32_t kmin = ALL, kmax = 0;
-  row.each([&](int t, const float (&x)[N]) {
+  row.each([&](int, const float (&x)[N]) {
 #pragma unroll
     for (int e = 0; e < N; ++e)
-      if (in_bin(x[e], row.index(t, e))) {
+      if (in_bin(x[e])) {
         kmin = min(kmin, ordered(x[e]));
         kmax = max(kmax, ordered(x[e]));
       }
@@ -944,12 +981,11 @@ __device__ __forceinline__ Cut search(const L& row, S& s, const Cut from, float 
   while (lo != hi) {
     const int shift = max(0, 22 - (int)__builtin_clz(hi - lo));   // hi - lo < BINS << shift
     clear();
-    row.each([&](int t, const float (&x)[N]) {
+    row.each([&](int, const float (&x)[N]) {
 #pragma unroll
       for (int e = 0; e < N; ++e) {
         const uint32_t o = ordered(x[e]), b = (hi - o) >> shift;
-        if (o >= lo && o <= hi && there(x[e], row.index(t, e)))
-          atomicAdd((unsigned long long*)&s.hist[b], MASS ? (unsigned long long)units(x[e], (double)m, c, bits) : 1ull);
+        if (o >= lo && o <= hi) atomicAdd((unsigned long long*)&s.hist[b], (unsigned long long)measure(x[e]));
       }
     });
     __syncthreads();
@@ -960,15 +996,7 @@ __device__ __forceinline__ Cut search(const L& row, S& s, const Cut from, float 
     lo = max(lo, hi - min(hi, (1u << shift) - 1u));
     __syncthreads();
   }
-  const float x = from_ordered(hi);
-  const uint64_t each = MASS ? units(x, (double)m, c, bits) : 1;
-  const uint64_t ties = (wanted - above + each - 1) / max(each, (uint64_t)1);
-  int index;
-  float z;
-  uint64_t all;
-  const Cut equal{x, LIMITED && x == from.x ? from.v : row.V};
-  pick<true>(row, s, equal, 0.0, 0.0, 0.0, [&](uint64_t) { return ties; }, &index, &z, &all);
-  return Cut{x, index};
+  return cut_at(from_ordered(hi), wanted, above, ~0ull);
 }
 
 // The value at place i of the table.
@@ -977,12 +1005,15 @@ __device__ __forceinline__ float zone_value(int i) {
   return __uint_as_float((mag | (i < ZONE ? 0x8000u : 0u)) << 16);
 }
 
-// The cut of a row of bf16 by mass, from how often each value occurs: a weight is computed once for a value instead of
-// for each logit (4096 rows of 32768: 301 us without).  Logits outside the table, of |x| below 2^-6 or from 2^6, are
-// kept in a list; false: too many of them, or the cut lies among them.
+// A row of bf16 by how often each value occurs, for its first look: the largest logit, m, and the cut by mass, for which
+// a weight is computed once for a value instead of for each logit.  Logits outside the table, of |x| below 2^-6 or from
+// 2^6, are kept in a list.  *known: m and odd are set.  True: the cut too; else there are too many others, or the cut
+// lies among them.
 template <typename L, typename S, typename F>
-__device__ __forceinline__ bool by_counts(const L& row, S& s, float m, double c, double bits, const F& want, Cut* cut) {
+__device__ __forceinline__ bool by_counts(const L& row, S& s, double c, double bits, const F& want, float* m, bool* odd,
+                                          bool* known, Cut* cut) {
   constexpr int WAVES = L::WAVES, THREADS = WAVES * 64, PER = 8, RUNS = 2 * ZONE / PER;   // values of a thread's turn
+  constexpr int TURNS = (RUNS + THREADS - 1) / THREADS;
   static_assert(sizeof(s.hist) + sizeof(s.list) >= 2 * ZONE * 4, "the table lies over hist and list");
   const int tid = threadIdx.x, lane = lane_id(), wave = tid >> 6;
   uint32_t* table = reinterpret_cast<uint32_t*>(s.hist);   // from the lowest value up
@@ -990,10 +1021,11 @@ __device__ __forceinline__ bool by_counts(const L& row, S& s, float m, double c,
   if (tid == 0) {
     s.n = 0;
     s.bin = -1;
+    s.hi = 0;
+    s.lo = 0;
   }
   __syncthreads();
-  for (int t = 0; t < row.turns; ++t) {
-    const uint4 r = row.raw(t);
+  const auto count = [&](const uint4& r) {
     const uint32_t u[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -1010,58 +1042,75 @@ __device__ __forceinline__ bool by_counts(const L& row, S& s, float m, double c,
         }
       }
     }
+  };
+  for (int t0 = 0; t0 < row.turns; t0 += 4) {   // four loads under way
+    uint4 raw[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (t0 + i < row.turns) raw[i] = row.load(t0 + i);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (t0 + i < row.turns) count(raw[i]);
   }
   __syncthreads();
   const int n = s.n;
+  __syncthreads();   // (who goes on without this sets s.n anew)
+  *known = n <= OTHERS;
   if (n > OTHERS) return false;
-  // what the others weigh: small ones, in the order between the table's halves, and those below all of it
-  uint64_t small = 0, below = 0;
-  for (int i = tid; i < n; i += THREADS) {
-    const float x = __uint_as_float((uint32_t)s.other[i] << 16);
-    const uint64_t w = units(x, (double)m, c, bits);
-    if (x > -0x1p-6f) small += w;
-    else below += w;
-  }
-  // the table from the top: a thread's values follow one another, threads take runs in turn
-  constexpr int TURNS = (RUNS + THREADS - 1) / THREADS;
-  uint64_t mine[TURNS], all = 0;
+  // the largest: ordered values of the others, or the topmost count
+  uint32_t top = 0;
+  for (int i = tid; i < n; i += THREADS) top = max(top, ordered(__uint_as_float((uint32_t)s.other[i] << 16)));
+  uint32_t k[TURNS][PER];
 #pragma unroll
   for (int q = 0; q < TURNS; ++q) {
     const int run = q * THREADS + tid;
-    mine[q] = 0;
-    if (run < RUNS) {
 #pragma unroll
-      for (int e0 = 0; e0 < PER; e0 += 4) {
+    for (int e = 0; e < PER; ++e) {   // from the top: a thread's values follow one another, threads take runs in turn
+      const int i = 2 * ZONE - 1 - (run * PER + e);
+      k[q][e] = run < RUNS ? table[i] : 0;
+      if (k[q][e]) top = max(top, ordered(zone_value(i)));
+    }
+  }
+  for (int o = 32; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
+  if (lane == 0 && top) atomicMax(&s.hi, top);
+  // NaN of a negative sign is ordered as any NaN; +inf and NaN: no distribution
+  __syncthreads();
+  top = s.hi;
+  *odd = top >= 0xff800000u;
+  *m = top ? from_ordered(top) : -INFINITY;
+  if (*odd || !top) return true;
+  const double dm = (double)*m;
+  // what the others weigh: small ones, in the order between the table's halves, and large ones above or below all of it
+  uint64_t small = 0, below = 0;
+  for (int i = tid; i < n; i += THREADS) {
+    const float x = __uint_as_float((uint32_t)s.other[i] << 16);
+    const uint64_t w = units(x, dm, c, bits);
+    if (x >= 0x1p6f) s.lo = 1;   // (any thread)
+    if (x > -0x1p-6f) small += w;
+    else below += w;
+  }
+  uint64_t mine[TURNS], all = 0;
+#pragma unroll
+  for (int q = 0; q < TURNS; ++q) {
+    mine[q] = 0;
+#pragma unroll
+    for (int e0 = 0; e0 < PER; e0 += 4) {
+      if (k[q][e0] | k[q][e0 + 1] | k[q][e0 + 2] | k[q][e0 + 3]) {
         float x[4];
         uint64_t w[4];
-        uint32_t k[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int i = 2 * ZONE - 1 - (run * PER + e0 + e);
-          k[e] = table[i];
-          x[e] = zone_value(i);
-        }
-        if (k[0] | k[1] | k[2] | k[3]) {
-          units_all<4>(x, (double)m, c, bits, w);
+        for (int e = 0; e < 4; ++e) x[e] = zone_value(2 * ZONE - 1 - ((q * THREADS + tid) * PER + e0 + e));
+        units_all<4>(x, dm, c, bits, w);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) mine[q] += k[e] ? k[e] * w[e] : 0;
-        }
+        for (int e = 0; e < 4; ++e) mine[q] += k[q][e0 + e] ? k[q][e0 + e] * w[e] : 0;
       }
     }
     all += mine[q];
   }
-  const auto block_total = [&](uint64_t v) {
-    v = wave_sum(v);
-    __syncthreads();
-    if (lane == 0) s.part[wave] = v;
-    __syncthreads();
-    v = 0;
-    for (int i = 0; i < WAVES; ++i) v += s.part[i];
-    return v;
-  };
-  small = block_total(small);
-  below = block_total(below);
-  const uint64_t wanted = want(block_total(all) + small + below);
+  small = block_total(s, small);
+  if (s.lo) return false;
+  below = block_total(s, below);
+  const uint64_t wanted = want(block_total(s, all) + small + below);
   uint64_t base = 0;
 #pragma unroll
   for (int q = 0; q < TURNS; ++q) {
@@ -1077,43 +1126,32 @@ __device__ __forceinline__ bool by_counts(const L& row, S& s, float m, double c,
     const int run = q * THREADS + tid;
     if (run * PER >= ZONE) a += small;   // (a run lies on one side)
     if (run < RUNS && a < wanted && a + mine[q] >= wanted) {
-      int e = 0;
       float x = 0.0f;
-      uint64_t w = 0, k = 0;
-      for (; e < PER; ++e) {
+      uint64_t w = 0, times = 0;
+#pragma unroll 1
+      for (int e = 0; e < PER; ++e) {
         const int i = 2 * ZONE - 1 - (run * PER + e);
-        k = table[i];
         x = zone_value(i);
-        w = k ? units(x, (double)m, c, bits) : 0;
-        if (a + k * w >= wanted) break;
-        a += k * w;
+        times = table[i];
+        w = times ? units(x, dm, c, bits) : 0;
+        if (a + times * w >= wanted) break;
+        a += times * w;
       }
-      const uint64_t ties = (wanted - a + w - 1) / w;
       s.x = x;
-      s.bin = ties < k ? 1 : 0;   // 1: the symbol of the last of them is to be found
-      s.total = ties;
+      s.bin = 1;
+      const uint64_t ties = (wanted - a + w - 1) / w;
+      s.left = ties < times ? (uint32_t)ties : ALL;
     }
   }
   __syncthreads();
   if (s.bin < 0) return false;
-  *cut = Cut{s.x, row.V};
-  if (s.bin == 1) {
-    const uint64_t ties = s.total;
-    int index;
-    float z;
-    uint64_t total;
-    pick<true>(row, s, *cut, 0.0, 0.0, 0.0, [&](uint64_t) { return ties; }, &index, &z, &total);
-    cut->v = index;
-  }
+  *cut = Cut{s.x, s.left};
   return true;
 }
 
-#ifndef LOCC
-#define LOCC 1
-#endif
-template <int TYPE, int THREADS>
-__global__ void __launch_bounds__(THREADS, LOCC) k_sample_long(SampleArgs a) {
-  typedef Long<TYPE, THREADS> L;
+template <int TYPE, int THREADS, bool KEEP>
+__global__ void __launch_bounds__(THREADS) k_sample_long(SampleArgs a) {
+  typedef Long<TYPE, THREADS, KEEP> L;
   constexpr int N = L::N, WAVES = L::WAVES, GROUPS = 4;
   __shared__ Shared<WAVES> s;
   const int64_t r = blockIdx.x;
@@ -1133,53 +1171,62 @@ __global__ void __launch_bounds__(THREADS, LOCC) k_sample_long(SampleArgs a) {
   row.V = a.V;
   row.turns = (a.V + N * THREADS - 1) / (N * THREADS);
   row.first = wave * row.turns * 64 + lane;
-  // the largest logit, and the largest of the thread's groups
+  extern __shared__ uint4 s_row[];   // the row, where it is kept, then its turns' sums
+  row.kept = s_row;
+  const double c = set.c, S = (double)a.S;
+  const bool by_count = set.k > 0 && set.k < a.V;
+  const auto share = [&](uint64_t t) { return share_up(set.p, t); };
+  float m = -INFINITY;
+  bool odd = false, known = false, found = false;
+  Cut cut{-INFINITY, ALL};   // nothing is cut off
+  if constexpr (TYPE == RENO_T_BF16 && THREADS > 64)
+    if (set.p < 1.0 && !by_count) found = by_counts(row, s, c, S, share, &m, &odd, &known, &cut);
   float group[GROUPS] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-  bool odd = false;
-  const auto look = [&](const uint4& raw) {
-    Vec<TYPE> x;
-    x.from(raw);
-    float top = -INFINITY;
+  if (!known) {
+    // the largest logit, and the largest of the thread's groups
+    const auto look = [&](const uint4& raw) {
+      Vec<TYPE> x;
+      x.from(raw);
+      float top = -INFINITY;
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-      odd |= !(x.x[e] < INFINITY);
-      top = fmaxf(top, x.x[e]);
+      for (int e = 0; e < N; ++e) {
+        odd |= !(x.x[e] < INFINITY);
+        top = fmaxf(top, x.x[e]);
+      }
+      const float first = fmaxf(group[0], top);
+#pragma unroll
+      for (int g = 0; g + 1 < GROUPS; ++g) group[g] = group[g + 1];
+      group[GROUPS - 1] = first;
+    };
+    for (int t0 = 0; t0 < row.turns; t0 += 4) {   // four loads under way
+      uint4 raw[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (t0 + i < row.turns) raw[i] = row.load(t0 + i);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (t0 + i < row.turns) look(raw[i]);
     }
-    const float first = fmaxf(group[0], top);
-#pragma unroll
-    for (int g = 0; g + 1 < GROUPS; ++g) group[g] = group[g + 1];
-    group[GROUPS - 1] = first;
-  };
-  for (int t0 = 0; t0 < row.turns; t0 += 4) {   // four loads under way
-    uint4 raw[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (t0 + i < row.turns) raw[i] = row.raw(t0 + i);
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (t0 + i < row.turns) look(raw[i]);
-  }
-  float m = fmaxf(fmaxf(group[0], group[1]), fmaxf(group[2], group[3]));
-  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-  const bool any_odd = __ballot(odd) != 0;
-  if (lane == 0) {
-    s.top[wave] = m;
-    s.odd[wave] = any_odd;
-  }
-  if (tid == 0) s.n = 0;
-  __syncthreads();
-  odd = false;
-  for (int i = 0; i < WAVES; ++i) {
-    m = fmaxf(m, s.top[i]);
-    odd |= s.odd[i] != 0;
+    m = fmaxf(fmaxf(group[0], group[1]), fmaxf(group[2], group[3]));
+    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+    const bool any_odd = __ballot(odd) != 0;
+    if (lane == 0) {
+      s.top[wave] = m;
+      s.odd[wave] = any_odd;
+    }
+    if (tid == 0) s.n = 0;
+    __syncthreads();
+    odd = false;
+    for (int i = 0; i < WAVES; ++i) {
+      m = fmaxf(m, s.top[i]);
+      odd |= s.odd[i] != 0;
+    }
   }
   if (odd || m == -INFINITY) {
     if (tid == 0) answer(-1, odd ? NAN : 0.0f);
     return;
   }
-  const double c = set.c, S = (double)a.S;
   const float least = from_ordered(least_key(set, m));
-  Cut cut{-INFINITY, -1};   // nothing is cut off
 
   if (set.k > 0 && set.k <= LIST_K && set.k < a.V) {
     // the largest 16-bit prefix that at least k groups' maxima reach bounds the k-th largest logit from below
@@ -1229,16 +1276,7 @@ __global__ void __launch_bounds__(THREADS, LOCC) k_sample_long(SampleArgs a) {
           if (rank[q] <= set.k) mine += s.hist[i];
         }
       }
-      const auto block_total = [&](uint64_t v) {
-        v = wave_sum(v);
-        __syncthreads();
-        if (lane == 0) s.part[wave] = v;
-        __syncthreads();
-        v = 0;
-        for (int i = 0; i < WAVES; ++i) v += s.part[i];
-        return v;
-      };
-      const uint64_t mass = block_total(mine);
+      const uint64_t mass = block_total(s, mine);
       const uint64_t wanted = set.p < 1.0 ? share_up(set.p, mass) : mass;
       mine = 0;
 #pragma unroll
@@ -1254,7 +1292,7 @@ __global__ void __launch_bounds__(THREADS, LOCC) k_sample_long(SampleArgs a) {
           rank[q] = 0;
         }
       }
-      const uint64_t total = block_total(mine);   // (its barriers: everyone has read the weights)
+      const uint64_t total = block_total(s, mine);   // (its barriers: everyone has read the weights)
       const uint64_t want = share_down(set.u, total) + 1;
 #pragma unroll
       for (int q = 0; q < PER; ++q) {
@@ -1287,40 +1325,33 @@ __global__ void __launch_bounds__(THREADS, LOCC) k_sample_long(SampleArgs a) {
       return;
     }
   }
-  if (set.k > 0 && set.k < a.V) {
-    if (set.k == 1) {
-      int index;
-      float z;
-      uint64_t n;
-      pick<true>(row, s, Cut{m, a.V}, 0.0, 0.0, 0.0, [&](uint64_t) { return (uint64_t)1; }, &index, &z, &n);
-      cut = Cut{m, index};
-    } else {
-      cut = search<false, false>(row, s, cut, m, (float)fmin(40.0 / c, 3e38), c, S, [&](uint64_t) { return (uint64_t)set.k; });
-    }
-  }
-  if (set.p < 1.0) {
-    const auto want = [&](uint64_t t) { return share_up(set.p, t); };
-    const float range = set.octaves * __builtin_amdgcn_rcpf((float)c);
-    bool found = false;
-    if constexpr (TYPE == RENO_T_BF16 && THREADS > 64)
-      if (cut.x == -INFINITY && m < 0x1p6f && fabsf(m) >= 0x1p-6f) found = by_counts(row, s, m, c, S, want, &cut);
-    if (!found)
-      cut = cut.x > -INFINITY ? search<true, true>(row, s, cut, m, range, c, S, want)
-                              : search<true, false>(row, s, cut, m, range, c, S, want);
-  }
-  if (set.least > 0.0 && least > cut.x) cut = Cut{least, a.V};
+  if (by_count)
+    cut = set.k == 1 ? Cut{m, 1}
+                     : search<false>(row, s, cut, m, (float)fmin(40.0 / c, 3e38), c, S, [&](uint64_t) { return (uint64_t)set.k; });
+  if (set.p < 1.0 && !found) cut = search<true>(row, s, cut, m, set.octaves * __builtin_amdgcn_rcpf((float)c), c, S, share);
+  if (set.least > 0.0 && least > cut.x) cut = Cut{least, ALL};
   int index;
   float z;
   uint64_t total;
-  pick<false>(row, s, cut, (double)m, c, S, [&](uint64_t all) { return share_down(set.u, all) + 1; }, &index, &z,
+  pick(row, s, cut, (double)m, c, S, [&](uint64_t all) { return share_down(set.u, all) + 1; }, &index, &z,
               &total);
   if (share_down(set.u, total) == 0) {   // a share of nothing: the first symbol of any weight, though it be less than a unit
+    const bool whole = cut.ties == ALL;   // (the cut's own weight is a unit at least, or it is none by mass)
     int first = a.V;
     row.each([&](int t, const float (&x)[N]) {
 #pragma unroll
       for (int e = N - 1; e >= 0; --e)
-        if (cut.keeps(x[e], row.index(t, e)) && ((double)x[e] - (double)m) * c >= -1074.0) first = min(first, row.index(t, e));
+        if ((x[e] > cut.x || (whole && x[e] == cut.x)) && ((double)x[e] - (double)m) * c >= -1074.0)
+          first = min(first, row.index(t, e));
     });
+    if (!whole && ((double)cut.x - (double)m) * c >= -1074.0) {
+      // the first that equals the cut is kept
+      row.each([&](int t, const float (&x)[N]) {
+#pragma unroll
+        for (int e = N - 1; e >= 0; --e)
+          if (x[e] == cut.x) first = min(first, row.index(t, e));
+      });
+    }
     __syncthreads();
     if (tid == 0) s.index = a.V;
     __syncthreads();
@@ -1343,22 +1374,26 @@ void run(const SampleArgs& a, int64_t rows, hipStream_t st) {
     return;
   }
   const int pieces = (a.V + Vec<TYPE>::N - 1) / Vec<TYPE>::N;
-  const auto go = [&](auto kern, int threads) {
+  const auto go = [&](auto kern, int threads, bool keep) {
     const int turns = (pieces + threads - 1) / threads;
-    hipLaunchKernelGGL(kern, dim3((unsigned)rows), dim3(threads), 32 * turns * (threads / 64), st, a);   // sums of each turn
+    const unsigned lds = (unsigned)sizeof(Turn) * turns * (threads / 64) + (keep ? 16 * turns * threads : 0);
+    hipLaunchKernelGGL(kern, dim3((unsigned)rows), dim3(threads), lds, st, a);
   };
   // Threads of a row.  With rows for every CU several blocks share one, and fewer threads wait less for one another
   // (2048 rows of 32768 fp32, top_p, with 128, 256, 512, 1024: 209, 203, 183, 256 us; 8192 of 4096: 107, 102, 136, 307);
-  // else a row is as quick as its threads are many (64 rows of 50021 fp16: 119, 69, 49, 42).
+  // else a row is as quick as its threads are many (64 rows of 50021 fp16: 119, 69, 49, 42), and is kept where it fits
+  // (38; with a mask 45 against 54).
   int threads = pieces <= 128 ? 64 : pieces <= 512 ? 128 : pieces <= 4096 ? 256 : 512;
   if (rows <= 256)
     while (threads < 1024 && threads * 2 < pieces) threads *= 2;
   switch (threads) {
-    case 64: go(k_sample_long<TYPE, 64>, 64); break;
-    case 128: go(k_sample_long<TYPE, 128>, 128); break;
-    case 256: go(k_sample_long<TYPE, 256>, 256); break;
-    case 512: go(k_sample_long<TYPE, 512>, 512); break;
-    default: go(k_sample_long<TYPE, 1024>, 1024);
+    case 64: go(k_sample_long<TYPE, 64, false>, 64, false); break;
+    case 128: go(k_sample_long<TYPE, 128, false>, 128, false); break;
+    case 256: go(k_sample_long<TYPE, 256, false>, 256, false); break;
+    case 512: go(k_sample_long<TYPE, 512, false>, 512, false); break;
+    default:
+      if (pieces <= 8 * 1024) go(k_sample_long<TYPE, 1024, true>, 1024, true);   // 128 of 160 KB
+      else go(k_sample_long<TYPE, 1024, false>, 1024, false);
   }
 }
 
