@@ -144,8 +144,7 @@ _HEAD_SIGS = {
     "reno_head_distill": (_int, [ctypes.POINTER(reno_head), ctypes.POINTER(reno_head_data), _vp, _vp, _int,
                                  ctypes.c_float, _vp, _i64, _vp]),
     "reno_top_logits": (_int, [_vp, _int, _i64, _int, _i64, _int, _vp, _vp, _vp, _vp]),
-    "reno_sample_symbols": (_int, [ctypes.POINTER(reno_sample), _vp, _vp, _vp, _vp, _vp, _i64, _vp]),
-    "reno_sample_workspace": (_int, [ctypes.POINTER(reno_sample), ctypes.POINTER(_i64)]),
+    "reno_sample_symbols": (_int, [ctypes.POINTER(reno_sample), _vp, _vp, _vp, _vp, _vp]),
     "reno_features": (_int, [_vp, _int, _vp]),
 }
 
@@ -744,7 +743,7 @@ class Samples(typing.NamedTuple):
     bits: object          # float32 [N], -log2 of the symbol's probability
 
 
-def sample_symbols(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, allowed=None, workspace=None,
+def sample_symbols(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, allowed=None,
                    stream=None) -> Samples:
     """A symbol of each row of logits [N][V] (float32, bfloat16 or float16, rows
     may be strided), drawn by the row's random number u float32 [N] in [0, 1)
@@ -759,8 +758,8 @@ def sample_symbols(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, al
     give symbol -1 and NaN bits.
 
     The same u gives the same symbol every time, whatever the other rows are:
-    masses are exact sums (include/reno_head.h).  workspace: a uint8 tensor of
-    sample_workspace bytes, or None to take it from torch's allocator."""
+    masses are exact sums (include/reno_head.h).  Enqueued on ``stream`` (default:
+    the current stream of the logits' device)."""
     import torch
     _need(logits.dim() == 2 and logits.is_cuda, "logits must be a device tensor [N][V]")
     kind = _type_of(logits.dtype)
@@ -791,32 +790,13 @@ def sample_symbols(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, al
             keep.append(t)
             p.allowed = t.data_ptr()
             p.allowed_stride = 0 if t.dim() == 1 else _stride(t)
-        need = ctypes.c_int64()
-        _head_check(lib().reno_sample_workspace(ctypes.byref(p), ctypes.byref(need)))
-        ws = workspace
-        if ws is None and need.value:
-            ws = torch.empty(need.value, dtype=torch.uint8, device=dev)
-        if ws is not None:
-            _need(ws.device == dev and ws.is_contiguous(), "workspace must be contiguous and on the device of the arguments")
-            keep.append(ws)
         symbol = torch.empty(n, dtype=torch.int32, device=dev)
         bits = torch.empty(n, dtype=torch.float32, device=dev)
         _head_check(lib().reno_sample_symbols(ctypes.byref(p), x.data_ptr(), uu.data_ptr(), symbol.data_ptr(),
-                                              bits.data_ptr(), 0 if ws is None else ws.data_ptr(),
-                                              0 if ws is None else ws.numel() * ws.element_size(), st.cuda_stream))
+                                              bits.data_ptr(), st.cuda_stream))
         _read_on(stream, *keep)
         return Samples(symbol, bits)
     return _on(dev, stream, run)
-
-
-def sample_workspace(rows: int, symbols: int, dtype) -> int:
-    """Bytes of workspace for such a call (reno_sample_workspace)."""
-    kind = _type_of(dtype)
-    _need(kind is not None, "dtype must be float32, bfloat16 or float16")
-    p = reno_sample(rows, symbols, kind, symbols, 1.0, 1.0, 0.0, 0)
-    n = ctypes.c_int64()
-    _head_check(lib().reno_sample_workspace(ctypes.byref(p), ctypes.byref(n)))
-    return n.value
 
 
 def _in_list(name, dev, *tensors):

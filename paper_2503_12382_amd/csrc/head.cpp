@@ -131,16 +131,8 @@ reno_status reno_top_logits(const void* logits, int type, int64_t rows, int symb
   return RENO_OK;
 }
 
-reno_status reno_sample_workspace(const reno_sample* how, int64_t* bytes_host) {
-  const reno_status s = check_sample(how);
-  if (s != RENO_OK) return s;
-  if (!bytes_host) return fail_thread(RENO_E_INVALID, "null argument");
-  *bytes_host = 0;
-  return RENO_OK;
-}
-
 reno_status reno_sample_symbols(const reno_sample* how, const void* logits, const float* u, int32_t* symbol, float* bits,
-                                void* ws, int64_t bytes, void* hip_stream) {
+                                void* hip_stream) {
   const reno_status s = check_sample(how);
   if (s != RENO_OK) return s;
   if (how->rows == 0) return RENO_OK;

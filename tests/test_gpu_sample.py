@@ -171,6 +171,53 @@ def test_strides(dt):
     assert r.symbol.shape == (0,) and r.bits.shape == (0,)
 
 
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("V", [257, 600, 1100, 2100, 4200, 9000, 33000, 66000])
+def test_many_rows(V, dt):
+    """More rows than CUs: other numbers of threads a row."""
+    N = 260
+    g = torch.Generator().manual_seed(V)
+    z, u = make(N, V, dt, V + 7)
+    z[:, 5] = -math.inf
+    z[3] = 0.0                          # one value
+    z[4, V // 2:] = 0.0                 # many logits of a value that is in no table
+    z[5] = z[5] * 0.001                 # all of them small
+    z[6] = z[6] * 40                    # far beyond
+    z[7, 9] = 90.0 if dt != torch.float16 else 60.0
+    z[8] = z[8].abs() * -1 - 3
+    z[9, 1] = math.nan
+    z[10, V - 1] = math.inf
+    z[11] = -math.inf
+    p = torch.rand(N, generator=g)
+    p[:20] = 0.9
+    k = torch.zeros(N, dtype=torch.int32)
+    k[100:180] = torch.randint(1, V, (80,), generator=g).int()
+    k[180:] = torch.randint(1, 300, (80,), generator=g).int()
+    p[100:140] = 1.0
+    least = torch.where(torch.rand(N, generator=g) < 0.2, 0.01, 0.0)
+    for kw in (dict(top_p=0.9), dict(top_p=p.cuda(), top_k=k.cuda(), min_p=least.cuda()), dict()):
+        say("sample, many rows", V, dt, sorted(kw))
+        assert check(reno.sample_symbols(z, u, **kw), draw(z, u, **kw), V, (V, dt, sorted(kw))) >= N - 2
+
+
+@pytest.mark.parametrize("dt", TYPES)
+def test_list_ends(dt):
+    """As many equal logits at the cut as the lists of long rows hold, and one more; counts up to and past those that
+    are cut in a list."""
+    V = 6000
+    for n in (511, 512, 513, 700):
+        z = torch.full((8, V), -4.0)
+        z[:, 100:100 + n] = 1.0
+        z[:, 3] = 2.0
+        z[4:] += torch.rand(4, V, generator=torch.Generator().manual_seed(n)) * 2.0 ** -6
+        z = z.to(dt).cuda()
+        u = torch.tensor([0.0, 0.3, 0.7, 1 - 2.0 ** -24] * 2).cuda()
+        for kw in (dict(top_k=n), dict(top_k=n // 2), dict(top_k=256), dict(top_k=257, top_p=0.5), dict(top_p=0.4),
+                   dict(top_k=1), dict(temperature=0.0), dict(top_k=255, top_p=0.99, min_p=0.5)):
+            say("sample, lists", n, dt, kw)
+            check(reno.sample_symbols(z, u, **kw), draw(z, u, **kw), V, (n, dt, kw))
+
+
 def test_long_offsets():
     """Rows whose offset passes 2^31 elements, the largest alphabet."""
     V = 1 << 20
@@ -190,6 +237,16 @@ def test_long_offsets():
     assert r.symbol.item() == V // 2 and r.bits.item() == 20.0
     r = reno.sample_symbols(z[-1:], u[-1:], top_k=V // 4, top_p=0.5)
     assert r.symbol.item() == V // 16 and r.bits.item() == 17.0
+    # the longest rows of 32 bits: the most turns of a wave
+    z = torch.zeros(300, V, device="cuda")
+    z[:, 0] = 1.0
+    for rows in (1, 300):
+        r = reno.sample_symbols(z[:rows], torch.full((rows,), 0.75, device="cuda"), top_p=0.5, top_k=V - 1)
+        # weights e and V - 2 ones: half of them are the first and n ones, and u lies within the ones
+        n = math.ceil(0.5 * (V - 2 + math.e) - math.e)
+        W = n + math.e
+        assert r.symbol.tolist() == [math.floor(0.75 * W - math.e) + 1] * rows
+        assert r.bits[0].item() == pytest.approx(math.log2(W), abs=1e-6)
 
 
 def test_capture_and_streams():
@@ -217,9 +274,6 @@ def test_capture_and_streams():
     torch.full_like(z, 7.0)
     s.synchronize()
     assert torch.equal(r.symbol, want[0]) and torch.equal(r.bits, want[1])
-    n = reno.sample_workspace(2, 60000, torch.bfloat16)
-    ws = torch.empty(max(n, 1), dtype=torch.uint8, device="cuda")
-    assert torch.equal(reno.sample_symbols(big, ub, top_k=40, top_p=0.9, workspace=ws).symbol, want[2])
 
 
 def test_frequencies():

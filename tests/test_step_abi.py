@@ -122,10 +122,9 @@ def test_adamw_rejects_bad_arguments():
 def test_sample_rejects_bad_arguments():
     L = reno.lib()
     good = dict(rows=4, symbols=100000, type=0, row_stride=100000, temperature=1.0, top_p=1.0, min_p=0.0, top_k=0)
-    n = ctypes.c_int64(-1)
 
-    def call(z=P, u=P, symbol=P, bits=P, ws=P, size=1 << 40, **kw):
-        return L.reno_sample_symbols(ctypes.byref(reno.reno_sample(**{**good, **kw})), z, u, symbol, bits, ws, size, None)
+    def call(z=P, u=P, symbol=P, bits=P, **kw):
+        return L.reno_sample_symbols(ctypes.byref(reno.reno_sample(**{**good, **kw})), z, u, symbol, bits, None)
     nan, inf = float("nan"), float("inf")
     for kw in (dict(rows=-1), dict(rows=1 << 31), dict(symbols=0), dict(symbols=(1 << 20) + 1, row_stride=1 << 21),
                dict(type=3), dict(row_stride=99999), dict(row_stride=1 << 31), dict(temperature=-1.0), dict(temperature=nan),
@@ -133,16 +132,10 @@ def test_sample_rejects_bad_arguments():
                dict(top_p=1.1), dict(top_p=nan), dict(min_p=-0.1), dict(min_p=1.1), dict(min_p=nan), dict(top_k=-1),
                dict(allowed=P, allowed_stride=99999), dict(allowed=P, allowed_stride=-1), dict(allowed=P, allowed_stride=1 << 31)):
         assert call(**kw) == INVALID, kw
-        assert L.reno_sample_workspace(ctypes.byref(reno.reno_sample(**{**good, **kw})), ctypes.byref(n)) == INVALID, kw
         assert L.reno_last_error(None)
     for kw in (dict(z=None), dict(u=None), dict(symbol=None), dict(bits=None), dict(z=P + 2), dict(u=P + 1),
                dict(symbol=P + 2), dict(bits=P + 2), dict(temperature_rows=P + 2), dict(top_k_rows=P + 1),
                dict(top_p_rows=P + 2), dict(min_p_rows=P + 3)):
         assert call(**kw) == INVALID, kw
-    assert call(rows=0, z=None, u=None, symbol=None, bits=None, ws=None, size=0) == reno.RENO_OK
-    assert L.reno_sample_workspace(None, ctypes.byref(n)) == INVALID
-    assert L.reno_sample_symbols(None, P, P, P, P, P, 0, None) == INVALID
-    assert L.reno_sample_workspace(ctypes.byref(reno.reno_sample(**good)), None) == INVALID
-    for rows in (0, 1, 64, (1 << 31) - 1):
-        assert L.reno_sample_workspace(ctypes.byref(reno.reno_sample(**{**good, "rows": rows})),
-                                       ctypes.byref(n)) == reno.RENO_OK and n.value >= 0
+    assert call(rows=0, z=None, u=None, symbol=None, bits=None) == reno.RENO_OK
+    assert L.reno_sample_symbols(None, P, P, P, P, None) == INVALID
