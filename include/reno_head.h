@@ -156,13 +156,13 @@ typedef struct {
  *   has top_p of their weight (one at least); of these those with w >= min_p.
  * With W the weight of what is left: symbol = the lowest index up to which
  * (inclusive) those that are left weigh more than u W together, and bits =
- * -log2(w_symbol / W), fp32.  Weights are computed in 64 bits, to 2^-46, and
- * summed exactly in units of 2^-51 of the largest for V up to 2048, of
- * 2^(ceil(log2 V) - 62) above; top_p W and u W are 64-bit floats.  A u W below one
- * unit draws the first symbol of any weight from 2^-1074 on.  A u outside [0, 1)
- * or NaN leaves its row out, and a row without symbols has none: symbol -1, bits
- * 0.  A logit of +inf or NaN that is allowed, and settings that are none: symbol
- * -1, bits NaN.  Needs no workspace. */
+ * -log2(w_symbol / W), fp32.  Weights are computed in 64 bits, to 2^-46 (those
+ * below 2^-64 of the largest to 2^-42), and summed exactly in units of 2^-51 of
+ * the largest for V up to 2048, of 2^(ceil(log2 V) - 62) above; top_p W and u W
+ * are 64-bit floats.  A u W below one unit draws the first symbol of any weight
+ * from 2^-1074 on.  A u outside [0, 1) or NaN leaves its row out, and a row
+ * without symbols has none: symbol -1, bits 0.  A logit of +inf or NaN that is
+ * allowed, and settings that are none: symbol -1, bits NaN.  Needs no workspace. */
 reno_status reno_sample_symbols(const reno_sample* how, const void* logits, const float* u, int32_t* symbol, float* bits,
                                 void* hip_stream);
 

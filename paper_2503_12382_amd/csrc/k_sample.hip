@@ -2,17 +2,31 @@
 //
 // Decisions next to borders have to be those of exact sums, so masses are
 // integers: a symbol's weight 2^y, y = (z - max) log2(e) / T, is computed in 64
-// bits to 2^-48 and counted in units of 2^-S of the largest, 2^S V < 2^63.  Sums
-// of them are exact in any order, LDS atomics among it.
+// bits and counted in units of 2^-S of the largest, 2^S V < 2^63.  Sums of them
+// are exact in any order, that of LDS atomics among it.
 //
-// What is kept is a prefix of the row in descending order, ties by index, so it
-// is given by a cut: the ordered value of the last logit kept, and the index up
-// to which logits equal to it are.  The cut of a count or of a mass is found
-// without sorting: a histogram over the row, the bin that holds the cut, a
-// histogram over that bin's range of values, until a bin is one value.
+// What is kept is a run of the row in descending order, ties by index: logits
+// above a cut, and some of those that equal it.  The cut of a count or a mass is
+// found without sorting: a histogram by value over the row, then among the few
+// logits of the bin that holds it the sums of all pairs (more than fit a list:
+// histograms over what the bin spans, until that is one value).  The symbol is
+// found by sums along the row, of a lane or of a wave's turn, and in the one that
+// holds it once more.
 //
-//   k_sample_short rows of up to 256: 16 lanes a row, in registers
-//   k_sample_long  a block a row, read again for each look at it
+// Bound by instructions, not by the read of the logits: an exact weight is 21 of
+// them, 17 in 64 bits, which run at the rate of 32.
+//   k_sample_short  rows of up to 256: 16 lanes a row, so that one wave's
+//                   instructions serve four rows, the row and its weights in
+//                   registers.  233737 x 256 fp32, top_p 0.95, a mask: 120 us,
+//                   2.0 TB/s, 1240 instructions of a wave, half of them a
+//                   logit's and half a row's
+//   k_sample_long   a block a row.  Small counts: the k-th largest of many
+//                   groups' maxima bounds the k-th largest logit, and what lies
+//                   above is cut, weighed and drawn from in a list (one row of
+//                   131071 fp32, top_k 50: 31 us, one block's latency).  bf16
+//                   by mass: values are counted first and weighed once each
+//                   (4096 x 32768, top_p 0.9: 157 us, 34 instructions a logit).
+//                   Else by a histogram of weights (2048 x 32768 fp32: 196 us)
 
 #include <algorithm>
 #include <cmath>
@@ -81,7 +95,7 @@ __device__ __forceinline__ uint64_t units(float x, double m, double c, double S)
   return u;
 }
 
-// log2 of a whole number from 1, to 2^-44: fp32's logarithm, and what 2 to its power lacks.
+// log2 of a whole number from 1, to 2^-42: fp32's logarithm, and what 2 to its power lacks.
 __device__ __forceinline__ double log2_of(uint64_t n) {
   const int e = 63 - __builtin_clzll(n);
   const double f = __builtin_ldexp((double)n, -e);           // 1 .. 2
@@ -90,6 +104,10 @@ __device__ __forceinline__ double log2_of(uint64_t n) {
   double w[1];
   exp2_all<1>(y, w);
   return (double)e + l + __builtin_fma(f, w[0], -1.0) * 1.4426950408889634;
+}
+
+__device__ __forceinline__ void add(uint64_t* to, uint64_t v) {   // LDS
+  atomicAdd(reinterpret_cast<unsigned long long*>(to), (unsigned long long)v);
 }
 
 // The units of a row of V: the sum of V of them stays below 2^63.
@@ -109,8 +127,8 @@ __device__ __forceinline__ uint64_t share_down(float u, uint64_t m) { return (ui
 // A row's settings.
 struct Row {
   double T, c, p, least, log_least;   // c: log2(e) / T, 0 for a T of 0
-  float octaves;           // below the largest weight: the cut by p lies above
-  int64_t k;        // 0: all
+  float octaves;                      // below the largest weight: the cut by p lies above
+  int64_t k;                          // 0: all
   float u;
   bool valid;
 };
@@ -223,7 +241,7 @@ __device__ __forceinline__ int row16_which(bool here) {
 
 // Shared memory of a wave.
 struct ShortShared {
-  uint64_t hist[SHORT_ROWS][SHORT_BINS + 16];   // 63 bins, then the last one of each lane: what lies far below meets there
+  uint64_t hist[SHORT_ROWS][SHORT_BINS + 16];   // 63 bins, then the last one, of each lane: most logits lie far below
   ulonglong2 cand[SHORT_ROWS][16];
   float x[SHORT_ROWS][16 * SHORT_LANE];   // the rows, for the turns that are rare: logit i of lane l at 16 i + l
 };
@@ -259,8 +277,8 @@ __device__ __forceinline__ float next_above(float x) {
 }
 
 // The bin of a histogram at which what is wanted is reached; q.above becomes what lies above it.
-__device__ __forceinline__ int short_bin(const ShortShared& s, ShortSearch& q, uint64_t (&h)[SHORT_BINS / 16], uint64_t mine,
-                                         uint64_t upto) {
+__device__ __forceinline__ int short_bin(const ShortShared& s, ShortSearch& q, uint64_t (&h)[SHORT_BINS / 16],
+                                         uint64_t mine, uint64_t upto) {
   constexpr int PER = SHORT_BINS / 16;
   uint64_t a = q.above + upto - mine;
   const int owner = row16_which(a < q.wanted && a + mine >= q.wanted);
@@ -301,8 +319,8 @@ __device__ __forceinline__ void short_pairs(const ShortShared& s, ShortSearch& q
 // The rare turns, for rows whose bin holds more than 16 logits (from what `in` says first): a histogram over what the
 // bin spans until few are left or all are equal.  One logit at a time from LDS.
 template <bool MASS, int PL, typename In>
-__device__ __forceinline__ void short_more(ShortShared& s, ShortSearch& q, int v0, float m, double c, double S, const In& in,
-                                        ShortCut* cut) {
+__device__ __forceinline__ void short_more(ShortShared& s, ShortSearch& q, int v0, float m, double c, double S,
+                                           const In& in, ShortCut* cut) {
   constexpr int PER = SHORT_BINS / 16;
   const int lane = lane_id(), l15 = lane & 15, rw = lane >> 4;
   uint32_t lo = 0, top = ALL;   // the ordered values that are left
@@ -368,7 +386,7 @@ __device__ __forceinline__ void short_more(ShortShared& s, ShortSearch& q, int v
 #pragma unroll 1
     for (int i = 0; i < PL; ++i) {
       const float x = s.x[rw][i * 16 + l15];
-      if (left(x)) atomicAdd((unsigned long long*)&s.hist[rw][(top - ordered(x)) >> shift], (unsigned long long)measure(x));
+      if (left(x)) add(&s.hist[rw][(top - ordered(x)) >> shift], measure(x));
     }
     wave_lds_fence();
     uint64_t h[PER], mine = 0;
@@ -399,7 +417,7 @@ __device__ __forceinline__ void short_search(const Short<PL>& row, ShortShared& 
   const float last = (float)(SHORT_BINS - 1 + l15);
 #pragma unroll
   for (int i = 0; i < PL; ++i)
-    atomicAdd((unsigned long long*)&s.hist[rw][(uint32_t)fminf(bin_of(row.x[i]), last)], MASS ? (unsigned long long)row.w[i] : 1ull);
+    add(&s.hist[rw][(uint32_t)fminf(bin_of(row.x[i]), last)], MASS ? row.w[i] : 1);
   wave_lds_fence();
   uint64_t h[PER], mine = 0;
 #pragma unroll
@@ -443,14 +461,15 @@ __device__ __forceinline__ void short_search(const Short<PL>& row, ShortShared& 
   if (few && l15 < (int)all_n) {
     const uint32_t p = list[l15];
     const float x = s.x[rw][p];
-    s.cand[rw][l15] = make_ulonglong2(place_of(x, (int)(p & 15u) * PL + (int)(p >> 4)), MASS ? units(x, (double)m, c, S) : 1);
+    s.cand[rw][l15] =
+        make_ulonglong2(place_of(x, (int)(p & 15u) * PL + (int)(p >> 4)), MASS ? units(x, (double)m, c, S) : 1);
   }
   short_pairs(s, q, few, all_n, cut);
   if (__any(q.active)) short_more<MASS, PL>(s, q, row.v0, m, c, S, in, cut);
 }
 
 // Whether logit i of the lane is kept: `lim`, the last of the lane whose ties are, is cut.v - v0.
-__device__ __forceinline__ bool itimesept(float x, int i, float cut, float above, int lim) {
+__device__ __forceinline__ bool is_kept(float x, int i, float cut, float above, int lim) {
   return x >= (i <= lim ? cut : above);
 }
 
@@ -488,11 +507,8 @@ __device__ __forceinline__ void short_mask(const uint8_t* allowed, int V, int v0
   }
 }
 
-#ifndef SHORT_OCC
-#define SHORT_OCC 4
-#endif
 template <int TYPE, int PL>
-__global__ void __launch_bounds__(256, SHORT_OCC) k_sample_short(SampleArgs a, int64_t rows) {
+__global__ void __launch_bounds__(256, 4) k_sample_short(SampleArgs a, int64_t rows) {
   __shared__ ShortShared s_all[4];
   const int lane = lane_id(), wave = threadIdx.x >> 6, l15 = lane & 15, rw = lane >> 4;
   const int64_t r0 = ((int64_t)blockIdx.x * 4 + wave) * SHORT_ROWS;
@@ -531,16 +547,16 @@ __global__ void __launch_bounds__(256, SHORT_OCC) k_sample_short(SampleArgs a, i
     const float over = next_above(cut.x);
 #pragma unroll
     for (int i = 0; i < PL; ++i)
-      if (!itimesept(row.x[i], i, cut.x, over, cut.v - row.v0)) {
+      if (!is_kept(row.x[i], i, cut.x, over, cut.v - row.v0)) {
         row.x[i] = -INFINITY;
         row.w[i] = 0;
         s.x[rw][i * 16 + l15] = -INFINITY;
       }
   }
   const bool by_mass = live && set.p < 1.0;
-  if (__any(by_mass)) {
-    short_search<true>(row, s, by_mass, m, set.octaves * __builtin_amdgcn_rcpf((float)c), c, S, [&](uint64_t t) { return share_up(set.p, t); }, &cut);
-  }
+  if (__any(by_mass))
+    short_search<true>(row, s, by_mass, m, set.octaves * __builtin_amdgcn_rcpf((float)c), c, S,
+                       [&](uint64_t t) { return share_up(set.p, t); }, &cut);
   if (__any(live && set.least > 0.0)) {
     const float least = from_ordered(least_key(set, m));
     if (live && set.least > 0.0 && least > cut.x) cut = ShortCut{least, 255, false};
@@ -549,7 +565,7 @@ __global__ void __launch_bounds__(256, SHORT_OCC) k_sample_short(SampleArgs a, i
   const float over = next_above(cut.x);
   if (__any(cut.split)) {   // among logits that equal the last one
 #pragma unroll
-    for (int i = 0; i < PL; ++i) row.w[i] = itimesept(row.x[i], i, cut.x, over, cut.v - row.v0) ? row.w[i] : 0;
+    for (int i = 0; i < PL; ++i) row.w[i] = is_kept(row.x[i], i, cut.x, over, cut.v - row.v0) ? row.w[i] : 0;
   } else {
 #pragma unroll
     for (int i = 0; i < PL; ++i) row.w[i] = row.x[i] >= cut.x ? row.w[i] : 0;
@@ -564,7 +580,8 @@ __global__ void __launch_bounds__(256, SHORT_OCC) k_sample_short(SampleArgs a, i
     uint64_t ones = 0;
 #pragma unroll
     for (int i = 0; i < PL; ++i) {
-      const bool some = itimesept(row.x[i], i, cut.x, over, cut.v - row.v0) && ((double)row.x[i] - (double)m) * c >= -1074.0;
+      const bool some =
+          is_kept(row.x[i], i, cut.x, over, cut.v - row.v0) && ((double)row.x[i] - (double)m) * c >= -1074.0;
       row.w[i] = any ? (some ? 1 : 0) : row.w[i];
       ones += row.w[i];
     }
@@ -618,6 +635,7 @@ __device__ __forceinline__ uint64_t wave_sum(uint64_t v) {   // in every lane
   const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), 63);
   return (uint64_t)hi << 32 | lo;
 }
+
 // bf16 logits of 2^-6 to 2^6 are counted by value, one of 12 times 128 values of either sign.
 constexpr int ZONE = 12 * 128, ZONE_FIRST = (127 - 6) << 7, OTHERS = 512;
 
@@ -634,8 +652,8 @@ struct Turn {
 
 // THREADS a row.  A wave's pieces of 16 bytes follow one another: the row's order is by wave, then by turn, then by
 // lane.  KEEP: the first look leaves the row in LDS, where a thread reads what it wrote itself.  Else the row is read
-// anew for each look: with rows for every CU LDS has no place for enough of them (4096 rows of 32768 bf16, two looks
-// more than now: 247 us, against 210).
+// anew for each look: with rows for every CU LDS has no place for enough of them (4096 rows of 32768 bf16, with four
+// looks a row: 210 us, and 247 with the row in LDS; with two looks now 157).
 template <int TYPE, int THREADS, bool KEEP>
 struct Long {
   static constexpr int N = Vec<TYPE>::N, WAVES = THREADS / 64, SIZE = 16 / N;
@@ -785,7 +803,8 @@ __device__ __forceinline__ void pick(const L& row, S& s, const Cut& cut, double 
 #pragma unroll
       for (int e = 0; e < N; ++e) {
         const uint64_t which = __ballot(x.x[e] >= from);
-        const uint32_t at = __builtin_amdgcn_mbcnt_hi((uint32_t)(which >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)which, (uint32_t)n));
+        const uint32_t at = __builtin_amdgcn_mbcnt_hi((uint32_t)(which >> 32),
+                                                      __builtin_amdgcn_mbcnt_lo((uint32_t)which, (uint32_t)n));
         if (x.x[e] >= from && (PUSHED >= 64 * N || at < PUSHED)) pushed[at] = x.x[e];
         n += (int)__popcll(which);
       }
@@ -909,7 +928,7 @@ __device__ __forceinline__ Cut search(const L& row, S& s, const Cut from, float 
 #pragma unroll
       for (int e = e0; e < e0 + 4; ++e)
         if (x[e] > from.x)
-          atomicAdd((unsigned long long*)&s.hist[(uint32_t)fminf(bin_of(x[e]), last)], MASS ? (unsigned long long)w[e - e0] : 1ull);
+          add(&s.hist[(uint32_t)fminf(bin_of(x[e]), last)], MASS ? w[e - e0] : 1);
     }
   });
   if (tid == 0) s.n = 0;
@@ -985,7 +1004,7 @@ __device__ __forceinline__ Cut search(const L& row, S& s, const Cut from, float 
 #pragma unroll
       for (int e = 0; e < N; ++e) {
         const uint32_t o = ordered(x[e]), b = (hi - o) >> shift;
-        if (o >= lo && o <= hi) atomicAdd((unsigned long long*)&s.hist[b], (unsigned long long)measure(x[e]));
+        if (o >= lo && o <= hi) add(&s.hist[b], measure(x[e]));
       }
     });
     __syncthreads();
@@ -1327,7 +1346,8 @@ __global__ void __launch_bounds__(THREADS) k_sample_long(SampleArgs a) {
   }
   if (by_count)
     cut = set.k == 1 ? Cut{m, 1}
-                     : search<false>(row, s, cut, m, (float)fmin(40.0 / c, 3e38), c, S, [&](uint64_t) { return (uint64_t)set.k; });
+                     : search<false>(row, s, cut, m, (float)fmin(40.0 / c, 3e38), c, S,
+                                     [&](uint64_t) { return (uint64_t)set.k; });
   if (set.p < 1.0 && !found) cut = search<true>(row, s, cut, m, set.octaves * __builtin_amdgcn_rcpf((float)c), c, S, share);
   if (set.least > 0.0 && least > cut.x) cut = Cut{least, ALL};
   int index;
