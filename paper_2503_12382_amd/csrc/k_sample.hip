@@ -1264,6 +1264,10 @@ __global__ void __launch_bounds__(THREADS) k_sample_long(SampleArgs a) {
     }
     const float low = from_ordered(max(bound, FIRST_LIVE));
     row.each([&](int t, const float (&x)[N]) {
+      float top = x[0];
+#pragma unroll
+      for (int e = 1; e < N; ++e) top = fmaxf(top, x[e]);
+      if (!__any(top >= low)) return;
 #pragma unroll
       for (int e = 0; e < N; ++e)
         if (x[e] >= low) {
