@@ -26,7 +26,7 @@
 //                   131071 fp32, top_k 50: 31 us, one block's latency).  bf16
 //                   by mass: values are counted first and weighed once each
 //                   (4096 x 32768, top_p 0.9: 157 us, 34 instructions a logit).
-//                   Else by a histogram of weights (2048 x 32768 fp32: 196 us)
+//                   Else by a histogram of weights (2048 x 32768 fp32: 177 us)
 
 #include <algorithm>
 #include <cmath>
@@ -782,34 +782,84 @@ __device__ __forceinline__ void find_bin(Shared<WAVES>& s, uint64_t above, const
   }
 }
 
+// A search by mass that has found its bin, and leaves the cut in it to the next look at the row: what lies above the
+// bin, and what the cut has to reach.
+struct Pending {
+  bool on;
+  float b0, b1, m, scale, over;   // the bin's logits: b0 <= (m - x) scale <= b1 and x > over
+  uint64_t above, wanted;
+};
+
+// The cut at x: as many of the logits that equal it, `equal` together and each of weight w, as it takes after what lies
+// above.
+__device__ __forceinline__ Cut cut_at(float x, uint64_t w, uint64_t wanted, uint64_t above, uint64_t equal) {
+  const uint64_t ties = (wanted - above + w - 1) / w;
+  return Cut{x, ties * w >= equal ? ALL : (uint32_t)ties};
+}
+
+// The cut among n listed logits (their ordered values in the upper halves) of the measures s.hist: sums of all pairs.
+template <int WAVES>
+__device__ __forceinline__ Cut pairs(Shared<WAVES>& s, int n, uint64_t wanted, uint64_t above) {
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += WAVES * 64) {
+    const uint32_t me = (uint32_t)(s.list[i] >> 32);
+    uint64_t more = above, equal = 0;
+    for (int j = 0; j < n; ++j) {
+      const uint32_t o = (uint32_t)(s.list[j] >> 32);
+      more += o > me ? s.hist[j] : 0;
+      equal += o == me ? s.hist[j] : 0;
+    }
+    if (more < wanted && more + equal >= wanted) {   // (all that are equal write the same)
+      s.x = from_ordered(me);
+      s.above = s.hist[i];
+      s.before = more;
+      s.total = equal;
+    }
+  }
+  __syncthreads();
+  return cut_at(s.x, s.above, wanted, s.before, s.total);
+}
+
 // The symbol at which the weights along the row of what the cut keeps reach want(total), at least 1, and its logit.
-template <typename L, typename S, typename W>
-__device__ __forceinline__ void pick(const L& row, S& s, const Cut& cut, double m, double c, double bits, const W& want,
-                                     int* index, float* logit, uint64_t* total) {
-  constexpr int N = L::N, WAVES = L::WAVES, PUSHED = (int)(sizeof(s.hist) + sizeof(s.list)) / 4 / WAVES;
+// PEND: a search is pending, and the cut found on the way (false: too many logits in its bin, nothing is done).
+template <bool PEND, typename L, typename S, typename W>
+__device__ __forceinline__ bool pick(const L& row, S& s, Cut& cut, const Pending& pend, double m, double c, double bits,
+                                     const W& want, int* index, float* logit, uint64_t* total) {
+  constexpr int N = L::N, WAVES = L::WAVES, PUSHED = (int)(sizeof(s.hist) + (PEND ? 0 : sizeof(s.list))) / 4 / WAVES;
   Turn* turns = row.sums();
   const int lane = lane_id(), wave = threadIdx.x >> 6;
   float* pushed = reinterpret_cast<float*>(s.hist) + wave * PUSHED;   // a turn's logits, where histogram and list were
-  const bool whole = cut.ties == ALL;                // of those that equal the cut too
-  const float from = whole ? cut.x : next_above(cut.x);
+  bool whole = cut.ties == ALL;                // of those that equal the cut too
+  float from = whole ? cut.x : next_above(cut.x);
   __syncthreads();
   for (int t = 0; t < row.turns; ++t) {
     const auto x = row.at(t);
     uint64_t mine = 0;
     int n = 0, equal = 0;
     // few are kept as a rule: they are pushed together first, so that a weight is computed by every lane
-    const bool all = from == -INFINITY;
-    if (!all) {
+    const bool all = !PEND && from == -INFINITY;
+    const auto push = [&](bool kept, float y) {
+      const uint64_t which = __ballot(kept);
+      const uint32_t at = __builtin_amdgcn_mbcnt_hi((uint32_t)(which >> 32),
+                                                    __builtin_amdgcn_mbcnt_lo((uint32_t)which, (uint32_t)n));
+      if (kept && (PUSHED >= 64 * N || at < PUSHED)) pushed[at] = y;
+      n += (int)__popcll(which);
+    };
+    if constexpr (PEND) {
 #pragma unroll
       for (int e = 0; e < N; ++e) {
-        const uint64_t which = __ballot(x.x[e] >= from);
-        const uint32_t at = __builtin_amdgcn_mbcnt_hi((uint32_t)(which >> 32),
-                                                      __builtin_amdgcn_mbcnt_lo((uint32_t)which, (uint32_t)n));
-        if (x.x[e] >= from && (PUSHED >= 64 * N || at < PUSHED)) pushed[at] = x.x[e];
-        n += (int)__popcll(which);
+        const float b = (pend.m - x.x[e]) * pend.scale;
+        push(b < pend.b0, x.x[e]);
+        if (b >= pend.b0 && b <= pend.b1 && x.x[e] > pend.over) {
+          const int i = atomicAdd(&s.n, 1);
+          if (i < LIST) s.list[i] = (uint64_t)ordered(x.x[e]) << 32 | (uint32_t)(wave * row.turns + t);
+        }
       }
+    } else if (!all) {
+#pragma unroll
+      for (int e = 0; e < N; ++e) push(x.x[e] >= from, x.x[e]);
     }
-    if (!whole) {
+    if (!PEND && !whole) {
 #pragma unroll
       for (int e = 0; e < N; ++e) equal += (int)__popcll(__ballot(x.x[e] == cut.x));
     }
@@ -823,13 +873,29 @@ __device__ __forceinline__ void pick(const L& row, S& s, const Cut& cut, double 
         uint64_t w[4];
         units_all<4>(x.x + e0, m, c, bits, w);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) mine += x.x[e0 + e] >= from ? w[e] : 0;   // (-inf weighs nothing)
+        for (int e = 0; e < 4; ++e)   // (-inf weighs nothing)
+          mine += (PEND ? (pend.m - x.x[e0 + e]) * pend.scale < pend.b0 : x.x[e0 + e] >= from) ? w[e] : 0;
       }
     }
     mine = wave_sum(mine);
     if (lane == 0) turns[wave * row.turns + t] = Turn{mine, (uint64_t)equal};
   }
   __syncthreads();
+  if constexpr (PEND) {
+    const int n = s.n;
+    if (n > LIST) return false;
+    for (int i = threadIdx.x; i < n; i += WAVES * 64) s.hist[i] = units(x_of(s.list[i]), m, c, bits);
+    cut = pairs(s, n, pend.wanted, pend.above);
+    whole = cut.ties == ALL;
+    from = whole ? cut.x : next_above(cut.x);
+    // the bin's part in the turns' sums
+    for (int i = threadIdx.x; i < n; i += WAVES * 64) {
+      Turn& to = turns[(uint32_t)s.list[i]];
+      if (x_of(s.list[i]) >= from) add(&to.above, s.hist[i]);
+      else if (x_of(s.list[i]) == cut.x) add(&to.equal, 1);
+    }
+    __syncthreads();
+  }
   const uint64_t each = whole ? 0 : units(cut.x, m, c, bits);
   if (wave == 0) {
     const int n = WAVES * row.turns, per = (n + 63) / 64, first = lane * per, end = min(n, first + per);
@@ -896,14 +962,16 @@ __device__ __forceinline__ void pick(const L& row, S& s, const Cut& cut, double 
   __syncthreads();
   *index = s.index;
   *logit = s.x;
+  return true;
 }
 
 // Where `want` of the measure (logits, or with MASS their weights) is reached in the row's order, of what `from` keeps;
 // want(total) is asked with the measure of all of it, and more than that leaves `from`.
-// range: how far below the largest, m, the cut lies at most, or is worth bins.
+// range: how far below the largest, m, the cut lies at most, or is worth bins.  pend: NULL, or takes what is left to do
+// once the bin is found.
 template <bool MASS, typename L, typename S, typename F>
 __device__ __forceinline__ Cut search(const L& row, S& s, const Cut from, float m, float range, double c, double bits,
-                                      const F& want) {
+                                      const F& want, Pending* pend) {
   constexpr int N = L::N, THREADS = L::WAVES * 64;
   const int tid = threadIdx.x;
   const float scale = range > 0.0f ? fminf((float)BINS / fminf(range, 3e38f), 3e38f) : 1.0f;
@@ -913,10 +981,8 @@ __device__ __forceinline__ Cut search(const L& row, S& s, const Cut from, float 
     for (int i = tid; i < BINS + 64; i += THREADS) s.hist[i] = 0;
     __syncthreads();
   };
-  // the cut at x: as many of the logits that equal it, `equal` together, as it takes after what lies above
-  const auto cut_at = [&](float x, uint64_t wanted, uint64_t above, uint64_t equal) {
-    const uint64_t w = max(measure(x), (uint64_t)1), ties = (wanted - above + w - 1) / w;
-    return Cut{x, MASS && ties * w >= equal ? ALL : (uint32_t)ties};   // (a search by mass asks a count for its number)
+  const auto at = [&](float x, uint64_t wanted, uint64_t above) {   // (equal to x: as many as it takes)
+    return cut_at(x, max(measure(x), (uint64_t)1), wanted, above, ~0ull);
   };
   clear();
   const float last = (float)(BINS - 1 + lane_id());
@@ -938,7 +1004,7 @@ __device__ __forceinline__ Cut search(const L& row, S& s, const Cut from, float 
   __syncthreads();
   const uint64_t wanted = want(s.total + tail);
   const int bin = s.bin;
-  if (bin < 0) return tail ? (wanted >= s.total + tail ? from : cut_at(from.x, wanted, s.total, ~0ull)) : from;
+  if (bin < 0) return tail && wanted < s.total + tail ? at(from.x, wanted, s.total) : from;
   uint64_t above = s.above;
   // the bin's logits
   const float b0 = (float)bin, b1 = bin == BINS - 1 ? INFINITY : next_below((float)(bin + 1));
@@ -946,35 +1012,25 @@ __device__ __forceinline__ Cut search(const L& row, S& s, const Cut from, float 
     const float b = bin_of(x);
     return b >= b0 && b <= b1 && x > from.x;
   };
-  uint32_t* list = reinterpret_cast<uint32_t*>(s.list);   // ordered values
+  if (pend) {
+    *pend = Pending{true, b0, b1, m, scale, from.x, above, wanted};
+    return from;
+  }
   row.each([&](int, const float (&x)[N]) {
 #pragma unroll
     for (int e = 0; e < N; ++e)
       if (in_bin(x[e])) {
         const int i = atomicAdd(&s.n, 1);
-        if (i < LIST) list[i] = ordered(x[e]);
+        if (i < LIST) s.list[i] = (uint64_t)ordered(x[e]) << 32;
       }
   });
   __syncthreads();
   const int n = s.n;
-  if (n <= LIST) {   // sums of all pairs
-    for (int i = tid; i < n; i += THREADS) s.hist[i] = measure(from_ordered(list[i]));
-    __syncthreads();
-    for (int i = tid; i < n; i += THREADS) {
-      const uint32_t me = list[i];
-      uint64_t more = above, equal = 0;
-      for (int j = 0; j < n; ++j) {
-        more += list[j] > me ? s.hist[j] : 0;
-        equal += list[j] == me ? s.hist[j] : 0;
-      }
-      if (more < wanted && more + equal >= wanted) {   // (all that are equal write the same)
-        s.x = from_ordered(me);
-        s.before = more;
-        s.total = equal;
-      }
-    }
-    __syncthreads();
-    return cut_at(s.x, wanted, s.before, s.total);
+  if (n <= LIST) {
+    for (int i = tid; i < n; i += THREADS) s.hist[i] = measure(x_of(s.list[i]));
+    const Cut cut = pairs(s, n, wanted, above);
+    // a search by mass asks a count for the number of its ties
+    return MASS || cut.ties != ALL ? cut : Cut{cut.x, (uint32_t)(wanted - s.before)};
   }
   // too many: histograms of ordered values over what the bin spans, until one value is left
   if (tid == 0) {
@@ -1015,7 +1071,7 @@ __device__ __forceinline__ Cut search(const L& row, S& s, const Cut from, float 
     lo = max(lo, hi - min(hi, (1u << shift) - 1u));
     __syncthreads();
   }
-  return cut_at(from_ordered(hi), wanted, above, ~0ull);
+  return at(from_ordered(hi), wanted, above);
 }
 
 // The value at place i of the table.
@@ -1351,14 +1407,30 @@ __global__ void __launch_bounds__(THREADS) k_sample_long(SampleArgs a) {
   if (by_count)
     cut = set.k == 1 ? Cut{m, 1}
                      : search<false>(row, s, cut, m, (float)fmin(40.0 / c, 3e38), c, S,
-                                     [&](uint64_t) { return (uint64_t)set.k; });
-  if (set.p < 1.0 && !found) cut = search<true>(row, s, cut, m, set.octaves * __builtin_amdgcn_rcpf((float)c), c, S, share);
-  if (set.least > 0.0 && least > cut.x) cut = Cut{least, ALL};
-  int index;
-  float z;
-  uint64_t total;
-  pick(row, s, cut, (double)m, c, S, [&](uint64_t all) { return share_down(set.u, all) + 1; }, &index, &z,
-              &total);
+                                     [&](uint64_t) { return (uint64_t)set.k; }, nullptr);
+  const bool by_least = set.least > 0.0;
+  bool by_mass = set.p < 1.0 && !found;
+  const float range = set.octaves * __builtin_amdgcn_rcpf((float)c);
+  const auto drawn = [&](uint64_t all) { return share_down(set.u, all) + 1; };
+  int index = 0;
+  float z = 0.0f;
+  uint64_t total = 0;
+  Pending pend{};
+  bool done = false;
+  // the cut is found while the kept are weighed: a look less (2048 rows of 32768 fp32: 196 us without), but not where a
+  // look is cheap or counts find it as a rule
+  if constexpr (!KEEP && TYPE != RENO_T_BF16)
+    if (by_mass && !by_least) {
+      Cut last = search<true>(row, s, cut, m, range, c, S, share, &pend);
+      if (pend.on) done = pick<true>(row, s, last, pend, (double)m, c, S, drawn, &index, &z, &total);
+      if (done || !pend.on) cut = last;
+      by_mass = pend.on && !done;
+    }
+  if (!done) {
+    if (by_mass) cut = search<true>(row, s, cut, m, range, c, S, share, nullptr);
+    if (by_least && least > cut.x) cut = Cut{least, ALL};
+    pick<false>(row, s, cut, pend, (double)m, c, S, drawn, &index, &z, &total);
+  }
   if (share_down(set.u, total) == 0) {   // a share of nothing: the first symbol of any weight, though it be less than a unit
     const bool whole = cut.ties == ALL;   // (the cut's own weight is a unit at least, or it is none by mass)
     int first = a.V;
