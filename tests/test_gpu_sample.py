@@ -249,6 +249,41 @@ def test_long_offsets():
         assert r.bits[0].item() == pytest.approx(math.log2(W), abs=1e-6)
 
 
+@pytest.mark.parametrize("V", [5, 270])
+def test_rows_of_several_launches(V):
+    """More rows than one launch takes: every row's own logits, settings and mask are found."""
+    N = (1 << 21) + 37
+    g = torch.Generator(device="cuda").manual_seed(V)
+    z = torch.randn(N, V, generator=g, device="cuda").to(torch.bfloat16)
+    u = torch.rand(N, generator=g, device="cuda")
+    T = 0.5 + torch.rand(N, generator=g, device="cuda")
+    k = torch.randint(0, 9, (N,), generator=g, device="cuda").int()
+    p = torch.rand(N, generator=g, device="cuda")
+    least = torch.rand(N, generator=g, device="cuda") * 0.1
+    allowed = torch.rand(N, V, generator=g, device="cuda") < 0.9
+    say("sample, launches", N, V)
+    r = reno.sample_symbols(z, u, T, k, p, least, allowed)
+    for a, b in ((0, 50), ((1 << 21) - 20, N)):
+        s = slice(a, b)
+        part = reno.sample_symbols(z[s], u[s], T[s], k[s], p[s], least[s], allowed[s])
+        assert torch.equal(r.symbol[s], part.symbol) and torch.equal(r.bits[s], part.bits)
+        check(part, draw(z[s], u[s], T[s], k[s], p[s], least[s], allowed[s]), V, V)
+
+
+def test_refusals():
+    z, u = torch.zeros(4, 9, device="cuda"), torch.zeros(4, device="cuda")
+    for bad in (dict(logits=z.cpu()), dict(logits=z.double()), dict(logits=z[0]), dict(u=u[:3]), dict(u=u.double()),
+                dict(u=u.cpu()), dict(temperature=u[:3]), dict(temperature=u.double()), dict(top_k=u), dict(top_k=1.5),
+                dict(top_k=-1), dict(top_k=1 << 31), dict(allowed=torch.ones(8, dtype=torch.bool, device="cuda")),
+                dict(allowed=torch.ones(4, 9, device="cuda")), dict(allowed=torch.ones(1, 1, 9, device="cuda").bool())):
+        with pytest.raises(ValueError):
+            reno.sample_symbols(**{**dict(logits=z, u=u), **bad})
+    for bad in (dict(temperature=-1.0), dict(temperature=math.nan), dict(top_p=1.5), dict(top_p=-0.1), dict(min_p=2.0)):
+        with pytest.raises(reno.RenoError) as e:
+            reno.sample_symbols(z, u, **bad)
+        assert e.value.status == reno.RENO_E_INVALID
+
+
 def test_capture_and_streams():
     z, u = make(100, 500, torch.float32, 3)
     big, ub = make(2, 60000, torch.bfloat16, 4)

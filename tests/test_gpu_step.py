@@ -99,6 +99,8 @@ def test_norms_at_the_ends_of_the_range():
     assert bool((out[0] == 0).all())
     out = reno.clip_grads([torch.zeros(5, device="cuda")], torch.zeros((), device="cuda"), 1.0)
     assert bool((out[0] == 0).all())
+    empty = torch.empty(0, device="cuda")
+    assert float(reno.grad_norm([empty])) == 0.0 and reno.clip_grads([empty], torch.zeros((), device="cuda"), 1.0)[0] is empty
     # gradients that are not rows of one another: columns are copied
     x = torch.randn(30, 40, device="cuda")
     assert torch.equal(reno.grad_norm([x.t()]), reno.grad_norm([x.t().contiguous()]))
