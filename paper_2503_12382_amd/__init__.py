@@ -607,13 +607,18 @@ def head_workspace(rows: int, channels: int, symbols: int, dtype, top_k: int = 1
     return n.value
 
 
+class _Stream(typing.NamedTuple):
+    cuda_stream: int
+
+
 def _on(dev, stream, call):
     """call(stream) on the device of the arguments, with the stream that it is
     enqueued on (default: torch's current one of that device) current."""
     import torch
     if stream is None:
         if torch.cuda.current_device() == dev.index:
-            return call(torch.cuda.current_stream())
+            raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # 2.5 us less than a Stream object
+            return call(_Stream(raw(dev.index)) if raw else torch.cuda.current_stream())
         with torch.cuda.device(dev):
             return call(torch.cuda.current_stream())
     _need(stream.device == dev, "stream must belong to the device of the arguments")
@@ -799,6 +804,12 @@ def sample_symbols(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, al
     return _on(dev, stream, run)
 
 
+def _kinds():
+    """reno_type by torch dtype."""
+    _type_of(None)
+    return _TYPES
+
+
 def _in_list(name, dev, *tensors):
     """What is wrong with tensors of a list that have to be dense, on one device and of one size."""
     for t in tensors:
@@ -832,11 +843,11 @@ def grad_norm(grads, scale: float = 1.0, workspace=None, stream=None):
     dev = grads[0].device
 
     def run(st):
-        at_dev, words, g = dev.index, [], []
+        at_dev, kind_of, words, g = dev.index, _kinds().get, [], []
         for t in grads:
             if not t.is_contiguous():
                 t = t.contiguous()
-            kind = _type_of(t.dtype)
+            kind = kind_of(t.dtype)
             if kind is None or t.get_device() != at_dev:
                 _in_list("grads", at_dev, t)
             g.append(t)
@@ -868,14 +879,14 @@ def clip_grads(grads, norm, max_norm: float, scale: float = 1.0, out=None, strea
     dev = grads[0].device
 
     def run(st):
-        at_dev, words, g = dev.index, [], []
+        at_dev, kind_of, words, g = dev.index, _kinds().get, [], []
         o = grads if out is None else list(out)
         _need(len(o) == len(grads), "out must have as many tensors as grads")
         for a, b in zip(grads, o):
             if out is not None and not a.is_contiguous():
                 a = a.contiguous()
             n, dt = a.numel(), a.dtype
-            kind = _type_of(dt)
+            kind = kind_of(dt)
             if (kind is None or b.dtype is not dt or b.numel() != n or a.get_device() != at_dev
                     or b.get_device() != at_dev or not b.is_contiguous()):
                 _in_list("grads and out", at_dev, a, b)
@@ -908,7 +919,7 @@ def adamw_step(params, grads, exp_avg, exp_avg_sq, steps, master=None, lr: float
     dev = params[0].device
 
     def run(st):
-        at_dev, words, keep, f32 = dev.index, [], [], torch.float32
+        at_dev, kind_of, words, keep, f32 = dev.index, _kinds().get, [], [], torch.float32
         lists = [params, list(grads), list(exp_avg), list(exp_avg_sq)]
         lists.append([None] * len(params) if master is None else list(master))
         _need(all(len(x) == len(params) for x in lists), "the lists must have as many tensors as params")
@@ -916,7 +927,7 @@ def adamw_step(params, grads, exp_avg, exp_avg_sq, steps, master=None, lr: float
             if not g.is_contiguous():
                 g = g.contiguous()
             n = p.numel()
-            kind, grad_kind = _type_of(p.dtype), _type_of(g.dtype)
+            kind, grad_kind = kind_of(p.dtype), kind_of(g.dtype)
             if (kind is None or grad_kind is None or m.dtype is not f32 or v.dtype is not f32 or g.numel() != n
                     or m.numel() != n or v.numel() != n or p.get_device() != at_dev or g.get_device() != at_dev
                     or m.get_device() != at_dev or v.get_device() != at_dev or not p.is_contiguous()

@@ -727,7 +727,7 @@ struct Long {
 template <int WAVES>
 struct Shared {
   uint64_t hist[BINS + 64];   // the last bin is one of each lane's: what lies far below meets there; then weights
-  uint64_t list[LIST];        // places: the ordered value, then the index complemented; or ordered values
+  uint64_t list[LIST];        // places: the ordered value, then the index complemented, or the turn
   uint16_t other[OTHERS];     // bf16 values outside the table of counts, which lies over both of the above
   uint64_t part[WAVES];
   uint64_t above, total, before;
