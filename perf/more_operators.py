@@ -162,7 +162,7 @@ def prepare(case, seed):
         x.fill_(True)
     size = 4.0 ** (uniform(1) - 0.25) / math.sqrt(sum(math.prod(x) for x in shapes))   # norms on both sides of the largest
     grad = (normal(total) * (size * scale) * used).to(dt)
-    s = {"case": case, "grad": grad, "scale": 1.0 / scale, "out": torch.zeros_like(grad)}
+    s = {"case": case, "grad": grad, "scale": 1.0 / scale, "out": torch.empty_like(grad)}
     if case["op"] == "adamw":
         weight = normal(total) * used * 0.05
         s["param"] = weight.to(dt)
