@@ -246,6 +246,8 @@ def run(s):
     if case["op"] == "norm":
         return {"norm": norm}
     if case["op"] == "clip":
+        if sum(t.numel() for t in x["out"]) < s["out"].numel():
+            s["out"].zero_()   # gaps between the tensors, which the call leaves as they were
         reno.clip_grads(x["grad"], norm, MOST_NORM, scale=s["scale"], out=x["out"])
         return {"norm": norm, "out": s["out"]}
     reno.adamw_step(x["param"], x["grad"], x["exp_avg"], x["exp_avg_sq"], s["steps"], master=x.get("master"), lr=LR,
