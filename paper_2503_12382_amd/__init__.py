@@ -835,8 +835,8 @@ def grad_norm(grads, scale: float = 1.0, workspace=None, stream=None):
     """scale times the 2-norm over all the tensors (float32, bfloat16 or float16,
     mixed; reno_grad_norm), as a float32 scalar on their device.  scale: one over
     a loss scale.  Sums are carried in 64 bits.  workspace: a uint8 tensor that
-    is large enough (reno_grad_workspace), or None to take it from torch's
-    allocator."""
+    is large enough (reno_grad_workspace) and no part of the gradients', or None
+    to take it from torch's allocator."""
     import torch
     grads = list(grads)
     _need(len(grads) and grads[0].is_cuda, "grads must be device tensors, one at least")

@@ -114,7 +114,14 @@ reno_status reno_grad_norm(const reno_gradient* g, int64_t count, double scale, 
   const int64_t need = 8 * reno::norm_parts(g, count);
   if (bytes < need) return fail_thread(RENO_E_INVALID, "workspace too small");
   if (need && (!ws || !aligned(ws, 256))) return fail_thread(RENO_E_INVALID, "workspace must be 256-byte aligned");
-  return done(reno::launch_norm(g, count, scale, norm, static_cast<double*>(ws), static_cast<hipStream_t>(stream)));
+  return guarded([&] {
+    std::vector<Range> r;
+    add(r, norm, 4, true);
+    add(r, ws, need, true);   // blocks would write partial sums over what others still read
+    for (int64_t i = 0; i < count; ++i) add(r, g[i].grad, g[i].n * size_of(g[i].type), false);
+    if (overlap(r)) return fail_thread(RENO_E_INVALID, "an output overlaps another operand");
+    return done(reno::launch_norm(g, count, scale, norm, static_cast<double*>(ws), static_cast<hipStream_t>(stream)));
+  });
 }
 
 reno_status reno_grad_clip(const reno_gradient* g, int64_t count, const float* norm, double scale, double max_norm,

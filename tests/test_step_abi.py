@@ -71,6 +71,24 @@ def test_grad_norm_rejects_bad_arguments():
     assert L.reno_grad_workspace(ctypes.addressof(a), 3, None) == INVALID
 
 
+def test_grad_norm_rejects_what_overlaps():
+    """What the call writes, the norm and the workspace, lies in nothing that it reads or writes besides."""
+    L = reno.lib()
+    n = ctypes.c_int64()
+    a = grads(dict(n=1000), dict(n=1 << 24, grad=1 << 30, type=1))
+    assert L.reno_grad_workspace(ctypes.addressof(a), 2, ctypes.byref(n)) == reno.RENO_OK and n.value > 16
+
+    def call(norm, ws):
+        return L.reno_grad_norm(ctypes.addressof(a), 2, 1.0, norm, ws, n.value, None)
+    end = (1 << 30) + (1 << 25)
+    for norm, ws in ((P, 1 << 20), (P + 3996, 1 << 20), (end - 4, 1 << 20),                   # the norm in a gradient
+                     (1 << 28, P), (1 << 28, P + 3840), (1 << 28, (1 << 30) + 4096), (1 << 28, end - 256),
+                     (1 << 28, (1 << 30) - 256),                                              # the workspace
+                     (1 << 20, 1 << 20), ((1 << 20) + n.value - 4, 1 << 20)):                 # one in the other
+        assert call(norm, ws) == INVALID, (norm, ws)
+        assert b"overlaps" in L.reno_last_error(None)
+
+
 def test_grad_clip_rejects_bad_arguments():
     L = reno.lib()
 
