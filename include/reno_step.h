@@ -85,9 +85,10 @@ reno_status reno_grad_clip(const reno_gradient* grads_host, int64_t count, const
  *   w -= lr (exp_avg / (1 - beta1^t) / (sqrt(exp_avg_sq / (1 - beta2^t)) + eps) + weight_decay w)
  * With a norm that is inf or NaN nothing is changed, steps neither.  lr and
  * weight_decay: 0 or more and finite; betas: in [0, 1); eps: a positive normal
- * float.  A gradient of |g'| above 2^64 has an infinite square and moves nothing
- * until exp_avg_sq is set anew.  Calls that share `steps` must not overlap, and
- * each counts as a step: parameter groups have one each. */
+ * float.  Where (1 - beta2) g'^2 exceeds fp32, exp_avg_sq becomes infinite and
+ * stays so, and its weight moves by the decay alone, until it is set anew; a g'
+ * that is infinite or NaN itself makes its weight NaN.  Calls that share `steps`
+ * must not overlap, and each counts as a step: parameter groups have one each. */
 reno_status reno_adamw_step(const reno_parameter* params_host, int64_t count, const reno_adamw* how, void* hip_stream);
 
 #ifdef __cplusplus

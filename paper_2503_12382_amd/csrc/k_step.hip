@@ -278,8 +278,9 @@ struct AdamTerms {
   __device__ __forceinline__ void update(float g0, float& m, float& v, float& w) const {
     const float g = f.of(g0);
     m = fmaf(b1, m, c1 * g);
-    v = fmaf(b2, v, c2 * g * g);
-    const float step = m * inv1 / (__builtin_sqrtf(v) * inv2 + eps);
+    // (infinite: it stays so, whatever b2 would make of it, and the step is none; m inv1 might be infinite too)
+    v = v == INFINITY ? v : fmaf(b2, v, c2 * g * g);
+    const float step = m / (__builtin_sqrtf(v) * inv2 + eps) * inv1;
     w = fmaf(-lr, fmaf(decay, w, step), w);   // decay inside: 1 - lr decay would be rounded
   }
 };

@@ -1,0 +1,59 @@
+"""The step after a gradient where single values tell: the moments' decay, squares past fp32, gradients and factors next
+to the ends of the range; and lists of many tensors of a kind, tensors past 2^31 elements."""
+import math
+
+import pytest
+import torch
+
+import paper_2503_12382_amd as reno
+from gpu_helpers import say
+
+pytestmark = pytest.mark.gpu
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+
+
+def half_step(x):
+    """Half of the distance from |x| to the next fp32 value, for x in 64 bits."""
+    a = x.abs().float()
+    return (torch.nextafter(a, torch.full_like(a, math.inf)) - a).double() / 2
+
+
+def state(n):
+    return [torch.zeros(n, device="cuda")], [torch.zeros(n, device="cuda")], torch.zeros(2, dtype=torch.int32, device="cuda")
+
+
+@pytest.mark.parametrize("beta2,big", [(0.0, 1e20), (0.999, 1e21), (0.5, 1e21), (0.999, torch.finfo(F32).max),
+                                       (0.0, torch.finfo(F32).max)])
+def test_a_square_past_fp32_stops_its_element(beta2, big):
+    """(1 - beta2) g^2 past fp32: exp_avg_sq is infinite and stays so, and the weight moves by its decay alone.  The
+    elements beside it are as if it were not there."""
+    n, lr, decay = 11, 0.25, 0.125
+    w = [torch.full((n,), 2.0, device="cuda")]
+    m, v, steps = state(n)
+    other = [w[0].clone()]
+    m1, v1, steps1 = state(n)
+    want = 2.0
+    for i in range(4):
+        g = torch.full((n,), 0.5, device="cuda")
+        reno.adamw_step(other, [g], m1, v1, steps1, lr=lr, betas=(0.9, beta2), weight_decay=decay)
+        if i == 1:
+            g[3], g[7] = big, -big
+        reno.adamw_step(w, [g], m, v, steps, lr=lr, betas=(0.9, beta2), weight_decay=decay)
+        if i == 0:
+            want = float(w[0][3])
+        else:
+            want *= 1 - lr * decay
+            for e in (3, 7):
+                assert math.isinf(float(v[0][e])) and math.isfinite(float(m[0][e]))
+                assert float(w[0][e]) == pytest.approx(want, rel=i * 2.0 ** -23)
+        rest = [e for e in range(n) if e not in (3, 7)]
+        assert torch.equal(w[0][rest], other[0][rest]) and torch.equal(v[0][rest], v1[0][rest])
+
+
+@pytest.mark.parametrize("beta1", [0.9, 0.053])   # 0.053: the first moment over 1 - beta1 is rounded past fp32
+def test_the_first_step_of_the_largest_gradient(beta1):
+    w = [torch.ones(4, device="cuda")]
+    m, v, steps = state(4)
+    reno.adamw_step(w, [torch.full((4,), torch.finfo(F32).max, device="cuda")], m, v, steps, lr=0.5, betas=(beta1, 0.999),
+                    weight_decay=0.25)
+    assert bool(v[0].isinf().all()) and w[0].tolist() == [0.875] * 4
