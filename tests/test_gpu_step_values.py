@@ -22,6 +22,38 @@ def state(n):
     return [torch.zeros(n, device="cuda")], [torch.zeros(n, device="cuda")], torch.zeros(2, dtype=torch.int32, device="cuda")
 
 
+@pytest.mark.parametrize("betas", [(0.9, 0.999), (0.95, 0.99), (0.3, 0.99999), (0.999, 0.999999), (0.0, 0.5)])
+def test_moments_decay_by_beta(betas):
+    """Without a gradient a moment is beta times what it was, rounded once.  The part of beta below fp32 is carried in
+    fp32 (2^-24 of 2^-25), and so is its product with the moment."""
+    g = torch.Generator().manual_seed(1)
+    n = 5003
+    m, v = torch.randn(n, generator=g).cuda(), torch.rand(n, generator=g).cuda() + 2.0 ** -10
+    steps = torch.zeros(2, dtype=torch.int32, device="cuda")
+    old = m.double(), v.double()
+    say("decay", betas)
+    reno.adamw_step([torch.zeros(n, device="cuda")], [torch.zeros(n, device="cuda")], [m], [v], steps, betas=betas)
+    for got, before, beta in zip((m, v), old, betas):
+        want = beta * before
+        assert bool(((got.double() - want).abs() <= half_step(want) + 2.0 ** -47 * before.abs()).all()), beta
+
+
+def test_second_moment_of_many_steps():
+    """The mean of exp_avg_sq over many elements after many steps.  Roundings of single elements have no sign (their mean
+    over 4096 is below 2^-25 of it); what remains is the rounding of 1 - beta2, 2^-24."""
+    n, beta2 = 4096, 0.999
+    g = torch.Generator(device="cuda").manual_seed(2)
+    w = [torch.zeros(n, device="cuda")]
+    m, v, steps = state(n)
+    v[0].fill_(1.0)
+    want = v[0].double()
+    for i in range(2000):
+        x = torch.randn(n, generator=g, device="cuda")
+        reno.adamw_step(w, [x], m, v, steps, lr=0.0, betas=(0.9, beta2))
+        want = beta2 * want + (1 - beta2) * x.double().square()
+    assert abs(float((v[0].double() / want - 1).mean())) <= 2.0 ** -22
+
+
 @pytest.mark.parametrize("beta2,big", [(0.0, 1e20), (0.999, 1e21), (0.5, 1e21), (0.999, torch.finfo(F32).max),
                                        (0.0, torch.finfo(F32).max)])
 def test_a_square_past_fp32_stops_its_element(beta2, big):
