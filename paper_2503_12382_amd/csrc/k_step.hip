@@ -184,18 +184,20 @@ __global__ void __launch_bounds__(1024) k_norm(const double* __restrict__ parts,
   if (threadIdx.x == 0) *norm = (float)(scale * __builtin_sqrt(s));
 }
 
-// What gradients are multiplied by, scale min(1, max_norm / norm), as a number below 1 and a power of two: the factor
-// may lie outside the floats where the product does not.  (In 64 bits the product's conversions bound clipping: 5e7
-// fp16 gradients took 56 us, 31 so.)
+// What gradients are multiplied by, scale min(1, max_norm / norm), as a float and a power of two for what passes the
+// floats' range: the factor may lie outside it where the product does not.  The power goes first, which rounds nothing
+// (what it makes subnormal the float, 2^-126 then, makes 0), so that the product is rounded once, subnormal or not.
+// (In 64 bits its conversions bound clipping: 5e7 fp16 gradients took 56 us, 31 so.)
 struct Factor {
-  float mant;
+  float f;
   int exp;
-  __device__ __forceinline__ float of(float g) const { return __builtin_amdgcn_ldexpf(g * mant, exp); }
+  __device__ __forceinline__ float of(float g) const { return __builtin_amdgcn_ldexpf(g, exp) * f; }
 };
 __device__ __forceinline__ Factor factor(const float* norm, double scale, double max_norm) {
   const double n = norm ? (double)*norm : 0.0;
   const double f = n <= max_norm ? scale : scale * (max_norm / n);
-  return Factor{(float)__builtin_amdgcn_frexp_mant(f), __builtin_amdgcn_frexp_exp(f)};
+  const int e = __builtin_amdgcn_frexp_exp(f), in = min(max(e, -125), 127);
+  return Factor{(float)__builtin_ldexp(__builtin_amdgcn_frexp_mant(f), in), e - in};
 }
 
 // ---------------------------------------------------------------------------

@@ -89,3 +89,24 @@ def test_the_first_step_of_the_largest_gradient(beta1):
     reno.adamw_step(w, [torch.full((4,), torch.finfo(F32).max, device="cuda")], m, v, steps, lr=0.5, betas=(beta1, 0.999),
                     weight_decay=0.25)
     assert bool(v[0].isinf().all()) and w[0].tolist() == [0.875] * 4
+
+
+@pytest.mark.parametrize("scale", [1.0, 3.0, 0.7, 1e10, 2.0 ** 120, 1e60, 1e-10, 1e-30, 1e-60])
+def test_clipping_rounds_once_anywhere(scale):
+    """Gradients from the least fp32 value to the largest, factors in and out of the floats: the product is off by the
+    rounding of the factor to 2^-24, and by half a step, that of subnormal values below 2^-126."""
+    g = torch.Generator().manual_seed(4)
+    x = torch.ldexp(1 + torch.rand(20000, generator=g, dtype=torch.float64), torch.randint(-149, 128, (20000,), generator=g))
+    x = (x * torch.where(torch.rand(20000, generator=g) < 0.5, -1.0, 1.0)).float().cuda()
+    for n, most in ((1.0, math.inf), (3.0, 1.0)):
+        c = scale * min(1.0, most / n)
+        say("clip, any size", scale, most)
+        out = [torch.zeros_like(x)]
+        reno.clip_grads([x], torch.tensor(n, device="cuda"), most, scale=scale, out=out)
+        want = x.double() * c
+        top = float(torch.finfo(F32).max)
+        fits = want.abs() <= top * (1 - 2.0 ** -23)
+        assert bool((out[0][want.abs() >= top * (1 + 2.0 ** -23)].isinf()).all())
+        bound = (2.0 ** -24 * 1.01) * want.abs() + half_step(want.clamp(-top / 2, top / 2)).maximum(2.0 ** -25 * want.abs())
+        bad = fits & ~((out[0].double() - want).abs() <= bound)
+        assert not bool(bad.any()), (scale, most, x[bad][:3].tolist(), out[0][bad][:3].tolist(), want[bad][:3].tolist())
