@@ -159,7 +159,11 @@ __host__ __device__ __forceinline__ float octaves_of(int V, double p) {
 __device__ __forceinline__ Row settings(const SampleArgs& a, int64_t r) {
   Row s;
   s.u = a.u[r];
-  s.T = a.T_rows ? (double)a.T_rows[r] : a.T;
+  s.T = a.T;
+  if (a.T_rows) {   // past the range: its end
+    const double T = (double)a.T_rows[r];
+    s.T = T > 0.0 && T < (double)INFINITY ? fmin(fmax(T, 0x1p-126), 0x1p126) : T;
+  }
   s.p = a.p_rows ? (double)a.p_rows[r] : a.p;
   s.least = a.least_rows ? (double)a.least_rows[r] : a.least;
   s.k = max(a.k_rows ? a.k_rows[r] : a.k, 0);
