@@ -810,15 +810,26 @@ def _kinds():
     return _TYPES
 
 
+def _alike(a, *others):
+    """Whether elements in memory stand for one another: tensors of one shape, or flat ones of as many."""
+    shape, n = a.shape, a.numel()
+    for t in others:
+        if t.shape != shape and (t.numel() != n or (t.dim() > 1 and len(shape) > 1)):
+            return False
+        if len(shape) < 2:
+            shape = t.shape
+    return True
+
+
 def _in_list(name, dev, *tensors):
-    """What is wrong with tensors of a list that have to be dense, on one device and of one size."""
+    """What is wrong with tensors of a list that have to be dense, on one device and of one shape."""
     for t in tensors:
         if t.get_device() != dev:
             raise ValueError(f"{name} must be on one device")
         if not t.is_contiguous():
             raise ValueError(f"{name} must be dense")
-        if t.numel() != tensors[0].numel():
-            raise ValueError(f"{name} must have the sizes of one another")
+    if not _alike(*tensors):
+        raise ValueError(f"{name} must have the shapes of one another, or be flat")
     raise ValueError(f"{name} must be float32, bfloat16 or float16 of matching types")
 
 
@@ -872,7 +883,8 @@ def grad_norm(grads, scale: float = 1.0, workspace=None, stream=None):
 def clip_grads(grads, norm, max_norm: float, scale: float = 1.0, out=None, stream=None):
     """The gradients times scale min(1, max_norm / norm) (reno_grad_clip), written
     to the tensors of ``out`` (default: in place; then they must be dense), which
-    is returned.  norm: grad_norm of the same gradients with the same scale."""
+    is returned; an out has its gradient's shape, or either is flat.  norm:
+    grad_norm of the same gradients with the same scale."""
     import torch
     grads = list(grads)
     _need(len(grads) and grads[0].is_cuda, "grads must be device tensors, one at least")
@@ -887,7 +899,7 @@ def clip_grads(grads, norm, max_norm: float, scale: float = 1.0, out=None, strea
                 a = a.contiguous()
             n, dt = a.numel(), a.dtype
             kind = kind_of(dt)
-            if (kind is None or b.dtype is not dt or b.numel() != n or a.get_device() != at_dev
+            if (kind is None or b.dtype is not dt or (b.shape != a.shape and not _alike(a, b)) or a.get_device() != at_dev
                     or b.get_device() != at_dev or not b.is_contiguous()):
                 _in_list("grads and out", at_dev, a, b)
             g.append(a)
@@ -905,7 +917,7 @@ def adamw_step(params, grads, exp_avg, exp_avg_sq, steps, master=None, lr: float
                scale: float = 1.0, lr_factor=None, stream=None) -> None:
     """One AdamW step in place (reno_adamw_step): lists of weights (float32,
     bfloat16 or float16, mixed), their gradients (of the weight's type or
-    float32), and their float32 moments.  steps: int32 [2] on the device, zeros
+    float32), and their float32 moments, all of a weight's shape or flat.  steps: int32 [2] on the device, zeros
     before the first step: the steps made so far, which the call counts up, and a
     word of its own.  master: None, or a list with the float32 copies of weights
     of 16 bits, and None for those without.  With ``norm`` (grad_norm with the
@@ -926,15 +938,17 @@ def adamw_step(params, grads, exp_avg, exp_avg_sq, steps, master=None, lr: float
         for p, g, m, v, w in zip(*lists):
             if not g.is_contiguous():
                 g = g.contiguous()
-            n = p.numel()
+            n, shape = p.numel(), p.shape
             kind, grad_kind = kind_of(p.dtype), kind_of(g.dtype)
-            if (kind is None or grad_kind is None or m.dtype is not f32 or v.dtype is not f32 or g.numel() != n
-                    or m.numel() != n or v.numel() != n or p.get_device() != at_dev or g.get_device() != at_dev
+            if (kind is None or grad_kind is None or m.dtype is not f32 or v.dtype is not f32
+                    or (not (g.shape == shape and m.shape == shape and v.shape == shape) and not _alike(p, g, m, v))
+                    or p.get_device() != at_dev or g.get_device() != at_dev
                     or m.get_device() != at_dev or v.get_device() != at_dev or not p.is_contiguous()
                     or not m.is_contiguous() or not v.is_contiguous()):
                 _in_list("weights, gradients and moments", at_dev, p, g, m, v)
-            if w is not None and (w.dtype is not f32 or w.numel() != n or w.get_device() != at_dev or not w.is_contiguous()):
-                _in_list("weights and their copies", at_dev, p, w)
+            if w is not None and (w.dtype is not f32 or (w.shape != shape and not _alike(p, g, m, v, w))
+                                  or w.get_device() != at_dev or not w.is_contiguous()):
+                _in_list("weights, gradients, moments and copies", at_dev, p, g, m, v, w)
             keep.append(g)
             words += (n, kind, grad_kind, p.data_ptr(), g.data_ptr(), 0 if w is None else w.data_ptr(), m.data_ptr(),
                       v.data_ptr())
