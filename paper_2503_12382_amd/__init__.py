@@ -833,6 +833,15 @@ def _in_list(name, dev, *tensors):
     raise ValueError(f"{name} must be float32, bfloat16 or float16 of matching types")
 
 
+def _written(tensors):
+    """Tells autograd that tensors were written, as operators in place do: a backward pass that saved one is refused."""
+    import torch
+    try:
+        torch.autograd.graph.increment_version(tensors)
+    except RuntimeError:   # made in inference mode: these have no version
+        torch.autograd.graph.increment_version([t for t in tensors if not t.is_inference()])
+
+
 def _scalar_on(t, name, dtype, dev, n=1):
     """The address of a scalar (n words) on the device, or None."""
     if t is None:
@@ -907,6 +916,7 @@ def clip_grads(grads, norm, max_norm: float, scale: float = 1.0, out=None, strea
         arr = array.array("q", words)
         at = _scalar_on(norm, "norm", torch.float32, dev)
         _head_check(lib().reno_grad_clip(arr.buffer_info()[0], len(g), at, float(scale), float(max_norm), st.cuda_stream))
+        _written(o)
         _read_on(stream, norm, *g, *(o if out is not None else ()))
         return o
     return _on(dev, stream, run)
@@ -924,7 +934,8 @@ def adamw_step(params, grads, exp_avg, exp_avg_sq, steps, master=None, lr: float
     same scale) gradients count scaled down to max_norm, and a norm that is not
     finite leaves everything as it is.  lr_factor: a float32 scalar on the device
     that multiplies lr, or None.  Weights may require gradients; nothing is
-    recorded for autograd."""
+    recorded for autograd, but that they have changed: a backward pass through a
+    graph that saved them before raises torch's error."""
     import torch
     params = list(params)
     _need(len(params) and params[0].is_cuda, "params must be device tensors, one at least")
@@ -957,8 +968,10 @@ def adamw_step(params, grads, exp_avg, exp_avg_sq, steps, master=None, lr: float
                          float(max_norm), _scalar_on(lr_factor, "lr_factor", torch.float32, dev),
                          _scalar_on(norm, "norm", torch.float32, dev), _scalar_on(steps, "steps", torch.int32, dev, 2))
         _head_check(lib().reno_adamw_step(arr.buffer_info()[0], len(params), ctypes.byref(how), st.cuda_stream))
+        copies = () if master is None else [w for w in lists[4] if w is not None]
+        _written([*params, *lists[2], *lists[3], *copies, steps])
         if stream is not None:
-            _read_on(stream, steps, norm, lr_factor, *keep, *lists[0], *lists[2], *lists[3], *lists[4])
+            _read_on(stream, steps, norm, lr_factor, *keep, *lists[0], *lists[2], *lists[3], *copies)
     _on(dev, stream, run)
 
 

@@ -1,4 +1,5 @@
-"""Calls of the step after a gradient from torch: tensors that do not stand for one another."""
+"""Calls of the step after a gradient from torch: tensors that do not stand for one another, graphs of autograd that saved
+what is written."""
 import pytest
 import torch
 
@@ -66,3 +67,51 @@ def test_flat_tensors_stand_for_any_shape():
     s["grads"], s["exp_avg"] = [s["grads"][0].view(1)], [torch.zeros(1, 1, device="cuda")]
     reno.adamw_step(**s)
     assert s["steps"].tolist() == [1, 0]
+
+
+def test_what_is_written_counts_as_changed():
+    """Autograd's error, and no wrong gradient, where a graph saved weights that a step has moved since."""
+    a = operands()
+    w = a["params"][0].requires_grad_()
+    y = (w * w).sum()
+    y.backward(retain_graph=True)
+    a["grads"] = [w.grad]
+    reno.adamw_step(**a)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
+    (w * w).sum().backward()          # a new graph
+    x = torch.ones(6, 10, device="cuda")
+    h = torch.ones(6, 10, device="cuda", requires_grad=True)
+    y = (h * x).sum()
+    reno.clip_grads([x], torch.ones((), device="cuda"), 0.5)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
+    # what is written, and nothing else
+    a = operands(dtype=torch.bfloat16)
+    a["master"] = [a["params"][0].float()]
+    n = reno.grad_norm(a["grads"])
+    flat = [t for k in ("params", "exp_avg", "exp_avg_sq", "master") for t in a[k]] + [a["steps"]]
+    before = [t._version for t in flat], a["grads"][0]._version, n._version
+    reno.adamw_step(**a, norm=n, max_norm=1.0)
+    assert all(t._version > b for t, b in zip(flat, before[0]))
+    assert (a["grads"][0]._version, n._version) == before[1:]
+    out = [torch.zeros(6, 10, dtype=torch.bfloat16, device="cuda")]
+    at = out[0]._version
+    reno.clip_grads(a["grads"], n, 1.0, out=out)
+    assert out[0]._version > at and a["grads"][0]._version == before[1]
+
+
+def test_tensors_of_inference_mode():
+    """They have no version: a step takes them in that mode and outside it."""
+    with torch.inference_mode():
+        a = operands()
+    b = operands()
+    b["steps"] = a["steps"].clone()
+    with torch.inference_mode():
+        reno.adamw_step(**a, lr=0.1)
+    reno.adamw_step(**a, lr=0.1)
+    reno.clip_grads(a["grads"], torch.ones((), device="cuda"), 0.5)
+    for _ in range(2):
+        reno.adamw_step(**b, lr=0.1)
+    reno.clip_grads(b["grads"], torch.ones((), device="cuda"), 0.5)
+    assert all(torch.equal(a[k][0], b[k][0]) for k in ("params", "exp_avg", "exp_avg_sq", "grads"))
