@@ -110,3 +110,43 @@ def test_clipping_rounds_once_anywhere(scale):
         bound = (2.0 ** -24 * 1.01) * want.abs() + half_step(want.clamp(-top / 2, top / 2)).maximum(2.0 ** -25 * want.abs())
         bad = fits & ~((out[0].double() - want).abs() <= bound)
         assert not bool(bad.any()), (scale, most, x[bad][:3].tolist(), out[0][bad][:3].tolist(), want[bad][:3].tolist())
+
+
+@pytest.mark.parametrize("kind", ["fp32", "bf16 copies"])
+def test_adamw_of_many_tensors_of_a_kind(kind):
+    """More tensors of one kind than a launch takes: each is updated once, and the step is counted once."""
+    dt, count = (F32, 200) if kind == "fp32" else (BF16, 128)
+    g = torch.Generator().manual_seed(6)
+    w0 = [torch.randn(1 + 37 * (i % 9), generator=g).to(dt).cuda() for i in range(count)]
+    grads = [torch.randn(t.shape, generator=g).to(dt).cuda() for t in w0]
+
+    def run(lists):
+        w = [t.clone() for t in w0]
+        x = [[torch.zeros(t.shape, device="cuda") for t in w0] for _ in range(2)]
+        c = [t.float() for t in w] if dt != F32 else None
+        steps = [torch.zeros(2, dtype=torch.int32, device="cuda") for _ in lists]
+        for _ in range(3):
+            for at, st in zip(lists, steps):
+                reno.adamw_step(w[at], grads[at], x[0][at], x[1][at], st, master=c and c[at], lr=0.1)
+        assert all(st.tolist() == [3, 0] for st in steps)
+        return w, *x, c or []
+    say("adamw, many", kind, count)
+    one = run([slice(0, count)])
+    each = run([slice(i, i + 1) for i in range(count)])
+    assert all(torch.equal(a, b) for x, y in zip(one, each) for a, b in zip(x, y))
+
+
+def test_adamw_past_31_bits():
+    """Elements past 2^31, in the last of which and one before alone there is a gradient."""
+    n = (1 << 31) + 4099
+    w, g = torch.zeros(n, dtype=BF16, device="cuda"), torch.zeros(n, dtype=BF16, device="cuda")
+    m, v = torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda")
+    steps = torch.zeros(2, dtype=torch.int32, device="cuda")
+    g[-1], g[5] = 1.0, -1.0
+    say("adamw, long", n)
+    reno.adamw_step([w], [g], [m], [v], steps, lr=0.5, betas=(0.5, 0.5))
+    # m / (1 - 0.5) = g, sqrt(v / (1 - 0.5)) = 1, eps is lost
+    assert float(w[-1]) == -0.5 and float(w[5]) == 0.5 and steps.tolist() == [1, 0]
+    assert float(m[-1]) == 0.5 and float(v[5]) == 0.5
+    for t in (w, m, v):
+        assert int(sum(torch.count_nonzero(x) for x in t.split(1 << 30))) == 2
