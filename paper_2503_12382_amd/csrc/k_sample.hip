@@ -17,16 +17,19 @@
 // them, 17 in 64 bits, which run at the rate of 32.
 //   k_sample_short  rows of up to 256: 16 lanes a row, so that one wave's
 //                   instructions serve four rows, the row and its weights in
-//                   registers.  233737 x 256 fp32, top_p 0.95, a mask: 120 us,
-//                   2.0 TB/s, 1240 instructions of a wave, half of them a
-//                   logit's and half a row's
+//                   registers.  233737 x 256 fp32, top_p 0.95, a mask: 119 us,
+//                   2.0 TB/s, 1241 vector instructions of a wave, 469 of them
+//                   the cut's (76 us and 772 without one)
 //   k_sample_long   a block a row.  Small counts: the k-th largest of many
 //                   groups' maxima bounds the k-th largest logit, and what lies
 //                   above is cut, weighed and drawn from in a list (one row of
-//                   131071 fp32, top_k 50: 31 us, one block's latency).  bf16
+//                   131071 fp32, top_k 50: 30 us, one block's latency).  bf16
 //                   by mass: values are counted first and weighed once each
-//                   (4096 x 32768, top_p 0.9: 157 us, 34 instructions a logit).
-//                   Else by a histogram of weights (2048 x 32768 fp32: 177 us)
+//                   (4096 x 32768, top_p 0.9, min_p 0.001: 148 us, 33 vector
+//                   instructions a logit).  Else by a histogram of weights
+//                   (2048 x 32768 fp32, top_p 0.9: 157 us, 805 MB read)
+// Times: of a call among many in a row on one input.  The first few after a
+// pause, as a short trace has them, take up to a sixth longer (137 us for 119).
 
 #include <algorithm>
 #include <cmath>
@@ -281,8 +284,8 @@ __device__ __forceinline__ float next_above(float x) {
 }
 
 // The bin of a histogram at which what is wanted is reached; q.above becomes what lies above it.
-__device__ __forceinline__ int short_bin(const ShortShared& s, ShortSearch& q, uint64_t (&h)[SHORT_BINS / 16],
-                                         uint64_t mine, uint64_t upto) {
+__device__ __forceinline__ int short_bin(ShortSearch& q, uint64_t (&h)[SHORT_BINS / 16], uint64_t mine,
+                                         uint64_t upto) {
   constexpr int PER = SHORT_BINS / 16;
   uint64_t a = q.above + upto - mine;
   const int owner = row16_which(a < q.wanted && a + mine >= q.wanted);
@@ -396,7 +399,7 @@ __device__ __forceinline__ void short_more(ShortShared& s, ShortSearch& q, int v
     uint64_t h[PER], mine = 0;
 #pragma unroll
     for (int i = 0; i < PER; ++i) mine += h[i] = s.hist[rw][l15 * PER + i];
-    const int bin = short_bin(s, q, h, mine, row16_scan(mine));
+    const int bin = short_bin(q, h, mine, row16_scan(mine));
     top -= (uint32_t)bin << shift;
     lo = max(lo, top - min(top, (1u << shift) - 1u));
   }
@@ -439,7 +442,7 @@ __device__ __forceinline__ void short_search(const Short<PL>& row, ShortShared& 
   }
   q.wanted = want(all);
   q.active = active && q.wanted <= all;
-  const int bin = short_bin(s, q, h, mine, upto);
+  const int bin = short_bin(q, h, mine, upto);
   // the bin's logits
   const float b0 = q.active ? (float)bin : NAN;
   const float b1 = bin == SHORT_BINS - 1 ? INFINITY : next_below((float)(bin + 1));
@@ -511,8 +514,8 @@ __device__ __forceinline__ void short_mask(const uint8_t* allowed, int V, int v0
   }
 }
 
-// (4 waves a SIMD leave 128 registers, which the row, its weights and four of those under way fill: 233737 x 256 takes
-// 139 us, 155 with 2 waves and 254 with 5, which spill.)
+// (4 waves a SIMD leave 128 registers, which the row, its weights and four of those under way fill, three to scratch:
+// 233737 x 256 takes 119 us, 136 with 2 waves and 250 with 5, which spill far more.)
 template <int TYPE, int PL>
 __global__ void __launch_bounds__(256, 4) k_sample_short(SampleArgs a, int64_t rows) {
   __shared__ ShortShared s_all[4];
@@ -659,7 +662,7 @@ struct Turn {
 // THREADS a row.  A wave's pieces of 16 bytes follow one another: the row's order is by wave, then by turn, then by
 // lane.  KEEP: the first look leaves the row in LDS, where a thread reads what it wrote itself.  Else the row is read
 // anew for each look: with rows for every CU LDS has no place for enough of them (4096 rows of 32768 bf16, with four
-// looks a row: 210 us, and 247 with the row in LDS; with two looks now 157).
+// looks a row: 210 us, and 247 with the row in LDS; two looks now).
 template <int TYPE, int THREADS, bool KEEP>
 struct Long {
   static constexpr int N = Vec<TYPE>::N, WAVES = THREADS / 64, SIZE = 16 / N;
@@ -1342,7 +1345,7 @@ __global__ void __launch_bounds__(THREADS) k_sample_long(SampleArgs a) {
     if (n <= LIST) {   // all that is left to do concerns the list: ranks and sums of all pairs
       for (int i = tid; i < n; i += THREADS) s.hist[i] = units(x_of(s.list[i]), (double)m, c, S);
       __syncthreads();
-      // what each thread's logits weigh with all above them (two of a thread at most)
+      // what each thread's logits weigh with all above them (LIST / THREADS of a thread, one at least)
       constexpr int PER = (LIST + THREADS - 1) / THREADS;
       uint64_t upto[PER], mine = 0;
       int rank[PER];
@@ -1423,7 +1426,7 @@ __global__ void __launch_bounds__(THREADS) k_sample_long(SampleArgs a) {
   uint64_t total = 0;
   Pending pend{};
   bool done = false;
-  // the cut is found while the kept are weighed: a look less (2048 rows of 32768 fp32: 196 us without), but not where a
+  // the cut is found while the kept are weighed: a look less (2048 rows of 32768 fp32: 157 us, 177 without), but not where a
   // look is cheap or counts find it as a rule
   if constexpr (!KEEP && TYPE != RENO_T_BF16)
     if (by_mass && !by_least) {
@@ -1482,9 +1485,9 @@ void run(const SampleArgs& a, int64_t rows, hipStream_t st) {
     hipLaunchKernelGGL(kern, dim3((unsigned)rows), dim3(threads), lds, st, a);
   };
   // Threads of a row.  With rows for every CU several blocks share one, and fewer threads wait less for one another
-  // (2048 rows of 32768 fp32, top_p, with 128, 256, 512, 1024: 209, 203, 183, 256 us; 8192 of 4096: 107, 102, 136, 307);
-  // else a row is as quick as its threads are many (64 rows of 50021 fp16: 119, 69, 49, 42), and is kept where it fits
-  // (38; with a mask 45 against 54).
+  // (2048 rows of 32768 fp32, top_p, with 128, 256, 512, 1024: 181, 170, 157, 233 us; 8192 of 4096: 105, 98, 144, 338);
+  // else a row is as quick as its threads are many (64 rows of 50021 fp16: 113, 65, 46, 40), and is kept where it fits
+  // (39; with a mask 40 against 46).
   int threads = pieces <= 128 ? 64 : pieces <= 512 ? 128 : pieces <= 4096 ? 256 : 512;
   if (rows <= 256)
     while (threads < 1024 && threads * 2 < pieces) threads *= 2;

@@ -5,12 +5,15 @@
 // in chunks of equal length, a block a chunk; a block finds its tensor by one
 // comparison a lane.  Loads and stores of 16 bytes wherever a tensor starts,
 // several in flight a lane; bound by their bytes:
-//   k_squares, k_norm  two launches.  2048 x 65536 + 65536 bf16: 46 us, 5.8 TB/s
-//   k_clip             1000 x 50021 + 50021 fp16: 31 us, 6.5 TB/s (read from the
+//   k_squares, k_norm  two launches.  2048 x 65536 + 65536 bf16: 48 and 5 us,
+//                      5.6 TB/s in the first; 40 where the gradients lie in the
+//                      memory side cache in part
+//   k_clip             1000 x 50021 + 50021 fp16: 32 us, 6.3 TB/s (read from the
 //                      memory side cache, where the norm left them); 8.3e6
 //                      fp32: 10 us
 //   k_adamw            1.3e8 bf16 weights with fp32 copies: 694 us, 5.4 TB/s;
-//                      8.3e6 fp32: 39 us, 6.0 TB/s; 1e5 fp32: 7 us, latency
+//                      8.3e6 fp32: 41 us, 5.6 TB/s; 1e5 fp32: 7 us, latency
+// Times: the mean of many calls in a row.
 
 #include <algorithm>
 #include <cmath>
